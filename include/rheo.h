@@ -55,7 +55,10 @@ enum {
     RHEO_STATUS_BAD_LOGIT = 1,       /* NaN or +inf in a row                  */
     RHEO_STATUS_EMPTY_ROW = 2,       /* a row with fewer than m+1 (draft) or no (target) finite logits */
     RHEO_STATUS_BAD_TEMPERATURE = 4, /* T <= 0, inf or NaN                    */
-    RHEO_STATUS_INTERNAL = 8         /* broken invariant (e.g. prune not ancestor-closed) */
+    RHEO_STATUS_INTERNAL = 8,        /* broken invariant (e.g. prune not ancestor-closed) */
+    RHEO_STATUS_BAD_LENGTH = 16,     /* a negative length, or one past the block table */
+    RHEO_STATUS_NO_PAGES = 32,       /* the pool has no page left for a request       */
+    RHEO_STATUS_BAD_INDEX = 64       /* a page, slot, position, row or token out of range */
 };
 
 /* Problem size.  K = deterministic slots per pool (pool = K+1), 0 <= m <= K,
@@ -253,6 +256,190 @@ int rheo_tree_attention(const rheo_config* cfg, const rheo_pruned* pruned, const
 /* Synchronise the stream, return the device status word in *status (host
  * memory) and clear it.  Returns RHEO_ELAUNCH if the stream reported an error. */
 int rheo_get_status(const rheo_config* cfg, void* workspace, rheo_stream_t stream, int32_t* status);
+
+/* ---------------------------------------------------------------------------
+ * The target forward over the pruned tree, with a paged key/value cache.
+ *
+ * One cycle of a model with a cache is:  rheo_cache_reserve  ->  per layer
+ * rheo_qk_norm_rope and rheo_tree_attend  ->  rheo_verify on the logits  ->
+ * rheo_cache_commit.  The paper leaves this forward to its code base
+ * (Sec. 5.1); the definitions are ours.  The functions follow the rules stated
+ * at the top (the caller owns every buffer, no allocation, asynchronous, host
+ * checks before any launch).  Their scratch buffers are zeroed once by
+ * rheo_scratch_init, and again after a call whose status was not zero; calls
+ * that may overlap in time need a scratch buffer each.
+ *
+ * Tokens.  A call handles up to T = cfg.tokens new tokens of each of B
+ * requests; request b has ctx_len[b] cached tokens (positions 0 .. ctx-1) and
+ * new_len[b] <= T new ones at cache positions ctx .. ctx+new-1 (new_len NULL:
+ * T everywhere).  A pruned tree is T = N+1 new tokens in pruned order.
+ * Pages.  Page p holds page_size tokens of every key/value head.  Position x
+ * of request b lies in page block_table[b][x / page_size], row x % page_size;
+ * its slot is page * page_size + row.  Table entries past a request's pages
+ * are never read. */
+
+/* batch 1..4096, tokens 1..4096, page_size 16, 32, 64 or 128, max_pages *
+ * page_size <= 2^30, batch * max_pages <= 2^31-1, pages * page_size <= 2^40,
+ * head_dim 64 or 128, q_heads a multiple of kv_heads, both at most 1024. */
+typedef struct {
+    int32_t batch;      /* B requests                                      */
+    int32_t tokens;     /* T, new tokens of a request at most              */
+    int32_t pages;      /* pages of the pool                               */
+    int32_t page_size;  /* tokens a page holds                             */
+    int32_t max_pages;  /* width of the block table                        */
+    int32_t q_heads;    /* query heads                                     */
+    int32_t kv_heads;   /* key/value heads; query head h reads h / (q_heads / kv_heads) */
+    int32_t head_dim;   /* D                                               */
+    int32_t dtype;      /* RHEO_F32 or RHEO_BF16: queries, keys, values, outputs */
+} rheo_cache_config;
+
+/* Which pages the requests hold, and the stack of free ones (device memory). */
+typedef struct {
+    int32_t* block_table;  /* [B,max_pages]                                 */
+    int32_t* n_pages;      /* [B] pages held                                */
+    int32_t* free_list;    /* [pages] free pages, free_list[0..n_free-1]    */
+    int32_t* n_free;       /* [1]                                           */
+} rheo_pages;
+
+/* Keys and values of one layer.  Strides in elements; a token's D elements are
+ * contiguous.  Pointers and strides (in bytes) are multiples of 16. */
+typedef struct {
+    void* key;
+    void* value;
+    int64_t key_page, key_head, key_token;
+    int64_t value_page, value_head, value_token;
+} rheo_kv;
+
+/* Scratch bytes of the four cache functions for a configuration. */
+int rheo_cache_sizes(const rheo_cache_config* cfg, size_t* scratch_bytes);
+
+/* Zero a scratch buffer (cudaMemsetAsync on stream). */
+int rheo_scratch_init(void* scratch, size_t bytes, rheo_stream_t stream);
+
+/* Synchronise the stream, return the scratch buffer's status word and clear it. */
+int rheo_scratch_status(void* scratch, rheo_stream_t stream, int32_t* status);
+
+/* Block tables, slots and positions for the next call's tokens.  Request b is to
+ * hold need = ceil((ctx_len + new_len) / page_size) pages.  First the pages
+ * that requests hold past their need go onto the free stack, in order of
+ * request, then of place (a request that ended has both lengths 0); then the
+ * missing ones are taken from its top in the same order.  A request whose
+ * pages the stack cannot give takes none, and neither does any behind it that
+ * lacks pages (RHEO_STATUS_NO_PAGES); one whose need is past max_pages or with
+ * a negative length or new_len > T keeps what it holds (RHEO_STATUS_BAD_LENGTH).
+ *   slot     [B,T] int64: of each new token; -1 past new_len and for requests
+ *            that were not served;
+ *   position [B,T] int32: ctx_len + depth[b][t] (depth [B,T] int32: the pruned
+ *            tree's depths; NULL: t), -1 where slot is -1.
+ * before and after are the same four buffers (in place) or eight distinct
+ * ones; entries that hold no page keep their value (from before). */
+int rheo_cache_reserve(const rheo_cache_config* cfg, const int32_t* ctx_len, const int32_t* new_len,
+                       const int32_t* depth, const rheo_pages* before, const rheo_pages* after, int64_t* slot,
+                       int32_t* position, void* scratch, rheo_stream_t stream);
+
+/* Queries, keys and values of the B*T new tokens of one layer; strides in
+ * elements (token: from t to t+1, batch: from b to b+1), D contiguous.
+ * Pointers and strides (in bytes) are multiples of 16. */
+typedef struct {
+    const void* q;
+    const void* k;
+    const void* v;
+    int64_t q_batch, q_token, q_head;
+    int64_t k_batch, k_token, k_head;
+    int64_t v_batch, v_token, v_head;
+} rheo_qkv;
+
+/* Norms of queries and keys, their rotation, and the store into the cache.  For
+ * each head of q and k of a token with slot >= 0:
+ *   y = x / sqrt(mean(x^2) + eps) * weight   (weight [D] of cfg.dtype; NULL: y = x)
+ *   the first `rot` elements turn by the token's position: with c, s =
+ *   cos_sin[position][i], cos_sin[position][rot/2 + i], the pair (y_i, y_{i+rot/2})
+ *   (interleaved: (y_2i, y_2i+1)) becomes (y_i c - y' s, y' c + y_i s);
+ * computed in fp32, rounded once.  q goes to q_out ([B,T,q_heads,D], strides
+ * like rheo_qkv's; it may be q itself), k and v to their slots (v unchanged).
+ * A token with slot < 0 stores nothing and its q_out is 0; so does one whose
+ * slot or position is out of range (RHEO_STATUS_BAD_INDEX).
+ * cos_sin: [max_position, rot] fp32, 16-byte aligned; rot a multiple of 8, 0..D
+ * (0: no rotation, cos_sin may be NULL). */
+int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* in, const void* q_weight, const void* k_weight,
+                      float eps, const float* cos_sin, int32_t max_position, int32_t rot, int32_t interleaved,
+                      const int64_t* slot, const int32_t* position, const rheo_kv* kv, void* q_out,
+                      int64_t q_out_batch, int64_t q_out_token, int64_t q_out_head, void* scratch,
+                      rheo_stream_t stream);
+
+/* Attention of the new tokens over the cache, in which their keys and values
+ * already are.  Token t < new_len of request b sees every position l < ctx_len
+ * and the new tokens j < new_len with mask[b][t][j] != 0 (mask [B,T,T] uint8 of
+ * rheo_tree_attention; NULL: j <= t):
+ *   out = sum_l w_l v_l,  w = softmax(scale * q.k_l),  lse = log sum_l exp(scale * q.k_l)
+ * with fp32 statistics (bf16: w is rounded to bf16 for its product with v, which
+ * sums in fp32).  What a token does not see does not reach its output, NaN and
+ * infinities included.  A token that sees nothing, and every t >= new_len, gets
+ * out = 0 and lse = -inf.
+ *   q, out [B,T,q_heads,D] with strides in elements (batch, token, head), D
+ *   contiguous, pointers and strides (in bytes) multiples of 16;
+ *   lse [B,T,q_heads] fp32, may be NULL.
+ * A request with a bad length (RHEO_STATUS_BAD_LENGTH) gets out = 0, lse = -inf;
+ * a bad page in the table (RHEO_STATUS_BAD_INDEX) reads as zeros. */
+typedef struct {
+    const void* q;
+    void* out;
+    float* lse;
+    int64_t q_batch, q_token, q_head;
+    int64_t out_batch, out_token, out_head;
+} rheo_attend_io;
+
+int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, const rheo_kv* kv,
+                     const int32_t* block_table, const int32_t* ctx_len, const int32_t* new_len, const uint8_t* mask,
+                     float scale, void* scratch, rheo_stream_t stream);
+
+/* After verification: the keys and values of the accepted path move to the
+ * positions behind the root, in `layers` layers (layer l at kv->key + l *
+ * key_layer elements, kv->value + l * value_layer).  For k = 0 .. accepted_len-1:
+ * position ctx_len + accepted_nodes[b][k] -> ctx_len + k + 1; next_len = ctx_len
+ * + 1 + accepted_len (the root and the path; the bonus token is the next root).
+ *   accepted_nodes [B,depth] int32 as rheo_verify writes it: ascending, entry k
+ *   in k+1 .. T-1.  A path that breaks this is not moved and its next_len is
+ *   ctx_len (RHEO_STATUS_BAD_INDEX); so for a bad length (RHEO_STATUS_BAD_LENGTH).
+ * next_len [B] int32, not the buffer of ctx_len.  depth <= 128. */
+int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, const rheo_kv* kv, int64_t key_layer,
+                      int64_t value_layer, const int32_t* block_table, const int32_t* ctx_len,
+                      const int32_t* accepted_len, const int32_t* accepted_nodes, int32_t depth, int32_t* next_len,
+                      void* scratch, rheo_stream_t stream);
+
+/* Log probabilities of given tokens, with rank, entropy and top alternatives
+ * (the logprobs of the emitted tokens, of a prompt, or of drafted nodes).
+ * rows 1..2^20, vocab 1..262144, top 0..32, rows_per_temperature >= 1. */
+typedef struct {
+    int32_t rows;                  /* R rows asked for                       */
+    int32_t vocab;                 /* V                                      */
+    int32_t top;                   /* alternatives reported per row          */
+    int32_t dtype;                 /* RHEO_F32 or RHEO_BF16                  */
+    int32_t rows_per_temperature;  /* row i uses temperature[i / this]       */
+} rheo_logprob_config;
+
+typedef struct {
+    float* logprob;       /* [R] log softmax(l/T) at the given token                    */
+    int32_t* rank;        /* [R] its place under (logit desc, id asc), 0 the first      */
+    float* entropy;       /* [R] -sum p log p of softmax(l/T), in nats                  */
+    int32_t* top_ids;     /* [R,top] the `top` first tokens in that order; -1 past the
+                             finite logits; may be NULL if top = 0                      */
+    float* top_logprobs;  /* [R,top] their log probabilities; -inf where the id is -1   */
+} rheo_logprobs;
+
+int rheo_logprob_sizes(const rheo_logprob_config* cfg, size_t* scratch_bytes);
+
+/* Row i reads logits row row_index[i] (NULL: i; [R] int32), of logit_rows rows
+ * with row_stride elements from one to the next, and the token token[i].
+ * temperature: fp32, NULL: 1 everywhere.  row_index -1 leaves the row out:
+ * logprob 0, rank -1, entropy 0, top_ids -1, top_logprobs -inf.  token -1 gives
+ * logprob 0 and rank -1, the rest as usual.  Other indices out of range count as
+ * -1 and set RHEO_STATUS_BAD_INDEX; NaN or +inf, an all -inf row and a bad
+ * temperature set their bits as in rheo_verify, and that row's outputs are
+ * unspecified. */
+int rheo_token_logprobs(const rheo_logprob_config* cfg, const void* logits, int64_t row_stride, int64_t logit_rows,
+                        const int32_t* row_index, const int32_t* token, const float* temperature,
+                        const rheo_logprobs* out, void* scratch, rheo_stream_t stream);
 
 #ifdef __cplusplus
 }

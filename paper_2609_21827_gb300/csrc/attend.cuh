@@ -1,0 +1,101 @@
+// attend.cuh -- what the attention kernels share: how the key tiles of all
+// requests are cut over the CTAs, and which places a token sees.
+//
+// An item is (request, key/value head, group of query rows): the rows of a
+// group are consecutive (token, query head of the key/value head) pairs, so
+// that one read of a key tile serves all query heads that share it.  An item of
+// request b has ceil((ctx + new) / tile) key tiles, one at least.  All tiles of
+// all items lie on one line, item after item; CTA i of n takes the tiles
+// [i total / n, (i+1) total / n), whatever the lengths are, so ragged contexts
+// and few requests keep every SM as busy as many equal ones.  An item cut by a
+// boundary leaves partial sums: CTA i keeps at most two, slot 2i for one that
+// began in an earlier CTA and slot 2i+1 for one that goes on in a later CTA.
+#pragma once
+
+#include "cache_kernels.h"
+#include "rheo_device.cuh"
+
+namespace rheo {
+
+struct AttendSpan {  // a request's lengths, checked
+    int ctx, add;    // cached tokens, new tokens; both 0 where a length is bad
+    bool bad;
+    __device__ __forceinline__ int len() const { return ctx + add; }
+};
+
+__device__ __forceinline__ AttendSpan attend_span(const AttendArgs& a, int b) {
+    const int ctx = a.ctx_len[b], add = a.new_len ? a.new_len[b] : a.T;
+    const bool bad = ctx < 0 || add < 0 || add > a.T || (int64_t)ctx + add > (int64_t)a.max_pages * a.P;
+    return bad ? AttendSpan{0, 0, true} : AttendSpan{ctx, add, false};
+}
+
+template <int TILE> __device__ __forceinline__ int attend_tiles(const AttendArgs& a, int b) {
+    const int n = (attend_span(a, b).len() + TILE - 1) / TILE;
+    return n > 0 ? n : 1;
+}
+
+struct AttendCut {    // one CTA's range of tiles, and where it starts
+    int64_t total;
+    int n;            // CTAs that take part
+    int64_t begin, end;
+    int b, item, tile;  // request, item within it, tile within that
+    __device__ __forceinline__ int owner(int64_t t) const { return (int)((t * n + n - 1) / total); }
+};
+
+// Computed by one warp; `per` items a request; at least min_tiles a CTA.
+template <int TILE>
+__device__ __forceinline__ AttendCut attend_cut(const AttendArgs& a, int per, int cta, int min_tiles) {
+    const int lane = threadIdx.x & 31;
+    AttendCut c;
+    int64_t sum = 0;
+    for (int b = lane; b < a.B; b += 32) sum += attend_tiles<TILE>(a, b);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    c.total = sum * per;
+    const int64_t most = c.total / min_tiles;
+    c.n = most < 1 ? 1 : most < a.ctas ? (int)most : a.ctas;
+    c.begin = cta < c.n ? (int64_t)cta * c.total / c.n : c.total;
+    c.end = cta < c.n ? (int64_t)(cta + 1) * c.total / c.n : c.total;
+    c.b = a.B;
+    c.item = c.tile = 0;
+    int64_t before = 0;  // tiles of the requests before this round of 32
+    for (int b0 = 0; b0 < a.B; b0 += 32) {
+        const int b = b0 + lane;
+        const int64_t mine = b < a.B ? (int64_t)attend_tiles<TILE>(a, b) * per : 0;
+        int64_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        const unsigned past = __ballot_sync(0xffffffffu, before + upto > c.begin);
+        if (past) {
+            const int l = __ffs(past) - 1;
+            const int64_t first = __shfl_sync(0xffffffffu, before + upto - mine, l);
+            const int tiles = (int)(__shfl_sync(0xffffffffu, mine, l) / per);
+            c.b = b0 + l;
+            c.item = (int)((c.begin - first) / tiles);
+            c.tile = (int)((c.begin - first) % tiles);
+            break;
+        }
+        before += __shfl_sync(0xffffffffu, upto, 31);
+    }
+    return c;
+}
+
+// Whether new token t (of `add`) sees place l of its request.
+__device__ __forceinline__ bool attend_sees(const AttendSpan& s, const uint8_t* mask_row, int t, int l) {
+    const int j = l - s.ctx;
+    if (j < 0) return true;
+    if (j >= s.add) return false;
+    return mask_row ? mask_row[j] != 0 : j <= t;
+}
+
+// The slot of a.part_o / a.part_ml for CTA `cta`'s part of an item that it does not hold whole.
+__device__ __forceinline__ int64_t attend_part(int cta, bool starts_here) { return 2 * (int64_t)cta + (starts_here ? 1 : 0); }
+
+__device__ __forceinline__ float attend_lse(float m, float l) {
+    return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+}  // namespace rheo

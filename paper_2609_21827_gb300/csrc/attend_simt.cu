@@ -1,0 +1,353 @@
+// attend_simt.cu -- attention of drafted tokens over the paged cache on the fp32
+// units, and the join of partial sums.
+//
+// For an item of R query rows and its key tiles of 64: scores s = q k (fp32 FMA
+// on register tiles of R/16 x 4 a thread), running maximum m and sum l a row in
+// log2 units, p = 2^(s - m), O = 2^(m_old - m) O + p V.  Half a warp owns R/16
+// rows, so the row statistics are four shuffles and p passes through shared
+// memory without a block barrier.
+#include <cuda_bf16.h>
+
+#include <type_traits>
+
+#include "attend.cuh"
+#include "rheo_kernels.h"
+
+namespace rheo {
+
+constexpr int kSimtThreads = 256;
+constexpr int kSimtTile = 64;
+
+__device__ __forceinline__ void cp_async16(void* dst, const void* src, bool valid) {
+    const unsigned d = (unsigned)__cvta_generic_to_shared(dst);
+    const int n = valid ? 16 : 0;  // 0: the 16 bytes are zeroed
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+// Four neighbouring outputs.
+template <int DT> __device__ __forceinline__ void store4(void* out, int64_t e, float4 v) {
+    if (DT == 0) {
+        *reinterpret_cast<float4*>(static_cast<float*>(out) + e) = v;
+    } else {
+        const __nv_bfloat162 x = __floats2bfloat162_rn(v.x, v.y), y = __floats2bfloat162_rn(v.z, v.w);
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + e) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+    }
+}
+
+template <int D, int R> struct SimtSmem {
+    float q[R][D + 4];
+    float k[2][kSimtTile][D + 4];
+    float v[2][kSimtTile][D];
+    float p[R][kSimtTile + 4];
+};
+
+template <int DT, int D, int R>
+__global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const AttendArgs a) {
+    grid_dependency_begin();
+    extern __shared__ __align__(16) unsigned char raw_smem[];
+    SimtSmem<D, R>& sm = *reinterpret_cast<SimtSmem<D, R>*>(raw_smem);
+    __shared__ AttendCut cut_s;
+    constexpr int RT = R / 16, DJ = D / 64, ES = DT == 1 ? 2 : 4;
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const int rows = a.T * a.G, groups = (rows + R - 1) / R, per = a.H * groups;
+    if (tid < 32) {
+        const AttendCut c = attend_cut<kSimtTile>(a, per, blockIdx.x, 1);
+        if (tid == 0) cut_s = c;
+    }
+    __syncthreads();
+    const AttendCut cut = cut_s;
+    if (tid == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
+
+    int b = cut.b, item = cut.item, tile = cut.tile;
+    for (int64_t at = cut.begin; at < cut.end;) {
+        const AttendSpan span = attend_span(a, b);
+        if (span.bad && tid == 0) atomicOr(a.status, kStBadLength);
+        const int len = span.len();
+        const int tiles = max(1, (len + kSimtTile - 1) / kSimtTile);
+        const int n = (int)min((int64_t)(tiles - tile), cut.end - at);
+        const int h = item / groups, r0 = (item % groups) * R;
+        const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
+
+        auto load = [&](int tl, int buf) {
+            constexpr int C = D * ES / 16;  // 16-byte pieces of a line
+            for (int i = tid; i < kSimtTile * C; i += kSimtThreads) {
+                const int kr = i / C, c = i % C, l = tl * kSimtTile + kr;
+                bool ok = l < len;
+                int64_t page = 0;
+                if (ok) {
+                    page = table[l >> a.page_shift];
+                    if (page < 0 || page >= a.pages) {
+                        atomicOr(a.status, kStBadIndex);
+                        ok = false;
+                        page = 0;
+                    }
+                }
+                const int64_t row = l & (a.P - 1);
+                const char* ks = static_cast<const char*>(a.kv.key) +
+                                 (page * a.kv.key_page + h * a.kv.key_head + row * a.kv.key_token) * ES + c * 16;
+                const char* vs = static_cast<const char*>(a.kv.value) +
+                                 (page * a.kv.value_page + h * a.kv.value_head + row * a.kv.value_token) * ES + c * 16;
+                if (DT == 0) {
+                    cp_async16(&sm.k[buf][kr][c * 4], ks, ok);
+                    cp_async16(&sm.v[buf][kr][c * 4], vs, ok);
+                } else {
+                    uint4 x = make_uint4(0, 0, 0, 0), y = x;
+                    if (ok) {
+                        x = *reinterpret_cast<const uint4*>(ks);
+                        y = *reinterpret_cast<const uint4*>(vs);
+                    }
+                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        sm.k[buf][kr][(c * 8 + 2 * u) % D] = bf_lo(xs[u]);
+                        sm.k[buf][kr][(c * 8 + 2 * u + 1) % D] = bf_hi(xs[u]);
+                        sm.v[buf][kr][(c * 8 + 2 * u) % D] = bf_lo(ys[u]);
+                        sm.v[buf][kr][(c * 8 + 2 * u + 1) % D] = bf_hi(ys[u]);
+                    }
+                }
+            }
+            cp_async_commit();
+        };
+
+        __syncthreads();  // the last item's tiles and queries have been read
+        load(tile, 0);
+        for (int i = tid; i < R * (D / 4); i += kSimtThreads) {
+            const int r = i / (D / 4), d = i % (D / 4) * 4, row = r0 + r, t = row / a.G;
+            float4 x = make_float4(0, 0, 0, 0);
+            if (row < rows && t < span.add) {
+                const char* src = static_cast<const char*>(a.io.q) +
+                                  (b * a.io.q_batch + t * a.io.q_token + (h * a.G + row % a.G) * a.io.q_head + d) * ES;
+                if (DT == 0) {
+                    x = *reinterpret_cast<const float4*>(src);
+                } else {
+                    const uint2 y = *reinterpret_cast<const uint2*>(src);
+                    x = make_float4(bf_lo(y.x), bf_hi(y.x), bf_lo(y.y), bf_hi(y.y));
+                }
+            }
+            *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
+        }
+
+        float m[RT], l[RT], o[RT][DJ * 4];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            m[i] = -INFINITY;
+            l[i] = 0.0f;
+#pragma unroll
+            for (int d = 0; d < DJ * 4; ++d) o[i][d] = 0.0f;
+        }
+        for (int q = 0; q < n; ++q) {
+            const int buf = q & 1, k0 = (tile + q) * kSimtTile;
+            if (q + 1 < n) load(tile + q + 1, buf ^ 1);
+            if (q + 1 < n) cp_async_wait<1>();
+            else cp_async_wait<0>();
+            __syncthreads();
+
+            float s[RT][4];
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[i][j] = 0.0f;
+#pragma unroll 4
+            for (int d = 0; d < D; d += 4) {
+                float4 kk[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) kk[j] = *reinterpret_cast<const float4*>(&sm.k[buf][tx + 16 * j][d]);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const float4 qq = *reinterpret_cast<const float4*>(&sm.q[ty * RT + i][d]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        s[i][j] += qq.x * kk[j].x + qq.y * kk[j].y + qq.z * kk[j].z + qq.w * kk[j].w;
+                }
+            }
+            const bool tail = k0 + kSimtTile > span.ctx;  // places that not every token sees
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const int row = r0 + ty * RT + i, t = row / a.G;
+                const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + min(t, a.T - 1)) * a.T : nullptr;
+                unsigned hidden = 0;
+                float top = -INFINITY;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    s[i][j] *= a.scale_log2;
+                    if (tail && !(t < span.add && attend_sees(span, mrow, t, k0 + tx + 16 * j))) {
+                        s[i][j] = -INFINITY;
+                        hidden |= 1u << j;
+                    }
+                    top = fmaxf(top, s[i][j]);
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                const float mn = fmaxf(m[i], top), ref = mn == -INFINITY ? 0.0f : mn;
+                const float keep = fast_exp2(m[i] - ref);
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float p = fast_exp2(s[i][j] - ref);
+                    // a hidden place is marked by the sign of its zero, so that V's NaN and infinities there are skipped
+                    if ((hidden >> j) & 1u) p = -0.0f;
+                    sum += p;
+                    sm.p[ty * RT + i][tx + 16 * j] = p;
+                }
+#pragma unroll
+                for (int w = 8; w > 0; w >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, w);
+                l[i] = l[i] * keep + sum;
+                m[i] = mn;
+#pragma unroll
+                for (int d = 0; d < DJ * 4; ++d) o[i][d] *= keep;
+            }
+            __syncwarp();
+            auto times_v = [&](auto skip) {
+#pragma unroll 2
+                for (int k = 0; k < kSimtTile; k += 4) {
+                    float4 pp[RT];
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) pp[i] = *reinterpret_cast<const float4*>(&sm.p[ty * RT + i][k]);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                        for (int c = 0; c < DJ; ++c) {
+                            const float4 vv = *reinterpret_cast<const float4*>(&sm.v[buf][k + u][tx * 4 + 64 * c]);
+#pragma unroll
+                            for (int i = 0; i < RT; ++i) {
+                                const float p = u == 0 ? pp[i].x : u == 1 ? pp[i].y : u == 2 ? pp[i].z : pp[i].w;
+                                if (decltype(skip)::value && __float_as_uint(p) == 0x80000000u) continue;
+                                o[i][4 * c] += p * vv.x;
+                                o[i][4 * c + 1] += p * vv.y;
+                                o[i][4 * c + 2] += p * vv.z;
+                                o[i][4 * c + 3] += p * vv.w;
+                            }
+                        }
+                    }
+                }
+            };
+            if (tail) times_v(std::true_type{});
+            else times_v(std::false_type{});
+            __syncthreads();  // the buffer is free for the tile after the next
+        }
+
+        const bool whole = n == tiles;
+        const int64_t part = attend_part(blockIdx.x, tile == 0);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int r = ty * RT + i, row = r0 + r;
+            if (row >= rows) continue;
+            const int t = row / a.G, head = h * a.G + row % a.G;
+            const float ll = t < span.add ? l[i] : 0.0f;
+            if (!whole) {
+                float* po = a.part_o + (part * R + r) * D;
+#pragma unroll
+                for (int c = 0; c < DJ; ++c)
+                    *reinterpret_cast<float4*>(po + tx * 4 + 64 * c) =
+                        make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
+                if (tx == 0) {
+                    a.part_ml[(part * R + r) * 2] = m[i];
+                    a.part_ml[(part * R + r) * 2 + 1] = ll;
+                }
+                continue;
+            }
+            const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+#pragma unroll
+            for (int c = 0; c < DJ; ++c) {
+                float4 y = make_float4(0, 0, 0, 0);
+                if (ll != 0.0f)
+                    y = make_float4(o[i][4 * c] * inv, o[i][4 * c + 1] * inv, o[i][4 * c + 2] * inv,
+                                    o[i][4 * c + 3] * inv);
+                store4<DT>(a.io.out, b * a.io.out_batch + t * a.io.out_token + head * a.io.out_head + tx * 4 + 64 * c,
+                           y);
+            }
+            if (a.io.lse && tx == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m[i], ll);
+        }
+        if (!whole && tile == 0 && tid == 0)
+            a.join[blockIdx.x] = make_int4(b, item, cut.owner(at + tiles - 1) - (int)blockIdx.x + 1, 0);
+        at += n;
+        tile = 0;
+        if (++item == per) {
+            item = 0;
+            ++b;
+        }
+    }
+}
+
+// Joins the parts of an item that several CTAs summed, in the order of its keys:
+// a warp a row, 8 rows a CTA; grid (CTAs of the sums, rows of an item / 8).
+template <int DT, int D>
+__global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, int R) {
+    grid_dependency_begin();
+    constexpr int W = D / 32;
+    const int4 rec = a.join[blockIdx.x];
+    const int segments = rec.z, lane = threadIdx.x & 31;
+    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
+    if (segments == 0 || r >= R) return;
+    const int b = rec.x, rows = a.T * a.G, groups = (rows + R - 1) / R;
+    const int h = rec.y / groups, row = rec.y % groups * R + r;
+    if (row >= rows) return;
+    const int t = row / a.G, head = h * a.G + row % a.G;
+    const auto part = [&](int s) { return attend_part(blockIdx.x + s, s == 0) * R + r; };
+    float m = -INFINITY;
+    for (int s = lane; s < segments; s += 32) m = fmaxf(m, a.part_ml[part(s) * 2]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, x[W];
+#pragma unroll
+    for (int i = 0; i < W; ++i) x[i] = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < segments; ++s) {
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + part(s) * 2);
+        const float w = fast_exp2(ml.x - ref);
+        const float* po = a.part_o + part(s) * D + lane * W;
+        l += w * ml.y;
+        if (W == 4) {
+            const float4 y = *reinterpret_cast<const float4*>(po);
+            x[0] += w * y.x;
+            x[1] += w * y.y;
+            x[2 % W] += w * y.z;
+            x[3 % W] += w * y.w;
+        } else {
+            const float2 y = *reinterpret_cast<const float2*>(po);
+            x[0] += w * y.x;
+            x[1] += w * y.y;
+        }
+    }
+    const int64_t e = b * a.io.out_batch + t * a.io.out_token + head * a.io.out_head + lane * W;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const float y = l == 0.0f ? 0.0f : x[i] / l;
+        if (DT == 0) static_cast<float*>(a.io.out)[e + i] = y;
+        else static_cast<__nv_bfloat16*>(a.io.out)[e + i] = __float2bfloat16_rn(y);
+    }
+    if (a.io.lse && lane == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m, l);
+}
+
+// 16 rows an item where that holds them all (single tokens and short chains: the
+// products are few and the bytes count), else 64.
+int attend_rows(int dtype, int T, int G) { return (int64_t)T * G <= 16 ? 16 : 64; }
+int attend_ctas(int dtype, int T, int G) { return 152; }
+
+template <int DT, int D, int R> static cudaError_t launch_simt(const AttendArgs& a, cudaStream_t s) {
+    const size_t smem = sizeof(SimtSmem<D, R>);
+    cudaError_t err = cudaFuncSetAttribute(attend_simt_kernel<DT, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)smem);
+    if (err != cudaSuccess) return err;
+    err = launch_dependent(attend_simt_kernel<DT, D, R>, dim3(a.ctas), dim3(kSimtThreads), smem, s, a);
+    if (err != cudaSuccess) return err;
+    return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, R / 8), dim3(256), 0, s, a, R);
+}
+
+template <int DT> static cudaError_t launch_simt_dt(const AttendArgs& a, cudaStream_t s) {
+    if (attend_rows(DT, a.T, a.G) == 16)
+        return a.D == 64 ? launch_simt<DT, 64, 16>(a, s) : launch_simt<DT, 128, 16>(a, s);
+    return a.D == 64 ? launch_simt<DT, 64, 64>(a, s) : launch_simt<DT, 128, 64>(a, s);
+}
+
+cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s) {
+    return dtype == 1 ? launch_simt_dt<1>(a, s) : launch_simt_dt<0>(a, s);
+}
+
+}  // namespace rheo

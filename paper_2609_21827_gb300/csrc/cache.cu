@@ -1,0 +1,423 @@
+// cache.cu -- the paged cache beside the attention: block tables and slots from
+// lengths (reserve), norms and rotation of queries and keys with the store into
+// the cache (qk_norm_rope), and the accepted path's move into place (commit).
+#include <cuda_bf16.h>
+
+#include "cache_kernels.h"
+#include "rheo_device.cuh"
+#include "rheo_kernels.h"
+
+namespace rheo {
+
+// ---------------------------------------------------------------------------
+// reserve.  One launch of up to one CTA per SM.  Every CTA derives the whole
+// plan itself: pages to give back and to take of all B requests (three ints a
+// request, read from L2), and their exclusive prefix sums in shared memory.
+// From these each request's pages follow without any order between CTAs: the
+// i-th page taken in the call is entry F-1-i of the stack as it stands after
+// all releases, which is an old entry of the free list or, past the old top, a
+// page that some request releases, found by a binary search over the release
+// sums and read from that request's row.  Released and taken entries never
+// overlap, so the tables may be updated in place; the counts, which every CTA
+// reads, are written by the last CTA to have read them (a ticket).
+// Latency bound: three dependent rounds of loads, a scan and the stores.
+// ---------------------------------------------------------------------------
+constexpr int kReserveThreads = 256;
+constexpr int kReserveBad = (int)0x80000000u;  // mark of a request that keeps what it holds
+
+// Inclusive sums of both components over the block.
+__device__ __forceinline__ int2 block_scan_pair(int2 v, int2* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, v.x, o), y = __shfl_up_sync(0xffffffffu, v.y, o);
+        if (lane >= o) {
+            v.x += x;
+            v.y += y;
+        }
+    }
+    if (lane == 31) warp_sums[warp] = v;
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) {
+        v.x += warp_sums[w].x;
+        v.y += warp_sums[w].y;
+    }
+    __syncthreads();
+    return v;
+}
+
+__global__ void __launch_bounds__(kReserveThreads) reserve_kernel(const ReserveArgs a) {
+    grid_dependency_begin();
+    extern __shared__ int rsm[];
+    __shared__ int2 warp_sums[kReserveThreads / 32];
+    __shared__ int2 carry;
+    __shared__ int s_last;
+    int* back_at = rsm;                // [B+1] pages given back before request b
+    int* take_at = back_at + a.B + 1;  // [B+1] pages asked for before request b
+    int* held = take_at + a.B + 1;     // [B] pages held, kReserveBad set where lengths are bad
+    const int tid = threadIdx.x;
+    const int64_t capacity = (int64_t)a.max_pages * a.P;
+
+    int free0 = *a.before.n_free;
+    if (free0 < 0 || free0 > a.pages) {
+        if (tid == 0) atomicOr(a.status, kStInternal);
+        free0 = free0 < 0 ? 0 : a.pages;
+    }
+    if (tid == 0) {
+        carry = make_int2(0, 0);
+        back_at[0] = take_at[0] = 0;
+    }
+    __syncthreads();
+    for (int b0 = 0; b0 < a.B; b0 += kReserveThreads) {
+        const int b = b0 + tid;
+        int2 v = make_int2(0, 0);
+        if (b < a.B) {
+            const int64_t ctx = a.ctx_len[b], add = a.new_len ? a.new_len[b] : a.T;
+            int own = a.before.n_pages[b];
+            if (own < 0 || own > a.max_pages) {
+                atomicOr(a.status, kStInternal);
+                own = own < 0 ? 0 : a.max_pages;
+            }
+            const bool bad = ctx < 0 || add < 0 || add > a.T || ctx + add > capacity;
+            if (bad) {
+                atomicOr(a.status, kStBadLength);
+                held[b] = own | kReserveBad;
+            } else {
+                const int need = (int)((ctx + add + a.P - 1) / a.P);
+                v = make_int2(max(own - need, 0), max(need - own, 0));
+                held[b] = own;
+            }
+        }
+        v = block_scan_pair(v, warp_sums);
+        const int2 c = carry;
+        if (b < a.B) {
+            back_at[b + 1] = c.x + v.x;
+            take_at[b + 1] = c.y + v.y;
+        }
+        __syncthreads();
+        if (tid == kReserveThreads - 1) carry = make_int2(c.x + v.x, c.y + v.y);
+        __syncthreads();
+    }
+    const int have = free0 + back_at[a.B];  // the stack's height after all releases
+    if (have > a.pages && tid == 0) atomicOr(a.status, kStInternal);
+    if (tid == 0) {
+        __threadfence();
+        s_last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+
+    // page i (0 = first) of those that request b takes
+    auto taken = [&](int b, int i) -> int {
+        const int at = have - 1 - (take_at[b] + i);
+        if (at < free0) return a.before.free_list[at];
+        const int r = at - free0;
+        int lo = 0, hi = a.B - 1;  // the request with back_at[lo] <= r < back_at[lo + 1]
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (back_at[mid] <= r) lo = mid;
+            else hi = mid - 1;
+        }
+        const int keep = (held[lo] & ~kReserveBad) - (back_at[lo + 1] - back_at[lo]);
+        return a.before.block_table[(int64_t)lo * a.max_pages + keep + (r - back_at[lo])];
+    };
+
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x) {
+        const int64_t row = (int64_t)b * a.max_pages;
+        const bool bad = held[b] & kReserveBad;
+        const int own = held[b] & ~kReserveBad;
+        const int back = back_at[b + 1] - back_at[b], want = take_at[b + 1] - take_at[b];
+        const bool served = !bad && (want == 0 || take_at[b + 1] <= have);
+        if (!bad && !served && tid == 0) atomicOr(a.status, kStNoPages);
+        const int take = served ? want : 0;
+        const int32_t* in = a.before.block_table + row;
+        int32_t* out = a.after.block_table + row;
+        if (a.in_place) {
+            for (int j = own + tid; j < own + take; j += kReserveThreads) out[j] = taken(b, j - own);
+        } else {
+            for (int j = tid; j < a.max_pages; j += kReserveThreads)
+                out[j] = (j >= own && j < own + take) ? taken(b, j - own) : in[j];
+        }
+        for (int r = tid; r < back; r += kReserveThreads) {
+            const int at = free0 + back_at[b] + r;
+            if (at < a.pages) a.after.free_list[at] = in[own - back + r];
+        }
+        const int ctx = a.ctx_len[b];
+        const int add = !served ? 0 : a.new_len ? a.new_len[b] : a.T;
+        for (int t = tid; t < a.T; t += kReserveThreads) {
+            int64_t slot = -1;
+            int pos = -1;
+            if (t < add) {
+                const int x = ctx + t, j = x / a.P;
+                const int page = j < own ? in[j] : taken(b, j - own);
+                if (page < 0 || page >= a.pages) {
+                    atomicOr(a.status, kStBadIndex);
+                } else {
+                    slot = (int64_t)page * a.P + x % a.P;
+                    pos = ctx + (a.depth ? a.depth[(int64_t)b * a.T + t] : t);
+                }
+            }
+            a.slot[(int64_t)b * a.T + t] = slot;
+            a.position[(int64_t)b * a.T + t] = pos;
+        }
+    }
+    if (!a.in_place)
+        for (int64_t i = (int64_t)blockIdx.x * kReserveThreads + tid; i < a.pages;
+             i += (int64_t)gridDim.x * kReserveThreads)
+            if (i < free0 || i >= have) a.after.free_list[i] = a.before.free_list[i];
+
+    if (s_last) {
+        // every CTA has its copy of the counts: they may change now
+        int most = 0;  // pages taken: the last prefix that the stack could give
+        for (int b = tid; b < a.B; b += kReserveThreads) {
+            const bool bad = held[b] & kReserveBad;
+            const int want = take_at[b + 1] - take_at[b];
+            const bool served = !bad && take_at[b + 1] <= have;
+            if (served) most = max(most, take_at[b + 1]);
+            a.after.n_pages[b] = (held[b] & ~kReserveBad) - (back_at[b + 1] - back_at[b]) + (served ? want : 0);
+        }
+        most = __reduce_max_sync(0xffffffffu, most);
+        if ((tid & 31) == 0) warp_sums[tid >> 5].x = most;
+        __syncthreads();
+        if (tid == 0) {
+            for (int w = 1; w < kReserveThreads / 32; ++w) most = max(most, warp_sums[w].x);
+            *a.after.n_free = min(have, a.pages) - most;
+            *a.ticket = 0;
+        }
+    }
+}
+
+cudaError_t launch_reserve(const ReserveArgs& a, int sms, cudaStream_t s) {
+    const size_t smem = sizeof(int) * (3 * (size_t)a.B + 2);
+    cudaError_t err =
+        cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(64 * 1024));
+    if (err != cudaSuccess) return err;
+    return launch_dependent(reserve_kernel, dim3(a.B < sms ? a.B : sms), dim3(kReserveThreads), smem, s, a);
+}
+
+// ---------------------------------------------------------------------------
+// qk_norm_rope.  A warp takes one token and a run of its heads (queries, keys,
+// then values); a lane holds four neighbouring elements of a head, so a head of
+// 128 fills the warp and two heads of 64 share it.  The loads of the whole run
+// are issued first, the sum of squares is a butterfly over the head's lanes, and
+// the pair of an element is in the same lane (interleaved) or rot/8 lanes away
+// (a shuffle).  Each input and output element crosses HBM once: HBM bound.
+// ---------------------------------------------------------------------------
+constexpr int kRopeThreads = 128;
+
+template <int DT> struct Quad;  // four neighbouring elements
+template <> struct Quad<0> {
+    using Raw = float4;
+    __device__ static __forceinline__ float4 wide(float4 r) { return r; }
+    __device__ static __forceinline__ float4 narrow(float4 r) { return r; }
+    __device__ static __forceinline__ float4 zero() { return make_float4(0, 0, 0, 0); }
+};
+template <> struct Quad<1> {
+    using Raw = uint2;
+    __device__ static __forceinline__ float4 wide(uint2 r) {
+        return make_float4(bf_lo(r.x), bf_hi(r.x), bf_lo(r.y), bf_hi(r.y));
+    }
+    __device__ static __forceinline__ uint2 narrow(float4 v) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+        return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    }
+    __device__ static __forceinline__ uint2 zero() { return make_uint2(0, 0); }
+};
+
+// heads of a token that a warp takes at a time: 16 registers of raw data a lane
+template <int DT, int D> constexpr int rope_rounds() { return DT == 1 ? 8 : 4; }
+template <int DT, int D> constexpr int rope_heads() { return rope_rounds<DT, D>() * (128 / D); }
+
+template <int DT, int D, bool INTERLEAVED>
+__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
+    grid_dependency_begin();
+    using Q = Quad<DT>;
+    using Raw = typename Q::Raw;
+    constexpr int LPH = D / 4, HPW = 32 / LPH, ROUNDS = rope_rounds<DT, D>(), HEADS = rope_heads<DT, D>();
+    constexpr int ES = DT == 1 ? 2 : 4;
+    const int lane = threadIdx.x & 31, ci = lane & (LPH - 1), sub = lane / LPH, e = ci * 4;
+    const int heads = a.Hq + 2 * a.H, runs = (heads + HEADS - 1) / HEADS;
+    const int64_t item = (int64_t)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
+    const int64_t token = item / runs;
+    if (token >= a.tokens) return;
+    const int h0 = (int)(item % runs) * HEADS + sub;
+    const int64_t b = token / a.T, t = token % a.T;
+
+    const int64_t slot = a.slot[token];
+    const int pos = a.position[token];
+    const bool inside = slot < a.slots && (a.rot == 0 || (pos >= 0 && pos < a.max_position));
+    if (slot >= 0 && !inside && lane == 0) atomicOr(a.status, kStBadIndex);
+    const bool live = slot >= 0 && inside;
+
+    char* q_out = static_cast<char*>(a.q_out) + (b * a.o_batch + t * a.o_token) * ES;
+    if (!live) {
+        for (int r = 0; r < ROUNDS; ++r) {
+            const int h = h0 + r * HPW;
+            if (h < a.Hq) *reinterpret_cast<Raw*>(q_out + (h * a.o_head + e) * ES) = Q::zero();
+        }
+        return;
+    }
+    const char* q = static_cast<const char*>(a.in.q) + (b * a.in.q_batch + t * a.in.q_token) * ES;
+    const char* k = static_cast<const char*>(a.in.k) + (b * a.in.k_batch + t * a.in.k_token) * ES;
+    const char* v = static_cast<const char*>(a.in.v) + (b * a.in.v_batch + t * a.in.v_token) * ES;
+    Raw raw[ROUNDS];
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int h = h0 + r * HPW;
+        const char* src = h < a.Hq           ? q + h * a.in.q_head * ES
+                          : h < a.Hq + a.H   ? k + (h - a.Hq) * a.in.k_head * ES
+                                             : v + (h - a.Hq - a.H) * a.in.v_head * ES;
+        raw[r] = h < heads ? *reinterpret_cast<const Raw*>(src + e * ES) : Q::zero();
+    }
+    float4 c = make_float4(1, 1, 1, 1), s = make_float4(0, 0, 0, 0);
+    int pair = lane;  // the lane that holds the pairs of this lane's elements
+    if (e < a.rot) {
+        const float* cs = a.cos_sin + (int64_t)pos * a.rot;
+        if (INTERLEAVED) {
+            const float2 c2 = *reinterpret_cast<const float2*>(cs + e / 2);
+            const float2 s2 = *reinterpret_cast<const float2*>(cs + a.rot / 2 + e / 2);
+            c = make_float4(c2.x, c2.x, c2.y, c2.y);
+            s = make_float4(-s2.x, s2.x, -s2.y, s2.y);
+        } else {
+            const bool first = e < a.rot / 2;
+            const int i = first ? e : e - a.rot / 2;
+            c = *reinterpret_cast<const float4*>(cs + i);
+            s = *reinterpret_cast<const float4*>(cs + a.rot / 2 + i);
+            if (first) s = make_float4(-s.x, -s.y, -s.z, -s.w);
+            pair = first ? lane + a.rot / 8 : lane - a.rot / 8;
+        }
+    }
+    float4 wq = make_float4(1, 1, 1, 1), wk = wq;
+    if (a.q_weight) wq = Q::wide(*reinterpret_cast<const Raw*>(static_cast<const char*>(a.q_weight) + e * ES));
+    if (a.k_weight) wk = Q::wide(*reinterpret_cast<const Raw*>(static_cast<const char*>(a.k_weight) + e * ES));
+    const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
+    char* key = static_cast<char*>(a.kv.key) + (page * a.kv.key_page + row * a.kv.key_token) * ES;
+    char* value = static_cast<char*>(a.kv.value) + (page * a.kv.value_page + row * a.kv.value_token) * ES;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int h = h0 + r * HPW;
+        if (h - sub >= heads) break;  // the same for the whole warp
+        float4 x = Q::wide(raw[r]);
+        float ss = x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w;
+#pragma unroll
+        for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        const bool is_q = h < a.Hq;
+        if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
+            const float4 w = is_q ? wq : wk;
+            const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
+            x = make_float4(x.x * inv * w.x, x.y * inv * w.y, x.z * inv * w.z, x.w * inv * w.w);
+        }
+        float4 y;
+        if (INTERLEAVED) {
+            y = make_float4(x.y, x.x, x.w, x.z);
+        } else {
+            y.x = __shfl_sync(0xffffffffu, x.x, pair);
+            y.y = __shfl_sync(0xffffffffu, x.y, pair);
+            y.z = __shfl_sync(0xffffffffu, x.z, pair);
+            y.w = __shfl_sync(0xffffffffu, x.w, pair);
+        }
+        if (e < a.rot)
+            x = make_float4(x.x * c.x + y.x * s.x, x.y * c.y + y.y * s.y, x.z * c.z + y.z * s.z, x.w * c.w + y.w * s.w);
+        if (h >= heads) continue;
+        if (is_q)
+            *reinterpret_cast<Raw*>(q_out + (h * a.o_head + e) * ES) = Q::narrow(x);
+        else if (h < a.Hq + a.H)
+            *reinterpret_cast<Raw*>(key + ((h - a.Hq) * a.kv.key_head + e) * ES) = Q::narrow(x);
+        else
+            *reinterpret_cast<Raw*>(value + ((h - a.Hq - a.H) * a.kv.value_head + e) * ES) = raw[r];
+    }
+}
+
+template <int DT, int D, bool I>
+static cudaError_t launch_rope_t(const RopeArgs& a, cudaStream_t s) {
+    const int runs = (a.Hq + 2 * a.H + rope_heads<DT, D>() - 1) / rope_heads<DT, D>();
+    const int64_t warps = a.tokens * runs, per = kRopeThreads / 32;
+    return launch_dependent(rope_kernel<DT, D, I>, dim3((unsigned)((warps + per - 1) / per)), dim3(kRopeThreads), 0, s,
+                            a);
+}
+
+cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, cudaStream_t s) {
+    if (dtype == 1) {
+        if (D == 128) return interleaved ? launch_rope_t<1, 128, true>(a, s) : launch_rope_t<1, 128, false>(a, s);
+        return interleaved ? launch_rope_t<1, 64, true>(a, s) : launch_rope_t<1, 64, false>(a, s);
+    }
+    if (D == 128) return interleaved ? launch_rope_t<0, 128, true>(a, s) : launch_rope_t<0, 128, false>(a, s);
+    return interleaved ? launch_rope_t<0, 64, true>(a, s) : launch_rope_t<0, 64, false>(a, s);
+}
+
+// ---------------------------------------------------------------------------
+// commit.  A thread owns one 16-byte column of (layer, key or value, head) and
+// moves it for all nodes of a request's path.  Places are written in ascending
+// order and node k lies at or behind place k+1, so a batch of loads followed by
+// its stores never overwrites a line that a later batch reads.  Lines already
+// in place are left alone.  The bytes are few: bound by launch and by two
+// dependent rounds of loads (path, table), then HBM.
+// ---------------------------------------------------------------------------
+constexpr int kCommitThreads = 256;
+constexpr int kCommitBatch = 8;
+constexpr int kMaxPath = 128;
+
+__global__ void __launch_bounds__(kCommitThreads) commit_kernel(const CommitArgs a, int cols) {
+    grid_dependency_begin();
+    __shared__ int2 src[kMaxPath], dst[kMaxPath];  // page, row
+    const int tid = threadIdx.x, b = blockIdx.y;
+    const int ctx = a.ctx_len[b], n = a.accepted_len[b];
+    const int64_t capacity = (int64_t)a.max_pages * a.P;
+    unsigned bad = 0;
+    if (n < 0 || n > a.depth) bad = kStBadIndex;
+    if (ctx < 0 || ctx + (int64_t)1 + (n > 0 ? n : 0) > capacity) bad |= kStBadLength;
+    int moves = 0;
+    if (!bad && tid < n) {
+        const int32_t* path = a.accepted_nodes + (int64_t)b * a.depth;
+        const int node = path[tid], before = tid > 0 ? path[tid - 1] : 0;
+        const int64_t from = (int64_t)ctx + node, to = (int64_t)ctx + tid + 1;
+        if (node <= before || node < tid + 1 || node >= a.T) {
+            bad = kStBadIndex;
+        } else if (from >= capacity) {
+            bad = kStBadLength;
+        } else {
+            const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
+            src[tid] = make_int2(table[from / a.P], (int)(from % a.P));
+            dst[tid] = make_int2(table[to / a.P], (int)(to % a.P));
+            if (src[tid].x < 0 || src[tid].x >= a.pages || dst[tid].x < 0 || dst[tid].x >= a.pages) bad = kStBadIndex;
+            moves = from != to;
+        }
+    }
+    if (bad) atomicOr(a.status, bad);
+    const int any_bad = __syncthreads_or(bad != 0);
+    const int any_move = __syncthreads_or(moves);
+    if (blockIdx.x == 0 && tid == 0) a.next_len[b] = any_bad ? ctx : ctx + 1 + n;
+    if (any_bad || !any_move) return;
+
+    const int64_t i = (int64_t)blockIdx.x * kCommitThreads + tid;
+    const int col = (int)(i % cols);
+    const int64_t line = i / cols;
+    const int h = (int)(line % a.H), which = (int)(line / a.H % 2);
+    const int64_t layer = line / a.H / 2;
+    if (layer >= a.layers) return;
+    const int es = a.kv_elem_bytes;
+    char* base = which ? static_cast<char*>(a.kv.value) + (layer * a.value_layer + h * a.kv.value_head) * es
+                       : static_cast<char*>(a.kv.key) + (layer * a.key_layer + h * a.kv.key_head) * es;
+    const int64_t page_stride = (which ? a.kv.value_page : a.kv.key_page) * es;
+    const int64_t row_stride = (which ? a.kv.value_token : a.kv.key_token) * es;
+    base += col * 16;
+    for (int k0 = 0; k0 < n; k0 += kCommitBatch) {
+        uint4 x[kCommitBatch];
+#pragma unroll
+        for (int u = 0; u < kCommitBatch; ++u)
+            if (k0 + u < n)
+                x[u] = *reinterpret_cast<const uint4*>(base + src[k0 + u].x * page_stride + src[k0 + u].y * row_stride);
+#pragma unroll
+        for (int u = 0; u < kCommitBatch; ++u)
+            if (k0 + u < n && (src[k0 + u].x != dst[k0 + u].x || src[k0 + u].y != dst[k0 + u].y))
+                *reinterpret_cast<uint4*>(base + dst[k0 + u].x * page_stride + dst[k0 + u].y * row_stride) = x[u];
+    }
+}
+
+cudaError_t launch_commit(const CommitArgs& a, int line_bytes, cudaStream_t s) {
+    const int cols = line_bytes / 16;
+    const int64_t threads = (int64_t)a.layers * 2 * a.H * cols;
+    return launch_dependent(commit_kernel, dim3((unsigned)((threads + kCommitThreads - 1) / kCommitThreads), a.B),
+                            dim3(kCommitThreads), 0, s, a, cols);
+}
+
+}  // namespace rheo

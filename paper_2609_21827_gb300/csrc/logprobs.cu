@@ -1,0 +1,350 @@
+// logprobs.cu -- log probabilities of given tokens with rank, entropy and the
+// top alternatives, in one pass over each row's logits.
+//
+// With a running reference m (the largest logit so far), c = log2(e)/T and
+// d = (l - m) c, a thread keeps Z = sum 2^d and W = sum 2^d d; a new reference m'
+// with D = (m - m') c turns them into 2^D Z and 2^D (W + D Z).  Then, in log2 units,
+//   log p(t) = (l_t - m) c - log2 Z,   H = log2 Z - W / Z.
+// The difference is taken before the product, so that logits near the type's
+// lowest value (a common mask) neither overflow nor lose their order.
+// The rank counts l > l_t, and l = l_t at smaller ids.
+// Top alternatives: the k-th largest of the threads' own maxima bounds the row's
+// k-th largest from below, so the stream needs nothing but each thread's
+// maximum; afterwards only the stripes of the k threads at or above the bound
+// are read again (from L2), and the few logits found there are ranked.  Keys are
+// (logit, -id) in 64 bits, all different, so ties need no care.
+// A row is cut into segments where there are fewer rows than SMs; the last CTA of
+// a row joins them.
+#include "cache_kernels.h"
+#include "rheo_device.cuh"
+#include "rheo_kernels.h"
+
+namespace rheo {
+
+constexpr int kLpThreads = 512;
+constexpr int kLpWarps = kLpThreads / 32;
+constexpr int kLpBatch = 4;       // vectors in flight a thread
+constexpr int kLpCand = 2048;     // candidates ranked at a time
+constexpr int kLpMaxSegments = kLpCand / kMaxTop;
+constexpr float kLpFloor = -10000.0f;  // 2^floor = 0: keeps (-inf) * 0 out of W
+
+struct LpSums {
+    float m, z, w;  // reference (a logit; -inf: nothing yet), Z, W
+};
+
+__device__ __forceinline__ LpSums lp_join(LpSums a, LpSums b, float c) {
+    const float m = fmaxf(a.m, b.m);
+    if (m == -INFINITY) return LpSums{m, a.z + b.z, a.w + b.w};  // zeros, or a NaN to keep
+    const float da = fmaxf((a.m - m) * c, kLpFloor), db = fmaxf((b.m - m) * c, kLpFloor);
+    const float ea = fast_exp2(da), eb = fast_exp2(db);
+    return LpSums{m, ea * a.z + eb * b.z, ea * (a.w + da * a.z) + eb * (b.w + db * b.z)};
+}
+
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// The next float below x; NaN for -inf.
+__device__ __forceinline__ float below(float x) {
+    if (x == -INFINITY) return __uint_as_float(0x7FC00000u);
+    if (x == 0.0f) return __uint_as_float(0x80000001u);
+    const uint32_t u = __float_as_uint(x);
+    return __uint_as_float(u & 0x80000000u ? u + 1 : u - 1);
+}
+
+// Larger for larger logits, then for smaller ids; 0 for -inf.
+__device__ __forceinline__ unsigned long long lp_key(float v, int id) {
+    if (v == -INFINITY) return 0ull;
+    return ((unsigned long long)ord_f32(v) << 32) | (0xFFFFFFFFu - (uint32_t)id);
+}
+__device__ __forceinline__ int lp_id(unsigned long long key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
+__device__ __forceinline__ float lp_value(unsigned long long key) { return Elem<0>::value_of_key((uint32_t)(key >> 32)); }
+
+struct LpShared {
+    unsigned long long cand[kLpCand];
+    unsigned long long best[kLpThreads];
+    unsigned long long top[kMaxTop];
+    unsigned long long red[kLpWarps];
+    LpSums sums[kLpWarps];
+    int count[kLpWarps];
+    int stripe[kMaxTop];
+    int n_stripe, n_cand, last;
+    unsigned long long floor;
+};
+
+// Ranks sm.cand[0..n) and leaves the k first in sm.top (0 where there are fewer).
+__device__ __forceinline__ void lp_rank(LpShared& sm, int n, int k) {
+    const int tid = threadIdx.x;
+    if (tid < k) sm.top[tid] = 0ull;
+    __syncthreads();
+    for (int i = tid; i < n; i += kLpThreads) {
+        const unsigned long long mine = sm.cand[i];
+        if (mine == 0ull) continue;
+        int above = 0;
+        for (int j = 0; j < n; ++j) above += sm.cand[j] > mine;
+        if (above < k) sm.top[above] = mine;
+    }
+    __syncthreads();
+}
+
+template <int DT, bool ALIGNED>
+__global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a) {
+    grid_dependency_begin();
+    using E = Elem<DT>;
+    constexpr int VEC = E::VEC;
+    __shared__ LpShared sm;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int i = blockIdx.x / a.segments, seg = blockIdx.x % a.segments;
+    const int V = a.V, k = a.k;
+
+    int64_t r = a.row_index ? a.row_index[i] : i;
+    if (r < -1 || r >= a.logit_rows) {
+        if (tid == 0) atomicOr(a.status, kStBadIndex);
+        r = -1;
+    }
+    if (r < 0) {
+        if (seg == 0) {
+            if (tid == 0) {
+                a.out.logprob[i] = 0.0f;
+                a.out.rank[i] = -1;
+                a.out.entropy[i] = 0.0f;
+            }
+            if (tid < k) {
+                a.out.top_ids[(int64_t)i * k + tid] = -1;
+                a.out.top_logprobs[(int64_t)i * k + tid] = -INFINITY;
+            }
+        }
+        return;
+    }
+    int tk = a.token[i];
+    if (tk < -1 || tk >= V) {
+        if (tid == 0) atomicOr(a.status, kStBadIndex);
+        tk = -1;
+    }
+    float T = a.temperature ? a.temperature[i / a.per_t] : 1.0f;
+    if (!(T > 0.0f && T < INFINITY)) {
+        if (tid == 0) atomicOr(a.status, kStBadTemperature);
+        T = 1.0f;
+    }
+    const float c = fminf(1.4426950408889634f / T, 3.0e38f);
+    const char* row = a.logits + r * a.row_stride_bytes;
+    const float lt = tk >= 0 ? E::value(E::load_scalar(row, tk)) : INFINITY;
+    const float lt_below = tk >= 0 ? below(lt) : INFINITY;
+    const int tv = tk >= 0 ? tk / VEC : -1;  // the vector that holds the token
+    const int vectors = (V + VEC - 1) / VEC;
+    const int v0 = (int)((int64_t)seg * vectors / a.segments), v1 = (int)((int64_t)(seg + 1) * vectors / a.segments);
+
+    LpSums s{-INFINITY, 0.0f, 0.0f};
+    int mv = -1, count = 0;  // the vector in which the reference was met first
+    for (int base = v0 + tid; base < v1; base += kLpThreads * kLpBatch) {
+        uint4 x[kLpBatch];
+#pragma unroll
+        for (int u = 0; u < kLpBatch; ++u)
+            if (base + u * kLpThreads < v1) x[u] = load_vec<DT, ALIGNED>(row, (int64_t)(base + u * kLpThreads) * VEC, V);
+#pragma unroll
+        for (int u = 0; u < kLpBatch; ++u) {
+            const int v = base + u * kLpThreads;
+            if (v >= v1) break;
+            float l[VEC], vm = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                l[e] = E::value(E::raw(x[u], e));
+                vm = max_nan(vm, l[e]);
+            }
+            if (!(vm <= s.m)) {
+                const float d = fmaxf((s.m - vm) * c, kLpFloor), f = fast_exp2(d);
+                s.w = f * (s.w + d * s.z);
+                s.z *= f;
+                s.m = vm;
+                mv = v;
+            }
+            if (s.m == -INFINITY) {
+                // nothing but -inf so far: it adds nothing to the sums
+                if (tk >= 0)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        count += v == tv ? (l[e] == lt && v * VEC + e < tk) : v < tv ? !(l[e] <= lt_below) : 0;
+                continue;
+            }
+            const float cut = v < tv ? lt_below : lt;
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float d = max_nan((l[e] - s.m) * c, kLpFloor), p = fast_exp2(d);
+                s.z += p;
+                s.w = fmaf(p, d, s.w);
+                count += !(l[e] <= cut);
+            }
+            if (v == tv)
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) count += l[e] == lt && v * VEC + e < tk;
+        }
+    }
+
+    const float mx = s.m;  // this thread's largest logit
+
+    // sums and count over the block
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        LpSums t{__shfl_xor_sync(0xffffffffu, s.m, o), __shfl_xor_sync(0xffffffffu, s.z, o),
+                 __shfl_xor_sync(0xffffffffu, s.w, o)};
+        s = lp_join(s, t, c);
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (lane == 0) {
+        sm.sums[warp] = s;
+        sm.count[warp] = count;
+    }
+    if (k > 0) {
+        unsigned long long key = 0ull;
+        if (mv >= 0 && mx > -INFINITY) {
+            const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)mv * VEC, V);
+            int id = -1;
+#pragma unroll
+            for (int e = VEC - 1; e >= 0; --e)
+                if (E::value(E::raw(x, e)) == mx) id = mv * VEC + e;
+            key = lp_key(mx, id);
+        }
+        sm.best[tid] = key;
+        if (tid == 0) {
+            sm.n_stripe = sm.n_cand = 0;
+            sm.floor = 1ull;
+        }
+        __syncthreads();
+        if (key != 0ull) {
+            int above = 0;
+#pragma unroll 8
+            for (int j = 0; j < kLpThreads; ++j) above += sm.best[j] > key;
+            if (above < k) sm.stripe[atomicAdd(&sm.n_stripe, 1)] = tid;
+            if (above == k - 1) sm.floor = key;
+        }
+        __syncthreads();
+        const unsigned long long floor = sm.floor;
+        const int n_stripe = sm.n_stripe;
+        for (int q = warp; q < n_stripe; q += kLpWarps) {
+            for (int v = v0 + sm.stripe[q] + lane * kLpThreads; v < v1; v += 32 * kLpThreads) {
+                const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
+                    if (y >= floor) {
+                        const int at = atomicAdd(&sm.n_cand, 1);
+                        if (at < kLpCand) sm.cand[at] = y;
+                    }
+                }
+            }
+        }
+        __syncthreads();
+        const int n = sm.n_cand;
+        if (n <= kLpCand) {
+            lp_rank(sm, n, k);
+        } else {
+            // more than the buffer holds (stripes full of large logits): one round of maxima an alternative
+            unsigned long long last = ~0ull;
+            for (int round = 0; round < k; ++round) {
+                unsigned long long top = 0ull;
+                for (int q = warp; q < n_stripe; q += kLpWarps)
+                    for (int v = v0 + sm.stripe[q] + lane * kLpThreads; v < v1; v += 32 * kLpThreads) {
+                        const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
+                            if (y < last && y > top) top = y;
+                        }
+                    }
+                top = warp_max_u64(top);
+                if (lane == 0) sm.red[warp] = top;
+                __syncthreads();
+                top = sm.red[0];
+                for (int w = 1; w < kLpWarps; ++w) top = sm.red[w] > top ? sm.red[w] : top;
+                if (tid == 0) sm.top[round] = top;
+                last = top;
+                __syncthreads();
+            }
+        }
+    }
+    __syncthreads();
+    if (a.segments > 1) {
+        const int64_t part = (int64_t)i * a.segments + seg;
+        if (tid < k) a.part_key[part * kMaxTop + tid] = sm.top[tid];
+        if (tid == 0) {
+            s = sm.sums[0];
+            count = sm.count[0];
+            for (int w = 1; w < kLpWarps; ++w) {
+                s = lp_join(s, sm.sums[w], c);
+                count += sm.count[w];
+            }
+            *reinterpret_cast<float4*>(a.part + part * 4) = make_float4(s.m, s.z, s.w, __int_as_float(count));
+        }
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) sm.last = atomicAdd(&a.ticket[i], 1u) == (unsigned)a.segments - 1;
+        __syncthreads();
+        if (!sm.last) return;
+        __threadfence();
+        if (tid == 0) a.ticket[i] = 0;
+        const int64_t first = (int64_t)i * a.segments;
+        if (k > 0) {
+            for (int j = tid; j < a.segments * k; j += kLpThreads)
+                sm.cand[j] = __ldcg(a.part_key + (first + j / k) * kMaxTop + j % k);
+            __syncthreads();
+            lp_rank(sm, a.segments * k, k);
+        }
+    }
+    if (tid < 32) {
+        // the sums once more, by one warp in a fixed order
+        LpSums t{-INFINITY, 0.0f, 0.0f};
+        int n = 0;
+        if (a.segments > 1) {
+            for (int j = lane; j < a.segments; j += 32) {
+                const float4 x = __ldcg(reinterpret_cast<const float4*>(a.part + ((int64_t)i * a.segments + j) * 4));
+                t = lp_join(t, LpSums{x.x, x.y, x.z}, c);
+                n += __float_as_int(x.w);
+            }
+        } else if (lane < kLpWarps) {
+            t = sm.sums[lane];
+            n = sm.count[lane];
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1)
+            t = lp_join(t, LpSums{__shfl_xor_sync(0xffffffffu, t.m, o), __shfl_xor_sync(0xffffffffu, t.z, o),
+                                  __shfl_xor_sync(0xffffffffu, t.w, o)}, c);
+        n = __reduce_add_sync(0xffffffffu, n);
+        const float lz = log2f(t.z);
+        constexpr float kLn2 = 0.69314718055994531f;
+        if (lane == 0) {
+            if (!(t.z == t.z) || t.m == INFINITY) atomicOr(a.status, kStBadLogit);
+            else if (t.m == -INFINITY) atomicOr(a.status, kStEmptyRow);
+            a.out.logprob[i] = tk >= 0 ? (lt - t.m) / T - lz * kLn2 : 0.0f;
+            a.out.rank[i] = tk >= 0 ? n : -1;
+            a.out.entropy[i] = (lz - t.w / t.z) * kLn2;
+        }
+        if (lane < k) {
+            const unsigned long long y = sm.top[lane];
+            a.out.top_ids[(int64_t)i * k + lane] = y ? lp_id(y) : -1;
+            a.out.top_logprobs[(int64_t)i * k + lane] = y ? (lp_value(y) - t.m) / T - lz * kLn2 : -INFINITY;
+        }
+    }
+}
+
+// CTAs a row: all SMs share the rows when there are few, with two full batches a
+// thread at least.
+int logprob_segments(int rows, int vocab, int dtype, int sms) {
+    const int vec = dtype == 1 ? 8 : 4, vectors = (vocab + vec - 1) / vec;
+    int n = sms / rows, most = vectors / (2 * kLpThreads);
+    n = n < most ? n : most;
+    n = n < kLpMaxSegments ? n : kLpMaxSegments;
+    return n < 1 ? 1 : n;
+}
+
+template <int DT, bool ALIGNED> static cudaError_t launch_lp(const LogprobArgs& a, cudaStream_t s) {
+    return launch_dependent(logprob_kernel<DT, ALIGNED>, dim3((unsigned)a.R * a.segments), dim3(kLpThreads), 0, s, a);
+}
+
+cudaError_t launch_logprobs(const LogprobArgs& a, int dtype, bool aligned, cudaStream_t s) {
+    if (dtype == 1) return aligned ? launch_lp<1, true>(a, s) : launch_lp<1, false>(a, s);
+    return aligned ? launch_lp<0, true>(a, s) : launch_lp<0, false>(a, s);
+}
+
+}  // namespace rheo

@@ -36,6 +36,9 @@ enum : uint32_t {
     kStEmptyRow = 2u,
     kStBadTemperature = 4u,
     kStInternal = 8u,
+    kStBadLength = 16u,
+    kStNoPages = 32u,
+    kStBadIndex = 64u,
 };
 
 enum : int { kTagSample = 1, kTagVerify = 2, kTagResidual = 3 };

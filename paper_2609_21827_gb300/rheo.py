@@ -18,11 +18,13 @@ RHEO_F32, RHEO_BF16 = 0, 1
 RHEO_OK, RHEO_EINVAL, RHEO_ELAUNCH, RHEO_ETOOLARGE = 0, -1, -2, -3
 VERIFY_RHEO, VERIFY_RRSW, VERIFY_ONEHOT = 0, 1, 2
 STATUS_BAD_LOGIT, STATUS_EMPTY_ROW, STATUS_BAD_TEMPERATURE, STATUS_INTERNAL = 1, 2, 4, 8
+STATUS_BAD_LENGTH, STATUS_NO_PAGES, STATUS_BAD_INDEX = 16, 32, 64
 SLOT_ROOT, SLOT_LEAD, SLOT_SAMPLED, SLOT_FILL = 0, 1, 2, 3
 
 EXPORTS = ("rheo_sizes", "rheo_workspace_init", "rheo_expand", "rheo_prune", "rheo_verify", "rheo_verify_static",
            "rheo_tree_attention", "rheo_verify_variant", "rheo_verify_full",
-           "rheo_get_status")
+           "rheo_get_status", "rheo_cache_sizes", "rheo_scratch_init", "rheo_scratch_status", "rheo_cache_reserve",
+           "rheo_qk_norm_rope", "rheo_tree_attend", "rheo_cache_commit", "rheo_logprob_sizes", "rheo_token_logprobs")
 
 
 class RheoError(RuntimeError):
@@ -55,6 +57,38 @@ class _VerifyOut(ctypes.Structure):
 
 class _TreeAttn(ctypes.Structure):
     _fields_ = [(n, _VP) for n in ("mask", "position", "retrieve", "n_leaves")]
+
+
+class _CacheConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "tokens", "pages", "page_size", "max_pages", "q_heads",
+                                              "kv_heads", "head_dim", "dtype")]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("block_table", "n_pages", "free_list", "n_free")]
+
+
+class _KV(ctypes.Structure):
+    _fields_ = [("key", _VP), ("value", _VP)] + [(n, ctypes.c_int64) for n in (
+        "key_page", "key_head", "key_token", "value_page", "value_head", "value_token")]
+
+
+class _QKV(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in "qkv"] + [(f"{n}_{d}", ctypes.c_int64) for n in "qkv"
+                                            for d in ("batch", "token", "head")]
+
+
+class _AttendIO(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("q", "out", "lse")] + [(f"{n}_{d}", ctypes.c_int64) for n in ("q", "out")
+                                                          for d in ("batch", "token", "head")]
+
+
+class _LogprobConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "vocab", "top", "dtype", "rows_per_temperature")]
+
+
+class _Logprobs(ctypes.Structure):
+    _fields_ = [(n, _VP) for n in ("logprob", "rank", "entropy", "top_ids", "top_logprobs")]
 
 
 _lib = None
@@ -90,6 +124,19 @@ def lib():
                                        ctypes.POINTER(_Tree), ctypes.POINTER(_Pruned), ctypes.POINTER(_VerifyOut),
                                        _VP, _VP]
         L.rheo_tree_attention.argtypes = [C, ctypes.POINTER(_Pruned), ctypes.POINTER(_TreeAttn), _VP, _VP]
+        K, i32, i64, f32 = ctypes.POINTER(_CacheConfig), ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+        KV, PG = ctypes.POINTER(_KV), ctypes.POINTER(_Pages)
+        L.rheo_cache_sizes.argtypes = [K, ctypes.POINTER(ctypes.c_size_t)]
+        L.rheo_scratch_init.argtypes = [_VP, ctypes.c_size_t, _VP]
+        L.rheo_scratch_status.argtypes = [_VP, _VP, ctypes.POINTER(i32)]
+        L.rheo_cache_reserve.argtypes = [K, _VP, _VP, _VP, PG, PG, _VP, _VP, _VP, _VP]
+        L.rheo_qk_norm_rope.argtypes = [K, ctypes.POINTER(_QKV), _VP, _VP, f32, _VP, i32, i32, i32, _VP, _VP, KV, _VP,
+                                        i64, i64, i64, _VP, _VP]
+        L.rheo_tree_attend.argtypes = [K, ctypes.POINTER(_AttendIO), KV, _VP, _VP, _VP, _VP, f32, _VP, _VP]
+        L.rheo_cache_commit.argtypes = [K, i32, KV, i64, i64, _VP, _VP, _VP, _VP, i32, _VP, _VP, _VP]
+        L.rheo_logprob_sizes.argtypes = [ctypes.POINTER(_LogprobConfig), ctypes.POINTER(ctypes.c_size_t)]
+        L.rheo_token_logprobs.argtypes = [ctypes.POINTER(_LogprobConfig), _VP, i64, i64, _VP, _VP, _VP,
+                                          ctypes.POINTER(_Logprobs), _VP, _VP]
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -337,5 +384,307 @@ def status(cfg: Config, ws: Workspace, stream=None) -> int:
     """Synchronise the stream, return and clear the device status word."""
     st = ctypes.c_int32()
     _check(lib().rheo_get_status(ctypes.byref(cfg.c()), ws.ptr(), _stream(stream), ctypes.byref(st)),
-           "rheo_get_status")
+           "rheo_get_status", "rheo_cache_sizes", "rheo_scratch_init", "rheo_scratch_status", "rheo_cache_reserve",
+           "rheo_qk_norm_rope", "rheo_tree_attend", "rheo_cache_commit", "rheo_logprob_sizes", "rheo_token_logprobs")
     return st.value
+
+
+# ---------------------------------------------------------------------------
+# The target forward over the pruned tree, with a paged key/value cache, and the
+# log probabilities of given tokens (include/rheo.h has the definitions).
+# ---------------------------------------------------------------------------
+
+_CODES = {"bf16": (RHEO_BF16, torch.bfloat16), "f32": (RHEO_F32, torch.float32)}
+
+
+def _dtype_of(name: str):
+    if name not in _CODES:
+        raise RheoError(f"dtype {name!r}: 'bf16' or 'f32' is wanted")
+    return _CODES[name]
+
+
+@dataclass(frozen=True)
+class CacheConfig:
+    """Sizes of the cache functions (include/rheo.h rheo_cache_config): up to `tokens` new tokens
+    (a pruned tree: budget + 1) of each of `batch` requests, over `pages` pages of `page_size`."""
+
+    batch: int
+    tokens: int
+    pages: int
+    page_size: int
+    max_pages: int
+    q_heads: int
+    kv_heads: int
+    head_dim: int
+    dtype: str = "bf16"
+
+    def __post_init__(self):
+        code, torch_dtype = _dtype_of(self.dtype)
+        c = _CacheConfig(self.batch, self.tokens, self.pages, self.page_size, self.max_pages, self.q_heads,
+                         self.kv_heads, self.head_dim, code)
+        object.__setattr__(self, "torch_dtype", torch_dtype)
+        object.__setattr__(self, "_c", c)
+        object.__setattr__(self, "_ref", ctypes.byref(c))
+        object.__setattr__(self, "_bytes", None)
+
+    def scratch_bytes(self) -> int:
+        if self._bytes is None:
+            n = ctypes.c_size_t()
+            _check(lib().rheo_cache_sizes(self._ref, ctypes.byref(n)), "rheo_cache_sizes")
+            object.__setattr__(self, "_bytes", n.value)
+        return self._bytes
+
+
+@dataclass(frozen=True)
+class LogprobConfig:
+    """Sizes of token_logprobs (include/rheo.h rheo_logprob_config)."""
+
+    rows: int
+    vocab: int
+    top: int = 0
+    dtype: str = "bf16"
+    rows_per_temperature: int = 1
+
+    def __post_init__(self):
+        code, torch_dtype = _dtype_of(self.dtype)
+        c = _LogprobConfig(self.rows, self.vocab, self.top, code, self.rows_per_temperature)
+        object.__setattr__(self, "torch_dtype", torch_dtype)
+        object.__setattr__(self, "_c", c)
+        object.__setattr__(self, "_ref", ctypes.byref(c))
+        object.__setattr__(self, "_bytes", None)
+
+    def scratch_bytes(self) -> int:
+        if self._bytes is None:
+            n = ctypes.c_size_t()
+            _check(lib().rheo_logprob_sizes(self._ref, ctypes.byref(n)), "rheo_logprob_sizes")
+            object.__setattr__(self, "_bytes", n.value)
+        return self._bytes
+
+
+class _Scratch:
+    """A scratch buffer, zeroed when made; one for each stream whose calls may overlap."""
+
+    def __init__(self, cfg, device="cuda", stream=None):
+        self.nbytes = cfg.scratch_bytes()
+        self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
+        self._ptr = self.buf.data_ptr()
+        self.init(stream)
+
+    def of(self, cfg) -> int:
+        """The buffer's pointer, if it is large enough for cfg."""
+        if self.nbytes < cfg.scratch_bytes():
+            raise RheoError(f"the workspace holds {self.nbytes} bytes, {cfg.scratch_bytes()} are wanted")
+        return self._ptr
+
+    def init(self, stream=None):
+        _check(lib().rheo_scratch_init(self._ptr, self.nbytes, _stream(stream)), "rheo_scratch_init")
+
+    def ptr(self) -> int:
+        return self._ptr
+
+
+class CacheWorkspace(_Scratch):
+    pass
+
+
+class LogprobWorkspace(_Scratch):
+    pass
+
+
+def scratch_status(ws: _Scratch, stream=None) -> int:
+    """Synchronise the stream, return and clear the status word of a cache or log-probability workspace."""
+    st = ctypes.c_int32()
+    _check(lib().rheo_scratch_status(ws.ptr(), _stream(stream), ctypes.byref(st)), "rheo_scratch_status")
+    return st.value
+
+
+def _want(x: torch.Tensor, name: str, dtype, shape) -> int:
+    """The pointer of a contiguous CUDA tensor of this type and shape."""
+    if x.dtype != dtype or not x.is_cuda or tuple(x.shape) != shape or not x.is_contiguous():
+        raise RheoError(f"{name}: a contiguous CUDA tensor of {dtype} and shape {list(shape)} is wanted, "
+                        f"got {x.dtype} {list(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+def _want_opt(x, name: str, dtype, shape) -> int:
+    return 0 if x is None else _want(x, name, dtype, shape)
+
+
+def _want_strided(x: torch.Tensor, name: str, dtype, shape) -> tuple:
+    """The pointer and the strides but the last of a CUDA tensor whose last dimension is contiguous."""
+    if x.dtype != dtype or not x.is_cuda or tuple(x.shape) != shape:
+        raise RheoError(f"{name}: a CUDA tensor of {dtype} and shape {list(shape)} is wanted, "
+                        f"got {x.dtype} {list(x.shape)} on {x.device}")
+    st = x.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        raise RheoError(f"{name}: the last dimension has to be contiguous")
+    return x.data_ptr(), st[:-1]
+
+
+class Pages:
+    """Pages of the requests and the stack of free ones.  Without arguments every page is free
+    (page 0 on top); given tensors are used as they are."""
+
+    def __init__(self, cfg: CacheConfig, device="cuda", block_table=None, n_pages=None, free_list=None, n_free=None):
+        i32 = torch.int32
+        if block_table is None:
+            block_table = torch.full((cfg.batch, cfg.max_pages), -1, dtype=i32, device=device)
+        if n_pages is None:
+            n_pages = torch.zeros(cfg.batch, dtype=i32, device=device)
+        if free_list is None:
+            free_list = torch.arange(cfg.pages - 1, -1, -1, dtype=i32, device=device)
+        if n_free is None:
+            n_free = torch.full((1,), cfg.pages, dtype=i32, device=device)
+        self.block_table, self.n_pages, self.free_list, self.n_free = block_table, n_pages, free_list, n_free
+
+    def c(self, cfg: CacheConfig) -> _Pages:
+        i32 = torch.int32
+        return _Pages(_want(self.block_table, "block_table", i32, (cfg.batch, cfg.max_pages)),
+                      _want(self.n_pages, "n_pages", i32, (cfg.batch,)),
+                      _want(self.free_list, "free_list", i32, (cfg.pages,)),
+                      _want(self.n_free, "n_free", i32, (1,)))
+
+
+class CachePlan:
+    """Slots [B, T] (int64) and positions [B, T] (int32) of a call's new tokens."""
+
+    def __init__(self, cfg: CacheConfig, device="cuda", slot=None, position=None):
+        shape = (cfg.batch, cfg.tokens)
+        self.slot = torch.full(shape, -1, dtype=torch.int64, device=device) if slot is None else slot
+        self.position = torch.full(shape, -1, dtype=torch.int32, device=device) if position is None else position
+
+
+def make_cache(cfg: CacheConfig, layers: int = 1, device="cuda"):
+    """Zeroed key and value pools [layers, pages, kv_heads, page_size, head_dim]."""
+    shape = (layers, cfg.pages, cfg.kv_heads, cfg.page_size, cfg.head_dim)
+    return (torch.zeros(shape, dtype=cfg.torch_dtype, device=device),
+            torch.zeros(shape, dtype=cfg.torch_dtype, device=device))
+
+
+def _kv(cfg: CacheConfig, key: torch.Tensor, value: torch.Tensor, layers=None):
+    shape = (cfg.pages, cfg.kv_heads, cfg.page_size, cfg.head_dim)
+    if layers is not None:
+        shape = (layers,) + shape
+    kp, ks = _want_strided(key, "key cache", cfg.torch_dtype, shape)
+    vp, vs = _want_strided(value, "value cache", cfg.torch_dtype, shape)
+    if layers is None:
+        return _KV(kp, vp, *ks, *vs)
+    return _KV(kp, vp, *ks[1:], *vs[1:]), ks[0], vs[0]
+
+
+def cache_reserve(cfg: CacheConfig, ctx_len: torch.Tensor, pages: Pages, plan: CachePlan, ws: CacheWorkspace,
+                  new_len: torch.Tensor = None, depth: torch.Tensor = None, out: Pages = None, stream=None) -> None:
+    """rheo_cache_reserve: pages for ctx_len + new_len tokens a request, slots and positions of the new ones.
+    `pages` is updated in place, or stays as it is and `out` receives the new state."""
+    B, T, i32 = cfg.batch, cfg.tokens, torch.int32
+    before = pages.c(cfg)
+    after = before if out is None or out is pages else out.c(cfg)
+    _check(lib().rheo_cache_reserve(
+        cfg._ref, _want(ctx_len, "ctx_len", i32, (B,)), _want_opt(new_len, "new_len", i32, (B,)),
+        _want_opt(depth, "depth", i32, (B, T)), ctypes.byref(before), ctypes.byref(after),
+        _want(plan.slot, "slot", torch.int64, (B, T)), _want(plan.position, "position", i32, (B, T)), ws.of(cfg),
+        _stream(stream)), "rheo_cache_reserve")
+
+
+def qk_norm_rope(cfg: CacheConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_weight, k_weight, cos_sin,
+                 plan: CachePlan, key_cache: torch.Tensor, value_cache: torch.Tensor, q_out: torch.Tensor,
+                 ws: CacheWorkspace, eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
+    """rheo_qk_norm_rope: q [B, T, q_heads, D], k and v [B, T, kv_heads, D] of one layer; weights [D] or None (no
+    norm); cos_sin [positions, rot] fp32 (cosines, then sines) or None (no rotation).  Queries go to q_out (may be
+    q), keys and values to the caches [pages, kv_heads, page_size, D] at plan.slot."""
+    B, T, D, dt = cfg.batch, cfg.tokens, cfg.head_dim, cfg.torch_dtype
+    qp, qs = _want_strided(q, "q", dt, (B, T, cfg.q_heads, D))
+    kp, ks = _want_strided(k, "k", dt, (B, T, cfg.kv_heads, D))
+    vp, vs = _want_strided(v, "v", dt, (B, T, cfg.kv_heads, D))
+    op, os_ = _want_strided(q_out, "q_out", dt, (B, T, cfg.q_heads, D))
+    if op == qp and os_ != qs:
+        raise RheoError("q_out on q's memory needs q's strides")
+    most = rot = table = 0
+    if cos_sin is not None:
+        if cos_sin.dim() != 2:
+            raise RheoError("cos_sin: [positions, rot] is wanted")
+        most, rot = cos_sin.shape
+        table = _want(cos_sin, "cos_sin", torch.float32, (most, rot))
+    kv = _kv(cfg, key_cache, value_cache)
+    x = _QKV(qp, kp, vp, *qs, *ks, *vs)
+    _check(lib().rheo_qk_norm_rope(
+        cfg._ref, ctypes.byref(x), _want_opt(q_weight, "q_weight", dt, (D,)), _want_opt(k_weight, "k_weight", dt, (D,)),
+        eps, table, most, rot, int(interleaved), _want(plan.slot, "slot", torch.int64, (B, T)),
+        _want(plan.position, "position", torch.int32, (B, T)), ctypes.byref(kv), op, *os_, ws.of(cfg), _stream(stream)),
+        "rheo_qk_norm_rope")
+
+
+def tree_attend(cfg: CacheConfig, q: torch.Tensor, key_cache: torch.Tensor, value_cache: torch.Tensor, pages: Pages,
+                ctx_len: torch.Tensor, out: torch.Tensor, ws: CacheWorkspace, new_len: torch.Tensor = None,
+                mask: torch.Tensor = None, lse: torch.Tensor = None, scale: float = None, stream=None) -> None:
+    """rheo_tree_attend: attention of the new tokens q [B, T, q_heads, D] over the cache, their own keys and values
+    included; mask [B, T, T] uint8 as tree_attention writes it (None: every earlier token); scale: 1/sqrt(D)."""
+    B, T, D, dt = cfg.batch, cfg.tokens, cfg.head_dim, cfg.torch_dtype
+    qp, qs = _want_strided(q, "q", dt, (B, T, cfg.q_heads, D))
+    op, os_ = _want_strided(out, "out", dt, (B, T, cfg.q_heads, D))
+    io = _AttendIO(qp, op, _want_opt(lse, "lse", torch.float32, (B, T, cfg.q_heads)), *qs, *os_)
+    kv = _kv(cfg, key_cache, value_cache)
+    i32 = torch.int32
+    _check(lib().rheo_tree_attend(
+        cfg._ref, ctypes.byref(io), ctypes.byref(kv),
+        _want(pages.block_table, "block_table", i32, (B, cfg.max_pages)), _want(ctx_len, "ctx_len", i32, (B,)),
+        _want_opt(new_len, "new_len", i32, (B,)), _want_opt(mask, "mask", torch.uint8, (B, T, T)),
+        D ** -0.5 if scale is None else scale, ws.of(cfg), _stream(stream)), "rheo_tree_attend")
+
+
+def cache_commit(cfg: CacheConfig, key_cache: torch.Tensor, value_cache: torch.Tensor, pages: Pages,
+                 ctx_len: torch.Tensor, accepted_len: torch.Tensor, accepted_nodes: torch.Tensor,
+                 next_len: torch.Tensor, ws: CacheWorkspace, stream=None) -> None:
+    """rheo_cache_commit: the accepted path's lines move behind the root in caches [layers, pages, kv_heads,
+    page_size, D]; next_len = ctx_len + 1 + accepted_len (another tensor than ctx_len)."""
+    B, i32 = cfg.batch, torch.int32
+    if key_cache.dim() != 5 or accepted_nodes.dim() != 2:
+        raise RheoError("caches [layers, pages, kv_heads, page_size, D] and accepted_nodes [B, depth] are wanted")
+    layers, depth = key_cache.shape[0], accepted_nodes.shape[1]
+    kv, key_layer, value_layer = _kv(cfg, key_cache, value_cache, layers)
+    _check(lib().rheo_cache_commit(
+        cfg._ref, layers, ctypes.byref(kv), key_layer, value_layer,
+        _want(pages.block_table, "block_table", i32, (B, cfg.max_pages)), _want(ctx_len, "ctx_len", i32, (B,)),
+        _want(accepted_len, "accepted_len", i32, (B,)), _want(accepted_nodes, "accepted_nodes", i32, (B, depth)), depth,
+        _want(next_len, "next_len", i32, (B,)), ws.of(cfg), _stream(stream)), "rheo_cache_commit")
+
+
+class Logprobs:
+    """Outputs of token_logprobs."""
+
+    def __init__(self, cfg: LogprobConfig, device="cuda"):
+        R, k = cfg.rows, cfg.top
+        self.logprob = torch.zeros(R, dtype=torch.float32, device=device)
+        self.rank = torch.zeros(R, dtype=torch.int32, device=device)
+        self.entropy = torch.zeros(R, dtype=torch.float32, device=device)
+        self.top_ids = torch.zeros((R, k), dtype=torch.int32, device=device)
+        self.top_logprobs = torch.zeros((R, k), dtype=torch.float32, device=device)
+
+    def c(self, cfg: LogprobConfig) -> _Logprobs:
+        R, k, f32, i32 = cfg.rows, cfg.top, torch.float32, torch.int32
+        return _Logprobs(_want(self.logprob, "logprob", f32, (R,)), _want(self.rank, "rank", i32, (R,)),
+                         _want(self.entropy, "entropy", f32, (R,)), _want(self.top_ids, "top_ids", i32, (R, k)),
+                         _want(self.top_logprobs, "top_logprobs", f32, (R, k)))
+
+
+def token_logprobs(cfg: LogprobConfig, logits: torch.Tensor, tokens: torch.Tensor, out: Logprobs,
+                   ws: LogprobWorkspace, temperature: torch.Tensor = None, rows: torch.Tensor = None,
+                   stream=None) -> None:
+    """rheo_token_logprobs: row i reads row rows[i] (None: i) of logits [..., V] and token tokens[i]; -1 leaves a
+    row or a token out; temperature [ceil(R / rows_per_temperature)] fp32 or None (1)."""
+    R, i32 = cfg.rows, torch.int32
+    if logits.dtype != cfg.torch_dtype or not logits.is_cuda or logits.shape[-1] != cfg.vocab:
+        raise RheoError(f"logits: a CUDA tensor of {cfg.torch_dtype} and {cfg.vocab} columns is wanted")
+    flat = logits if logits.dim() == 2 else logits.reshape(-1, cfg.vocab)
+    if logits.stride(-1) != 1 or flat.data_ptr() != logits.data_ptr():
+        raise RheoError("logits rows must be contiguous and addressable with a single row stride")
+    n = flat.shape[0]
+    if rows is None and n < R:
+        raise RheoError(f"{R} rows are asked for, logits have {n}")
+    groups = -(-R // cfg.rows_per_temperature)
+    c = out.c(cfg)
+    _check(lib().rheo_token_logprobs(
+        cfg._ref, flat.data_ptr(), max(flat.stride(0), cfg.vocab) if n == 1 else flat.stride(0), n,
+        _want_opt(rows, "rows", i32, (R,)), _want(tokens, "tokens", i32, (R,)),
+        _want_opt(temperature, "temperature", torch.float32, (groups,)), ctypes.byref(c), ws.of(cfg), _stream(stream)),
+        "rheo_token_logprobs")
