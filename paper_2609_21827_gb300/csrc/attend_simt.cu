@@ -1,5 +1,5 @@
-// attend_simt.cu -- attention of drafted tokens over the paged cache on the fp32
-// units, and the join of partial sums.
+// attend_simt.cu -- attention of drafted tokens over a paged fp32 cache on the
+// fp32 units, and the join of partial sums of either type.
 //
 // For an item of R query rows and its key tiles of 64: scores s = q k (fp32 FMA
 // on register tiles of R/16 x 4 a thread), running maximum m and sum l a row in
@@ -28,17 +28,6 @@ template <int N> __device__ __forceinline__ void cp_async_wait() {
     asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
-// Four neighbouring outputs.
-template <int DT> __device__ __forceinline__ void store4(void* out, int64_t e, float4 v) {
-    if (DT == 0) {
-        *reinterpret_cast<float4*>(static_cast<float*>(out) + e) = v;
-    } else {
-        const __nv_bfloat162 x = __floats2bfloat162_rn(v.x, v.y), y = __floats2bfloat162_rn(v.z, v.w);
-        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(out) + e) =
-            make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
-    }
-}
-
 template <int D, int R> struct SimtSmem {
     float q[R][D + 4];
     float k[2][kSimtTile][D + 4];
@@ -46,17 +35,17 @@ template <int D, int R> struct SimtSmem {
     float p[R][kSimtTile + 4];
 };
 
-template <int DT, int D, int R>
+template <int D, int R>
 __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const AttendArgs a) {
     grid_dependency_begin();
     extern __shared__ __align__(16) unsigned char raw_smem[];
     SimtSmem<D, R>& sm = *reinterpret_cast<SimtSmem<D, R>*>(raw_smem);
     __shared__ AttendCut cut_s;
-    constexpr int RT = R / 16, DJ = D / 64, ES = DT == 1 ? 2 : 4;
+    constexpr int RT = R / 16, DJ = D / 64, ES = 4;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int rows = a.T * a.G, groups = (rows + R - 1) / R, per = a.H * groups;
     if (tid < 32) {
-        const AttendCut c = attend_cut<kSimtTile>(a, per, blockIdx.x, 1);
+        const AttendCut c = attend_cut<kSimtTile>(a, per, blockIdx.x, a.min_tiles);
         if (tid == 0) cut_s = c;
     }
     __syncthreads();
@@ -92,24 +81,8 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
                                  (page * a.kv.key_page + h * a.kv.key_head + row * a.kv.key_token) * ES + c * 16;
                 const char* vs = static_cast<const char*>(a.kv.value) +
                                  (page * a.kv.value_page + h * a.kv.value_head + row * a.kv.value_token) * ES + c * 16;
-                if (DT == 0) {
-                    cp_async16(&sm.k[buf][kr][c * 4], ks, ok);
-                    cp_async16(&sm.v[buf][kr][c * 4], vs, ok);
-                } else {
-                    uint4 x = make_uint4(0, 0, 0, 0), y = x;
-                    if (ok) {
-                        x = *reinterpret_cast<const uint4*>(ks);
-                        y = *reinterpret_cast<const uint4*>(vs);
-                    }
-                    const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        sm.k[buf][kr][(c * 8 + 2 * u) % D] = bf_lo(xs[u]);
-                        sm.k[buf][kr][(c * 8 + 2 * u + 1) % D] = bf_hi(xs[u]);
-                        sm.v[buf][kr][(c * 8 + 2 * u) % D] = bf_lo(ys[u]);
-                        sm.v[buf][kr][(c * 8 + 2 * u + 1) % D] = bf_hi(ys[u]);
-                    }
-                }
+                cp_async16(&sm.k[buf][kr][c * 4], ks, ok);
+                cp_async16(&sm.v[buf][kr][c * 4], vs, ok);
             }
             cp_async_commit();
         };
@@ -122,12 +95,7 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
             if (row < rows && t < span.add) {
                 const char* src = static_cast<const char*>(a.io.q) +
                                   (b * a.io.q_batch + t * a.io.q_token + (h * a.G + row % a.G) * a.io.q_head + d) * ES;
-                if (DT == 0) {
-                    x = *reinterpret_cast<const float4*>(src);
-                } else {
-                    const uint2 y = *reinterpret_cast<const uint2*>(src);
-                    x = make_float4(bf_lo(y.x), bf_hi(y.x), bf_lo(y.y), bf_hi(y.y));
-                }
+                x = *reinterpret_cast<const float4*>(src);
             }
             *reinterpret_cast<float4*>(&sm.q[r][d]) = x;
         }
@@ -240,14 +208,14 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
             const int t = row / a.G, head = h * a.G + row % a.G;
             const float ll = t < span.add ? l[i] : 0.0f;
             if (!whole) {
-                float* po = a.part_o + (part * R + r) * D;
+                float* po = a.part_o + (part * a.part_rows + r) * D;
 #pragma unroll
                 for (int c = 0; c < DJ; ++c)
                     *reinterpret_cast<float4*>(po + tx * 4 + 64 * c) =
                         make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
                 if (tx == 0) {
-                    a.part_ml[(part * R + r) * 2] = m[i];
-                    a.part_ml[(part * R + r) * 2 + 1] = ll;
+                    a.part_ml[(part * a.part_rows + r) * 2] = m[i];
+                    a.part_ml[(part * a.part_rows + r) * 2 + 1] = ll;
                 }
                 continue;
             }
@@ -258,8 +226,8 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
                 if (ll != 0.0f)
                     y = make_float4(o[i][4 * c] * inv, o[i][4 * c + 1] * inv, o[i][4 * c + 2] * inv,
                                     o[i][4 * c + 3] * inv);
-                store4<DT>(a.io.out, b * a.io.out_batch + t * a.io.out_token + head * a.io.out_head + tx * 4 + 64 * c,
-                           y);
+                *reinterpret_cast<float4*>(static_cast<float*>(a.io.out) + b * a.io.out_batch + t * a.io.out_token +
+                                           head * a.io.out_head + tx * 4 + 64 * c) = y;
             }
             if (a.io.lse && tx == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m[i], ll);
         }
@@ -277,18 +245,18 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
 // Joins the parts of an item that several CTAs summed, in the order of its keys:
 // a warp a row, 8 rows a CTA; grid (CTAs of the sums, rows of an item / 8).
 template <int DT, int D>
-__global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, int R) {
+__global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a) {
     grid_dependency_begin();
     constexpr int W = D / 32;
     const int4 rec = a.join[blockIdx.x];
     const int segments = rec.z, lane = threadIdx.x & 31;
     const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
-    if (segments == 0 || r >= R) return;
-    const int b = rec.x, rows = a.T * a.G, groups = (rows + R - 1) / R;
-    const int h = rec.y / groups, row = rec.y % groups * R + r;
+    if (segments == 0 || r >= a.part_rows) return;
+    const int b = rec.x, rows = a.T * a.G, groups = (rows + a.item_rows - 1) / a.item_rows;
+    const int h = rec.y / groups, row = rec.y % groups * a.item_rows + r;
     if (row >= rows) return;
     const int t = row / a.G, head = h * a.G + row % a.G;
-    const auto part = [&](int s) { return attend_part(blockIdx.x + s, s == 0) * R + r; };
+    const auto part = [&](int s) { return attend_part(blockIdx.x + s, s == 0) * a.part_rows + r; };
     float m = -INFINITY;
     for (int s = lane; s < segments; s += 32) m = fmaxf(m, a.part_ml[part(s) * 2]);
 #pragma unroll
@@ -325,29 +293,41 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a, in
     if (a.io.lse && lane == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m, l);
 }
 
-// 16 rows an item where that holds them all (single tokens and short chains: the
-// products are few and the bytes count), else 64.
-int attend_rows(int dtype, int T, int G) { return (int64_t)T * G <= 16 ? 16 : 64; }
-int attend_ctas(int dtype, int T, int G) { return 152; }
-
-template <int DT, int D, int R> static cudaError_t launch_simt(const AttendArgs& a, cudaStream_t s) {
-    const size_t smem = sizeof(SimtSmem<D, R>);
-    cudaError_t err = cudaFuncSetAttribute(attend_simt_kernel<DT, D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           (int)smem);
-    if (err != cudaSuccess) return err;
-    err = launch_dependent(attend_simt_kernel<DT, D, R>, dim3(a.ctas), dim3(kSimtThreads), smem, s, a);
-    if (err != cudaSuccess) return err;
-    return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, R / 8), dim3(256), 0, s, a, R);
+// fp32: 16 rows an item where that holds them all (single tokens and short
+// chains: the products are few and the bytes count), else 64.  bf16: the 128 rows
+// of one stream, or the 256 of two.
+int attend_item_rows(int dtype, int T, int G) {
+    const int64_t rows = (int64_t)T * G;
+    return dtype == 1 ? (rows <= 128 ? 128 : 256) : (rows <= 16 ? 16 : 64);
+}
+int attend_part_rows(int dtype, int T, int G) {
+    const int64_t rows = ((int64_t)T * G + 7) / 8 * 8, most = attend_item_rows(dtype, T, G);
+    return (int)(rows < most ? rows : most);
 }
 
-template <int DT> static cudaError_t launch_simt_dt(const AttendArgs& a, cudaStream_t s) {
-    if (attend_rows(DT, a.T, a.G) == 16)
-        return a.D == 64 ? launch_simt<DT, 64, 16>(a, s) : launch_simt<DT, 128, 16>(a, s);
-    return a.D == 64 ? launch_simt<DT, 64, 64>(a, s) : launch_simt<DT, 128, 64>(a, s);
+template <int DT, int D> static cudaError_t launch_join(const AttendArgs& a, cudaStream_t s) {
+    return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, (a.part_rows + 7) / 8), dim3(256), 0, s, a);
+}
+
+template <int D, int R> static cudaError_t launch_simt(const AttendArgs& a, cudaStream_t s) {
+    const size_t smem = sizeof(SimtSmem<D, R>);
+    cudaError_t err = cudaFuncSetAttribute(attend_simt_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)smem);
+    if (err != cudaSuccess) return err;
+    return launch_dependent(attend_simt_kernel<D, R>, dim3(a.ctas), dim3(kSimtThreads), smem, s, a);
 }
 
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s) {
-    return dtype == 1 ? launch_simt_dt<1>(a, s) : launch_simt_dt<0>(a, s);
+    cudaError_t err;
+    if (dtype == 1) {
+        err = launch_attend_tc(a, s);
+        if (err != cudaSuccess) return err;
+        return a.D == 64 ? launch_join<1, 64>(a, s) : launch_join<1, 128>(a, s);
+    }
+    if (a.item_rows == 16) err = a.D == 64 ? launch_simt<64, 16>(a, s) : launch_simt<128, 16>(a, s);
+    else err = a.D == 64 ? launch_simt<64, 64>(a, s) : launch_simt<128, 64>(a, s);
+    if (err != cudaSuccess) return err;
+    return a.D == 64 ? launch_join<0, 64>(a, s) : launch_join<0, 128>(a, s);
 }
 
 }  // namespace rheo

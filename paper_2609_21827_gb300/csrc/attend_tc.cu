@@ -1,0 +1,712 @@
+// attend_tc.cu -- attention of drafted tokens over the paged bf16 cache on the
+// tensor cores.
+//
+// One CTA an SM, eleven warps:
+//   warps 0-3, 4-7   two softmax groups, one a stream; thread = query row
+//   warp 8           loads key and value tiles (TMA) into a ring of shared memory
+//   warps 9, 10      issue the matrix products of stream 0 and 1
+// A stream holds up to 128 query rows (token, head of the key/value head): its
+// scores S = Q K^T (128 x 128 fp32) and its sums O (128 x D fp32) lie in tensor
+// memory.  Per key tile: S by tcgen05.mma from shared memory; the group reads its
+// rows, p = 2^(s - m), writes p (bf16) over S; O += P V by tcgen05.mma with P from
+// tensor memory.  While one stream's group computes exponentials, the other
+// stream's products run.
+//   PAIR:   an item has up to 256 rows, each stream takes 128 of them and both
+//           read every key tile: the tile crosses HBM once for all heads and tokens;
+//   !PAIR:  up to 128 rows (single tokens, short chains): the streams take the
+//           key tiles alternately and their sums are joined at the end.
+// The reference m of a row follows its largest score only when that has grown by
+// more than kSlack in log2 units: then O is multiplied in place (rare after the
+// first tiles); until then p <= 2^kSlack, which bf16 and the fp32 sums hold with
+// the same relative error.
+//
+// Places that a token does not see: their scores become -inf before the maximum
+// (tiles that reach past the cached tokens only).  Rows of V that nobody may see
+// (the rest of the last page) are zeroed in shared memory, and so are elements
+// of drafted tokens' V that are not finite (0 * inf would spoil every row); the
+// rows that do see such a token get the element added at the end.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include "attend.cuh"
+#include "rheo_kernels.h"
+
+namespace rheo {
+namespace {
+
+constexpr int kTile = 128;                   // keys a tile
+constexpr int kTcThreads = 11 * 32;
+constexpr float kSlack = 8.0f;
+constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
+constexpr int kDrainLimit = 1 << 16;         // and of a drain after that
+
+template <int D, bool PAIR> struct TcShape {
+    static constexpr int kUnit = kTile * D * 2;       // bytes of a key or value tile
+    static constexpr int kHalves = D / 64;            // 128-byte wide parts of a line
+    // Ring.  !PAIR: a multiple of 4 (key and value tiles of two streams), so that a slot serves one stream only: a
+    // stream that met a slot's barrier every other time could take the phase before last for its own.
+    static constexpr int kUnits = (PAIR ? 5 : 4) * (128 / D);
+    static constexpr int kQ = 128 * D * 2;            // bytes of a stream's queries
+    static constexpr int kO = 256;                    // first tensor-memory column of the sums
+};
+
+struct TcControl {
+    unsigned long long full[10], empty[10];
+    unsigned long long s_full[2], p_ready[2], pv_done[2], drained[2], q_ready, q_taken, all_sync;
+    uint32_t tmem;
+    int abort;
+    int any_odd;          // some drafted value is not finite
+    uint32_t odd[128];    // which drafted tokens'
+    float2 ml[128];       // !PAIR: stream 1's reference and sum, then the weights of both streams
+    AttendCut cut;
+};
+
+template <int D, bool PAIR> constexpr size_t tc_smem_bytes() {
+    using S = TcShape<D, PAIR>;
+    return 1024 + 2 * S::kQ + (size_t)S::kUnits * S::kUnit + sizeof(TcControl);
+}
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void bar_init(unsigned long long* b, int count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(unsigned long long* b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+__device__ __forceinline__ void bar_expect(unsigned long long* b, int bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
+}
+// Waits for the phase of this parity to end (called by whole warps); false, for all lanes, after kWaitLimit polls or
+// where another warp gave up.  A drain (the last waits before the CTA ends) goes on where another warp gave up.
+template <bool DRAIN = false>
+__device__ __forceinline__ bool bar_wait(unsigned long long* b, uint32_t parity, TcControl& c) {
+    const uint32_t at = smem_u32(b);
+    uint32_t done = 0;
+    for (int i = 0; i < kWaitLimit; ++i) {
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done)
+            : "r"(at), "r"(parity)
+            : "memory");
+        if (done || (!DRAIN && (i & 255) == 255 && *(volatile int*)&c.abort)) break;
+        if (DRAIN && i > kDrainLimit && *(volatile int*)&c.abort) break;
+    }
+    if (__all_sync(0xffffffffu, done)) return true;
+    *(volatile int*)&c.abort = 1;
+    return false;
+}
+
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { __syncwarp(); asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { __syncwarp(); asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(unsigned long long* b) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+
+#define RHEO_R32(M) M(0), M(1), M(2), M(3), M(4), M(5), M(6), M(7), M(8), M(9), M(10), M(11), M(12), M(13), M(14), M(15), \
+    M(16), M(17), M(18), M(19), M(20), M(21), M(22), M(23), M(24), M(25), M(26), M(27), M(28), M(29), M(30), M(31)
+#define RHEO_R16(M) M(0), M(1), M(2), M(3), M(4), M(5), M(6), M(7), M(8), M(9), M(10), M(11), M(12), M(13), M(14), M(15)
+
+// 32 columns of this thread's row.
+__device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t at) {
+    __syncwarp();  // .sync.aligned: the whole warp at once
+#define OUT(i) "=r"(r[i])
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : RHEO_R32(OUT)
+        : "r"(at));
+#undef OUT
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+    __syncwarp();
+#define IN(i) "r"(r[i])
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::RHEO_R32(IN),
+        "r"(at)
+        : "memory");
+#undef IN
+}
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
+    __syncwarp();
+#define IN(i) "r"(r[i])
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::RHEO_R16(IN),
+        "r"(at)
+        : "memory");
+#undef IN
+}
+
+// Shared-memory operand in 128-byte swizzle: start, leading and stride byte offsets.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint32_t stride) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(stride >> 4) << 32) |
+           (1ull << 46) | (2ull << 61);
+}
+// bf16 x bf16 -> fp32, M = 128; B along K, or along N.
+__device__ __forceinline__ constexpr uint32_t mma_desc(int n, bool b_along_n) {
+    return (1u << 4) | (1u << 7) | (1u << 10) | (b_along_n ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap* map, int x, int head, int page,
+                                         unsigned long long* bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+        "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(0), "r"(head), "r"(page)
+        : "memory");
+}
+
+// One CTA's run through its items, the same in every warp.
+struct TcWalk {
+    int b, item, tile;
+    int64_t at, end;
+    __device__ __forceinline__ explicit TcWalk(const AttendCut& c) : b(c.b), item(c.item), tile(c.tile), at(c.begin), end(c.end) {}
+    __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ int tiles(int len) const { return max(1, (len + kTile - 1) / kTile); }
+    __device__ __forceinline__ int count(int len) const { return (int)min((int64_t)(tiles(len) - tile), end - at); }
+    __device__ __forceinline__ void next(int n, int per) {
+        at += n;
+        tile = 0;
+        if (++item == per) {
+            item = 0;
+            ++b;
+        }
+    }
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Elements of a pair that are not finite.
+__device__ __forceinline__ uint32_t odd_mask(uint32_t w) {
+    return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+}
+
+// The softmax group of stream `st`.
+template <int D, bool PAIR>
+__device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, char* q_smem, char* ring, int st) {
+    using S = TcShape<D, PAIR>;
+    const int tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
+    const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
+              per = a.H * groups;
+    const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+    const uint32_t t_s = c.tmem + lanes + st * 128, t_o = c.tmem + lanes + S::kO + st * D;
+    const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);  // above 0, so that hidden places stay at -inf
+    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;  // a negative scale turns the queries' signs
+    uint32_t items = 0, tiles_done = 0, syncs = 0, unit0 = 0;
+    auto sync_all = [&]() -> bool {
+        bar_arrive(&c.all_sync);
+        return bar_wait(&c.all_sync, syncs++ & 1, c);
+    };
+    for (TcWalk w(c.cut); w.more();) {
+        const AttendSpan span = attend_span(a, w.b);
+        const int len = span.len(), all = w.tiles(len), n = w.count(len);
+        const int h = w.item / groups, r0 = w.item % groups * item_rows;
+        if (span.bad && threadIdx.x == 0) atomicOr(a.status, kStBadLength);
+        if (!sync_all()) return;  // both streams are through with the last item
+        // and both product warps have seen its start: one without tiles in it waits for nothing else
+        if (items > 0 && !bar_wait(&c.q_taken, (items - 1) & 1, c)) return;
+        ++items;
+        if (threadIdx.x < 128) c.odd[threadIdx.x] = 0;
+        if (threadIdx.x == 0) c.any_odd = 0;
+        {
+            // queries, rows past the item's are 0; 16-byte pieces in the swizzled order of the operand
+            constexpr int C = D / 8;
+            const int in_item = min(item_rows, rows - r0);
+            for (int i = threadIdx.x; i < item_rows * C; i += 256) {
+                const int r = i / C, p = i % C, row = r0 + r, t = row / a.G;
+                uint4 x = make_uint4(0, 0, 0, 0);
+                if (r < in_item && t < span.add)
+                    x = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.io.q) +
+                                                        (w.b * a.io.q_batch + t * a.io.q_token +
+                                                         (h * a.G + row % a.G) * a.io.q_head + p * 8) * 2);
+                x.x ^= flip;
+                x.y ^= flip;
+                x.z ^= flip;
+                x.w ^= flip;
+                const int rr = r & 127;
+                *reinterpret_cast<uint4*>(q_smem + (r >> 7) * S::kQ + (p >> 3) * 16384 + rr * 128 +
+                                          (((p & 7) ^ (rr & 7)) << 4)) = x;
+            }
+            fence_async();
+            tc_fence_before();
+            bar_arrive(&c.q_ready);
+        }
+        const int row = r0 + (PAIR ? st * 128 : 0) + tid, t = row / a.G;
+        const bool live = row < rows && t < span.add;
+        const bool warp_live = __any_sync(0xffffffffu, live);
+        const bool stream_live = PAIR ? r0 + st * 128 < rows : true;
+        float m = -INFINITY, l = 0.0f;
+        int mine = 0;  // tiles of this stream in this item so far
+        for (int q = PAIR ? 0 : st; q < n && stream_live; q += PAIR ? 1 : 2) {
+            const int k0 = (w.tile + q) * kTile;
+            const bool tail = k0 + kTile > span.ctx;
+            uint32_t vis[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
+            if (tail && warp_live) {
+                // the warp's tokens one after the other, 32 places a vote
+                const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
+                for (int tt = (row - lane) / a.G; tt <= t_last; ++tt) {
+                    const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + tt) * a.T : nullptr;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const bool sees = tt < span.add && attend_sees(span, mrow, tt, k0 + 32 * v + lane);
+                        const uint32_t bits = __ballot_sync(0xffffffffu, sees);
+                        if (tt == t) vis[v] = bits;
+                    }
+                }
+            }
+            if (!bar_wait(&c.s_full[st], tiles_done & 1, c)) return;
+            tc_fence_after();
+            if (warp_live) {
+                uint32_t s[4][32];
+#pragma unroll
+                for (int v = 0; v < 4; ++v) tmem_ld32(s[v], t_s + 32 * v);
+                tc_wait_ld();
+                if (tail) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!((vis[v] >> i) & 1u)) s[v][i] = 0xFF800000u;
+                }
+                float top = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[v][i]));
+                top *= sc;
+                if (mine == 0) {
+                    m = top;
+                } else {
+                    const bool grow = top > m + kSlack || (m == -INFINITY && top > m);
+                    if (__any_sync(0xffffffffu, grow)) {
+                        // the sums so far move to the new reference
+                        if (!bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) return;
+                        tc_fence_after();
+                        const float f = !grow || m == -INFINITY ? 1.0f : fast_exp2(m - top);
+#pragma unroll 1
+                        for (int d = 0; d < D; d += 32) {
+                            uint32_t o[32];
+                            tmem_ld32(o, t_o + d);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st32(t_o + d, o);
+                        }
+                        l *= f;
+                        if (grow) m = top;
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.0f : m;
+                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    uint32_t p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x = __uint_as_float(s[v][2 * i]), y = __uint_as_float(s[v][2 * i + 1]);
+                        x = fast_exp2(fmaf(x, sc, -ref));
+                        y = fast_exp2(fmaf(y, sc, -ref));
+                        sum[(2 * i) & 3] += x;
+                        sum[(2 * i + 1) & 3] += y;
+                        p[i] = pack_bf16(x, y);
+                    }
+                    tmem_st16(t_s + 16 * v, p);
+                }
+                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                tc_wait_st();
+            }
+            if (tail) {
+                const uint32_t u = unit0 + 2 * q + 1;  // this tile's values
+                if (!bar_wait(&c.full[u % S::kUnits], (u / S::kUnits) & 1, c)) return;
+                const int place = k0 + tid;
+                if (place >= span.ctx) {
+                    char* line = ring + (u % S::kUnits) * S::kUnit + tid * 128;
+#pragma unroll
+                    for (int p = 0; p < D / 8; ++p) {
+                        uint4* at = reinterpret_cast<uint4*>(line + (p >> 3) * 16384 + (((p & 7) ^ (tid & 7)) << 4));
+                        const uint4 x = *at;
+                        uint4 y = make_uint4(odd_mask(x.x), odd_mask(x.y), odd_mask(x.z), odd_mask(x.w));
+                        if (place >= len) {
+                            if (x.x | x.y | x.z | x.w) *at = make_uint4(0, 0, 0, 0);
+                        } else if (y.x | y.y | y.z | y.w) {
+                            const int j = place - span.ctx;
+                            atomicOr(&c.odd[j >> 5], 1u << (j & 31));
+                            c.any_odd = 1;
+                            __threadfence_block();  // the other stream's group finds either the element or the mark
+                            *at = make_uint4(x.x & ~y.x, x.y & ~y.y, x.z & ~y.z, x.w & ~y.w);
+                        }
+                    }
+                }
+                fence_async();
+            }
+            tc_fence_before();
+            bar_arrive(&c.p_ready[st]);
+            ++tiles_done;
+            ++mine;
+        }
+        unit0 += 2 * n;
+
+        // ---- the item's sums
+        if (mine > 0) {
+            if (!bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) return;
+            tc_fence_after();
+        }
+        float other_f = 0.0f;  // !PAIR: the weight of the other stream's sums
+        char* spare = q_smem + S::kQ;
+        if (!PAIR) {
+            // stream 1 hands its sums to stream 0, 32 columns at a time
+            float2* ml = c.ml;
+            if (st == 1) ml[tid] = make_float2(m, mine > 0 ? l : 0.0f);
+            if (!sync_all()) return;
+            if (st == 0) {
+                const float2 x = ml[tid];
+                if (mine == 0) l = 0.0f;
+                const float mm = fmaxf(m, x.x), ref = mm == -INFINITY ? 0.0f : mm;
+                const float f0 = fast_exp2(m - ref);
+                other_f = fast_exp2(x.x - ref);
+                // this stream's factor is applied below through l and o
+                l = l * f0 + x.y * other_f;
+                m = mm;
+                ml[tid] = make_float2(f0, other_f);
+            }
+        }
+        const bool whole = n == all;
+        const int64_t part = attend_part(blockIdx.x, w.tile == 0);
+        const int r_in = (PAIR ? st * 128 : 0) + tid;
+        const float ll = live ? l : 0.0f;
+        const int head = h * a.G + row % a.G;
+        __threadfence_block();
+        const bool odd = *(volatile int*)&c.any_odd != 0;
+#pragma unroll 1
+        for (int d = 0; d < D; d += 32) {
+            float o[32];
+            if (warp_live && mine > 0) {
+                uint32_t x[32];
+                tmem_ld32(x, t_o + d);
+                tc_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = 0.0f;
+            }
+            if (!PAIR) {
+                float4* x = reinterpret_cast<float4*>(spare);
+                if (st == 1)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i * 128 + tid] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                if (!sync_all()) return;
+                if (st == 0) {
+                    const float f0 = c.ml[tid].x;
+                    const bool has0 = mine > 0, has1 = n > 1;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float4 y = x[i * 128 + tid];
+                        o[4 * i] = (has0 ? o[4 * i] * f0 : 0.0f) + (has1 ? y.x * other_f : 0.0f);
+                        o[4 * i + 1] = (has0 ? o[4 * i + 1] * f0 : 0.0f) + (has1 ? y.y * other_f : 0.0f);
+                        o[4 * i + 2] = (has0 ? o[4 * i + 2] * f0 : 0.0f) + (has1 ? y.z * other_f : 0.0f);
+                        o[4 * i + 3] = (has0 ? o[4 * i + 3] * f0 : 0.0f) + (has1 ? y.w * other_f : 0.0f);
+                    }
+                }
+                if (!sync_all()) return;
+                if (st == 1) continue;
+            }
+            if (odd && live) {
+                // drafted values that are not finite, for the rows that see them
+                const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + t) * a.T : nullptr;
+                for (int word = 0; word < (span.add + 31) / 32; ++word) {
+                    for (uint32_t bits = c.odd[word]; bits; bits &= bits - 1) {
+                        const int j = word * 32 + __ffs(bits) - 1, x = span.ctx + j;
+                        if (!(mrow ? mrow[j] != 0 : j <= t)) continue;
+                        const int64_t page = a.block_table[(int64_t)w.b * a.max_pages + (x >> a.page_shift)];
+                        if (page < 0 || page >= a.pages) continue;
+                        const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.kv.value) + page * a.kv.value_page +
+                                                 h * a.kv.value_head + (x & (a.P - 1)) * a.kv.value_token + d;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float y = __bfloat162float(v[i]);
+                            if (!(fabsf(y) < INFINITY)) o[i] += y;
+                        }
+                    }
+                }
+            }
+            // (no lane leaves the iteration early: the next one begins with a warp-wide load)
+            if (row < rows && whole) {
+                const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+                uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.io.out) + w.b * a.io.out_batch +
+                                                      t * a.io.out_token + head * a.io.out_head + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint4 y = make_uint4(0, 0, 0, 0);
+                    if (ll != 0.0f) {
+                        y.x = pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv);
+                        y.y = pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv);
+                        y.z = pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv);
+                        y.w = pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv);
+                    }
+                    out[i] = y;
+                }
+            } else if (row < rows) {
+                float4* po = reinterpret_cast<float4*>(a.part_o + (part * a.part_rows + r_in) * D + d);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) po[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+        }
+        if ((PAIR || st == 0) && row < rows) {
+            if (whole) {
+                if (a.io.lse) a.io.lse[((int64_t)w.b * a.T + t) * a.H * a.G + head] = attend_lse(m, ll);
+            } else {
+                *reinterpret_cast<float2*>(a.part_ml + (part * a.part_rows + r_in) * 2) = make_float2(m, ll);
+            }
+        }
+        if (!whole && w.tile == 0 && threadIdx.x == 0)
+            a.join[blockIdx.x] = make_int4(w.b, w.item, c.cut.owner(w.at + all - 1) - (int)blockIdx.x + 1, 0);
+        w.next(n, per);
+    }
+}
+
+// Key and value tiles into the ring: lane = (page, half) of a tile.
+template <int D, bool PAIR>
+__device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const CUtensorMap* key, const CUtensorMap* value,
+                                        char* ring) {
+    using S = TcShape<D, PAIR>;
+    const int lane = threadIdx.x & 31;
+    const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
+              per = a.H * groups;
+    const int boxes = kTile / a.P * S::kHalves;
+    const int pi = lane / S::kHalves, half = lane % S::kHalves;
+    uint32_t u = 0;
+    for (TcWalk w(c.cut); w.more();) {
+        const int len = attend_span(a, w.b).len(), n = w.count(len), h = w.item / groups;
+        const int32_t* table = a.block_table + (int64_t)w.b * a.max_pages;
+        auto page_of = [&](int q) {
+            const int l0 = (w.tile + q) * kTile + pi * a.P;
+            int page = a.pages;  // past the pool: reads as zeros
+            if (q < n && lane < boxes && l0 < len) {
+                page = table[l0 >> a.page_shift];
+                if (page < 0 || page >= a.pages) {
+                    atomicOr(a.status, kStBadIndex);
+                    page = a.pages;
+                }
+            }
+            return page;
+        };
+        int page = page_of(0);
+        for (int q = 0; q < n; ++q) {
+            const int next = page_of(q + 1);
+#pragma unroll
+            for (int kv = 0; kv < 2; ++kv, ++u) {
+                const int slot = u % S::kUnits;
+                if (u >= S::kUnits && !bar_wait(&c.empty[slot], (u / S::kUnits - 1) & 1, c)) goto out;
+                if (lane == 0) bar_expect(&c.full[slot], S::kUnit);
+                __syncwarp();
+                if (lane < boxes)
+                    tma_tile(smem_u32(ring + slot * S::kUnit + half * 16384 + pi * a.P * 128), kv ? value : key, half * 64, h,
+                             page, &c.full[slot]);
+            }
+            page = next;
+        }
+        w.next(n, per);
+    }
+out:
+    // no copy is in flight when the CTA ends, and no arrival of a product that read one
+    for (uint32_t x = u > S::kUnits ? u - S::kUnits : 0; x < u; ++x) {
+        bar_wait<true>(&c.full[x % S::kUnits], (x / S::kUnits) & 1, c);
+        bar_wait<true>(&c.empty[x % S::kUnits], (x / S::kUnits) & 1, c);
+    }
+}
+
+// The matrix products of stream `st`.
+template <int D, bool PAIR>
+__device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, char* q_smem, char* ring, int st) {
+    using S = TcShape<D, PAIR>;
+    const int lane = threadIdx.x & 31;
+    const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
+              per = a.H * groups;
+    const uint32_t t_s = c.tmem + st * 128, t_o = c.tmem + S::kO + st * D;
+    const uint32_t q_at = smem_u32(q_smem + (PAIR ? st * S::kQ : 0));
+    uint32_t items = 0, tiles_done = 0, unit0 = 0;
+    for (TcWalk w(c.cut); w.more();) {
+        const int n = w.count(attend_span(a, w.b).len());
+        const bool stream_live = PAIR ? w.item % groups * item_rows + st * 128 < rows : true;
+        if (!bar_wait(&c.q_ready, items++ & 1, c)) goto out;
+        tc_fence_after();
+        if (lane == 0) bar_arrive(&c.q_taken);
+        for (int q = PAIR ? 0 : st; q < n; q += PAIR ? 1 : 2) {
+            const uint32_t uk = unit0 + 2 * q, uv = uk + 1;
+            if (!bar_wait(&c.full[uk % S::kUnits], (uk / S::kUnits) & 1, c)) goto out;
+            if (!stream_live) {
+                if (lane == 0) bar_arrive(&c.empty[uk % S::kUnits]);
+                if (!bar_wait(&c.full[uv % S::kUnits], (uv / S::kUnits) & 1, c)) goto out;
+                if (lane == 0) bar_arrive(&c.empty[uv % S::kUnits]);
+                continue;
+            }
+            // S overwrites the last tile's P: its product has to be done
+            if (tiles_done > 0 && !bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) goto out;
+            tc_fence_after();
+            if (lane == 0) {
+                const uint32_t k_at = smem_u32(ring + (uk % S::kUnits) * S::kUnit);
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i) {
+                    const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
+                    mma_ss(t_s, smem_desc(q_at + off, 16, 1024), smem_desc(k_at + off, 16, 1024), mma_desc(kTile, false), i > 0);
+                }
+                tc_commit(&c.empty[uk % S::kUnits]);
+                tc_commit(&c.s_full[st]);
+            }
+            __syncwarp();
+            if (!bar_wait(&c.full[uv % S::kUnits], (uv / S::kUnits) & 1, c)) goto out;
+            if (!bar_wait(&c.p_ready[st], tiles_done & 1, c)) goto out;
+            tc_fence_after();
+            if (lane == 0) {
+                const uint32_t v_at = smem_u32(ring + (uv % S::kUnits) * S::kUnit);
+#pragma unroll
+                for (int i = 0; i < kTile / 16; ++i)
+                    mma_ts(t_o, t_s + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024), mma_desc(D, true),
+                           i > 0 || q >= (PAIR ? 1 : 2));
+                tc_commit(&c.empty[uv % S::kUnits]);
+                tc_commit(&c.pv_done[st]);
+            }
+            __syncwarp();
+            ++tiles_done;
+        }
+        unit0 += 2 * n;
+        w.next(n, per);
+    }
+out:
+    // nothing of this stream is in flight when the CTA ends
+    __syncwarp();
+    if (lane == 0) tc_commit(&c.drained[st]);
+    bar_wait<true>(&c.drained[st], 0, c);
+}
+
+template <int D, bool PAIR>
+__global__ void __launch_bounds__(kTcThreads, 1)
+    attend_tc_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap key, const __grid_constant__ CUtensorMap value) {
+    using S = TcShape<D, PAIR>;
+    extern __shared__ char raw[];
+    char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    char* q_smem = base;
+    char* ring = base + 2 * S::kQ;
+    TcControl& c = *reinterpret_cast<TcControl*>(ring + S::kUnits * S::kUnit);
+    const int warp = threadIdx.x >> 5;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::kUnits; ++i) {
+            bar_init(&c.full[i], 1);
+            bar_init(&c.empty[i], PAIR ? 2 : 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            bar_init(&c.s_full[i], 1);
+            bar_init(&c.p_ready[i], 128);
+            bar_init(&c.pv_done[i], 1);
+            bar_init(&c.drained[i], 1);
+        }
+        bar_init(&c.q_ready, 256);
+        bar_init(&c.q_taken, 2);
+        bar_init(&c.all_sync, 256);
+        c.abort = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    grid_dependency_begin();
+    if (warp == 8) {
+        __syncwarp();
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c.tmem)), "r"(512)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (warp == 9) {
+        const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128;
+        const AttendCut cut = attend_cut<kTile>(a, a.H * ((rows + item_rows - 1) / item_rows), blockIdx.x, a.min_tiles);
+        if ((threadIdx.x & 31) == 0) c.cut = cut;
+    }
+    if (threadIdx.x == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp < 8) tc_softmax<D, PAIR>(a, c, q_smem, ring, warp >> 2);
+    else if (warp == 8) tc_load<D, PAIR>(a, c, &key, &value, ring);
+    else tc_products<D, PAIR>(a, c, q_smem, ring, warp - 9);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after();
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(c.tmem), "r"(512));
+        if (c.abort && (threadIdx.x & 31) == 0) atomicOr(a.status, kStInternal);
+    }
+}
+
+using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                              const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                              CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encode_fn() {
+    static const EncodeFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult how;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &how) != cudaSuccess ||
+            how != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeFn>(p);
+    }();
+    return fn;
+}
+
+// [page][head][token][D] with any strides, a page of one head and 64 elements a box.
+bool encode(CUtensorMap* map, const AttendArgs& a, void* base, int64_t page, int64_t head, int64_t token) {
+    const EncodeFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)a.P, (cuuint64_t)a.H, (cuuint64_t)a.pages};
+    const cuuint64_t strides[3] = {(cuuint64_t)token * 2, a.H == 1 ? 16 : (cuuint64_t)head * 2,
+                                   a.pages == 1 ? 16 : (cuuint64_t)page * 2};
+    const cuuint32_t box[4] = {64, (cuuint32_t)a.P, 1, 1}, one[4] = {1, 1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, base, dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool PAIR> cudaError_t launch_tc(const AttendArgs& a, cudaStream_t s) {
+    CUtensorMap key, value;
+    if (!encode(&key, a, a.kv.key, a.kv.key_page, a.kv.key_head, a.kv.key_token) ||
+        !encode(&value, a, a.kv.value, a.kv.value_page, a.kv.value_head, a.kv.value_token))
+        return cudaErrorInvalidValue;
+    constexpr size_t smem = tc_smem_bytes<D, PAIR>();
+    static_assert(smem <= 227 * 1024);
+    cudaError_t err = cudaFuncSetAttribute(attend_tc_kernel<D, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (err != cudaSuccess) return err;
+    return launch_dependent(attend_tc_kernel<D, PAIR>, dim3(a.ctas), dim3(kTcThreads), smem, s, a, key, value);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s) {
+    const bool pair = (int64_t)a.T * a.G > 128;
+    if (a.D == 64) return pair ? launch_tc<64, true>(a, s) : launch_tc<64, false>(a, s);
+    return pair ? launch_tc<128, true>(a, s) : launch_tc<128, false>(a, s);
+}
+
+}  // namespace rheo

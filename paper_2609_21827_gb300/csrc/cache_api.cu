@@ -62,7 +62,7 @@ struct CacheLayout {
 
 CacheLayout cache_layout(const rheo_cache_config& c) {
     const int G = c.q_heads / c.kv_heads;
-    const size_t ctas = attend_ctas(c.dtype, c.tokens, G), rows = attend_rows(c.dtype, c.tokens, G);
+    const size_t ctas = kAttendCtas, rows = attend_part_rows(c.dtype, c.tokens, G);
     CacheLayout L{};
     size_t o = 0;
     auto take = [&](size_t bytes) {
@@ -230,7 +230,10 @@ extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_
     a.page_shift = page_shift(cfg->page_size);
     a.pages = cfg->pages;
     a.max_pages = cfg->max_pages;
-    a.ctas = attend_ctas(cfg->dtype, a.T, a.G);
+    a.ctas = kAttendCtas;
+    a.min_tiles = 1;
+    a.item_rows = attend_item_rows(cfg->dtype, a.T, a.G);
+    a.part_rows = attend_part_rows(cfg->dtype, a.T, a.G);
     a.io = *io;
     a.kv = *kv;
     a.block_table = block_table;

@@ -58,6 +58,9 @@ struct CommitArgs {
 struct AttendArgs {
     int B, T, H, G, D, P, page_shift, pages, max_pages;
     int ctas;                 // CTAs that share the tiles
+    int min_tiles;            // tiles a CTA takes at least
+    int item_rows;            // query rows of an item
+    int part_rows;            // rows kept of an item's partial sums
     rheo_attend_io io;
     rheo_kv kv;
     const int32_t* block_table;
@@ -65,8 +68,8 @@ struct AttendArgs {
     const int32_t* new_len;   // or null: T
     const uint8_t* mask;      // or null: j <= t
     float scale_log2;         // scale * log2(e)
-    float* part_o;            // [2 * ctas][rows of an item][D] unnormalised sums
-    float* part_ml;           // [2 * ctas][rows of an item][2] running maximum (log2 units) and sum
+    float* part_o;            // [2 * ctas][part_rows][D] unnormalised sums
+    float* part_ml;           // [2 * ctas][part_rows][2] running maximum (log2 units) and sum
     int4* join;               // [ctas] the item that a CTA begins and others go on with: request, item, segments
     unsigned* status;
 };
@@ -89,9 +92,10 @@ cudaError_t launch_reserve(const ReserveArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, cudaStream_t s);
 cudaError_t launch_commit(const CommitArgs& a, int line_bytes, cudaStream_t s);
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s);
-// rows of query tokens x heads of one work item, and CTAs that share the items
-int attend_rows(int dtype, int T, int G);
-int attend_ctas(int dtype, int T, int G);
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s);
+int attend_item_rows(int dtype, int T, int G);
+int attend_part_rows(int dtype, int T, int G);
+constexpr int kAttendCtas = 152;  // one a multiprocessor
 cudaError_t launch_logprobs(const LogprobArgs& a, int dtype, bool aligned, cudaStream_t s);
 int logprob_segments(int rows, int vocab, int dtype, int sms);
 

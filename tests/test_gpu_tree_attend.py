@@ -208,6 +208,57 @@ def test_large_scores_and_negative_scale(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,G", [(1, 4), (9, 2), (61, 4)])
+def test_scores_that_rise_along_the_context(dtype, T, G):
+    """Each stretch of keys is larger than the one before: the running maximum moves again and again."""
+    p = Problem([1500, 700, 40], None, T, 2 * G, 2, 128, 16, dtype, seed=12)
+    for b, n in enumerate(p.ctx):
+        for l in range(n + T):
+            page, row = ref.place(p.table[b], l, 16)
+            p.key[page, :, row] *= 1 + l // 100
+    p.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,G", [(1, 4), (49, 4)])
+def test_many_calls_one_after_the_other(dtype, T, G):
+    """Calls that nothing waits between, each with its own tensors and workspace, many key tiles a CTA."""
+    ps = [Problem([4000 - 500 * b for b in range(8)], None, T, 8 * G, 8, 128, 16, dtype, seed=20 + i) for i in range(3)]
+    first = []
+    for p in ps:
+        first.append([x.clone() for x in p.run(new=False)])
+        torch.cuda.synchronize()
+    ctx, pages = _i32(ps[0].ctx), [rheo.Pages(p.cfg, block_table=p.table) for p in ps]
+    for p in ps:
+        p.out.fill_(1.0)
+        p.lse.fill_(1.0)
+    torch.cuda.synchronize()
+    for i in range(60):
+        p = ps[i % 3]
+        rheo.tree_attend(p.cfg, p.q, p.key, p.value, pages[i % 3], ctx, p.out, p.ws, lse=p.lse, scale=p.scale)
+    torch.cuda.synchronize()
+    for p, (out, lse) in zip(ps, first):
+        assert torch.equal(p.out, out) and torch.equal(p.lse, lse)
+        assert rheo.scratch_status(p.ws) == 0
+    ps[2].check(new=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,G", [(1, 4), (65, 2)])
+def test_runs_of_short_items_between_long_ones(dtype, T, G):
+    """Many items of one key tile in a row in every CTA, in calls that nothing waits between."""
+    ctx = [(37 * b) % 60 for b in range(500)]
+    ctx[100] = ctx[300] = 2000
+    ps = [Problem(ctx, None, T, 8 * G, 8, 64, 16, dtype, seed=30 + i) for i in range(2)]
+    for p in ps:
+        p.run(new=False)
+    for i in range(20):
+        ps[i % 2].run(new=False)
+    for p in ps:
+        p.check(new=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_same_bits_every_time_and_on_another_stream(dtype):
     p = Problem([3000, 40, 1200], None, 17, 8, 2, 128, 16, dtype, seed=4)
     first = [x.clone() for x in p.check()]
