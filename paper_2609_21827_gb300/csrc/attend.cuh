@@ -94,6 +94,11 @@ __device__ __forceinline__ bool attend_sees(const AttendSpan& s, const uint8_t* 
 // The slot of a.part_o / a.part_ml for CTA `cta`'s part of an item that it does not hold whole.
 __device__ __forceinline__ int64_t attend_part(int cta, bool starts_here) { return 2 * (int64_t)cta + (starts_here ? 1 : 0); }
 
+// Four columns (group c4) of row r of a part: rows side by side, as the threads that write and read them are.
+__device__ __forceinline__ int64_t attend_part_at(const AttendArgs& a, int64_t part, int r, int c4) {
+    return (part * (a.D / 4) + c4) * a.part_rows + r;
+}
+
 __device__ __forceinline__ float attend_lse(float m, float l) {
     return l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
 }

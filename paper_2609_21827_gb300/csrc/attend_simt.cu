@@ -208,10 +208,9 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
             const int t = row / a.G, head = h * a.G + row % a.G;
             const float ll = t < span.add ? l[i] : 0.0f;
             if (!whole) {
-                float* po = a.part_o + (part * a.part_rows + r) * D;
 #pragma unroll
                 for (int c = 0; c < DJ; ++c)
-                    *reinterpret_cast<float4*>(po + tx * 4 + 64 * c) =
+                    reinterpret_cast<float4*>(a.part_o)[attend_part_at(a, part, r, tx + 16 * c)] =
                         make_float4(o[i][4 * c], o[i][4 * c + 1], o[i][4 * c + 2], o[i][4 * c + 3]);
                 if (tx == 0) {
                     a.part_ml[(part * a.part_rows + r) * 2] = m[i];
@@ -242,55 +241,63 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
     }
 }
 
-// Joins the parts of an item that several CTAs summed, in the order of its keys:
-// a warp a row, 8 rows a CTA; grid (CTAs of the sums, rows of an item / 8).
+// Joins the parts of an item that several CTAs summed, in the order of its keys.  A
+// thread takes eight columns of a row; neighbouring threads take neighbouring
+// rows, as the parts lie.  Grid (CTAs of the sums, pieces of 256 threads).
 template <int DT, int D>
 __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a) {
     grid_dependency_begin();
-    constexpr int W = D / 32;
     const int4 rec = a.join[blockIdx.x];
-    const int segments = rec.z, lane = threadIdx.x & 31;
-    const int r = blockIdx.y * 8 + (threadIdx.x >> 5);
-    if (segments == 0 || r >= a.part_rows) return;
+    const int segments = rec.z, i = blockIdx.y * 256 + threadIdx.x;
+    const int c8 = i / a.part_rows, r = i - c8 * a.part_rows;
+    if (segments == 0 || c8 >= D / 8) return;
     const int b = rec.x, rows = a.T * a.G, groups = (rows + a.item_rows - 1) / a.item_rows;
     const int h = rec.y / groups, row = rec.y % groups * a.item_rows + r;
     if (row >= rows) return;
     const int t = row / a.G, head = h * a.G + row % a.G;
-    const auto part = [&](int s) { return attend_part(blockIdx.x + s, s == 0) * a.part_rows + r; };
+    const auto ml = [&](int s) {
+        return *reinterpret_cast<const float2*>(a.part_ml + (attend_part(blockIdx.x + s, s == 0) * a.part_rows + r) * 2);
+    };
     float m = -INFINITY;
-    for (int s = lane; s < segments; s += 32) m = fmaxf(m, a.part_ml[part(s) * 2]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+#pragma unroll 8
+    for (int s = 0; s < segments; ++s) m = fmaxf(m, ml(s).x);
     const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, x[W];
-#pragma unroll
-    for (int i = 0; i < W; ++i) x[i] = 0.0f;
+    float l = 0.0f, x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll 4
     for (int s = 0; s < segments; ++s) {
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + part(s) * 2);
-        const float w = fast_exp2(ml.x - ref);
-        const float* po = a.part_o + part(s) * D + lane * W;
-        l += w * ml.y;
-        if (W == 4) {
-            const float4 y = *reinterpret_cast<const float4*>(po);
-            x[0] += w * y.x;
-            x[1] += w * y.y;
-            x[2 % W] += w * y.z;
-            x[3 % W] += w * y.w;
-        } else {
-            const float2 y = *reinterpret_cast<const float2*>(po);
-            x[0] += w * y.x;
-            x[1] += w * y.y;
-        }
+        const float2 y = ml(s);
+        const float w = fast_exp2(y.x - ref);
+        const float4* po = reinterpret_cast<const float4*>(a.part_o) +
+                           attend_part_at(a, attend_part(blockIdx.x + s, s == 0), r, 2 * c8);
+        const float4 u = po[0], v = po[a.part_rows];
+        l += w * y.y;
+        x[0] += w * u.x;
+        x[1] += w * u.y;
+        x[2] += w * u.z;
+        x[3] += w * u.w;
+        x[4] += w * v.x;
+        x[5] += w * v.y;
+        x[6] += w * v.z;
+        x[7] += w * v.w;
     }
-    const int64_t e = b * a.io.out_batch + t * a.io.out_token + head * a.io.out_head + lane * W;
+    const float inv = 1.0f / l;
 #pragma unroll
-    for (int i = 0; i < W; ++i) {
-        const float y = l == 0.0f ? 0.0f : x[i] / l;
-        if (DT == 0) static_cast<float*>(a.io.out)[e + i] = y;
-        else static_cast<__nv_bfloat16*>(a.io.out)[e + i] = __float2bfloat16_rn(y);
+    for (int k = 0; k < 8; ++k) x[k] = l == 0.0f ? 0.0f : x[k] * inv;
+    const int64_t e = b * a.io.out_batch + t * a.io.out_token + head * a.io.out_head + 8 * c8;
+    if (DT == 0) {
+        float4* out = reinterpret_cast<float4*>(static_cast<float*>(a.io.out) + e);
+        out[0] = make_float4(x[0], x[1], x[2], x[3]);
+        out[1] = make_float4(x[4], x[5], x[6], x[7]);
+    } else {
+        uint32_t y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __nv_bfloat162 z = __floats2bfloat162_rn(x[2 * k], x[2 * k + 1]);
+            y[k] = *reinterpret_cast<const uint32_t*>(&z);
+        }
+        *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.io.out) + e) = make_uint4(y[0], y[1], y[2], y[3]);
     }
-    if (a.io.lse && lane == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m, l);
+    if (a.io.lse && c8 == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m, l);
 }
 
 // fp32: 16 rows an item where that holds them all (single tokens and short
@@ -306,7 +313,7 @@ int attend_part_rows(int dtype, int T, int G) {
 }
 
 template <int DT, int D> static cudaError_t launch_join(const AttendArgs& a, cudaStream_t s) {
-    return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, (a.part_rows + 7) / 8), dim3(256), 0, s, a);
+    return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, (a.part_rows * (D / 8) + 255) / 256), dim3(256), 0, s, a);
 }
 
 template <int D, int R> static cudaError_t launch_simt(const AttendArgs& a, cudaStream_t s) {

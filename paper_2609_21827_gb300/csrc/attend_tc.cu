@@ -1,9 +1,9 @@
 // attend_tc.cu -- attention of drafted tokens over the paged bf16 cache on the
 // tensor cores.
 //
-// One CTA an SM, eleven warps:
+// One CTA an SM, twelve warps:
 //   warps 0-3, 4-7   two softmax groups, one a stream; thread = query row
-//   warp 8           loads key and value tiles (TMA) into a ring of shared memory
+//   warps 8, 11      load key tiles and value tiles (TMA) into two rings of shared memory
 //   warps 9, 10      issue the matrix products of stream 0 and 1
 // A stream holds up to 128 query rows (token, head of the key/value head): its
 // scores S = Q K^T (128 x 128 fp32) and its sums O (128 x D fp32) lie in tensor
@@ -35,23 +35,26 @@ namespace rheo {
 namespace {
 
 constexpr int kTile = 128;                   // keys a tile
-constexpr int kTcThreads = 11 * 32;
+constexpr int kTcThreads = 12 * 32;
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
 constexpr int kDrainLimit = 1 << 16;         // and of a drain after that
 
 template <int D, bool PAIR> struct TcShape {
-    static constexpr int kUnit = kTile * D * 2;       // bytes of a key or value tile
-    static constexpr int kHalves = D / 64;            // 128-byte wide parts of a line
-    // Ring.  !PAIR: a multiple of 4 (key and value tiles of two streams), so that a slot serves one stream only: a
-    // stream that met a slot's barrier every other time could take the phase before last for its own.
-    static constexpr int kUnits = (PAIR ? 5 : 4) * (128 / D);
-    static constexpr int kQ = 128 * D * 2;            // bytes of a stream's queries
-    static constexpr int kO = 256;                    // first tensor-memory column of the sums
+    static constexpr int kUnit = kTile * D * 2;  // bytes of a key or value tile
+    static constexpr int kHalves = D / 64;       // 128-byte wide parts of a line
+    // Slots of the key ring and of the value ring.  !PAIR: even, so that within an item a slot serves one stream
+    // only; a stream that met a slot's barrier every other time could take the phase before last for its own.
+    // (Between items all tiles are consumed before either stream waits for the next item's.)
+    static constexpr int kK = D == 128 ? 2 : PAIR ? 5 : 4;
+    static constexpr int kV = D == 128 ? (PAIR ? 3 : 2) : PAIR ? 5 : 4;
+    static constexpr int kQ = 128 * D * 2;       // bytes of 128 rows of queries
+    static constexpr int kMerge = PAIR ? 0 : 16384;
+    static constexpr int kO = 256;               // first tensor-memory column of the sums
 };
 
 struct TcControl {
-    unsigned long long full[10], empty[10];
+    unsigned long long full_k[5], empty_k[5], full_v[5], empty_v[5];
     unsigned long long s_full[2], p_ready[2], pv_done[2], drained[2], q_ready, q_taken, all_sync;
     uint32_t tmem;
     int abort;
@@ -63,7 +66,7 @@ struct TcControl {
 
 template <int D, bool PAIR> constexpr size_t tc_smem_bytes() {
     using S = TcShape<D, PAIR>;
-    return 1024 + 2 * S::kQ + (size_t)S::kUnits * S::kUnit + sizeof(TcControl);
+    return 1024 + 2 * S::kQ + (size_t)(S::kK + S::kV) * S::kUnit + S::kMerge + sizeof(TcControl);
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -73,6 +76,11 @@ __device__ __forceinline__ void bar_init(unsigned long long* b, int count) {
 }
 __device__ __forceinline__ void bar_arrive(unsigned long long* b) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+}
+// One arrival for a warp, after all its lanes' accesses.
+__device__ __forceinline__ void bar_arrive_warp(unsigned long long* b) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(b);
 }
 __device__ __forceinline__ void bar_expect(unsigned long long* b, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
@@ -124,16 +132,15 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t at) {
         : "r"(at));
 #undef OUT
 }
-__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t at) {
     __syncwarp();
-#define IN(i) "r"(r[i])
+#define OUT(i) "=r"(r[i])
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::RHEO_R32(IN),
-        "r"(at)
-        : "memory");
-#undef IN
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : RHEO_R16(OUT)
+        : "r"(at));
+#undef OUT
 }
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
     __syncwarp();
@@ -195,6 +202,8 @@ struct TcWalk {
     }
 };
 
+__device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
+
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -205,9 +214,24 @@ __device__ __forceinline__ uint32_t odd_mask(uint32_t w) {
     return ((w & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((w & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
 }
 
+// This thread's share of the copies of an item's query rows into the swizzled operand (asynchronous).  Rows that the
+// item does not have keep what is there: they only reach their own, unused, rows of the products.
+template <int D>
+__device__ __forceinline__ void tc_queries(const AttendArgs& a, int b, int h, int first, int count, char* to, int tid,
+                                           int threads) {
+    constexpr int C = D / 8;  // 16-byte pieces of a row
+    const char* q = static_cast<const char*>(a.io.q) + (int64_t)b * a.io.q_batch * 2;
+    for (int i = tid; i < count * C; i += threads) {
+        const int r = i / C, p = i % C, row = first + r, t = row / a.G;
+        const char* src = q + (t * a.io.q_token + (h * a.G + row - t * a.G) * a.io.q_head + p * 8) * 2;
+        const uint32_t dst = smem_u32(to + (p >> 3) * 16384 + r * 128 + (((p & 7) ^ (r & 7)) << 4));
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    }
+}
+
 // The softmax group of stream `st`.
 template <int D, bool PAIR>
-__device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, char* q_smem, char* ring, int st) {
+__device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, char* q_smem, char* v_ring, char* merge, int st) {
     using S = TcShape<D, PAIR>;
     const int tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
@@ -215,50 +239,53 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t t_s = c.tmem + lanes + st * 128, t_o = c.tmem + lanes + S::kO + st * D;
     const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);  // above 0, so that hidden places stay at -inf
-    const uint32_t flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;  // a negative scale turns the queries' signs
-    uint32_t items = 0, tiles_done = 0, syncs = 0, unit0 = 0;
+    const bool negative = a.scale_log2 < 0.0f;
+    uint32_t items = 0, tiles_done = 0, syncs = 0, tile0 = 0;
     auto sync_all = [&]() -> bool {
-        bar_arrive(&c.all_sync);
+        bar_arrive_warp(&c.all_sync);
         return bar_wait(&c.all_sync, syncs++ & 1, c);
     };
-    for (TcWalk w(c.cut); w.more();) {
-        const AttendSpan span = attend_span(a, w.b);
+    // queries of the item at (b, item) into this stream's rows (PAIR) or the buffer of that turn
+    auto fetch = [&](int b, int item, uint32_t turn) {
+        const int h = item / groups, first = item % groups * item_rows + (PAIR ? st * 128 : 0);
+        const int count = min(128, rows - first);
+        if (PAIR) tc_queries<D>(a, b, h, first, count, q_smem + st * S::kQ, tid, 128);
+        else tc_queries<D>(a, b, h, first, count, q_smem + (turn & 1) * S::kQ, threadIdx.x, 256);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    TcWalk w(c.cut);
+    AttendSpan next_span{0, 0, false};
+    if (w.more()) {
+        next_span = attend_span(a, w.b);
+        fetch(w.b, w.item, 0);
+    }
+    while (w.more()) {
+        const AttendSpan span = next_span;
         const int len = span.len(), all = w.tiles(len), n = w.count(len);
         const int h = w.item / groups, r0 = w.item % groups * item_rows;
         if (span.bad && threadIdx.x == 0) atomicOr(a.status, kStBadLength);
         if (!sync_all()) return;  // both streams are through with the last item
         // and both product warps have seen its start: one without tiles in it waits for nothing else
         if (items > 0 && !bar_wait(&c.q_taken, (items - 1) & 1, c)) return;
-        ++items;
         if (threadIdx.x < 128) c.odd[threadIdx.x] = 0;
         if (threadIdx.x == 0) c.any_odd = 0;
-        {
-            // queries, rows past the item's are 0; 16-byte pieces in the swizzled order of the operand
-            constexpr int C = D / 8;
-            const int in_item = min(item_rows, rows - r0);
-            for (int i = threadIdx.x; i < item_rows * C; i += 256) {
-                const int r = i / C, p = i % C, row = r0 + r, t = row / a.G;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                if (r < in_item && t < span.add)
-                    x = *reinterpret_cast<const uint4*>(static_cast<const char*>(a.io.q) +
-                                                        (w.b * a.io.q_batch + t * a.io.q_token +
-                                                         (h * a.G + row % a.G) * a.io.q_head + p * 8) * 2);
-                x.x ^= flip;
-                x.y ^= flip;
-                x.z ^= flip;
-                x.w ^= flip;
-                const int rr = r & 127;
-                *reinterpret_cast<uint4*>(q_smem + (r >> 7) * S::kQ + (p >> 3) * 16384 + rr * 128 +
-                                          (((p & 7) ^ (rr & 7)) << 4)) = x;
-            }
-            fence_async();
-            tc_fence_before();
-            bar_arrive(&c.q_ready);
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_async();
+        tc_fence_before();
+        bar_arrive_warp(&c.q_ready);
+        const bool last = w.at + n >= w.end;
+        const int next_b = w.item + 1 == per ? w.b + 1 : w.b, next_item = w.item + 1 == per ? 0 : w.item + 1;
+        if (!last) {
+            next_span = attend_span(a, next_b);
+            if (!PAIR) fetch(next_b, next_item, items + 1);  // the other buffer is free: its item is over
         }
+        ++items;
+
         const int row = r0 + (PAIR ? st * 128 : 0) + tid, t = row / a.G;
         const bool live = row < rows && t < span.add;
         const bool warp_live = __any_sync(0xffffffffu, live);
         const bool stream_live = PAIR ? r0 + st * 128 < rows : true;
+        if (PAIR && !stream_live && !last) fetch(next_b, next_item, 0);
         float m = -INFINITY, l = 0.0f;
         int mine = 0;  // tiles of this stream in this item so far
         for (int q = PAIR ? 0 : st; q < n && stream_live; q += PAIR ? 1 : 2) {
@@ -266,25 +293,41 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
             const bool tail = k0 + kTile > span.ctx;
             uint32_t vis[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
             if (tail && warp_live) {
-                // the warp's tokens one after the other, 32 places a vote
+                // the warp's tokens, four at a time, 32 places a vote
                 const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
-                for (int tt = (row - lane) / a.G; tt <= t_last; ++tt) {
-                    const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + tt) * a.T : nullptr;
+                for (int tt = (row - lane) / a.G; tt <= t_last; tt += 4) {
+                    bool sees[4][4];
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        const bool sees = tt < span.add && attend_sees(span, mrow, tt, k0 + 32 * v + lane);
-                        const uint32_t bits = __ballot_sync(0xffffffffu, sees);
-                        if (tt == t) vis[v] = bits;
+                    for (int u = 0; u < 4; ++u) {
+                        const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + min(tt + u, t_last)) * a.T : nullptr;
+#pragma unroll
+                        for (int v = 0; v < 4; ++v)
+                            sees[u][v] = tt + u < span.add && attend_sees(span, mrow, tt + u, k0 + 32 * v + lane);
                     }
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+#pragma unroll
+                        for (int v = 0; v < 4; ++v) {
+                            const uint32_t bits = __ballot_sync(0xffffffffu, sees[u][v]);
+                            if (tt + u == t) vis[v] = bits;
+                        }
                 }
             }
             if (!bar_wait(&c.s_full[st], tiles_done & 1, c)) return;
             tc_fence_after();
+            // the item's last scores are there: this stream's queries have been read
+            if (PAIR && q == n - 1 && !last) fetch(next_b, next_item, 0);
             if (warp_live) {
                 uint32_t s[4][32];
 #pragma unroll
                 for (int v = 0; v < 4; ++v) tmem_ld32(s[v], t_s + 32 * v);
                 tc_wait_ld();
+                if (negative) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) s[v][i] ^= 0x80000000u;
+                }
                 if (tail) {
 #pragma unroll
                     for (int v = 0; v < 4; ++v)
@@ -292,12 +335,15 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                         for (int i = 0; i < 32; ++i)
                             if (!((vis[v] >> i) & 1u)) s[v][i] = 0xFF800000u;
                 }
-                float top = -INFINITY;
+                float tops[4];
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
+                for (int v = 0; v < 4; ++v) {
+                    float x = max3(__uint_as_float(s[v][0]), __uint_as_float(s[v][1]), __uint_as_float(s[v][2]));
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(s[v][i]));
-                top *= sc;
+                    for (int i = 3; i + 1 < 32; i += 2) x = max3(x, __uint_as_float(s[v][i]), __uint_as_float(s[v][i + 1]));
+                    tops[v] = fmaxf(x, __uint_as_float(s[v][31]));
+                }
+                const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * sc;
                 if (mine == 0) {
                     m = top;
                 } else {
@@ -308,43 +354,42 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                         tc_fence_after();
                         const float f = !grow || m == -INFINITY ? 1.0f : fast_exp2(m - top);
 #pragma unroll 1
-                        for (int d = 0; d < D; d += 32) {
-                            uint32_t o[32];
-                            tmem_ld32(o, t_o + d);
+                        for (int d = 0; d < D; d += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o, t_o + d);
                             tc_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st32(t_o + d, o);
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                            tmem_st16(t_o + d, o);
                         }
                         l *= f;
                         if (grow) m = top;
                     }
                 }
                 const float ref = m == -INFINITY ? 0.0f : m;
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const unsigned long long sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
+                unsigned long long sum[4] = {0ull, 0ull, 0ull, 0ull};
 #pragma unroll
                 for (int v = 0; v < 4; ++v) {
                     uint32_t p[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        float x = __uint_as_float(s[v][2 * i]), y = __uint_as_float(s[v][2 * i + 1]);
-                        x = fast_exp2(fmaf(x, sc, -ref));
-                        y = fast_exp2(fmaf(y, sc, -ref));
-                        sum[(2 * i) & 3] += x;
-                        sum[(2 * i + 1) & 3] += y;
-                        p[i] = pack_bf16(x, y);
+                        const unsigned long long x = f2_exp2(
+                            f2_fma(f2_pack(__uint_as_float(s[v][2 * i]), __uint_as_float(s[v][2 * i + 1])), sc2, ref2));
+                        sum[i & 3] = f2_add(sum[i & 3], x);
+                        p[i] = pack_bf16(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
                     }
                     tmem_st16(t_s + 16 * v, p);
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+                l += f2_fold(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])));
                 tc_wait_st();
             }
             if (tail) {
-                const uint32_t u = unit0 + 2 * q + 1;  // this tile's values
-                if (!bar_wait(&c.full[u % S::kUnits], (u / S::kUnits) & 1, c)) return;
+                const uint32_t u = tile0 + q;  // this tile's values
+                if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) return;
                 const int place = k0 + tid;
                 if (place >= span.ctx) {
-                    char* line = ring + (u % S::kUnits) * S::kUnit + tid * 128;
+                    char* line = v_ring + (u % S::kV) * S::kUnit + tid * 128;
 #pragma unroll
                     for (int p = 0; p < D / 8; ++p) {
                         uint4* at = reinterpret_cast<uint4*>(line + (p >> 3) * 16384 + (((p & 7) ^ (tid & 7)) << 4));
@@ -364,117 +409,128 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 fence_async();
             }
             tc_fence_before();
-            bar_arrive(&c.p_ready[st]);
+            bar_arrive_warp(&c.p_ready[st]);
             ++tiles_done;
             ++mine;
         }
-        unit0 += 2 * n;
+        tile0 += n;
 
         // ---- the item's sums
         if (mine > 0) {
             if (!bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) return;
             tc_fence_after();
         }
-        float other_f = 0.0f;  // !PAIR: the weight of the other stream's sums
-        char* spare = q_smem + S::kQ;
-        if (!PAIR) {
-            // stream 1 hands its sums to stream 0, 32 columns at a time
-            float2* ml = c.ml;
-            if (st == 1) ml[tid] = make_float2(m, mine > 0 ? l : 0.0f);
-            if (!sync_all()) return;
-            if (st == 0) {
-                const float2 x = ml[tid];
-                if (mine == 0) l = 0.0f;
-                const float mm = fmaxf(m, x.x), ref = mm == -INFINITY ? 0.0f : mm;
-                const float f0 = fast_exp2(m - ref);
-                other_f = fast_exp2(x.x - ref);
-                // this stream's factor is applied below through l and o
-                l = l * f0 + x.y * other_f;
-                m = mm;
-                ml[tid] = make_float2(f0, other_f);
-            }
-        }
         const bool whole = n == all;
         const int64_t part = attend_part(blockIdx.x, w.tile == 0);
-        const int r_in = (PAIR ? st * 128 : 0) + tid;
-        const float ll = live ? l : 0.0f;
-        const int head = h * a.G + row % a.G;
-        __threadfence_block();
-        const bool odd = *(volatile int*)&c.any_odd != 0;
-#pragma unroll 1
-        for (int d = 0; d < D; d += 32) {
-            float o[32];
-            if (warp_live && mine > 0) {
-                uint32_t x[32];
-                tmem_ld32(x, t_o + d);
-                tc_wait_ld();
+        const int r_in = (PAIR ? st * 128 : 0) + tid, head = h * a.G + row - t * a.G;
+        float f0 = 1.0f, f1 = 0.0f;  // !PAIR: the weights of the two streams
+        int columns = D;             // that the streams exchange at a time
+        const int kept = PAIR ? 128 : min(128, (rows + 31) / 32 * 32);  // rows of an item, to whole warps
+        if (!PAIR && n > 1) {
+            columns = min(D, 4096 / kept / 32 * 32);
+            if (st == 1) c.ml[tid] = make_float2(m, l);
+        } else if (!PAIR && st == 1) {
+            columns = 0;  // a single tile: it was stream 0's
+        }
+        float4* pass = reinterpret_cast<float4*>(merge);  // [columns / 4][kept]
+        float ll = live ? l : 0.0f;
+        for (int d0 = 0; d0 < D && columns > 0; d0 += columns) {
+            if (!PAIR && n > 1) {
+                if (st == 1 && warp_live) {
+                    for (int d = d0; d < d0 + columns; d += 32) {
+                        uint32_t x[32];
+                        tmem_ld32(x, t_o + d);
+                        tc_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = 0.0f;
-            }
-            if (!PAIR) {
-                float4* x = reinterpret_cast<float4*>(spare);
-                if (st == 1)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) x[i * 128 + tid] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                if (!sync_all()) return;
-                if (st == 0) {
-                    const float f0 = c.ml[tid].x;
-                    const bool has0 = mine > 0, has1 = n > 1;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float4 y = x[i * 128 + tid];
-                        o[4 * i] = (has0 ? o[4 * i] * f0 : 0.0f) + (has1 ? y.x * other_f : 0.0f);
-                        o[4 * i + 1] = (has0 ? o[4 * i + 1] * f0 : 0.0f) + (has1 ? y.y * other_f : 0.0f);
-                        o[4 * i + 2] = (has0 ? o[4 * i + 2] * f0 : 0.0f) + (has1 ? y.z * other_f : 0.0f);
-                        o[4 * i + 3] = (has0 ? o[4 * i + 3] * f0 : 0.0f) + (has1 ? y.w * other_f : 0.0f);
+                        for (int i = 0; i < 8; ++i)
+                            pass[((d - d0) / 4 + i) * kept + tid] =
+                                make_float4(__uint_as_float(x[4 * i]), __uint_as_float(x[4 * i + 1]),
+                                            __uint_as_float(x[4 * i + 2]), __uint_as_float(x[4 * i + 3]));
                     }
                 }
                 if (!sync_all()) return;
-                if (st == 1) continue;
+                if (st == 0 && d0 == 0) {
+                    const float2 x = c.ml[tid];
+                    const float mm = fmaxf(m, x.x), ref = mm == -INFINITY ? 0.0f : mm;
+                    f0 = fast_exp2(m - ref);
+                    f1 = fast_exp2(x.x - ref);
+                    l = l * f0 + x.y * f1;
+                    m = mm;
+                    ll = live ? l : 0.0f;
+                }
             }
-            if (odd && live) {
-                // drafted values that are not finite, for the rows that see them
-                const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + t) * a.T : nullptr;
-                for (int word = 0; word < (span.add + 31) / 32; ++word) {
-                    for (uint32_t bits = c.odd[word]; bits; bits &= bits - 1) {
-                        const int j = word * 32 + __ffs(bits) - 1, x = span.ctx + j;
-                        if (!(mrow ? mrow[j] != 0 : j <= t)) continue;
-                        const int64_t page = a.block_table[(int64_t)w.b * a.max_pages + (x >> a.page_shift)];
-                        if (page < 0 || page >= a.pages) continue;
-                        const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.kv.value) + page * a.kv.value_page +
-                                                 h * a.kv.value_head + (x & (a.P - 1)) * a.kv.value_token + d;
+            if (PAIR || st == 0) {
+                __threadfence_block();
+                const bool odd = *(volatile int*)&c.any_odd != 0;
+                const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
+#pragma unroll 1
+                for (int d = d0; d < d0 + columns; d += 32) {
+                    float o[32];
+                    if (warp_live) {
+                        uint32_t x[32];
+                        tmem_ld32(x, t_o + d);
+                        tc_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float y = __bfloat162float(v[i]);
-                            if (!(fabsf(y) < INFINITY)) o[i] += y;
+                        for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
+                        if (!PAIR && n > 1) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const float4 y = pass[((d - d0) / 4 + i) * kept + tid];
+                                o[4 * i] = o[4 * i] * f0 + y.x * f1;
+                                o[4 * i + 1] = o[4 * i + 1] * f0 + y.y * f1;
+                                o[4 * i + 2] = o[4 * i + 2] * f0 + y.z * f1;
+                                o[4 * i + 3] = o[4 * i + 3] * f0 + y.w * f1;
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0.0f;
+                    }
+                    if (odd && live) {
+                        // drafted values that are not finite, for the rows that see them
+                        const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + t) * a.T : nullptr;
+                        for (int word = 0; word < (span.add + 31) / 32; ++word) {
+                            for (uint32_t bits = c.odd[word]; bits; bits &= bits - 1) {
+                                const int j = word * 32 + __ffs(bits) - 1, x = span.ctx + j;
+                                if (!(mrow ? mrow[j] != 0 : j <= t)) continue;
+                                const int64_t page = a.block_table[(int64_t)w.b * a.max_pages + (x >> a.page_shift)];
+                                if (page < 0 || page >= a.pages) continue;
+                                const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.kv.value) +
+                                                         page * a.kv.value_page + h * a.kv.value_head +
+                                                         (x & (a.P - 1)) * a.kv.value_token + d;
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) {
+                                    const float y = __bfloat162float(v[i]);
+                                    if (!(fabsf(y) < INFINITY)) o[i] += y;
+                                }
+                            }
                         }
                     }
-                }
-            }
-            // (no lane leaves the iteration early: the next one begins with a warp-wide load)
-            if (row < rows && whole) {
-                const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
-                uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.io.out) + w.b * a.io.out_batch +
-                                                      t * a.io.out_token + head * a.io.out_head + d);
+                    // (no lane leaves the iteration early: the next one begins with a warp-wide load)
+                    if (row < rows && whole) {
+                        uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.io.out) + w.b * a.io.out_batch +
+                                                              t * a.io.out_token + head * a.io.out_head + d);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint4 y = make_uint4(0, 0, 0, 0);
-                    if (ll != 0.0f) {
-                        y.x = pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv);
-                        y.y = pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv);
-                        y.z = pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv);
-                        y.w = pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv);
+                        for (int i = 0; i < 4; ++i) {
+                            uint4 y = make_uint4(0, 0, 0, 0);
+                            if (ll != 0.0f) {
+                                y.x = pack_bf16(o[8 * i] * inv, o[8 * i + 1] * inv);
+                                y.y = pack_bf16(o[8 * i + 2] * inv, o[8 * i + 3] * inv);
+                                y.z = pack_bf16(o[8 * i + 4] * inv, o[8 * i + 5] * inv);
+                                y.w = pack_bf16(o[8 * i + 6] * inv, o[8 * i + 7] * inv);
+                            }
+                            out[i] = y;
+                        }
+                    } else if (row < rows) {
+                        float4* po = reinterpret_cast<float4*>(a.part_o) + attend_part_at(a, part, r_in, d / 4);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            po[i * a.part_rows] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                     }
-                    out[i] = y;
                 }
-            } else if (row < rows) {
-                float4* po = reinterpret_cast<float4*>(a.part_o + (part * a.part_rows + r_in) * D + d);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) po[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             }
+            // stream 1 writes the next columns when stream 0 has read these
+            if (!PAIR && n > 1 && d0 + columns < D && !sync_all()) return;
         }
         if ((PAIR || st == 0) && row < rows) {
             if (whole) {
@@ -487,12 +543,13 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
             a.join[blockIdx.x] = make_int4(w.b, w.item, c.cut.owner(w.at + all - 1) - (int)blockIdx.x + 1, 0);
         w.next(n, per);
     }
+    asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// Key and value tiles into the ring: lane = (page, half) of a tile.
-template <int D, bool PAIR>
-__device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const CUtensorMap* key, const CUtensorMap* value,
-                                        char* ring) {
+// Key tiles, or value tiles, into their ring: lane = (page, half) of a tile.
+template <int D, bool PAIR, int SLOTS>
+__device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const CUtensorMap* map, char* ring,
+                                        unsigned long long* full, unsigned long long* empty, bool report) {
     using S = TcShape<D, PAIR>;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
@@ -506,27 +563,23 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
         auto page_of = [&](int q) {
             const int l0 = (w.tile + q) * kTile + pi * a.P;
             int page = a.pages;  // past the pool: reads as zeros
-            if (q < n && lane < boxes && l0 < len) {
-                page = table[l0 >> a.page_shift];
-                if (page < 0 || page >= a.pages) {
-                    atomicOr(a.status, kStBadIndex);
-                    page = a.pages;
-                }
-            }
+            if (q < n && lane < boxes && l0 < len) page = table[l0 >> a.page_shift];
             return page;
         };
         int page = page_of(0);
-        for (int q = 0; q < n; ++q) {
+        for (int q = 0; q < n; ++q, ++u) {
             const int next = page_of(q + 1);
-#pragma unroll
-            for (int kv = 0; kv < 2; ++kv, ++u) {
-                const int slot = u % S::kUnits;
-                if (u >= S::kUnits && !bar_wait(&c.empty[slot], (u / S::kUnits - 1) & 1, c)) goto out;
-                if (lane == 0) bar_expect(&c.full[slot], S::kUnit);
-                __syncwarp();
-                if (lane < boxes)
-                    tma_tile(smem_u32(ring + slot * S::kUnit + half * 16384 + pi * a.P * 128), kv ? value : key, half * 64, h,
-                             page, &c.full[slot]);
+            const int slot = u % SLOTS;
+            if (u >= SLOTS && !bar_wait(&empty[slot], (u / SLOTS - 1) & 1, c)) goto out;
+            if (lane == 0) bar_expect(&full[slot], S::kUnit);
+            __syncwarp();
+            if (page < 0 || page > a.pages) {
+                if (report) atomicOr(a.status, kStBadIndex);
+                page = a.pages;
+            }
+            if (lane < boxes) {
+                if (report && page == a.pages && (w.tile + q) * kTile + pi * a.P < len) atomicOr(a.status, kStBadIndex);
+                tma_tile(smem_u32(ring + slot * S::kUnit + half * 16384 + pi * a.P * 128), map, half * 64, h, page, &full[slot]);
             }
             page = next;
         }
@@ -534,67 +587,70 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
     }
 out:
     // no copy is in flight when the CTA ends, and no arrival of a product that read one
-    for (uint32_t x = u > S::kUnits ? u - S::kUnits : 0; x < u; ++x) {
-        bar_wait<true>(&c.full[x % S::kUnits], (x / S::kUnits) & 1, c);
-        bar_wait<true>(&c.empty[x % S::kUnits], (x / S::kUnits) & 1, c);
+    for (uint32_t x = u > SLOTS ? u - SLOTS : 0; x < u; ++x) {
+        bar_wait<true>(&full[x % SLOTS], (x / SLOTS) & 1, c);
+        bar_wait<true>(&empty[x % SLOTS], (x / SLOTS) & 1, c);
     }
 }
 
 // The matrix products of stream `st`.
 template <int D, bool PAIR>
-__device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, char* q_smem, char* ring, int st) {
+__device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, char* q_smem, char* k_ring, char* v_ring,
+                                            int st) {
     using S = TcShape<D, PAIR>;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = a.H * groups;
     const uint32_t t_s = c.tmem + st * 128, t_o = c.tmem + S::kO + st * D;
-    const uint32_t q_at = smem_u32(q_smem + (PAIR ? st * S::kQ : 0));
-    uint32_t items = 0, tiles_done = 0, unit0 = 0;
-    for (TcWalk w(c.cut); w.more();) {
+    uint32_t items = 0, tiles_done = 0, tile0 = 0;
+    for (TcWalk w(c.cut); w.more(); ++items) {
         const int n = w.count(attend_span(a, w.b).len());
         const bool stream_live = PAIR ? w.item % groups * item_rows + st * 128 < rows : true;
-        if (!bar_wait(&c.q_ready, items++ & 1, c)) goto out;
+        const uint32_t q_at = smem_u32(q_smem + (PAIR ? st : items & 1) * S::kQ);
+        if (!bar_wait(&c.q_ready, items & 1, c)) goto out;
         tc_fence_after();
         if (lane == 0) bar_arrive(&c.q_taken);
         for (int q = PAIR ? 0 : st; q < n; q += PAIR ? 1 : 2) {
-            const uint32_t uk = unit0 + 2 * q, uv = uk + 1;
-            if (!bar_wait(&c.full[uk % S::kUnits], (uk / S::kUnits) & 1, c)) goto out;
+            const uint32_t u = tile0 + q;
+            unsigned long long *full_k = &c.full_k[u % S::kK], *full_v = &c.full_v[u % S::kV],
+                               *empty_k = &c.empty_k[u % S::kK], *empty_v = &c.empty_v[u % S::kV];
+            if (!bar_wait(full_k, (u / S::kK) & 1, c)) goto out;
             if (!stream_live) {
-                if (lane == 0) bar_arrive(&c.empty[uk % S::kUnits]);
-                if (!bar_wait(&c.full[uv % S::kUnits], (uv / S::kUnits) & 1, c)) goto out;
-                if (lane == 0) bar_arrive(&c.empty[uv % S::kUnits]);
+                if (lane == 0) bar_arrive(empty_k);
+                if (!bar_wait(full_v, (u / S::kV) & 1, c)) goto out;
+                if (lane == 0) bar_arrive(empty_v);
                 continue;
             }
             // S overwrites the last tile's P: its product has to be done
             if (tiles_done > 0 && !bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) goto out;
             tc_fence_after();
             if (lane == 0) {
-                const uint32_t k_at = smem_u32(ring + (uk % S::kUnits) * S::kUnit);
+                const uint32_t k_at = smem_u32(k_ring + (u % S::kK) * S::kUnit);
 #pragma unroll
                 for (int i = 0; i < D / 16; ++i) {
                     const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
                     mma_ss(t_s, smem_desc(q_at + off, 16, 1024), smem_desc(k_at + off, 16, 1024), mma_desc(kTile, false), i > 0);
                 }
-                tc_commit(&c.empty[uk % S::kUnits]);
+                tc_commit(empty_k);
                 tc_commit(&c.s_full[st]);
             }
             __syncwarp();
-            if (!bar_wait(&c.full[uv % S::kUnits], (uv / S::kUnits) & 1, c)) goto out;
+            if (!bar_wait(full_v, (u / S::kV) & 1, c)) goto out;
             if (!bar_wait(&c.p_ready[st], tiles_done & 1, c)) goto out;
             tc_fence_after();
             if (lane == 0) {
-                const uint32_t v_at = smem_u32(ring + (uv % S::kUnits) * S::kUnit);
+                const uint32_t v_at = smem_u32(v_ring + (u % S::kV) * S::kUnit);
 #pragma unroll
                 for (int i = 0; i < kTile / 16; ++i)
                     mma_ts(t_o, t_s + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024), mma_desc(D, true),
                            i > 0 || q >= (PAIR ? 1 : 2));
-                tc_commit(&c.empty[uv % S::kUnits]);
+                tc_commit(empty_v);
                 tc_commit(&c.pv_done[st]);
             }
             __syncwarp();
             ++tiles_done;
         }
-        unit0 += 2 * n;
+        tile0 += n;
         w.next(n, per);
     }
 out:
@@ -611,23 +667,29 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     extern __shared__ char raw[];
     char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     char* q_smem = base;
-    char* ring = base + 2 * S::kQ;
-    TcControl& c = *reinterpret_cast<TcControl*>(ring + S::kUnits * S::kUnit);
+    char* k_ring = q_smem + 2 * S::kQ;
+    char* v_ring = k_ring + S::kK * S::kUnit;
+    char* merge = v_ring + S::kV * S::kUnit;
+    TcControl& c = *reinterpret_cast<TcControl*>(merge + S::kMerge);
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < S::kUnits; ++i) {
-            bar_init(&c.full[i], 1);
-            bar_init(&c.empty[i], PAIR ? 2 : 1);
+        for (int i = 0; i < S::kK; ++i) {
+            bar_init(&c.full_k[i], 1);
+            bar_init(&c.empty_k[i], PAIR ? 2 : 1);
+        }
+        for (int i = 0; i < S::kV; ++i) {
+            bar_init(&c.full_v[i], 1);
+            bar_init(&c.empty_v[i], PAIR ? 2 : 1);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&c.s_full[i], 1);
-            bar_init(&c.p_ready[i], 128);
+            bar_init(&c.p_ready[i], 4);
             bar_init(&c.pv_done[i], 1);
             bar_init(&c.drained[i], 1);
         }
-        bar_init(&c.q_ready, 256);
+        bar_init(&c.q_ready, 8);
         bar_init(&c.q_taken, 2);
-        bar_init(&c.all_sync, 256);
+        bar_init(&c.all_sync, 8);
         c.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -647,9 +709,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp < 8) tc_softmax<D, PAIR>(a, c, q_smem, ring, warp >> 2);
-    else if (warp == 8) tc_load<D, PAIR>(a, c, &key, &value, ring);
-    else tc_products<D, PAIR>(a, c, q_smem, ring, warp - 9);
+    if (warp < 8) tc_softmax<D, PAIR>(a, c, q_smem, v_ring, merge, warp >> 2);
+    else if (warp == 8) tc_load<D, PAIR, S::kK>(a, c, &key, k_ring, c.full_k, c.empty_k, true);
+    else if (warp == 11) tc_load<D, PAIR, S::kV>(a, c, &value, v_ring, c.full_v, c.empty_v, false);
+    else tc_products<D, PAIR>(a, c, q_smem, k_ring, v_ring, warp - 9);
     tc_fence_before();
     __syncthreads();
     if (warp == 8) {
