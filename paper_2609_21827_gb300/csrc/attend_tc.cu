@@ -110,8 +110,8 @@ __device__ __forceinline__ bool bar_wait(unsigned long long* b, uint32_t parity,
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_ld() { __syncwarp(); asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void tc_wait_st() { __syncwarp(); asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_commit(unsigned long long* b) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
 }
@@ -120,9 +120,9 @@ __device__ __forceinline__ void tc_commit(unsigned long long* b) {
     M(16), M(17), M(18), M(19), M(20), M(21), M(22), M(23), M(24), M(25), M(26), M(27), M(28), M(29), M(30), M(31)
 #define RHEO_R16(M) M(0), M(1), M(2), M(3), M(4), M(5), M(6), M(7), M(8), M(9), M(10), M(11), M(12), M(13), M(14), M(15)
 
-// 32 columns of this thread's row.
+// Columns of this thread's row.  These are .sync.aligned: callers come with the whole warp together (after a bar_wait,
+// which ends in a vote, or a __syncwarp where lanes took different ways before).
 __device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t at) {
-    __syncwarp();  // .sync.aligned: the whole warp at once
 #define OUT(i) "=r"(r[i])
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
@@ -133,7 +133,6 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t at) {
 #undef OUT
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t at) {
-    __syncwarp();
 #define OUT(i) "=r"(r[i])
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
@@ -143,7 +142,6 @@ __device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t at) {
 #undef OUT
 }
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
-    __syncwarp();
 #define IN(i) "r"(r[i])
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
@@ -286,6 +284,12 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         const bool warp_live = __any_sync(0xffffffffu, live);
         const bool stream_live = PAIR ? r0 + st * 128 < rows : true;
         if (PAIR && !stream_live && !last) fetch(next_b, next_item, 0);
+        if (a.mask && live) {
+            // the row of the mask comes near before the last tiles ask for it
+            const uint8_t* mrow = a.mask + ((int64_t)w.b * a.T + t) * a.T;
+            asm volatile("prefetch.global.L1 [%0];" ::"l"(mrow));
+            asm volatile("prefetch.global.L1 [%0];" ::"l"(mrow + span.add - 1));
+        }
         float m = -INFINITY, l = 0.0f;
         int mine = 0;  // tiles of this stream in this item so far
         for (int q = PAIR ? 0 : st; q < n && stream_live; q += PAIR ? 1 : 2) {
@@ -388,21 +392,35 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 const uint32_t u = tile0 + q;  // this tile's values
                 if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) return;
                 const int place = k0 + tid;
-                if (place >= span.ctx) {
-                    char* line = v_ring + (u % S::kV) * S::kUnit + tid * 128;
+                char* line = v_ring + (u % S::kV) * S::kUnit + tid * 128;
+                auto piece = [&](int p) {
+                    return reinterpret_cast<uint4*>(line + (p >> 3) * 16384 + (((p & 7) ^ (tid & 7)) << 4));
+                };
+                if (place >= len) {
+#pragma unroll
+                    for (int p = 0; p < D / 8; ++p) *piece(p) = make_uint4(0, 0, 0, 0);
+                } else if (place >= span.ctx) {
+                    // 0 * v summed over the line is NaN exactly if some element is not finite
+                    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.0f, 0.0f);
+                    __nv_bfloat162 acc = zero;
 #pragma unroll
                     for (int p = 0; p < D / 8; ++p) {
-                        uint4* at = reinterpret_cast<uint4*>(line + (p >> 3) * 16384 + (((p & 7) ^ (tid & 7)) << 4));
-                        const uint4 x = *at;
-                        uint4 y = make_uint4(odd_mask(x.x), odd_mask(x.y), odd_mask(x.z), odd_mask(x.w));
-                        if (place >= len) {
-                            if (x.x | x.y | x.z | x.w) *at = make_uint4(0, 0, 0, 0);
-                        } else if (y.x | y.y | y.z | y.w) {
-                            const int j = place - span.ctx;
-                            atomicOr(&c.odd[j >> 5], 1u << (j & 31));
-                            c.any_odd = 1;
-                            __threadfence_block();  // the other stream's group finds either the element or the mark
-                            *at = make_uint4(x.x & ~y.x, x.y & ~y.y, x.z & ~y.z, x.w & ~y.w);
+                        const uint4 x = *piece(p);
+                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.x), zero, acc);
+                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.y), zero, acc);
+                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.z), zero, acc);
+                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.w), zero, acc);
+                    }
+                    if (!(__low2float(acc) == 0.0f && __high2float(acc) == 0.0f)) {
+                        const int j = place - span.ctx;
+                        atomicOr(&c.odd[j >> 5], 1u << (j & 31));
+                        c.any_odd = 1;
+                        __threadfence_block();  // the other stream's group finds either the elements or the mark
+#pragma unroll 1
+                        for (int p = 0; p < D / 8; ++p) {
+                            const uint4 x = *piece(p);
+                            *piece(p) = make_uint4(x.x & ~odd_mask(x.x), x.y & ~odd_mask(x.y), x.z & ~odd_mask(x.z),
+                                                   x.w & ~odd_mask(x.w));
                         }
                     }
                 }
@@ -439,6 +457,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 if (st == 1 && warp_live) {
                     for (int d = d0; d < d0 + columns; d += 32) {
                         uint32_t x[32];
+                        __syncwarp();
                         tmem_ld32(x, t_o + d);
                         tc_wait_ld();
 #pragma unroll
@@ -466,6 +485,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
 #pragma unroll 1
                 for (int d = d0; d < d0 + columns; d += 32) {
                     float o[32];
+                    __syncwarp();
                     if (warp_live) {
                         uint32_t x[32];
                         tmem_ld32(x, t_o + d);
