@@ -6,15 +6,19 @@
 //   warps 8, 11      load key tiles and value tiles (TMA) into two rings of shared memory
 //   warps 9, 10      issue the matrix products of stream 0 and 1
 // A stream holds up to 128 query rows (token, head of the key/value head): its
-// scores S = Q K^T (128 x 128 fp32) and its sums O (128 x D fp32) lie in tensor
-// memory.  Per key tile: S by tcgen05.mma from shared memory; the group reads its
-// rows, p = 2^(s - m), writes p (bf16) over S; O += P V by tcgen05.mma with P from
-// tensor memory.  While one stream's group computes exponentials, the other
-// stream's products run.
-//   PAIR:   an item has up to 256 rows, each stream takes 128 of them and both
-//           read every key tile: the tile crosses HBM once for all heads and tokens;
-//   !PAIR:  up to 128 rows (single tokens, short chains): the streams take the
-//           key tiles alternately and their sums are joined at the end.
+// scores S = Q K^T (128 x 64 fp32), weights P (two buffers of 128 x 64 bf16) and
+// sums O (128 x D fp32) lie in tensor memory.  Per 64 keys: S by tcgen05.mma from
+// shared memory; the group reads its rows, which frees S for the next 64 keys'
+// product, computes p = 2^(s - m) and writes P; O += P V by tcgen05.mma with P
+// from tensor memory.  So the next scores are there when a group has written its
+// weights, and both groups compute exponentials all the time.
+//   PAIR:   an item has up to 256 rows, each stream takes 128 of them and all
+//           keys: a tile crosses HBM once for all heads and tokens;
+//   !PAIR:  up to 128 rows (single tokens, short chains): stream 0 takes the
+//           first 64 keys of every tile, stream 1 the others, and their sums are
+//           joined at the end.
+// Each stream meets every tile of both rings, whether it has a product there or
+// not: a barrier's parity tells phases apart only for who waits for all of them.
 // The reference m of a row follows its largest score only when that has grown by
 // more than kSlack in log2 units: then O is multiplied in place (rare after the
 // first tiles); until then p <= 2^kSlack, which bf16 and the fp32 sums hold with
@@ -34,7 +38,8 @@
 namespace rheo {
 namespace {
 
-constexpr int kTile = 128;                   // keys a tile
+constexpr int kTile = 128;                   // keys a tile: what is loaded at a time
+constexpr int kSub = 64;                     // keys of a score product: half a tile
 constexpr int kTcThreads = 12 * 32;
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
@@ -43,19 +48,19 @@ constexpr int kDrainLimit = 1 << 16;         // and of a drain after that
 template <int D, bool PAIR> struct TcShape {
     static constexpr int kUnit = kTile * D * 2;  // bytes of a key or value tile
     static constexpr int kHalves = D / 64;       // 128-byte wide parts of a line
-    // Slots of the key ring and of the value ring.  !PAIR: even, so that within an item a slot serves one stream
-    // only; a stream that met a slot's barrier every other time could take the phase before last for its own.
-    // (Between items all tiles are consumed before either stream waits for the next item's.)
-    static constexpr int kK = D == 128 ? 2 : PAIR ? 5 : 4;
-    static constexpr int kV = D == 128 ? (PAIR ? 3 : 2) : PAIR ? 5 : 4;
+    static constexpr int kK = D == 128 ? 2 : 5;  // slots of the key ring
+    static constexpr int kV = D == 128 ? 3 : 5;  // and of the value ring, which is read later
     static constexpr int kQ = 128 * D * 2;       // bytes of 128 rows of queries
+    static constexpr int kQueries = PAIR ? 2 * kQ : kQ;
     static constexpr int kMerge = PAIR ? 0 : 16384;
-    static constexpr int kO = 256;               // first tensor-memory column of the sums
+    // Tensor memory: stream s has its scores at column 128 s (64 columns), two buffers of weights at 128 s + 64 and
+    // + 96 (32 each, bf16 pairs), its sums at kO + s D.
+    static constexpr int kO = 256;
 };
 
 struct TcControl {
     unsigned long long full_k[5], empty_k[5], full_v[5], empty_v[5];
-    unsigned long long s_full[2], p_ready[2], pv_done[2], drained[2], q_ready, q_taken, all_sync;
+    unsigned long long s_full[2], s_free[2], p_ready[2][2], pv_done[2][2], drained[2], q_ready, q_taken, all_sync;
     uint32_t tmem;
     int abort;
     int any_odd;          // some drafted value is not finite
@@ -66,7 +71,7 @@ struct TcControl {
 
 template <int D, bool PAIR> constexpr size_t tc_smem_bytes() {
     using S = TcShape<D, PAIR>;
-    return 1024 + 2 * S::kQ + (size_t)(S::kK + S::kV) * S::kUnit + S::kMerge + sizeof(TcControl);
+    return 1024 + S::kQueries + (size_t)(S::kK + S::kV) * S::kUnit + S::kMerge + sizeof(TcControl);
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -132,14 +137,15 @@ __device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t at) {
         : "r"(at));
 #undef OUT
 }
-__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t at) {
-#define OUT(i) "=r"(r[i])
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t (&r)[32]) {
+#define IN(i) "r"(r[i])
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : RHEO_R16(OUT)
-        : "r"(at));
-#undef OUT
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::RHEO_R32(IN),
+        "r"(at)
+        : "memory");
+#undef IN
 }
 __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t (&r)[16]) {
 #define IN(i) "r"(r[i])
@@ -181,6 +187,9 @@ __device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap* map, i
         "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(0), "r"(head), "r"(page)
         : "memory");
 }
+
+// Score products of tile `tile` of an item of `len` places: the second half only where it has a place.
+__device__ __forceinline__ int tc_subs(int len, int tile) { return len - tile * kTile > kSub ? 2 : 1; }
 
 // One CTA's run through its items, the same in every warp.
 struct TcWalk {
@@ -238,24 +247,22 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
     const uint32_t t_s = c.tmem + lanes + st * 128, t_o = c.tmem + lanes + S::kO + st * D;
     const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);  // above 0, so that hidden places stay at -inf
     const bool negative = a.scale_log2 < 0.0f;
-    uint32_t items = 0, tiles_done = 0, syncs = 0, tile0 = 0;
+    uint32_t items = 0, products = 0, syncs = 0, tile0 = 0;
     auto sync_all = [&]() -> bool {
         bar_arrive_warp(&c.all_sync);
         return bar_wait(&c.all_sync, syncs++ & 1, c);
     };
-    // queries of the item at (b, item) into this stream's rows (PAIR) or the buffer of that turn
-    auto fetch = [&](int b, int item, uint32_t turn) {
+    // queries of an item: each stream's group fetches its own rows (PAIR), or stream 0's all of them
+    auto fetch = [&](int b, int item) {
         const int h = item / groups, first = item % groups * item_rows + (PAIR ? st * 128 : 0);
-        const int count = min(128, rows - first);
-        if (PAIR) tc_queries<D>(a, b, h, first, count, q_smem + st * S::kQ, tid, 128);
-        else tc_queries<D>(a, b, h, first, count, q_smem + (turn & 1) * S::kQ, threadIdx.x, 256);
+        tc_queries<D>(a, b, h, first, min(128, rows - first), q_smem + (PAIR ? st * S::kQ : 0), tid, 128);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     TcWalk w(c.cut);
     AttendSpan next_span{0, 0, false};
     if (w.more()) {
         next_span = attend_span(a, w.b);
-        fetch(w.b, w.item, 0);
+        if (PAIR || st == 0) fetch(w.b, w.item);
     }
     while (w.more()) {
         const AttendSpan span = next_span;
@@ -273,187 +280,214 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         bar_arrive_warp(&c.q_ready);
         const bool last = w.at + n >= w.end;
         const int next_b = w.item + 1 == per ? w.b + 1 : w.b, next_item = w.item + 1 == per ? 0 : w.item + 1;
-        if (!last) {
-            next_span = attend_span(a, next_b);
-            if (!PAIR) fetch(next_b, next_item, items + 1);  // the other buffer is free: its item is over
-        }
+        if (!last) next_span = attend_span(a, next_b);
         ++items;
 
         const int row = r0 + (PAIR ? st * 128 : 0) + tid, t = row / a.G;
         const bool live = row < rows && t < span.add;
         const bool warp_live = __any_sync(0xffffffffu, live);
         const bool stream_live = PAIR ? r0 + st * 128 < rows : true;
-        if (PAIR && !stream_live && !last) fetch(next_b, next_item, 0);
+        if (PAIR && !stream_live && !last) fetch(next_b, next_item);
         if (a.mask && live) {
             // the row of the mask comes near before the last tiles ask for it
             const uint8_t* mrow = a.mask + ((int64_t)w.b * a.T + t) * a.T;
             asm volatile("prefetch.global.L1 [%0];" ::"l"(mrow));
             asm volatile("prefetch.global.L1 [%0];" ::"l"(mrow + span.add - 1));
         }
+        // Values of the tile at place k0 (tile u of this CTA) before a product of this stream reads them: nothing behind
+        // the request's places, and no element that is not finite among the drafted tokens'.  PAIR: a thread a line;
+        // !PAIR: the stream's half of the lines, two threads a line.
+        auto clean = [&](int k0, uint32_t u) -> bool {
+            if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) return false;
+            constexpr int pieces = PAIR ? D / 8 : D / 16;
+            const int r = PAIR ? tid : st * kSub + tid / 2, p0 = PAIR ? 0 : tid % 2 * pieces, place = k0 + r;
+            char* line = v_ring + (u % S::kV) * S::kUnit + r * 128;
+            auto piece = [&](int i) {
+                const int p = p0 + i;
+                return reinterpret_cast<uint4*>(line + (p >> 3) * 16384 + (((p & 7) ^ (r & 7)) << 4));
+            };
+            if (place >= len) {
+#pragma unroll
+                for (int i = 0; i < pieces; ++i) *piece(i) = make_uint4(0, 0, 0, 0);
+            } else if (place >= span.ctx) {
+                // 0 * v summed over the line is NaN exactly if some element is not finite
+                const __nv_bfloat162 zero = __floats2bfloat162_rn(0.0f, 0.0f);
+                __nv_bfloat162 acc = zero;
+#pragma unroll
+                for (int i = 0; i < pieces; ++i) {
+                    const uint4 x = *piece(i);
+                    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.x), zero, acc);
+                    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.y), zero, acc);
+                    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.z), zero, acc);
+                    acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.w), zero, acc);
+                }
+                if (!(__low2float(acc) == 0.0f && __high2float(acc) == 0.0f)) {
+                    const int j = place - span.ctx;
+                    atomicOr(&c.odd[j >> 5], 1u << (j & 31));
+                    c.any_odd = 1;
+                    __threadfence_block();  // the other stream's group finds either the elements or the mark
+#pragma unroll 1
+                    for (int i = 0; i < pieces; ++i) {
+                        const uint4 x = *piece(i);
+                        *piece(i) = make_uint4(x.x & ~odd_mask(x.x), x.y & ~odd_mask(x.y), x.z & ~odd_mask(x.z),
+                                               x.w & ~odd_mask(x.w));
+                    }
+                }
+            }
+            fence_async();
+            return true;
+        };
         float m = -INFINITY, l = 0.0f;
-        int mine = 0;  // tiles of this stream in this item so far
-        for (int q = PAIR ? 0 : st; q < n && stream_live; q += PAIR ? 1 : 2) {
-            const int k0 = (w.tile + q) * kTile;
-            const bool tail = k0 + kTile > span.ctx;
-            uint32_t vis[4] = {0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu};
-            if (tail && warp_live) {
-                // the warp's tokens, four at a time, 32 places a vote
-                const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
-                for (int tt = (row - lane) / a.G; tt <= t_last; tt += 4) {
-                    bool sees[4][4];
+        int mine = 0;  // score products of this stream in this item so far
+        for (int q = 0; q < n && stream_live; ++q) {
+            const int tile_k0 = (w.tile + q) * kTile, subs = tc_subs(len, w.tile + q);
+            for (int sub = PAIR ? 0 : st; sub < subs; sub += PAIR ? 1 : 2) {
+                const int k0 = tile_k0 + sub * kSub;
+                const bool tail = k0 + kSub > span.ctx;
+                uint32_t vis[2] = {0xffffffffu, 0xffffffffu};
+                if (tail && warp_live) {
+                    // the warp's tokens, four at a time, 32 places a vote
+                    const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
+                    for (int tt = (row - lane) / a.G; tt <= t_last; tt += 4) {
+                        bool sees[4][2];
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + min(tt + u, t_last)) * a.T : nullptr;
+                        for (int u = 0; u < 4; ++u) {
+                            const uint8_t* mrow =
+                                a.mask ? a.mask + ((int64_t)w.b * a.T + min(tt + u, t_last)) * a.T : nullptr;
 #pragma unroll
-                        for (int v = 0; v < 4; ++v)
-                            sees[u][v] = tt + u < span.add && attend_sees(span, mrow, tt + u, k0 + 32 * v + lane);
-                    }
-#pragma unroll
-                    for (int u = 0; u < 4; ++u)
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) {
-                            const uint32_t bits = __ballot_sync(0xffffffffu, sees[u][v]);
-                            if (tt + u == t) vis[v] = bits;
+                            for (int v = 0; v < 2; ++v)
+                                sees[u][v] = tt + u < span.add && attend_sees(span, mrow, tt + u, k0 + 32 * v + lane);
                         }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+#pragma unroll
+                            for (int v = 0; v < 2; ++v) {
+                                const uint32_t bits = __ballot_sync(0xffffffffu, sees[u][v]);
+                                if (tt + u == t) vis[v] = bits;
+                            }
+                    }
                 }
-            }
-            if (!bar_wait(&c.s_full[st], tiles_done & 1, c)) return;
-            tc_fence_after();
-            // the item's last scores are there: this stream's queries have been read
-            if (PAIR && q == n - 1 && !last) fetch(next_b, next_item, 0);
-            if (warp_live) {
-                uint32_t s[4][32];
-#pragma unroll
-                for (int v = 0; v < 4; ++v) tmem_ld32(s[v], t_s + 32 * v);
-                tc_wait_ld();
-                if (negative) {
-#pragma unroll
-                    for (int v = 0; v < 4; ++v)
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) s[v][i] ^= 0x80000000u;
+                if (!bar_wait(&c.s_full[st], products & 1, c)) return;
+                tc_fence_after();
+                // the item's last scores are there: this stream's queries have been read
+                if (PAIR && q == n - 1 && sub == subs - 1 && !last) fetch(next_b, next_item);
+                uint32_t s[2][32];
+                __syncwarp();
+                if (warp_live) {
+                    tmem_ld32(s[0], t_s);
+                    tmem_ld32(s[1], t_s + 32);
+                    tc_wait_ld();
                 }
-                if (tail) {
+                tc_fence_before();
+                bar_arrive_warp(&c.s_free[st]);
+                // the buffer of these weights was read by the product before last
+                const uint32_t buf = products & 1;
+                if (products > 1 && !bar_wait(&c.pv_done[st][buf], (products / 2 - 1) & 1, c)) return;
+                tc_fence_after();
+                if (warp_live) {
+                    if (negative) {
 #pragma unroll
-                    for (int v = 0; v < 4; ++v)
+                        for (int v = 0; v < 2; ++v)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!((vis[v] >> i) & 1u)) s[v][i] = 0xFF800000u;
-                }
-                float tops[4];
+                            for (int i = 0; i < 32; ++i) s[v][i] ^= 0x80000000u;
+                    }
+                    if (tail) {
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    float x = max3(__uint_as_float(s[v][0]), __uint_as_float(s[v][1]), __uint_as_float(s[v][2]));
+                        for (int v = 0; v < 2; ++v)
 #pragma unroll
-                    for (int i = 3; i + 1 < 32; i += 2) x = max3(x, __uint_as_float(s[v][i]), __uint_as_float(s[v][i + 1]));
-                    tops[v] = fmaxf(x, __uint_as_float(s[v][31]));
-                }
-                const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * sc;
-                if (mine == 0) {
-                    m = top;
-                } else {
-                    const bool grow = top > m + kSlack || (m == -INFINITY && top > m);
-                    if (__any_sync(0xffffffffu, grow)) {
-                        // the sums so far move to the new reference
-                        if (!bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) return;
-                        tc_fence_after();
-                        const float f = !grow || m == -INFINITY ? 1.0f : fast_exp2(m - top);
+                            for (int i = 0; i < 32; ++i)
+                                if (!((vis[v] >> i) & 1u)) s[v][i] = 0xFF800000u;
+                    }
+                    float tops[4];
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        const uint32_t* x = s[v / 2] + v % 2 * 16;
+                        tops[v] = max3(__uint_as_float(x[0]), __uint_as_float(x[1]), __uint_as_float(x[2]));
+#pragma unroll
+                        for (int i = 3; i + 1 < 16; i += 2)
+                            tops[v] = max3(tops[v], __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+                        tops[v] = fmaxf(tops[v], __uint_as_float(x[15]));
+                    }
+                    const float top = fmaxf(max3(tops[0], tops[1], tops[2]), tops[3]) * sc;
+                    if (mine == 0) {
+                        m = top;
+                    } else {
+                        const bool grow = top > m + kSlack || (m == -INFINITY && top > m);
+                        if (__any_sync(0xffffffffu, grow)) {
+                            // the sums so far move to the new reference
+                            if (!bar_wait(&c.pv_done[st][buf ^ 1], ((products - 1) / 2) & 1, c)) return;
+                            tc_fence_after();
+                            const float f = !grow || m == -INFINITY ? 1.0f : fast_exp2(m - top);
 #pragma unroll 1
-                        for (int d = 0; d < D; d += 16) {
-                            uint32_t o[16];
-                            tmem_ld16(o, t_o + d);
-                            tc_wait_ld();
+                            for (int d = 0; d < D; d += 32) {
+                                uint32_t o[32];
+                                __syncwarp();
+                                tmem_ld32(o, t_o + d);
+                                tc_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                            tmem_st16(t_o + d, o);
-                        }
-                        l *= f;
-                        if (grow) m = top;
-                    }
-                }
-                const float ref = m == -INFINITY ? 0.0f : m;
-                const unsigned long long sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
-                unsigned long long sum[4] = {0ull, 0ull, 0ull, 0ull};
-#pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    uint32_t p[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const unsigned long long x = f2_exp2(
-                            f2_fma(f2_pack(__uint_as_float(s[v][2 * i]), __uint_as_float(s[v][2 * i + 1])), sc2, ref2));
-                        sum[i & 3] = f2_add(sum[i & 3], x);
-                        p[i] = pack_bf16(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
-                    }
-                    tmem_st16(t_s + 16 * v, p);
-                }
-                l += f2_fold(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])));
-                tc_wait_st();
-            }
-            if (tail) {
-                const uint32_t u = tile0 + q;  // this tile's values
-                if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) return;
-                const int place = k0 + tid;
-                char* line = v_ring + (u % S::kV) * S::kUnit + tid * 128;
-                auto piece = [&](int p) {
-                    return reinterpret_cast<uint4*>(line + (p >> 3) * 16384 + (((p & 7) ^ (tid & 7)) << 4));
-                };
-                if (place >= len) {
-#pragma unroll
-                    for (int p = 0; p < D / 8; ++p) *piece(p) = make_uint4(0, 0, 0, 0);
-                } else if (place >= span.ctx) {
-                    // 0 * v summed over the line is NaN exactly if some element is not finite
-                    const __nv_bfloat162 zero = __floats2bfloat162_rn(0.0f, 0.0f);
-                    __nv_bfloat162 acc = zero;
-#pragma unroll
-                    for (int p = 0; p < D / 8; ++p) {
-                        const uint4 x = *piece(p);
-                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.x), zero, acc);
-                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.y), zero, acc);
-                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.z), zero, acc);
-                        acc = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&x.w), zero, acc);
-                    }
-                    if (!(__low2float(acc) == 0.0f && __high2float(acc) == 0.0f)) {
-                        const int j = place - span.ctx;
-                        atomicOr(&c.odd[j >> 5], 1u << (j & 31));
-                        c.any_odd = 1;
-                        __threadfence_block();  // the other stream's group finds either the elements or the mark
-#pragma unroll 1
-                        for (int p = 0; p < D / 8; ++p) {
-                            const uint4 x = *piece(p);
-                            *piece(p) = make_uint4(x.x & ~odd_mask(x.x), x.y & ~odd_mask(x.y), x.z & ~odd_mask(x.z),
-                                                   x.w & ~odd_mask(x.w));
+                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                                tmem_st32(t_o + d, o);
+                            }
+                            l *= f;
+                            if (grow) m = top;
                         }
                     }
+                    const float ref = m == -INFINITY ? 0.0f : m;
+                    const unsigned long long sc2 = f2_pack(sc, sc), ref2 = f2_pack(-ref, -ref);
+                    unsigned long long sum[4] = {0ull, 0ull, 0ull, 0ull};
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        uint32_t p[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const unsigned long long x = f2_exp2(
+                                f2_fma(f2_pack(__uint_as_float(s[v][2 * i]), __uint_as_float(s[v][2 * i + 1])), sc2, ref2));
+                            sum[i & 3] = f2_add(sum[i & 3], x);
+                            p[i] = pack_bf16(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
+                        }
+                        if (v == 0) __syncwarp();
+                        tmem_st16(t_s + 64 + 32 * buf + 16 * v, p);
+                    }
+                    l += f2_fold(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])));
+                    tc_wait_st();
                 }
-                fence_async();
+                if ((!PAIR || sub == 0) && tile_k0 + kTile > span.ctx) {
+                    if (!clean(tile_k0, tile0 + q)) return;
+                }
+                tc_fence_before();
+                bar_arrive_warp(&c.p_ready[st][buf]);
+                ++products;
+                ++mine;
             }
-            tc_fence_before();
-            bar_arrive_warp(&c.p_ready[st]);
-            ++tiles_done;
-            ++mine;
         }
         tile0 += n;
 
         // ---- the item's sums
+        // both buffers' last products
         if (mine > 0) {
-            if (!bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) return;
+            const uint32_t x = products - 1;
+            if (x > 0 && !bar_wait(&c.pv_done[st][(x - 1) & 1], ((x - 1) / 2) & 1, c)) return;
+            if (!bar_wait(&c.pv_done[st][x & 1], (x / 2) & 1, c)) return;
             tc_fence_after();
         }
         const bool whole = n == all;
         const int64_t part = attend_part(blockIdx.x, w.tile == 0);
         const int r_in = (PAIR ? st * 128 : 0) + tid, head = h * a.G + row - t * a.G;
-        float f0 = 1.0f, f1 = 0.0f;  // !PAIR: the weights of the two streams
+        const bool both = !PAIR && (n > 1 || tc_subs(len, w.tile) == 2);  // stream 1 has a share of the sums
+        float f0 = 1.0f, f1 = 0.0f;                                      // the weights of the two streams
         int columns = D;             // that the streams exchange at a time
         const int kept = PAIR ? 128 : min(128, (rows + 31) / 32 * 32);  // rows of an item, to whole warps
-        if (!PAIR && n > 1) {
+        if (both) {
             columns = min(D, 4096 / kept / 32 * 32);
             if (st == 1) c.ml[tid] = make_float2(m, l);
         } else if (!PAIR && st == 1) {
-            columns = 0;  // a single tile: it was stream 0's
+            columns = 0;
         }
+        if (!PAIR && !both && st == 0 && !last) fetch(next_b, next_item);
         float4* pass = reinterpret_cast<float4*>(merge);  // [columns / 4][kept]
         float ll = live ? l : 0.0f;
         for (int d0 = 0; d0 < D && columns > 0; d0 += columns) {
-            if (!PAIR && n > 1) {
+            if (both) {
                 if (st == 1 && warp_live) {
                     for (int d = d0; d < d0 + columns; d += 32) {
                         uint32_t x[32];
@@ -469,6 +503,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 }
                 if (!sync_all()) return;
                 if (st == 0 && d0 == 0) {
+                    if (!last) fetch(next_b, next_item);  // both streams are through with the queries
                     const float2 x = c.ml[tid];
                     const float mm = fmaxf(m, x.x), ref = mm == -INFINITY ? 0.0f : mm;
                     f0 = fast_exp2(m - ref);
@@ -492,7 +527,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                         tc_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = __uint_as_float(x[i]);
-                        if (!PAIR && n > 1) {
+                        if (both) {
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 const float4 y = pass[((d - d0) / 4 + i) * kept + tid];
@@ -550,7 +585,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 }
             }
             // stream 1 writes the next columns when stream 0 has read these
-            if (!PAIR && n > 1 && d0 + columns < D && !sync_all()) return;
+            if (both && d0 + columns < D && !sync_all()) return;
         }
         if ((PAIR || st == 0) && row < rows) {
             if (whole) {
@@ -622,53 +657,74 @@ __device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, c
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = a.H * groups;
     const uint32_t t_s = c.tmem + st * 128, t_o = c.tmem + S::kO + st * D;
-    uint32_t items = 0, tiles_done = 0, tile0 = 0;
+    uint32_t items = 0, scored = 0, weighed = 0, tile0 = 0;
     for (TcWalk w(c.cut); w.more(); ++items) {
-        const int n = w.count(attend_span(a, w.b).len());
+        const int len = attend_span(a, w.b).len(), n = w.count(len);
         const bool stream_live = PAIR ? w.item % groups * item_rows + st * 128 < rows : true;
-        const uint32_t q_at = smem_u32(q_smem + (PAIR ? st : items & 1) * S::kQ);
+        const uint32_t q_at = smem_u32(q_smem + (PAIR ? st * S::kQ : 0));
         if (!bar_wait(&c.q_ready, items & 1, c)) goto out;
         tc_fence_after();
         if (lane == 0) bar_arrive(&c.q_taken);
-        for (int q = PAIR ? 0 : st; q < n; q += PAIR ? 1 : 2) {
-            const uint32_t u = tile0 + q;
-            unsigned long long *full_k = &c.full_k[u % S::kK], *full_v = &c.full_v[u % S::kV],
-                               *empty_k = &c.empty_k[u % S::kK], *empty_v = &c.empty_v[u % S::kV];
-            if (!bar_wait(full_k, (u / S::kK) & 1, c)) goto out;
-            if (!stream_live) {
-                if (lane == 0) bar_arrive(empty_k);
-                if (!bar_wait(full_v, (u / S::kV) & 1, c)) goto out;
-                if (lane == 0) bar_arrive(empty_v);
-                continue;
-            }
-            // S overwrites the last tile's P: its product has to be done
-            if (tiles_done > 0 && !bar_wait(&c.pv_done[st], (tiles_done - 1) & 1, c)) goto out;
-            tc_fence_after();
-            if (lane == 0) {
-                const uint32_t k_at = smem_u32(k_ring + (u % S::kK) * S::kUnit);
+        const uint32_t before = weighed;
+        // The scores' place (tile kq, half ksub) runs one product ahead of the weights' (q, sub).
+        int kq = 0, ksub = PAIR ? 0 : st, q = 0, sub = ksub;
+        while (q < n) {
+            while (kq < n && kq <= q + 1 && scored <= weighed + 1) {
+                const uint32_t u = tile0 + kq;
+                const int subs = stream_live ? tc_subs(len, w.tile + kq) : 0, next = ksub + (PAIR ? 1 : 2);
+                if (!bar_wait(&c.full_k[u % S::kK], (u / S::kK) & 1, c)) goto out;
+                if (ksub < subs) {
+                    // the group has taken the last scores
+                    if (scored > 0 && !bar_wait(&c.s_free[st], (scored - 1) & 1, c)) goto out;
+                    tc_fence_after();
+                    if (lane == 0) {
+                        const uint32_t k_at = smem_u32(k_ring + (u % S::kK) * S::kUnit) + ksub * kSub * 128;
 #pragma unroll
-                for (int i = 0; i < D / 16; ++i) {
-                    const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
-                    mma_ss(t_s, smem_desc(q_at + off, 16, 1024), smem_desc(k_at + off, 16, 1024), mma_desc(kTile, false), i > 0);
+                        for (int i = 0; i < D / 16; ++i) {
+                            const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
+                            mma_ss(t_s, smem_desc(q_at + off, 16, 1024), smem_desc(k_at + off, 16, 1024),
+                                   mma_desc(kSub, false), i > 0);
+                        }
+                        if (next >= subs) tc_commit(&c.empty_k[u % S::kK]);
+                        tc_commit(&c.s_full[st]);
+                    }
+                    __syncwarp();
+                    ++scored;
+                } else if (lane == 0) {
+                    bar_arrive(&c.empty_k[u % S::kK]);  // nothing of the tile is this stream's
                 }
-                tc_commit(empty_k);
-                tc_commit(&c.s_full[st]);
+                ksub = next;
+                if (ksub >= subs) {
+                    ksub = PAIR ? 0 : st;
+                    ++kq;
+                }
             }
-            __syncwarp();
-            if (!bar_wait(full_v, (u / S::kV) & 1, c)) goto out;
-            if (!bar_wait(&c.p_ready[st], tiles_done & 1, c)) goto out;
-            tc_fence_after();
-            if (lane == 0) {
-                const uint32_t v_at = smem_u32(v_ring + (u % S::kV) * S::kUnit);
+            const uint32_t u = tile0 + q;
+            const int subs = stream_live ? tc_subs(len, w.tile + q) : 0, next = sub + (PAIR ? 1 : 2);
+            if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) goto out;
+            if (sub < subs) {
+                if (!bar_wait(&c.p_ready[st][weighed & 1], (weighed / 2) & 1, c)) goto out;
+                tc_fence_after();
+                if (lane == 0) {
+                    const uint32_t v_at = smem_u32(v_ring + (u % S::kV) * S::kUnit) + sub * kSub * 128;
+                    const uint32_t p_at = t_s + 64 + 32 * (weighed & 1);
 #pragma unroll
-                for (int i = 0; i < kTile / 16; ++i)
-                    mma_ts(t_o, t_s + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024), mma_desc(D, true),
-                           i > 0 || q >= (PAIR ? 1 : 2));
-                tc_commit(empty_v);
-                tc_commit(&c.pv_done[st]);
+                    for (int i = 0; i < kSub / 16; ++i)
+                        mma_ts(t_o, p_at + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024), mma_desc(D, true),
+                               i > 0 || weighed != before);
+                    if (next >= subs) tc_commit(&c.empty_v[u % S::kV]);
+                    tc_commit(&c.pv_done[st][weighed & 1]);
+                }
+                __syncwarp();
+                ++weighed;
+            } else if (lane == 0) {
+                bar_arrive(&c.empty_v[u % S::kV]);
             }
-            __syncwarp();
-            ++tiles_done;
+            sub = next;
+            if (sub >= subs) {
+                sub = PAIR ? 0 : st;
+                ++q;
+            }
         }
         tile0 += n;
         w.next(n, per);
@@ -687,7 +743,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     extern __shared__ char raw[];
     char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     char* q_smem = base;
-    char* k_ring = q_smem + 2 * S::kQ;
+    char* k_ring = q_smem + S::kQueries;
     char* v_ring = k_ring + S::kK * S::kUnit;
     char* merge = v_ring + S::kV * S::kUnit;
     TcControl& c = *reinterpret_cast<TcControl*>(merge + S::kMerge);
@@ -695,16 +751,19 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kK; ++i) {
             bar_init(&c.full_k[i], 1);
-            bar_init(&c.empty_k[i], PAIR ? 2 : 1);
+            bar_init(&c.empty_k[i], 2);
         }
         for (int i = 0; i < S::kV; ++i) {
             bar_init(&c.full_v[i], 1);
-            bar_init(&c.empty_v[i], PAIR ? 2 : 1);
+            bar_init(&c.empty_v[i], 2);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&c.s_full[i], 1);
-            bar_init(&c.p_ready[i], 4);
-            bar_init(&c.pv_done[i], 1);
+            bar_init(&c.p_ready[i][0], 4);
+            bar_init(&c.p_ready[i][1], 4);
+            bar_init(&c.s_free[i], 4);
+            bar_init(&c.pv_done[i][0], 1);
+            bar_init(&c.pv_done[i][1], 1);
             bar_init(&c.drained[i], 1);
         }
         bar_init(&c.q_ready, 8);
