@@ -117,9 +117,16 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// The whole warp calls the next ones with the same operands; one elected lane, always the same, issues.  (A branch on
+// the lane would keep the operands out of the uniform registers that these instructions read: 110 cycles a product.)
 __device__ __forceinline__ void tc_commit(unsigned long long* b) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(b))
+        : "memory");
 }
+// A value that is the same in all lanes, in a register that the compiler knows to be.
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
 
 #define RHEO_R32(M) M(0), M(1), M(2), M(3), M(4), M(5), M(6), M(7), M(8), M(9), M(10), M(11), M(12), M(13), M(14), M(15), \
     M(16), M(17), M(18), M(19), M(20), M(21), M(22), M(23), M(24), M(25), M(26), M(27), M(28), M(29), M(30), M(31)
@@ -168,15 +175,15 @@ __device__ __forceinline__ constexpr uint32_t mma_desc(int n, bool b_along_n) {
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
         : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
         : "memory");
 }
@@ -656,12 +663,12 @@ __device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, c
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = a.H * groups;
-    const uint32_t t_s = c.tmem + st * 128, t_o = c.tmem + S::kO + st * D;
+    const uint32_t t_s = uniform(c.tmem + st * 128), t_o = uniform(c.tmem + S::kO + st * D);
+    const uint32_t q_at = uniform(smem_u32(q_smem + (PAIR ? st * S::kQ : 0)));
     uint32_t items = 0, scored = 0, weighed = 0, tile0 = 0;
     for (TcWalk w(c.cut); w.more(); ++items) {
         const int len = attend_span(a, w.b).len(), n = w.count(len);
         const bool stream_live = PAIR ? w.item % groups * item_rows + st * 128 < rows : true;
-        const uint32_t q_at = smem_u32(q_smem + (PAIR ? st * S::kQ : 0));
         if (!bar_wait(&c.q_ready, items & 1, c)) goto out;
         tc_fence_after();
         if (lane == 0) bar_arrive(&c.q_taken);
@@ -677,8 +684,8 @@ __device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, c
                     // the group has taken the last scores
                     if (scored > 0 && !bar_wait(&c.s_free[st], (scored - 1) & 1, c)) goto out;
                     tc_fence_after();
-                    if (lane == 0) {
-                        const uint32_t k_at = smem_u32(k_ring + (u % S::kK) * S::kUnit) + ksub * kSub * 128;
+                    {
+                        const uint32_t k_at = uniform(smem_u32(k_ring + (u % S::kK) * S::kUnit) + ksub * kSub * 128);
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
                             const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
@@ -688,7 +695,6 @@ __device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, c
                         if (next >= subs) tc_commit(&c.empty_k[u % S::kK]);
                         tc_commit(&c.s_full[st]);
                     }
-                    __syncwarp();
                     ++scored;
                 } else if (lane == 0) {
                     bar_arrive(&c.empty_k[u % S::kK]);  // nothing of the tile is this stream's
@@ -705,17 +711,17 @@ __device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, c
             if (sub < subs) {
                 if (!bar_wait(&c.p_ready[st][weighed & 1], (weighed / 2) & 1, c)) goto out;
                 tc_fence_after();
-                if (lane == 0) {
-                    const uint32_t v_at = smem_u32(v_ring + (u % S::kV) * S::kUnit) + sub * kSub * 128;
-                    const uint32_t p_at = t_s + 64 + 32 * (weighed & 1);
+                {
+                    const uint32_t v_at = uniform(smem_u32(v_ring + (u % S::kV) * S::kUnit) + sub * kSub * 128);
+                    const uint32_t p_at = uniform(t_s + 64 + 32 * (weighed & 1));
+                    const bool add = uniform(weighed != before);
 #pragma unroll
                     for (int i = 0; i < kSub / 16; ++i)
                         mma_ts(t_o, p_at + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024), mma_desc(D, true),
-                               i > 0 || weighed != before);
+                               i > 0 || add);
                     if (next >= subs) tc_commit(&c.empty_v[u % S::kV]);
                     tc_commit(&c.pv_done[st][weighed & 1]);
                 }
-                __syncwarp();
                 ++weighed;
             } else if (lane == 0) {
                 bar_arrive(&c.empty_v[u % S::kV]);
@@ -732,7 +738,7 @@ __device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, c
 out:
     // nothing of this stream is in flight when the CTA ends
     __syncwarp();
-    if (lane == 0) tc_commit(&c.drained[st]);
+    tc_commit(&c.drained[st]);
     bar_wait<true>(&c.drained[st], 0, c);
 }
 
