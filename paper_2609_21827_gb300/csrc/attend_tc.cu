@@ -4,7 +4,7 @@
 // One CTA an SM, twelve warps:
 //   warps 0-3, 4-7   two softmax groups, one a stream; thread = query row
 //   warps 8, 11      load key tiles and value tiles (TMA) into two rings of shared memory
-//   warps 9, 10      issue the matrix products of stream 0 and 1
+//   warps 9, 10      issue the score products and the products with the values
 // A stream holds up to 128 query rows (token, head of the key/value head): its
 // scores S = Q K^T (128 x 64 fp32), weights P (two buffers of 128 x 64 bf16) and
 // sums O (128 x D fp32) lie in tensor memory.  Per 64 keys: S by tcgen05.mma from
@@ -17,8 +17,8 @@
 //   !PAIR:  up to 128 rows (single tokens, short chains): stream 0 takes the
 //           first 64 keys of every tile, stream 1 the others, and their sums are
 //           joined at the end.
-// Each stream meets every tile of both rings, whether it has a product there or
-// not: a barrier's parity tells phases apart only for who waits for all of them.
+// Whoever waits at a barrier meets each of its phases in turn: a parity tells a
+// phase only from its neighbours.
 // The reference m of a row follows its largest score only when that has grown by
 // more than kSlack in log2 units: then O is multiplied in place (rare after the
 // first tiles); until then p <= 2^kSlack, which bf16 and the fp32 sums hold with
@@ -117,13 +117,17 @@ __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence:
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-// The whole warp calls the next ones with the same operands; one elected lane, always the same, issues.  (A branch on
-// the lane would keep the operands out of the uniform registers that these instructions read: 110 cycles a product.)
-__device__ __forceinline__ void tc_commit(unsigned long long* b) {
+// True in one lane of the warp, always the same one.  Products and commits are issued under it, with operands that the
+// compiler knows to be uniform; a branch on the lane instead cost 110 cycles a product.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
     asm volatile(
-        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\t"
-        "@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(smem_u32(b))
-        : "memory");
+        "{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}"
+        : "=r"(e)::"memory");
+    return e != 0;
+}
+__device__ __forceinline__ void tc_commit(unsigned long long* b) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
 }
 // A value that is the same in all lanes, in a register that the compiler knows to be.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
@@ -175,15 +179,15 @@ __device__ __forceinline__ constexpr uint32_t mma_desc(int n, bool b_along_n) {
 }
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
         "l"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
         : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t desc, bool add) {
     asm volatile(
-        "{\n\t.reg .pred p, e;\n\tsetp.ne.u32 p, %4, 0;\n\telect.sync _|e, 0xffffffff;\n\t"
-        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
         "r"(a), "l"(b), "r"(desc), "r"((uint32_t)add)
         : "memory");
 }
@@ -277,7 +281,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         const int h = w.item / groups, r0 = w.item % groups * item_rows;
         if (span.bad && threadIdx.x == 0) atomicOr(a.status, kStBadLength);
         if (!sync_all()) return;  // both streams are through with the last item
-        // and both product warps have seen its start: one without tiles in it waits for nothing else
+        // and the scores' warp has seen its start (it has to meet every phase of q_ready)
         if (items > 0 && !bar_wait(&c.q_taken, (items - 1) & 1, c)) return;
         if (threadIdx.x < 128) c.odd[threadIdx.x] = 0;
         if (threadIdx.x == 0) c.any_odd = 0;
@@ -655,91 +659,121 @@ out:
     }
 }
 
-// The matrix products of stream `st`.
+// A place in a ring: slot and the parity of its phase, one step at a time.
+template <int SLOTS> struct TcSlot {
+    uint32_t slot = 0, parity = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == SLOTS) {
+            slot = 0;
+            parity ^= 1;
+        }
+    }
+};
+
+// Which streams have a product with half `sub` of a tile that has `subs` halves.
+template <bool PAIR> __device__ __forceinline__ bool tc_has(int st, int sub, int subs, bool second) {
+    return PAIR ? sub < subs && (st == 0 || second) : st == sub && sub < subs;
+}
+
+// The score products of both streams, tile after tile.
 template <int D, bool PAIR>
-__device__ __forceinline__ void tc_products(const AttendArgs& a, TcControl& c, char* q_smem, char* k_ring, char* v_ring,
-                                            int st) {
+__device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, char* q_smem, char* k_ring) {
     using S = TcShape<D, PAIR>;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = a.H * groups;
-    const uint32_t t_s = uniform(c.tmem + st * 128), t_o = uniform(c.tmem + S::kO + st * D);
-    const uint32_t q_at = uniform(smem_u32(q_smem + (PAIR ? st * S::kQ : 0)));
-    uint32_t items = 0, scored = 0, weighed = 0, tile0 = 0;
+    const uint32_t t_s = uniform(c.tmem), q_at = uniform(smem_u32(q_smem)), ring = uniform(smem_u32(k_ring));
+    uint32_t items = 0, done[2] = {0, 0};
+    TcSlot<S::kK> at;
     for (TcWalk w(c.cut); w.more(); ++items) {
         const int len = attend_span(a, w.b).len(), n = w.count(len);
-        const bool stream_live = PAIR ? w.item % groups * item_rows + st * 128 < rows : true;
+        const bool second = PAIR && w.item % groups * item_rows + 128 < rows;  // stream 1 has rows
         if (!bar_wait(&c.q_ready, items & 1, c)) goto out;
         tc_fence_after();
         if (lane == 0) bar_arrive(&c.q_taken);
-        const uint32_t before = weighed;
-        // The scores' place (tile kq, half ksub) runs one product ahead of the weights' (q, sub).
-        int kq = 0, ksub = PAIR ? 0 : st, q = 0, sub = ksub;
-        while (q < n) {
-            while (kq < n && kq <= q + 1 && scored <= weighed + 1) {
-                const uint32_t u = tile0 + kq;
-                const int subs = stream_live ? tc_subs(len, w.tile + kq) : 0, next = ksub + (PAIR ? 1 : 2);
-                if (!bar_wait(&c.full_k[u % S::kK], (u / S::kK) & 1, c)) goto out;
-                if (ksub < subs) {
+        for (int q = 0; q < n; ++q, at.next()) {
+            const int subs = tc_subs(len, w.tile + q);
+            if (!bar_wait(&c.full_k[at.slot], at.parity, c)) goto out;
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    if (!tc_has<PAIR>(st, sub, subs, second)) continue;
                     // the group has taken the last scores
-                    if (scored > 0 && !bar_wait(&c.s_free[st], (scored - 1) & 1, c)) goto out;
+                    if (done[st] > 0 && !bar_wait(&c.s_free[st], (done[st] - 1) & 1, c)) goto out;
+                    ++done[st];
                     tc_fence_after();
-                    {
-                        const uint32_t k_at = uniform(smem_u32(k_ring + (u % S::kK) * S::kUnit) + ksub * kSub * 128);
+                    const uint32_t k_at = uniform(ring + at.slot * S::kUnit) + sub * kSub * 128;
+                    if (elect_one()) {
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
                             const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
-                            mma_ss(t_s, smem_desc(q_at + off, 16, 1024), smem_desc(k_at + off, 16, 1024),
-                                   mma_desc(kSub, false), i > 0);
+                            mma_ss(t_s + st * 128, smem_desc(q_at + (PAIR ? st * S::kQ : 0) + off, 16, 1024),
+                                   smem_desc(k_at + off, 16, 1024), mma_desc(kSub, false), i > 0);
                         }
-                        if (next >= subs) tc_commit(&c.empty_k[u % S::kK]);
                         tc_commit(&c.s_full[st]);
                     }
-                    ++scored;
-                } else if (lane == 0) {
-                    bar_arrive(&c.empty_k[u % S::kK]);  // nothing of the tile is this stream's
+                    __syncwarp();
                 }
-                ksub = next;
-                if (ksub >= subs) {
-                    ksub = PAIR ? 0 : st;
-                    ++kq;
-                }
-            }
-            const uint32_t u = tile0 + q;
-            const int subs = stream_live ? tc_subs(len, w.tile + q) : 0, next = sub + (PAIR ? 1 : 2);
-            if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) goto out;
-            if (sub < subs) {
-                if (!bar_wait(&c.p_ready[st][weighed & 1], (weighed / 2) & 1, c)) goto out;
-                tc_fence_after();
-                {
-                    const uint32_t v_at = uniform(smem_u32(v_ring + (u % S::kV) * S::kUnit) + sub * kSub * 128);
-                    const uint32_t p_at = uniform(t_s + 64 + 32 * (weighed & 1));
-                    const bool add = uniform(weighed != before);
-#pragma unroll
-                    for (int i = 0; i < kSub / 16; ++i)
-                        mma_ts(t_o, p_at + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024), mma_desc(D, true),
-                               i > 0 || add);
-                    if (next >= subs) tc_commit(&c.empty_v[u % S::kV]);
-                    tc_commit(&c.pv_done[st][weighed & 1]);
-                }
-                ++weighed;
-            } else if (lane == 0) {
-                bar_arrive(&c.empty_v[u % S::kV]);
-            }
-            sub = next;
-            if (sub >= subs) {
-                sub = PAIR ? 0 : st;
-                ++q;
-            }
+            if (elect_one()) tc_commit(&c.empty_k[at.slot]);
+            __syncwarp();
         }
-        tile0 += n;
         w.next(n, per);
     }
 out:
-    // nothing of this stream is in flight when the CTA ends
+    // nothing is in flight when the CTA ends
     __syncwarp();
-    tc_commit(&c.drained[st]);
-    bar_wait<true>(&c.drained[st], 0, c);
+    if (elect_one()) tc_commit(&c.drained[0]);
+    __syncwarp();
+    bar_wait<true>(&c.drained[0], 0, c);
+}
+
+// The products of weights and values of both streams.
+template <int D, bool PAIR>
+__device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char* v_ring) {
+    using S = TcShape<D, PAIR>;
+    const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
+              per = a.H * groups;
+    const uint32_t t_s = uniform(c.tmem), ring = uniform(smem_u32(v_ring));
+    uint32_t done[2] = {0, 0};
+    TcSlot<S::kV> at;
+    for (TcWalk w(c.cut); w.more();) {
+        const int len = attend_span(a, w.b).len(), n = w.count(len);
+        const bool second = PAIR && w.item % groups * item_rows + 128 < rows;
+        for (int q = 0; q < n; ++q, at.next()) {
+            const int subs = tc_subs(len, w.tile + q);
+            if (!bar_wait(&c.full_v[at.slot], at.parity, c)) goto out;
+#pragma unroll
+            for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    if (!tc_has<PAIR>(st, sub, subs, second)) continue;
+                    const uint32_t buf = done[st] & 1;
+                    if (!bar_wait(&c.p_ready[st][buf], (done[st] / 2) & 1, c)) goto out;
+                    ++done[st];
+                    tc_fence_after();
+                    const uint32_t v_at = uniform(ring + at.slot * S::kUnit) + sub * kSub * 128;
+                    const uint32_t p_at = uniform(t_s + st * 128 + 64 + 32 * buf);
+                    const bool add = uniform((PAIR ? sub > 0 : 0) | q);  // the first of an item starts the sums
+                    if (elect_one()) {
+#pragma unroll
+                        for (int i = 0; i < kSub / 16; ++i)
+                            mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024),
+                                   mma_desc(D, true), i > 0 || add);
+                        tc_commit(&c.pv_done[st][buf]);
+                    }
+                    __syncwarp();
+                }
+            if (elect_one()) tc_commit(&c.empty_v[at.slot]);
+            __syncwarp();
+        }
+        w.next(n, per);
+    }
+out:
+    __syncwarp();
+    if (elect_one()) tc_commit(&c.drained[1]);
+    __syncwarp();
+    bar_wait<true>(&c.drained[1], 0, c);
 }
 
 template <int D, bool PAIR>
@@ -757,11 +791,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::kK; ++i) {
             bar_init(&c.full_k[i], 1);
-            bar_init(&c.empty_k[i], 2);
+            bar_init(&c.empty_k[i], 1);
         }
         for (int i = 0; i < S::kV; ++i) {
             bar_init(&c.full_v[i], 1);
-            bar_init(&c.empty_v[i], 2);
+            bar_init(&c.empty_v[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
             bar_init(&c.s_full[i], 1);
@@ -773,7 +807,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             bar_init(&c.drained[i], 1);
         }
         bar_init(&c.q_ready, 8);
-        bar_init(&c.q_taken, 2);
+        bar_init(&c.q_taken, 1);
         bar_init(&c.all_sync, 8);
         c.abort = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -797,7 +831,8 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (warp < 8) tc_softmax<D, PAIR>(a, c, q_smem, v_ring, merge, warp >> 2);
     else if (warp == 8) tc_load<D, PAIR, S::kK>(a, c, &key, k_ring, c.full_k, c.empty_k, true);
     else if (warp == 11) tc_load<D, PAIR, S::kV>(a, c, &value, v_ring, c.full_v, c.empty_v, false);
-    else tc_products<D, PAIR>(a, c, q_smem, k_ring, v_ring, warp - 9);
+    else if (warp == 9) tc_scores<D, PAIR>(a, c, q_smem, k_ring);
+    else tc_sums<D, PAIR>(a, c, v_ring);
     tc_fence_before();
     __syncthreads();
     if (warp == 8) {
