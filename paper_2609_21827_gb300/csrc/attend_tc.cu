@@ -6,12 +6,12 @@
 //   warps 8, 11      load key tiles and value tiles (TMA) into two rings of shared memory
 //   warps 9, 10      issue the score products and the products with the values
 // A stream holds up to 128 query rows (token, head of the key/value head): its
-// scores S = Q K^T (128 x 64 fp32), weights P (two buffers of 128 x 64 bf16) and
-// sums O (128 x D fp32) lie in tensor memory.  Per 64 keys: S by tcgen05.mma from
-// shared memory; the group reads its rows, which frees S for the next 64 keys'
-// product, computes p = 2^(s - m) and writes P; O += P V by tcgen05.mma with P
-// from tensor memory.  So the next scores are there when a group has written its
-// weights, and both groups compute exponentials all the time.
+// scores S = Q K^T (two buffers of 128 x 64 fp32) and sums O (128 x D fp32) lie in
+// tensor memory.  Per 64 keys: S by tcgen05.mma from shared memory; the group
+// reads its rows, computes p = 2^(s - m) and writes them (bf16) over S; O += P V
+// by tcgen05.mma with P from tensor memory, which frees the buffer for the scores
+// after next.  So the next scores are there when a group has written its weights,
+// and both groups compute exponentials all the time.
 //   PAIR:   an item has up to 256 rows, each stream takes 128 of them and all
 //           keys: a tile crosses HBM once for all heads and tokens;
 //   !PAIR:  up to 128 rows (single tokens, short chains): stream 0 takes the
@@ -53,14 +53,14 @@ template <int D, bool PAIR> struct TcShape {
     static constexpr int kQ = 128 * D * 2;       // bytes of 128 rows of queries
     static constexpr int kQueries = PAIR ? 2 * kQ : kQ;
     static constexpr int kMerge = PAIR ? 0 : 16384;
-    // Tensor memory: stream s has its scores at column 128 s (64 columns), two buffers of weights at 128 s + 64 and
-    // + 96 (32 each, bf16 pairs), its sums at kO + s D.
+    // Tensor memory: stream s has two buffers of scores at columns 128 s and 128 s + 64, whose first 32 columns take
+    // the weights (bf16 pairs), and its sums at kO + s D.
     static constexpr int kO = 256;
 };
 
 struct TcControl {
     unsigned long long full_k[5], empty_k[5], full_v[5], empty_v[5];
-    unsigned long long s_full[2], s_free[2], p_ready[2][2], pv_done[2][2], drained[2], q_ready, q_taken, all_sync;
+    unsigned long long s_full[2][2], p_ready[2][2], pv_done[2][2], drained[2], q_ready, q_taken, all_sync;
     uint32_t tmem;
     int abort;
     int any_odd;          // some drafted value is not finite
@@ -378,24 +378,17 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                             }
                     }
                 }
-                if (!bar_wait(&c.s_full[st], products & 1, c)) return;
+                const uint32_t buf = products & 1, t_b = t_s + 64 * buf;
+                if (!bar_wait(&c.s_full[st][buf], (products / 2) & 1, c)) return;
                 tc_fence_after();
                 // the item's last scores are there: this stream's queries have been read
                 if (PAIR && q == n - 1 && sub == subs - 1 && !last) fetch(next_b, next_item);
-                uint32_t s[2][32];
                 __syncwarp();
                 if (warp_live) {
-                    tmem_ld32(s[0], t_s);
-                    tmem_ld32(s[1], t_s + 32);
+                    uint32_t s[2][32];
+                    tmem_ld32(s[0], t_b);
+                    tmem_ld32(s[1], t_b + 32);
                     tc_wait_ld();
-                }
-                tc_fence_before();
-                bar_arrive_warp(&c.s_free[st]);
-                // the buffer of these weights was read by the product before last
-                const uint32_t buf = products & 1;
-                if (products > 1 && !bar_wait(&c.pv_done[st][buf], (products / 2 - 1) & 1, c)) return;
-                tc_fence_after();
-                if (warp_live) {
                     if (negative) {
 #pragma unroll
                         for (int v = 0; v < 2; ++v)
@@ -457,7 +450,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                             p[i] = pack_bf16(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32)));
                         }
                         if (v == 0) __syncwarp();
-                        tmem_st16(t_s + 64 + 32 * buf + 16 * v, p);
+                        tmem_st16(t_b + 16 * v, p);  // over scores that are in registers by now
                     }
                     l += f2_fold(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])));
                     tc_wait_st();
@@ -699,19 +692,21 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
 #pragma unroll
                 for (int st = 0; st < 2; ++st) {
                     if (!tc_has<PAIR>(st, sub, subs, second)) continue;
-                    // the group has taken the last scores
-                    if (done[st] > 0 && !bar_wait(&c.s_free[st], (done[st] - 1) & 1, c)) goto out;
+                    // the buffer's last weights have been read
+                    const uint32_t buf = done[st] & 1;
+                    if (done[st] > 1 && !bar_wait(&c.pv_done[st][buf], (done[st] / 2 - 1) & 1, c)) goto out;
                     ++done[st];
                     tc_fence_after();
+                    const uint32_t s_at = uniform(t_s + st * 128 + 64 * buf);
                     const uint32_t k_at = uniform(ring + at.slot * S::kUnit) + sub * kSub * 128;
                     if (elect_one()) {
 #pragma unroll
                         for (int i = 0; i < D / 16; ++i) {
                             const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
-                            mma_ss(t_s + st * 128, smem_desc(q_at + (PAIR ? st * S::kQ : 0) + off, 16, 1024),
+                            mma_ss(s_at, smem_desc(q_at + (PAIR ? st * S::kQ : 0) + off, 16, 1024),
                                    smem_desc(k_at + off, 16, 1024), mma_desc(kSub, false), i > 0);
                         }
-                        tc_commit(&c.s_full[st]);
+                        tc_commit(&c.s_full[st][buf]);
                     }
                     __syncwarp();
                 }
@@ -753,7 +748,7 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
                     ++done[st];
                     tc_fence_after();
                     const uint32_t v_at = uniform(ring + at.slot * S::kUnit) + sub * kSub * 128;
-                    const uint32_t p_at = uniform(t_s + st * 128 + 64 + 32 * buf);
+                    const uint32_t p_at = uniform(t_s + st * 128 + 64 * buf);
                     const bool add = uniform((PAIR ? sub > 0 : 0) | q);  // the first of an item starts the sums
                     if (elect_one()) {
 #pragma unroll
@@ -798,12 +793,11 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             bar_init(&c.empty_v[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
-            bar_init(&c.s_full[i], 1);
-            bar_init(&c.p_ready[i][0], 4);
-            bar_init(&c.p_ready[i][1], 4);
-            bar_init(&c.s_free[i], 4);
-            bar_init(&c.pv_done[i][0], 1);
-            bar_init(&c.pv_done[i][1], 1);
+            for (int buf = 0; buf < 2; ++buf) {
+                bar_init(&c.s_full[i][buf], 1);
+                bar_init(&c.p_ready[i][buf], 4);
+                bar_init(&c.pv_done[i][buf], 1);
+            }
             bar_init(&c.drained[i], 1);
         }
         bar_init(&c.q_ready, 8);
