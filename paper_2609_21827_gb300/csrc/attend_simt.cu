@@ -45,21 +45,20 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const int rows = a.T * a.G, groups = (rows + R - 1) / R, per = a.H * groups;
     if (tid < 32) {
-        const AttendCut c = attend_cut<kSimtTile>(a, per, blockIdx.x, a.min_tiles);
+        const AttendCut c = attend_cut<kSimtTile>(a, per, blockIdx.x);
         if (tid == 0) cut_s = c;
     }
     __syncthreads();
     const AttendCut cut = cut_s;
     if (tid == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
 
-    int b = cut.b, item = cut.item, tile = cut.tile;
-    for (int64_t at = cut.begin; at < cut.end;) {
+    for (AttendWalk<kSimtTile> walk(cut); walk.more(); walk.next(per)) {
+        const int b = walk.b;
         const AttendSpan span = attend_span(a, b);
         if (span.bad && tid == 0) atomicOr(a.status, kStBadLength);
         const int len = span.len();
-        const int tiles = max(1, (len + kSimtTile - 1) / kSimtTile);
-        const int n = (int)min((int64_t)(tiles - tile), cut.end - at);
-        const int h = item / groups, r0 = (item % groups) * R;
+        walk.open(len);
+        const int tile = walk.tile, n = walk.n, h = walk.item / groups, r0 = (walk.item % groups) * R;
         const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
 
         auto load = [&](int tl, int buf) {
@@ -199,7 +198,7 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
             __syncthreads();  // the buffer is free for the tile after the next
         }
 
-        const bool whole = n == tiles;
+        const bool whole = n == walk.all;
         const int64_t part = attend_part(blockIdx.x, tile == 0);
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
@@ -231,13 +230,7 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
             if (a.io.lse && tx == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m[i], ll);
         }
         if (!whole && tile == 0 && tid == 0)
-            a.join[blockIdx.x] = make_int4(b, item, cut.owner(at + tiles - 1) - (int)blockIdx.x + 1, 0);
-        at += n;
-        tile = 0;
-        if (++item == per) {
-            item = 0;
-            ++b;
-        }
+            a.join[blockIdx.x] = make_int4(b, walk.item, walk.segments(cut, blockIdx.x), 0);
     }
 }
 
@@ -311,6 +304,10 @@ int attend_part_rows(int dtype, int T, int G) {
     const int64_t rows = ((int64_t)T * G + 7) / 8 * 8, most = attend_item_rows(dtype, T, G);
     return (int)(rows < most ? rows : most);
 }
+
+// An item's start and end against a tile's time: queries, masks and results take as long as four tiles of the tensor
+// cores' kernel, and half a tile of the fp32 kernel.
+int attend_lead(int dtype) { return dtype == 1 ? 4 : 1; }
 
 template <int DT, int D> static cudaError_t launch_join(const AttendArgs& a, cudaStream_t s) {
     return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, (a.part_rows * (D / 8) + 255) / 256), dim3(256), 0, s, a);

@@ -202,23 +202,7 @@ __device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap* map, i
 // Score products of tile `tile` of an item of `len` places: the second half only where it has a place.
 __device__ __forceinline__ int tc_subs(int len, int tile) { return len - tile * kTile > kSub ? 2 : 1; }
 
-// One CTA's run through its items, the same in every warp.
-struct TcWalk {
-    int b, item, tile;
-    int64_t at, end;
-    __device__ __forceinline__ explicit TcWalk(const AttendCut& c) : b(c.b), item(c.item), tile(c.tile), at(c.begin), end(c.end) {}
-    __device__ __forceinline__ bool more() const { return at < end; }
-    __device__ __forceinline__ int tiles(int len) const { return max(1, (len + kTile - 1) / kTile); }
-    __device__ __forceinline__ int count(int len) const { return (int)min((int64_t)(tiles(len) - tile), end - at); }
-    __device__ __forceinline__ void next(int n, int per) {
-        at += n;
-        tile = 0;
-        if (++item == per) {
-            item = 0;
-            ++b;
-        }
-    }
-};
+using TcWalk = AttendWalk<kTile>;
 
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
@@ -247,6 +231,31 @@ __device__ __forceinline__ void tc_queries(const AttendArgs& a, int b, int h, in
     }
 }
 
+// Which of the 64 places from the j0-th drafted token on the tokens tt0 .. t_last see, a vote a word; the lane of token t
+// keeps its words.  TOKENS at a time, so that as many loads are under way.
+template <int TOKENS>
+__device__ __forceinline__ void tc_votes(const AttendArgs& a, const AttendSpan& span, int b, int j0, int tt0, int t_last, int t,
+                                         uint32_t (&words)[2]) {
+    const int lane = threadIdx.x & 31;
+    for (int tt = tt0; tt <= t_last; tt += TOKENS) {
+        bool sees[TOKENS][2];
+#pragma unroll
+        for (int u = 0; u < TOKENS; ++u) {
+            const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + min(tt + u, t_last)) * a.T : nullptr;
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+                sees[u][v] = tt + u < span.add && attend_sees(span, mrow, tt + u, span.ctx + j0 + 32 * v + lane);
+        }
+#pragma unroll
+        for (int u = 0; u < TOKENS; ++u)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                const uint32_t bits = __ballot_sync(0xffffffffu, sees[u][v]);
+                if (tt + u == t) words[v] = bits;
+            }
+    }
+}
+
 // The softmax group of stream `st`.
 template <int D, bool PAIR>
 __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, char* q_smem, char* v_ring, char* merge, int st) {
@@ -259,6 +268,8 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
     const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);  // above 0, so that hidden places stay at -inf
     const bool negative = a.scale_log2 < 0.0f;
     uint32_t items = 0, products = 0, syncs = 0, tile0 = 0;
+    unsigned long long seen = 0;  // T <= 64: drafted tokens that this row sees, of request seen_b's rows from seen_r0
+    int seen_b = -1, seen_r0 = -1;
     auto sync_all = [&]() -> bool {
         bar_arrive_warp(&c.all_sync);
         return bar_wait(&c.all_sync, syncs++ & 1, c);
@@ -277,8 +288,9 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
     }
     while (w.more()) {
         const AttendSpan span = next_span;
-        const int len = span.len(), all = w.tiles(len), n = w.count(len);
-        const int h = w.item / groups, r0 = w.item % groups * item_rows;
+        const int len = span.len();
+        w.open(len);
+        const int n = w.n, h = w.item / groups, r0 = w.item % groups * item_rows;
         if (span.bad && threadIdx.x == 0) atomicOr(a.status, kStBadLength);
         if (!sync_all()) return;  // both streams are through with the last item
         // and the scores' warp has seen its start (it has to meet every phase of q_ready)
@@ -289,7 +301,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         fence_async();
         tc_fence_before();
         bar_arrive_warp(&c.q_ready);
-        const bool last = w.at + n >= w.end;
+        const bool last = w.last();
         const int next_b = w.item + 1 == per ? w.b + 1 : w.b, next_item = w.item + 1 == per ? 0 : w.item + 1;
         if (!last) next_span = attend_span(a, next_b);
         ++items;
@@ -299,11 +311,14 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         const bool warp_live = __any_sync(0xffffffffu, live);
         const bool stream_live = PAIR ? r0 + st * 128 < rows : true;
         if (PAIR && !stream_live && !last) fetch(next_b, next_item);
-        if (a.mask && live) {
-            // the row of the mask comes near before the last tiles ask for it
-            const uint8_t* mrow = a.mask + ((int64_t)w.b * a.T + t) * a.T;
-            asm volatile("prefetch.global.L1 [%0];" ::"l"(mrow));
-            asm volatile("prefetch.global.L1 [%0];" ::"l"(mrow + span.add - 1));
+        if (a.T <= 64 && (w.b != seen_b || r0 != seen_r0) && warp_live) {
+            // which drafted tokens the row sees: once for all heads of a request
+            uint32_t x[2] = {0u, 0u};
+            const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
+            tc_votes<8>(a, span, w.b, 0, (row - lane) / a.G, t_last, t, x);
+            seen = ((unsigned long long)x[1] << 32) | x[0];
+            seen_b = w.b;
+            seen_r0 = r0;
         }
         // Values of the tile at place k0 (tile u of this CTA) before a product of this stream reads them: nothing behind
         // the request's places, and no element that is not finite among the drafted tokens'.  PAIR: a thread a line;
@@ -357,25 +372,16 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 const bool tail = k0 + kSub > span.ctx;
                 uint32_t vis[2] = {0xffffffffu, 0xffffffffu};
                 if (tail && warp_live) {
-                    // the warp's tokens, four at a time, 32 places a vote
-                    const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
-                    for (int tt = (row - lane) / a.G; tt <= t_last; tt += 4) {
-                        bool sees[4][2];
-#pragma unroll
-                        for (int u = 0; u < 4; ++u) {
-                            const uint8_t* mrow =
-                                a.mask ? a.mask + ((int64_t)w.b * a.T + min(tt + u, t_last)) * a.T : nullptr;
-#pragma unroll
-                            for (int v = 0; v < 2; ++v)
-                                sees[u][v] = tt + u < span.add && attend_sees(span, mrow, tt + u, k0 + 32 * v + lane);
-                        }
-#pragma unroll
-                        for (int u = 0; u < 4; ++u)
-#pragma unroll
-                            for (int v = 0; v < 2; ++v) {
-                                const uint32_t bits = __ballot_sync(0xffffffffu, sees[u][v]);
-                                if (tt + u == t) vis[v] = bits;
-                            }
+                    if (a.T <= 64) {
+                        // seen: bit j is drafted token j; bits below it are the cached places
+                        const int off = k0 - span.ctx;
+                        const unsigned long long x = off >= 0 ? (off < 64 ? seen >> off : 0ull)
+                                                              : (seen << -off) | ((1ull << -off) - 1);
+                        vis[0] = (uint32_t)x;
+                        vis[1] = (uint32_t)(x >> 32);
+                    } else {
+                        const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
+                        tc_votes<8>(a, span, w.b, k0 - span.ctx, (row - lane) / a.G, t_last, t, vis);
                     }
                 }
                 const uint32_t buf = products & 1, t_b = t_s + 64 * buf;
@@ -474,7 +480,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
             if (!bar_wait(&c.pv_done[st][x & 1], (x / 2) & 1, c)) return;
             tc_fence_after();
         }
-        const bool whole = n == all;
+        const bool whole = n == w.all;
         const int64_t part = attend_part(blockIdx.x, w.tile == 0);
         const int r_in = (PAIR ? st * 128 : 0) + tid, head = h * a.G + row - t * a.G;
         const bool both = !PAIR && (n > 1 || tc_subs(len, w.tile) == 2);  // stream 1 has a share of the sums
@@ -599,8 +605,8 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
             }
         }
         if (!whole && w.tile == 0 && threadIdx.x == 0)
-            a.join[blockIdx.x] = make_int4(w.b, w.item, c.cut.owner(w.at + all - 1) - (int)blockIdx.x + 1, 0);
-        w.next(n, per);
+            a.join[blockIdx.x] = make_int4(w.b, w.item, w.segments(c.cut, blockIdx.x), 0);
+        w.next(per);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
@@ -617,7 +623,9 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
     const int pi = lane / S::kHalves, half = lane % S::kHalves;
     uint32_t u = 0;
     for (TcWalk w(c.cut); w.more();) {
-        const int len = attend_span(a, w.b).len(), n = w.count(len), h = w.item / groups;
+        const int len = attend_span(a, w.b).len(), h = w.item / groups;
+        w.open(len);
+        const int n = w.n;
         const int32_t* table = a.block_table + (int64_t)w.b * a.max_pages;
         auto page_of = [&](int q) {
             const int l0 = (w.tile + q) * kTile + pi * a.P;
@@ -642,7 +650,7 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
             }
             page = next;
         }
-        w.next(n, per);
+        w.next(per);
     }
 out:
     // no copy is in flight when the CTA ends, and no arrival of a product that read one
@@ -679,7 +687,9 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
     uint32_t items = 0, done[2] = {0, 0};
     TcSlot<S::kK> at;
     for (TcWalk w(c.cut); w.more(); ++items) {
-        const int len = attend_span(a, w.b).len(), n = w.count(len);
+        const int len = attend_span(a, w.b).len();
+        w.open(len);
+        const int n = w.n;
         const bool second = PAIR && w.item % groups * item_rows + 128 < rows;  // stream 1 has rows
         if (!bar_wait(&c.q_ready, items & 1, c)) goto out;
         tc_fence_after();
@@ -713,7 +723,7 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
             if (elect_one()) tc_commit(&c.empty_k[at.slot]);
             __syncwarp();
         }
-        w.next(n, per);
+        w.next(per);
     }
 out:
     // nothing is in flight when the CTA ends
@@ -733,7 +743,9 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
     uint32_t done[2] = {0, 0};
     TcSlot<S::kV> at;
     for (TcWalk w(c.cut); w.more();) {
-        const int len = attend_span(a, w.b).len(), n = w.count(len);
+        const int len = attend_span(a, w.b).len();
+        w.open(len);
+        const int n = w.n;
         const bool second = PAIR && w.item % groups * item_rows + 128 < rows;
         for (int q = 0; q < n; ++q, at.next()) {
             const int subs = tc_subs(len, w.tile + q);
@@ -762,7 +774,7 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
             if (elect_one()) tc_commit(&c.empty_v[at.slot]);
             __syncwarp();
         }
-        w.next(n, per);
+        w.next(per);
     }
 out:
     __syncwarp();
@@ -815,7 +827,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
     if (warp == 9) {
         const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128;
-        const AttendCut cut = attend_cut<kTile>(a, a.H * ((rows + item_rows - 1) / item_rows), blockIdx.x, a.min_tiles);
+        const AttendCut cut = attend_cut<kTile>(a, a.H * ((rows + item_rows - 1) / item_rows), blockIdx.x);
         if ((threadIdx.x & 31) == 0) c.cut = cut;
     }
     if (threadIdx.x == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);

@@ -58,7 +58,7 @@ struct CommitArgs {
 struct AttendArgs {
     int B, T, H, G, D, P, page_shift, pages, max_pages;
     int ctas;                 // CTAs that share the tiles
-    int min_tiles;            // tiles a CTA takes at least
+    int lead;                 // what an item's start and end cost, in tiles
     int item_rows;            // query rows of an item
     int part_rows;            // rows kept of an item's partial sums
     rheo_attend_io io;
@@ -95,6 +95,7 @@ cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s);
 int attend_item_rows(int dtype, int T, int G);
 int attend_part_rows(int dtype, int T, int G);
+int attend_lead(int dtype);
 constexpr int kAttendCtas = 152;  // one a multiprocessor
 cudaError_t launch_logprobs(const LogprobArgs& a, int dtype, bool aligned, cudaStream_t s);
 int logprob_segments(int rows, int vocab, int dtype, int sms);
