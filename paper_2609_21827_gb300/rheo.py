@@ -143,10 +143,16 @@ def lib():
     return _lib
 
 
+# The current stream's handle without a Stream object (3 us less a call), where this build of torch has it.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream(stream) -> int:
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return stream.cuda_stream
+    if stream is not None:
+        return stream.cuda_stream
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
+    return torch.cuda.current_stream().cuda_stream
 
 
 def _check(rc: int, what: str):
@@ -422,10 +428,12 @@ class CacheConfig:
         code, torch_dtype = _dtype_of(self.dtype)
         c = _CacheConfig(self.batch, self.tokens, self.pages, self.page_size, self.max_pages, self.q_heads,
                          self.kv_heads, self.head_dim, code)
-        object.__setattr__(self, "torch_dtype", torch_dtype)
-        object.__setattr__(self, "_c", c)
-        object.__setattr__(self, "_ref", ctypes.byref(c))
-        object.__setattr__(self, "_bytes", None)
+        B, T, H, D = self.batch, self.tokens, self.kv_heads, self.head_dim
+        for name, value in (("torch_dtype", torch_dtype), ("_c", c), ("_ref", ctypes.byref(c)), ("_bytes", None),
+                            ("_one", (B,)), ("_each", (B, T)), ("_table", (B, self.max_pages)),
+                            ("_q", (B, T, self.q_heads, D)), ("_k", (B, T, H, D)), ("_lse", (B, T, self.q_heads)),
+                            ("_mask", (B, T, T)), ("_pool", (self.pages, H, self.page_size, D))):
+            object.__setattr__(self, name, value)
 
     def scratch_bytes(self) -> int:
         if self._bytes is None:
@@ -448,10 +456,10 @@ class LogprobConfig:
     def __post_init__(self):
         code, torch_dtype = _dtype_of(self.dtype)
         c = _LogprobConfig(self.rows, self.vocab, self.top, code, self.rows_per_temperature)
-        object.__setattr__(self, "torch_dtype", torch_dtype)
-        object.__setattr__(self, "_c", c)
-        object.__setattr__(self, "_ref", ctypes.byref(c))
-        object.__setattr__(self, "_bytes", None)
+        for name, value in (("torch_dtype", torch_dtype), ("_c", c), ("_ref", ctypes.byref(c)), ("_bytes", None),
+                            ("_rows", (self.rows,)),
+                            ("_groups", (-(-self.rows // max(self.rows_per_temperature, 1)),))):
+            object.__setattr__(self, name, value)
 
     def scratch_bytes(self) -> int:
         if self._bytes is None:
@@ -472,7 +480,7 @@ class _Scratch:
 
     def of(self, cfg) -> int:
         """The buffer's pointer, if it is large enough for cfg."""
-        if self.nbytes < cfg.scratch_bytes():
+        if self.nbytes < (cfg._bytes or cfg.scratch_bytes()):
             raise RheoError(f"the workspace holds {self.nbytes} bytes, {cfg.scratch_bytes()} are wanted")
         return self._ptr
 
@@ -500,7 +508,7 @@ def scratch_status(ws: _Scratch, stream=None) -> int:
 
 def _want(x: torch.Tensor, name: str, dtype, shape) -> int:
     """The pointer of a contiguous CUDA tensor of this type and shape."""
-    if x.dtype != dtype or not x.is_cuda or tuple(x.shape) != shape or not x.is_contiguous():
+    if x.dtype is not dtype or not x.is_cuda or x.shape != shape or not x.is_contiguous():
         raise RheoError(f"{name}: a contiguous CUDA tensor of {dtype} and shape {list(shape)} is wanted, "
                         f"got {x.dtype} {list(x.shape)} on {x.device}")
     return x.data_ptr()
@@ -511,17 +519,31 @@ def _want_opt(x, name: str, dtype, shape) -> int:
 
 
 def _want_strided(x: torch.Tensor, name: str, dtype, shape) -> tuple:
-    """The pointer and the strides but the last of a CUDA tensor whose last dimension is contiguous."""
-    if x.dtype != dtype or not x.is_cuda or tuple(x.shape) != shape:
+    """The pointer and the strides of a CUDA tensor whose last dimension is contiguous."""
+    if x.dtype is not dtype or not x.is_cuda or x.shape != shape:
         raise RheoError(f"{name}: a CUDA tensor of {dtype} and shape {list(shape)} is wanted, "
                         f"got {x.dtype} {list(x.shape)} on {x.device}")
     st = x.stride()
-    if st[-1] != 1 and shape[-1] > 1:
+    if st[-1] != 1:
         raise RheoError(f"{name}: the last dimension has to be contiguous")
-    return x.data_ptr(), st[:-1]
+    return x.data_ptr(), st
 
 
-class Pages:
+class _Buffers:
+    """Tensors whose checked pointers are kept until one of them is replaced."""
+
+    _held = None
+
+    def __setattr__(self, name, value):
+        object.__setattr__(self, name, value)
+        object.__setattr__(self, "_held", None)
+
+    def _keep(self, cfg, made):
+        object.__setattr__(self, "_held", (cfg, made))
+        return made
+
+
+class Pages(_Buffers):
     """Pages of the requests and the stack of free ones.  Without arguments every page is free
     (page 0 on top); given tensors are used as they are."""
 
@@ -538,20 +560,30 @@ class Pages:
         self.block_table, self.n_pages, self.free_list, self.n_free = block_table, n_pages, free_list, n_free
 
     def c(self, cfg: CacheConfig) -> _Pages:
+        held = self._held
+        if held is not None and held[0] is cfg:
+            return held[1]
         i32 = torch.int32
-        return _Pages(_want(self.block_table, "block_table", i32, (cfg.batch, cfg.max_pages)),
-                      _want(self.n_pages, "n_pages", i32, (cfg.batch,)),
-                      _want(self.free_list, "free_list", i32, (cfg.pages,)),
-                      _want(self.n_free, "n_free", i32, (1,)))
+        return self._keep(cfg, _Pages(_want(self.block_table, "block_table", i32, cfg._table),
+                                      _want(self.n_pages, "n_pages", i32, cfg._one),
+                                      _want(self.free_list, "free_list", i32, (cfg.pages,)),
+                                      _want(self.n_free, "n_free", i32, (1,))))
 
 
-class CachePlan:
+class CachePlan(_Buffers):
     """Slots [B, T] (int64) and positions [B, T] (int32) of a call's new tokens."""
 
     def __init__(self, cfg: CacheConfig, device="cuda", slot=None, position=None):
         shape = (cfg.batch, cfg.tokens)
         self.slot = torch.full(shape, -1, dtype=torch.int64, device=device) if slot is None else slot
         self.position = torch.full(shape, -1, dtype=torch.int32, device=device) if position is None else position
+
+    def ptrs(self, cfg: CacheConfig) -> tuple:
+        held = self._held
+        if held is not None and held[0] is cfg:
+            return held[1]
+        return self._keep(cfg, (_want(self.slot, "slot", torch.int64, cfg._each),
+                                _want(self.position, "position", torch.int32, cfg._each)))
 
 
 def make_cache(cfg: CacheConfig, layers: int = 1, device="cuda"):
@@ -561,29 +593,24 @@ def make_cache(cfg: CacheConfig, layers: int = 1, device="cuda"):
             torch.zeros(shape, dtype=cfg.torch_dtype, device=device))
 
 
-def _kv(cfg: CacheConfig, key: torch.Tensor, value: torch.Tensor, layers=None):
-    shape = (cfg.pages, cfg.kv_heads, cfg.page_size, cfg.head_dim)
-    if layers is not None:
-        shape = (layers,) + shape
-    kp, ks = _want_strided(key, "key cache", cfg.torch_dtype, shape)
-    vp, vs = _want_strided(value, "value cache", cfg.torch_dtype, shape)
-    if layers is None:
-        return _KV(kp, vp, *ks, *vs)
-    return _KV(kp, vp, *ks[1:], *vs[1:]), ks[0], vs[0]
+def _kv(cfg: CacheConfig, key: torch.Tensor, value: torch.Tensor) -> _KV:
+    kp, (kb, kh, kt, _) = _want_strided(key, "key cache", cfg.torch_dtype, cfg._pool)
+    vp, (vb, vh, vt, _) = _want_strided(value, "value cache", cfg.torch_dtype, cfg._pool)
+    return _KV(kp, vp, kb, kh, kt, vb, vh, vt)
 
 
 def cache_reserve(cfg: CacheConfig, ctx_len: torch.Tensor, pages: Pages, plan: CachePlan, ws: CacheWorkspace,
                   new_len: torch.Tensor = None, depth: torch.Tensor = None, out: Pages = None, stream=None) -> None:
     """rheo_cache_reserve: pages for ctx_len + new_len tokens a request, slots and positions of the new ones.
     `pages` is updated in place, or stays as it is and `out` receives the new state."""
-    B, T, i32 = cfg.batch, cfg.tokens, torch.int32
+    i32 = torch.int32
     before = pages.c(cfg)
-    after = before if out is None or out is pages else out.c(cfg)
+    after = before if out is None else out.c(cfg)
+    slot, position = plan.ptrs(cfg)
     _check(lib().rheo_cache_reserve(
-        cfg._ref, _want(ctx_len, "ctx_len", i32, (B,)), _want_opt(new_len, "new_len", i32, (B,)),
-        _want_opt(depth, "depth", i32, (B, T)), ctypes.byref(before), ctypes.byref(after),
-        _want(plan.slot, "slot", torch.int64, (B, T)), _want(plan.position, "position", i32, (B, T)), ws.of(cfg),
-        _stream(stream)), "rheo_cache_reserve")
+        cfg._ref, _want(ctx_len, "ctx_len", i32, cfg._one), _want_opt(new_len, "new_len", i32, cfg._one),
+        _want_opt(depth, "depth", i32, cfg._each), before, after, slot, position, ws.of(cfg), _stream(stream)),
+        "rheo_cache_reserve")
 
 
 def qk_norm_rope(cfg: CacheConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, q_weight, k_weight, cos_sin,
@@ -592,11 +619,11 @@ def qk_norm_rope(cfg: CacheConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     """rheo_qk_norm_rope: q [B, T, q_heads, D], k and v [B, T, kv_heads, D] of one layer; weights [D] or None (no
     norm); cos_sin [positions, rot] fp32 (cosines, then sines) or None (no rotation).  Queries go to q_out (may be
     q), keys and values to the caches [pages, kv_heads, page_size, D] at plan.slot."""
-    B, T, D, dt = cfg.batch, cfg.tokens, cfg.head_dim, cfg.torch_dtype
-    qp, qs = _want_strided(q, "q", dt, (B, T, cfg.q_heads, D))
-    kp, ks = _want_strided(k, "k", dt, (B, T, cfg.kv_heads, D))
-    vp, vs = _want_strided(v, "v", dt, (B, T, cfg.kv_heads, D))
-    op, os_ = _want_strided(q_out, "q_out", dt, (B, T, cfg.q_heads, D))
+    dt, one = cfg.torch_dtype, (cfg.head_dim,)
+    qp, qs = _want_strided(q, "q", dt, cfg._q)
+    kp, ks = _want_strided(k, "k", dt, cfg._k)
+    vp, vs = _want_strided(v, "v", dt, cfg._k)
+    op, os_ = _want_strided(q_out, "q_out", dt, cfg._q)
     if op == qp and os_ != qs:
         raise RheoError("q_out on q's memory needs q's strides")
     most = rot = table = 0
@@ -606,11 +633,11 @@ def qk_norm_rope(cfg: CacheConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Te
         most, rot = cos_sin.shape
         table = _want(cos_sin, "cos_sin", torch.float32, (most, rot))
     kv = _kv(cfg, key_cache, value_cache)
-    x = _QKV(qp, kp, vp, *qs, *ks, *vs)
+    x = _QKV(qp, kp, vp, qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2])
+    slot, position = plan.ptrs(cfg)
     _check(lib().rheo_qk_norm_rope(
-        cfg._ref, ctypes.byref(x), _want_opt(q_weight, "q_weight", dt, (D,)), _want_opt(k_weight, "k_weight", dt, (D,)),
-        eps, table, most, rot, int(interleaved), _want(plan.slot, "slot", torch.int64, (B, T)),
-        _want(plan.position, "position", torch.int32, (B, T)), ctypes.byref(kv), op, *os_, ws.of(cfg), _stream(stream)),
+        cfg._ref, x, _want_opt(q_weight, "q_weight", dt, one), _want_opt(k_weight, "k_weight", dt, one), eps, table, most,
+        rot, 1 if interleaved else 0, slot, position, kv, op, os_[0], os_[1], os_[2], ws.of(cfg), _stream(stream)),
         "rheo_qk_norm_rope")
 
 
@@ -619,17 +646,15 @@ def tree_attend(cfg: CacheConfig, q: torch.Tensor, key_cache: torch.Tensor, valu
                 mask: torch.Tensor = None, lse: torch.Tensor = None, scale: float = None, stream=None) -> None:
     """rheo_tree_attend: attention of the new tokens q [B, T, q_heads, D] over the cache, their own keys and values
     included; mask [B, T, T] uint8 as tree_attention writes it (None: every earlier token); scale: 1/sqrt(D)."""
-    B, T, D, dt = cfg.batch, cfg.tokens, cfg.head_dim, cfg.torch_dtype
-    qp, qs = _want_strided(q, "q", dt, (B, T, cfg.q_heads, D))
-    op, os_ = _want_strided(out, "out", dt, (B, T, cfg.q_heads, D))
-    io = _AttendIO(qp, op, _want_opt(lse, "lse", torch.float32, (B, T, cfg.q_heads)), *qs, *os_)
+    dt, i32 = cfg.torch_dtype, torch.int32
+    qp, qs = _want_strided(q, "q", dt, cfg._q)
+    op, os_ = _want_strided(out, "out", dt, cfg._q)
+    io = _AttendIO(qp, op, _want_opt(lse, "lse", torch.float32, cfg._lse), qs[0], qs[1], qs[2], os_[0], os_[1], os_[2])
     kv = _kv(cfg, key_cache, value_cache)
-    i32 = torch.int32
     _check(lib().rheo_tree_attend(
-        cfg._ref, ctypes.byref(io), ctypes.byref(kv),
-        _want(pages.block_table, "block_table", i32, (B, cfg.max_pages)), _want(ctx_len, "ctx_len", i32, (B,)),
-        _want_opt(new_len, "new_len", i32, (B,)), _want_opt(mask, "mask", torch.uint8, (B, T, T)),
-        D ** -0.5 if scale is None else scale, ws.of(cfg), _stream(stream)), "rheo_tree_attend")
+        cfg._ref, io, kv, pages.c(cfg).block_table, _want(ctx_len, "ctx_len", i32, cfg._one),
+        _want_opt(new_len, "new_len", i32, cfg._one), _want_opt(mask, "mask", torch.uint8, cfg._mask),
+        cfg.head_dim ** -0.5 if scale is None else scale, ws.of(cfg), _stream(stream)), "rheo_tree_attend")
 
 
 def cache_commit(cfg: CacheConfig, key_cache: torch.Tensor, value_cache: torch.Tensor, pages: Pages,
@@ -637,19 +662,21 @@ def cache_commit(cfg: CacheConfig, key_cache: torch.Tensor, value_cache: torch.T
                  next_len: torch.Tensor, ws: CacheWorkspace, stream=None) -> None:
     """rheo_cache_commit: the accepted path's lines move behind the root in caches [layers, pages, kv_heads,
     page_size, D]; next_len = ctx_len + 1 + accepted_len (another tensor than ctx_len)."""
-    B, i32 = cfg.batch, torch.int32
+    i32 = torch.int32
     if key_cache.dim() != 5 or accepted_nodes.dim() != 2:
         raise RheoError("caches [layers, pages, kv_heads, page_size, D] and accepted_nodes [B, depth] are wanted")
     layers, depth = key_cache.shape[0], accepted_nodes.shape[1]
-    kv, key_layer, value_layer = _kv(cfg, key_cache, value_cache, layers)
+    shape = (layers,) + cfg._pool
+    kp, ks = _want_strided(key_cache, "key cache", cfg.torch_dtype, shape)
+    vp, vs = _want_strided(value_cache, "value cache", cfg.torch_dtype, shape)
     _check(lib().rheo_cache_commit(
-        cfg._ref, layers, ctypes.byref(kv), key_layer, value_layer,
-        _want(pages.block_table, "block_table", i32, (B, cfg.max_pages)), _want(ctx_len, "ctx_len", i32, (B,)),
-        _want(accepted_len, "accepted_len", i32, (B,)), _want(accepted_nodes, "accepted_nodes", i32, (B, depth)), depth,
-        _want(next_len, "next_len", i32, (B,)), ws.of(cfg), _stream(stream)), "rheo_cache_commit")
+        cfg._ref, layers, _KV(kp, vp, ks[1], ks[2], ks[3], vs[1], vs[2], vs[3]), ks[0], vs[0], pages.c(cfg).block_table,
+        _want(ctx_len, "ctx_len", i32, cfg._one), _want(accepted_len, "accepted_len", i32, cfg._one),
+        _want(accepted_nodes, "accepted_nodes", i32, (cfg.batch, depth)), depth,
+        _want(next_len, "next_len", i32, cfg._one), ws.of(cfg), _stream(stream)), "rheo_cache_commit")
 
 
-class Logprobs:
+class Logprobs(_Buffers):
     """Outputs of token_logprobs."""
 
     def __init__(self, cfg: LogprobConfig, device="cuda"):
@@ -661,10 +688,14 @@ class Logprobs:
         self.top_logprobs = torch.zeros((R, k), dtype=torch.float32, device=device)
 
     def c(self, cfg: LogprobConfig) -> _Logprobs:
+        held = self._held
+        if held is not None and held[0] is cfg:
+            return held[1]
         R, k, f32, i32 = cfg.rows, cfg.top, torch.float32, torch.int32
-        return _Logprobs(_want(self.logprob, "logprob", f32, (R,)), _want(self.rank, "rank", i32, (R,)),
-                         _want(self.entropy, "entropy", f32, (R,)), _want(self.top_ids, "top_ids", i32, (R, k)),
-                         _want(self.top_logprobs, "top_logprobs", f32, (R, k)))
+        return self._keep(cfg, _Logprobs(
+            _want(self.logprob, "logprob", f32, (R,)), _want(self.rank, "rank", i32, (R,)),
+            _want(self.entropy, "entropy", f32, (R,)), _want(self.top_ids, "top_ids", i32, (R, k)),
+            _want(self.top_logprobs, "top_logprobs", f32, (R, k))))
 
 
 def token_logprobs(cfg: LogprobConfig, logits: torch.Tensor, tokens: torch.Tensor, out: Logprobs,
@@ -672,19 +703,17 @@ def token_logprobs(cfg: LogprobConfig, logits: torch.Tensor, tokens: torch.Tenso
                    stream=None) -> None:
     """rheo_token_logprobs: row i reads row rows[i] (None: i) of logits [..., V] and token tokens[i]; -1 leaves a
     row or a token out; temperature [ceil(R / rows_per_temperature)] fp32 or None (1)."""
-    R, i32 = cfg.rows, torch.int32
-    if logits.dtype != cfg.torch_dtype or not logits.is_cuda or logits.shape[-1] != cfg.vocab:
-        raise RheoError(f"logits: a CUDA tensor of {cfg.torch_dtype} and {cfg.vocab} columns is wanted")
-    flat = logits if logits.dim() == 2 else logits.reshape(-1, cfg.vocab)
-    if logits.stride(-1) != 1 or flat.data_ptr() != logits.data_ptr():
+    R, V, i32 = cfg.rows, cfg.vocab, torch.int32
+    if logits.dtype is not cfg.torch_dtype or not logits.is_cuda or logits.shape[-1] != V:
+        raise RheoError(f"logits: a CUDA tensor of {cfg.torch_dtype} and {V} columns is wanted")
+    flat = logits if logits.dim() == 2 else logits.reshape(-1, V)
+    st, p = flat.stride(), flat.data_ptr()
+    if (st[1] != 1 and V > 1) or (flat is not logits and p != logits.data_ptr()):
         raise RheoError("logits rows must be contiguous and addressable with a single row stride")
     n = flat.shape[0]
     if rows is None and n < R:
         raise RheoError(f"{R} rows are asked for, logits have {n}")
-    groups = -(-R // cfg.rows_per_temperature)
-    c = out.c(cfg)
     _check(lib().rheo_token_logprobs(
-        cfg._ref, flat.data_ptr(), max(flat.stride(0), cfg.vocab) if n == 1 else flat.stride(0), n,
-        _want_opt(rows, "rows", i32, (R,)), _want(tokens, "tokens", i32, (R,)),
-        _want_opt(temperature, "temperature", torch.float32, (groups,)), ctypes.byref(c), ws.of(cfg), _stream(stream)),
-        "rheo_token_logprobs")
+        cfg._ref, p, max(st[0], V) if n == 1 else st[0], n, _want_opt(rows, "rows", i32, cfg._rows),
+        _want(tokens, "tokens", i32, cfg._rows), _want_opt(temperature, "temperature", torch.float32, cfg._groups),
+        out.c(cfg), ws.of(cfg), _stream(stream)), "rheo_token_logprobs")
