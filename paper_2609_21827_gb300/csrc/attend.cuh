@@ -10,8 +10,9 @@
 // and end and one unit a tile; CTA i of n takes the units [i total / n, (i+1)
 // total / n), whatever the lengths are, so ragged contexts keep every SM as busy
 // as equal ones.  Few items (a quarter of the CTAs at most): each is cut by
-// itself, into chunks of at most the least size with which the chunks of all
-// items fit the CTAs, so that no CTA pays for the start of two.
+// itself, into chunks of at most the least size (from `least` on: smaller ones
+// cost more in their join than they save) with which the chunks of all items fit
+// the CTAs, so that no CTA pays for the start of two.
 // An item cut by a boundary leaves partial sums: CTA i keeps at most two, slot
 // 2i for one that began in an earlier CTA and slot 2i+1 for one that goes on in
 // a later CTA.
@@ -55,7 +56,7 @@ template <int TILE> __device__ __forceinline__ AttendCut attend_cut(const Attend
     AttendCut c;
     if (a.B <= 32 && 4 * (int64_t)a.B * per <= a.ctas) {
         const int tiles = lane < a.B ? attend_tiles<TILE>(a, lane) : 0;
-        int lo = 1, hi = __reduce_max_sync(0xffffffffu, tiles);  // the least size of a chunk that fits
+        int hi = __reduce_max_sync(0xffffffffu, tiles), lo = min(a.least, hi);  // the least size of a chunk that fits
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
             if (__reduce_add_sync(0xffffffffu, (tiles + mid - 1) / mid) * per <= a.ctas) hi = mid;

@@ -306,8 +306,11 @@ int attend_part_rows(int dtype, int T, int G) {
 }
 
 // An item's start and end against a tile's time: queries, masks and results take as long as four tiles of the tensor
-// cores' kernel, and half a tile of the fp32 kernel.
+// cores' kernel (64 trees of 61 tokens: 262, 253, 247, 250, 253 us with 2, 3, 4, 6, 8), less than one of the fp32 kernel's.
 int attend_lead(int dtype) { return dtype == 1 ? 4 : 1; }
+// One tree of 61 tokens over 1,911 cached ones (bf16): 22.0, 19.7, 21.1, 21.3 us with chunks of 1, 2, 3, 4 tiles at
+// least; four short fp32 trees: 18.1, 22.0, 26.6, 31.4.
+int attend_least(int dtype) { return dtype == 1 ? 2 : 1; }
 
 template <int DT, int D> static cudaError_t launch_join(const AttendArgs& a, cudaStream_t s) {
     return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, (a.part_rows * (D / 8) + 255) / 256), dim3(256), 0, s, a);

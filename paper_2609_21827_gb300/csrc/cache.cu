@@ -196,127 +196,147 @@ cudaError_t launch_reserve(const ReserveArgs& a, int sms, cudaStream_t s) {
 
 // ---------------------------------------------------------------------------
 // qk_norm_rope.  A warp takes one token and a run of its heads (queries, keys,
-// then values); a lane holds four neighbouring elements of a head, so a head of
-// 128 fills the warp and two heads of 64 share it.  The loads of the whole run
-// are issued first, the sum of squares is a butterfly over the head's lanes, and
-// the pair of an element is in the same lane (interleaved) or rot/8 lanes away
-// (a shuffle).  Each input and output element crosses HBM once: HBM bound.
+// then values).  A lane holds 16 bytes of a head (VEC elements; 8 where the
+// rotated part does not divide into pieces of 16), so 16 lanes hold a bf16 head of
+// 128.  The loads of the whole run are issued first, before the token's slot and
+// position have come; the sum of squares is a butterfly over the head's lanes, and
+// the pair of an element is in the same lane (interleaved) or rot / (2 VEC) lanes
+// away (a shuffle).  Each input and output element crosses HBM once: HBM bound.
 // ---------------------------------------------------------------------------
 constexpr int kRopeThreads = 128;
 
-template <int DT> struct Quad;  // four neighbouring elements
-template <> struct Quad<0> {
+template <int DT, int VEC> struct Piece;  // VEC neighbouring elements
+template <> struct Piece<0, 4> {
     using Raw = float4;
-    __device__ static __forceinline__ float4 wide(float4 r) { return r; }
-    __device__ static __forceinline__ float4 narrow(float4 r) { return r; }
+    __device__ static __forceinline__ void wide(float4 r, float (&x)[4]) { x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w; }
+    __device__ static __forceinline__ float4 narrow(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
     __device__ static __forceinline__ float4 zero() { return make_float4(0, 0, 0, 0); }
 };
-template <> struct Quad<1> {
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
+template <> struct Piece<1, 4> {
     using Raw = uint2;
-    __device__ static __forceinline__ float4 wide(uint2 r) {
-        return make_float4(bf_lo(r.x), bf_hi(r.x), bf_lo(r.y), bf_hi(r.y));
+    __device__ static __forceinline__ void wide(uint2 r, float (&x)[4]) {
+        x[0] = bf_lo(r.x), x[1] = bf_hi(r.x), x[2] = bf_lo(r.y), x[3] = bf_hi(r.y);
     }
-    __device__ static __forceinline__ uint2 narrow(float4 v) {
-        const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
-        return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    __device__ static __forceinline__ uint2 narrow(const float (&x)[4]) {
+        return make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
     }
     __device__ static __forceinline__ uint2 zero() { return make_uint2(0, 0); }
 };
+template <> struct Piece<1, 8> {
+    using Raw = uint4;
+    __device__ static __forceinline__ void wide(uint4 r, float (&x)[8]) {
+        x[0] = bf_lo(r.x), x[1] = bf_hi(r.x), x[2] = bf_lo(r.y), x[3] = bf_hi(r.y);
+        x[4] = bf_lo(r.z), x[5] = bf_hi(r.z), x[6] = bf_lo(r.w), x[7] = bf_hi(r.w);
+    }
+    __device__ static __forceinline__ uint4 narrow(const float (&x)[8]) {
+        return make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+    }
+    __device__ static __forceinline__ uint4 zero() { return make_uint4(0, 0, 0, 0); }
+};
 
-// heads of a token that a warp takes at a time: 16 registers of raw data a lane
-template <int DT, int D> constexpr int rope_rounds() { return DT == 1 ? 8 : 4; }
-template <int DT, int D> constexpr int rope_heads() { return rope_rounds<DT, D>() * (128 / D); }
+constexpr int kRopeRounds = 4;  // loads a lane has under way
+template <int D, int VEC> constexpr int rope_heads() { return kRopeRounds * (32 * VEC / D); }  // heads of a run
 
-template <int DT, int D, bool INTERLEAVED>
+template <int DT, int D, int VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
     grid_dependency_begin();
-    using Q = Quad<DT>;
+    using Q = Piece<DT, VEC>;
     using Raw = typename Q::Raw;
-    constexpr int LPH = D / 4, HPW = 32 / LPH, ROUNDS = rope_rounds<DT, D>(), HEADS = rope_heads<DT, D>();
+    constexpr int LPH = D / VEC, HPW = 32 / LPH, HEADS = rope_heads<D, VEC>();
     constexpr int ES = DT == 1 ? 2 : 4;
-    const int lane = threadIdx.x & 31, ci = lane & (LPH - 1), sub = lane / LPH, e = ci * 4;
+    const int lane = threadIdx.x & 31, ci = lane & (LPH - 1), sub = lane / LPH, e = ci * VEC;
     const int heads = a.Hq + 2 * a.H, runs = (heads + HEADS - 1) / HEADS;
     const int64_t item = (int64_t)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
     const int64_t token = item / runs;
     if (token >= a.tokens) return;
-    const int h0 = (int)(item % runs) * HEADS + sub;
-    const int64_t b = token / a.T, t = token % a.T;
+    const int h0 = (int)(item - token * runs) * HEADS + sub;
+    const int64_t b = token / a.T, t = token - b * a.T;
 
     const int64_t slot = a.slot[token];
     const int pos = a.position[token];
+    const char* q = static_cast<const char*>(a.in.q) + (b * a.in.q_batch + t * a.in.q_token) * ES;
+    const char* k = static_cast<const char*>(a.in.k) + (b * a.in.k_batch + t * a.in.k_token) * ES;
+    const char* v = static_cast<const char*>(a.in.v) + (b * a.in.v_batch + t * a.in.v_token) * ES;
+    Raw raw[kRopeRounds];
+#pragma unroll
+    for (int r = 0; r < kRopeRounds; ++r) {
+        const int h = h0 + r * HPW;
+        const char* src = h < a.Hq         ? q + h * a.in.q_head * ES
+                          : h < a.Hq + a.H ? k + (h - a.Hq) * a.in.k_head * ES
+                                           : v + (h - a.Hq - a.H) * a.in.v_head * ES;
+        raw[r] = h < heads ? *reinterpret_cast<const Raw*>(src + e * ES) : Q::zero();
+    }
     const bool inside = slot < a.slots && (a.rot == 0 || (pos >= 0 && pos < a.max_position));
     if (slot >= 0 && !inside && lane == 0) atomicOr(a.status, kStBadIndex);
-    const bool live = slot >= 0 && inside;
-
     char* q_out = static_cast<char*>(a.q_out) + (b * a.o_batch + t * a.o_token) * ES;
-    if (!live) {
-        for (int r = 0; r < ROUNDS; ++r) {
+    if (slot < 0 || !inside) {
+        for (int r = 0; r < kRopeRounds; ++r) {
             const int h = h0 + r * HPW;
             if (h < a.Hq) *reinterpret_cast<Raw*>(q_out + (h * a.o_head + e) * ES) = Q::zero();
         }
         return;
     }
-    const char* q = static_cast<const char*>(a.in.q) + (b * a.in.q_batch + t * a.in.q_token) * ES;
-    const char* k = static_cast<const char*>(a.in.k) + (b * a.in.k_batch + t * a.in.k_token) * ES;
-    const char* v = static_cast<const char*>(a.in.v) + (b * a.in.v_batch + t * a.in.v_token) * ES;
-    Raw raw[ROUNDS];
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int h = h0 + r * HPW;
-        const char* src = h < a.Hq           ? q + h * a.in.q_head * ES
-                          : h < a.Hq + a.H   ? k + (h - a.Hq) * a.in.k_head * ES
-                                             : v + (h - a.Hq - a.H) * a.in.v_head * ES;
-        raw[r] = h < heads ? *reinterpret_cast<const Raw*>(src + e * ES) : Q::zero();
-    }
-    float4 c = make_float4(1, 1, 1, 1), s = make_float4(0, 0, 0, 0);
+    float c[VEC], s[VEC];
     int pair = lane;  // the lane that holds the pairs of this lane's elements
     if (e < a.rot) {
         const float* cs = a.cos_sin + (int64_t)pos * a.rot;
         if (INTERLEAVED) {
-            const float2 c2 = *reinterpret_cast<const float2*>(cs + e / 2);
-            const float2 s2 = *reinterpret_cast<const float2*>(cs + a.rot / 2 + e / 2);
-            c = make_float4(c2.x, c2.x, c2.y, c2.y);
-            s = make_float4(-s2.x, s2.x, -s2.y, s2.y);
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) {
+                const float2 c2 = *reinterpret_cast<const float2*>(cs + (e + i) / 2);
+                const float2 s2 = *reinterpret_cast<const float2*>(cs + a.rot / 2 + (e + i) / 2);
+                c[i] = c[i + 1] = c2.x, c[i + 2] = c[i + 3] = c2.y;
+                s[i] = -s2.x, s[i + 1] = s2.x, s[i + 2] = -s2.y, s[i + 3] = s2.y;
+            }
         } else {
             const bool first = e < a.rot / 2;
-            const int i = first ? e : e - a.rot / 2;
-            c = *reinterpret_cast<const float4*>(cs + i);
-            s = *reinterpret_cast<const float4*>(cs + a.rot / 2 + i);
-            if (first) s = make_float4(-s.x, -s.y, -s.z, -s.w);
-            pair = first ? lane + a.rot / 8 : lane - a.rot / 8;
+            const int at = first ? e : e - a.rot / 2;
+            const float sign = first ? -1.0f : 1.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; i += 4) {
+                const float4 c4 = *reinterpret_cast<const float4*>(cs + at + i);
+                const float4 s4 = *reinterpret_cast<const float4*>(cs + a.rot / 2 + at + i);
+                c[i] = c4.x, c[i + 1] = c4.y, c[i + 2] = c4.z, c[i + 3] = c4.w;
+                s[i] = sign * s4.x, s[i + 1] = sign * s4.y, s[i + 2] = sign * s4.z, s[i + 3] = sign * s4.w;
+            }
+            pair = first ? lane + a.rot / (2 * VEC) : lane - a.rot / (2 * VEC);
         }
     }
-    float4 wq = make_float4(1, 1, 1, 1), wk = wq;
-    if (a.q_weight) wq = Q::wide(*reinterpret_cast<const Raw*>(static_cast<const char*>(a.q_weight) + e * ES));
-    if (a.k_weight) wk = Q::wide(*reinterpret_cast<const Raw*>(static_cast<const char*>(a.k_weight) + e * ES));
+    Raw wq = Q::zero(), wk = Q::zero();
+    if (a.q_weight) wq = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.q_weight) + e * ES);
+    if (a.k_weight) wk = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.k_weight) + e * ES);
     const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
     char* key = static_cast<char*>(a.kv.key) + (page * a.kv.key_page + row * a.kv.key_token) * ES;
     char* value = static_cast<char*>(a.kv.value) + (page * a.kv.value_page + row * a.kv.value_token) * ES;
 #pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
+    for (int r = 0; r < kRopeRounds; ++r) {
         const int h = h0 + r * HPW;
         if (h - sub >= heads) break;  // the same for the whole warp
-        float4 x = Q::wide(raw[r]);
-        float ss = x.x * x.x + x.y * x.y + x.z * x.z + x.w * x.w;
+        float x[VEC], y[VEC];
+        Q::wide(raw[r], x);
+        float ss = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
         for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
         const bool is_q = h < a.Hq;
         if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
-            const float4 w = is_q ? wq : wk;
+            float w[VEC];
+            Q::wide(is_q ? wq : wk, w);
             const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
-            x = make_float4(x.x * inv * w.x, x.y * inv * w.y, x.z * inv * w.z, x.w * inv * w.w);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] *= inv * w[i];
         }
-        float4 y;
-        if (INTERLEAVED) {
-            y = make_float4(x.y, x.x, x.w, x.z);
-        } else {
-            y.x = __shfl_sync(0xffffffffu, x.x, pair);
-            y.y = __shfl_sync(0xffffffffu, x.y, pair);
-            y.z = __shfl_sync(0xffffffffu, x.z, pair);
-            y.w = __shfl_sync(0xffffffffu, x.w, pair);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) y[i] = INTERLEAVED ? x[i ^ 1] : __shfl_sync(0xffffffffu, x[i], pair);
+        if (e < a.rot) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) x[i] = fmaf(x[i], c[i], y[i] * s[i]);
         }
-        if (e < a.rot)
-            x = make_float4(x.x * c.x + y.x * s.x, x.y * c.y + y.y * s.y, x.z * c.z + y.z * s.z, x.w * c.w + y.w * s.w);
         if (h >= heads) continue;
         if (is_q)
             *reinterpret_cast<Raw*>(q_out + (h * a.o_head + e) * ES) = Q::narrow(x);
@@ -327,21 +347,22 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
     }
 }
 
-template <int DT, int D, bool I>
+template <int DT, int D, int VEC, bool I>
 static cudaError_t launch_rope_t(const RopeArgs& a, cudaStream_t s) {
-    const int runs = (a.Hq + 2 * a.H + rope_heads<DT, D>() - 1) / rope_heads<DT, D>();
+    const int runs = (a.Hq + 2 * a.H + rope_heads<D, VEC>() - 1) / rope_heads<D, VEC>();
     const int64_t warps = a.tokens * runs, per = kRopeThreads / 32;
-    return launch_dependent(rope_kernel<DT, D, I>, dim3((unsigned)((warps + per - 1) / per)), dim3(kRopeThreads), 0, s,
+    return launch_dependent(rope_kernel<DT, D, VEC, I>, dim3((unsigned)((warps + per - 1) / per)), dim3(kRopeThreads), 0, s,
                             a);
+}
+template <int DT, int D, int VEC> static cudaError_t launch_rope_i(const RopeArgs& a, bool interleaved, cudaStream_t s) {
+    return interleaved ? launch_rope_t<DT, D, VEC, true>(a, s) : launch_rope_t<DT, D, VEC, false>(a, s);
 }
 
 cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, cudaStream_t s) {
-    if (dtype == 1) {
-        if (D == 128) return interleaved ? launch_rope_t<1, 128, true>(a, s) : launch_rope_t<1, 128, false>(a, s);
-        return interleaved ? launch_rope_t<1, 64, true>(a, s) : launch_rope_t<1, 64, false>(a, s);
-    }
-    if (D == 128) return interleaved ? launch_rope_t<0, 128, true>(a, s) : launch_rope_t<0, 128, false>(a, s);
-    return interleaved ? launch_rope_t<0, 64, true>(a, s) : launch_rope_t<0, 64, false>(a, s);
+    if (dtype == 0) return D == 128 ? launch_rope_i<0, 128, 4>(a, interleaved, s) : launch_rope_i<0, 64, 4>(a, interleaved, s);
+    if (a.rot % 16 == 0)
+        return D == 128 ? launch_rope_i<1, 128, 8>(a, interleaved, s) : launch_rope_i<1, 64, 8>(a, interleaved, s);
+    return D == 128 ? launch_rope_i<1, 128, 4>(a, interleaved, s) : launch_rope_i<1, 64, 4>(a, interleaved, s);
 }
 
 // ---------------------------------------------------------------------------

@@ -232,6 +232,7 @@ extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_
     a.max_pages = cfg->max_pages;
     a.ctas = kAttendCtas;
     a.lead = attend_lead(cfg->dtype);
+    a.least = attend_least(cfg->dtype);
     a.item_rows = attend_item_rows(cfg->dtype, a.T, a.G);
     a.part_rows = attend_part_rows(cfg->dtype, a.T, a.G);
     a.io = *io;

@@ -59,6 +59,7 @@ struct AttendArgs {
     int B, T, H, G, D, P, page_shift, pages, max_pages;
     int ctas;                 // CTAs that share the tiles
     int lead;                 // what an item's start and end cost, in tiles
+    int least;                // tiles of a chunk at least, where few items are cut by themselves
     int item_rows;            // query rows of an item
     int part_rows;            // rows kept of an item's partial sums
     rheo_attend_io io;
@@ -96,6 +97,7 @@ cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s);
 int attend_item_rows(int dtype, int T, int G);
 int attend_part_rows(int dtype, int T, int G);
 int attend_lead(int dtype);
+int attend_least(int dtype);
 constexpr int kAttendCtas = 152;  // one a multiprocessor
 cudaError_t launch_logprobs(const LogprobArgs& a, int dtype, bool aligned, cudaStream_t s);
 int logprob_segments(int rows, int vocab, int dtype, int sms);
