@@ -195,13 +195,16 @@ cudaError_t launch_reserve(const ReserveArgs& a, int sms, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------------------
-// qk_norm_rope.  A warp takes one token and a run of its heads (queries, keys,
-// then values).  A lane holds 16 bytes of a head (VEC elements; 8 where the
-// rotated part does not divide into pieces of 16), so 16 lanes hold a bf16 head of
-// 128.  The loads of the whole run are issued first, before the token's slot and
-// position have come; the sum of squares is a butterfly over the head's lanes, and
-// the pair of an element is in the same lane (interleaved) or rot / (2 VEC) lanes
-// away (a shuffle).  Each input and output element crosses HBM once: HBM bound.
+// qk_norm_rope.  A warp takes one token and a run of its query heads, its key heads
+// or its value heads.  A lane holds 16 bytes of a head (VEC elements; 8 bytes where
+// the rotated part does not divide into pieces of 16), so 16 lanes hold a bf16 head
+// of 128.  The loads of the run are issued first, before the token's slot and
+// position have come.  With w the weights, c and s the turn, x an element and y its
+// pair, the result is (x (w c) + y (w' s)) / rms(x): the two factors of a lane's
+// elements are made once for the run, the sum of squares is a butterfly over the
+// head's lanes, and the pair is in the same lane (interleaved) or rot / (2 VEC)
+// lanes away (a shuffle of the raw elements).  HBM bound: each input and output
+// element crosses once.
 // ---------------------------------------------------------------------------
 constexpr int kRopeThreads = 128;
 
@@ -239,7 +242,17 @@ template <> struct Piece<1, 8> {
 };
 
 constexpr int kRopeRounds = 4;  // loads a lane has under way
-template <int D, int VEC> constexpr int rope_heads() { return kRopeRounds * (32 * VEC / D); }  // heads of a run
+template <int D, int VEC> __host__ __device__ constexpr int rope_heads() { return kRopeRounds * (32 * VEC / D); }
+
+__device__ __forceinline__ uint32_t shfl_raw(uint32_t x, int from) { return __shfl_sync(0xffffffffu, x, from); }
+__device__ __forceinline__ uint2 shfl_raw(uint2 x, int from) { return make_uint2(shfl_raw(x.x, from), shfl_raw(x.y, from)); }
+__device__ __forceinline__ uint4 shfl_raw(uint4 x, int from) {
+    return make_uint4(shfl_raw(x.x, from), shfl_raw(x.y, from), shfl_raw(x.z, from), shfl_raw(x.w, from));
+}
+__device__ __forceinline__ float4 shfl_raw(float4 x, int from) {
+    return make_float4(__shfl_sync(0xffffffffu, x.x, from), __shfl_sync(0xffffffffu, x.y, from),
+                       __shfl_sync(0xffffffffu, x.z, from), __shfl_sync(0xffffffffu, x.w, from));
+}
 
 template <int DT, int D, int VEC, bool INTERLEAVED>
 __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
@@ -249,107 +262,124 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
     constexpr int LPH = D / VEC, HPW = 32 / LPH, HEADS = rope_heads<D, VEC>();
     constexpr int ES = DT == 1 ? 2 : 4;
     const int lane = threadIdx.x & 31, ci = lane & (LPH - 1), sub = lane / LPH, e = ci * VEC;
-    const int heads = a.Hq + 2 * a.H, runs = (heads + HEADS - 1) / HEADS;
+    const int q_runs = (a.Hq + HEADS - 1) / HEADS, kv_runs = (a.H + HEADS - 1) / HEADS, runs = q_runs + 2 * kv_runs;
     const int64_t item = (int64_t)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
     const int64_t token = item / runs;
     if (token >= a.tokens) return;
-    const int h0 = (int)(item - token * runs) * HEADS + sub;
+    int run = (int)(item - token * runs);
     const int64_t b = token / a.T, t = token - b * a.T;
-
     const int64_t slot = a.slot[token];
     const int pos = a.position[token];
-    const char* q = static_cast<const char*>(a.in.q) + (b * a.in.q_batch + t * a.in.q_token) * ES;
-    const char* k = static_cast<const char*>(a.in.k) + (b * a.in.k_batch + t * a.in.k_token) * ES;
-    const char* v = static_cast<const char*>(a.in.v) + (b * a.in.v_batch + t * a.in.v_token) * ES;
+
+    // which: 0 queries, 1 keys, 2 values; the same for the whole warp
+    const int which = run < q_runs ? 0 : run < q_runs + kv_runs ? 1 : 2;
+    if (which == 1) run -= q_runs;
+    if (which == 2) run -= q_runs + kv_runs;
+    const int h0 = run * HEADS + sub, heads = which == 0 ? a.Hq : a.H;
+    const char* in = static_cast<const char*>(which == 0 ? a.in.q : which == 1 ? a.in.k : a.in.v);
+    const int64_t in_batch = which == 0 ? a.in.q_batch : which == 1 ? a.in.k_batch : a.in.v_batch;
+    const int64_t in_token = which == 0 ? a.in.q_token : which == 1 ? a.in.k_token : a.in.v_token;
+    const int64_t in_head = which == 0 ? a.in.q_head : which == 1 ? a.in.k_head : a.in.v_head;
+    in += (b * in_batch + t * in_token + h0 * in_head + e) * ES;
     Raw raw[kRopeRounds];
 #pragma unroll
-    for (int r = 0; r < kRopeRounds; ++r) {
-        const int h = h0 + r * HPW;
-        const char* src = h < a.Hq         ? q + h * a.in.q_head * ES
-                          : h < a.Hq + a.H ? k + (h - a.Hq) * a.in.k_head * ES
-                                           : v + (h - a.Hq - a.H) * a.in.v_head * ES;
-        raw[r] = h < heads ? *reinterpret_cast<const Raw*>(src + e * ES) : Q::zero();
-    }
+    for (int r = 0; r < kRopeRounds; ++r)
+        raw[r] = h0 + r * HPW < heads ? *reinterpret_cast<const Raw*>(in + r * HPW * in_head * ES) : Q::zero();
+
     const bool inside = slot < a.slots && (a.rot == 0 || (pos >= 0 && pos < a.max_position));
     if (slot >= 0 && !inside && lane == 0) atomicOr(a.status, kStBadIndex);
-    char* q_out = static_cast<char*>(a.q_out) + (b * a.o_batch + t * a.o_token) * ES;
-    if (slot < 0 || !inside) {
-        for (int r = 0; r < kRopeRounds; ++r) {
-            const int h = h0 + r * HPW;
-            if (h < a.Hq) *reinterpret_cast<Raw*>(q_out + (h * a.o_head + e) * ES) = Q::zero();
-        }
+    const bool live = slot >= 0 && inside;
+    char* out;
+    int64_t out_head;
+    if (which == 0) {
+        out = static_cast<char*>(a.q_out) + (b * a.o_batch + t * a.o_token) * ES;
+        out_head = a.o_head;
+    } else {
+        if (!live) return;
+        const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
+        out = static_cast<char*>(which == 1 ? a.kv.key : a.kv.value) +
+              (page * (which == 1 ? a.kv.key_page : a.kv.value_page) + row * (which == 1 ? a.kv.key_token : a.kv.value_token)) * ES;
+        out_head = which == 1 ? a.kv.key_head : a.kv.value_head;
+    }
+    out += (h0 * out_head + e) * ES;
+    if (which == 2 || !live) {
+#pragma unroll
+        for (int r = 0; r < kRopeRounds; ++r)
+            if (h0 + r * HPW < heads) *reinterpret_cast<Raw*>(out + r * HPW * out_head * ES) = live ? raw[r] : Q::zero();
         return;
     }
-    float c[VEC], s[VEC];
+
+    // factors of an element and of its pair
+    const char* weight = static_cast<const char*>(which == 0 ? a.q_weight : a.k_weight);
+    float fx[VEC], fy[VEC];
     int pair = lane;  // the lane that holds the pairs of this lane's elements
-    if (e < a.rot) {
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) fx[i] = 1.0f, fy[i] = 0.0f;
+    const bool turns = e < a.rot;
+    if (weight) Q::wide(*reinterpret_cast<const Raw*>(weight + e * ES), fx);
+    if (turns) {
         const float* cs = a.cos_sin + (int64_t)pos * a.rot;
         if (INTERLEAVED) {
 #pragma unroll
             for (int i = 0; i < VEC; i += 4) {
                 const float2 c2 = *reinterpret_cast<const float2*>(cs + (e + i) / 2);
                 const float2 s2 = *reinterpret_cast<const float2*>(cs + a.rot / 2 + (e + i) / 2);
-                c[i] = c[i + 1] = c2.x, c[i + 2] = c[i + 3] = c2.y;
-                s[i] = -s2.x, s[i + 1] = s2.x, s[i + 2] = -s2.y, s[i + 3] = s2.y;
+                fy[i] = -s2.x * fx[i + 1], fy[i + 1] = s2.x * fx[i];
+                fy[i + 2] = -s2.y * fx[i + 3], fy[i + 3] = s2.y * fx[i + 2];
+                fx[i] *= c2.x, fx[i + 1] *= c2.x, fx[i + 2] *= c2.y, fx[i + 3] *= c2.y;
             }
         } else {
             const bool first = e < a.rot / 2;
             const int at = first ? e : e - a.rot / 2;
             const float sign = first ? -1.0f : 1.0f;
+            float w[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[i] = 1.0f;
+            if (weight) Q::wide(*reinterpret_cast<const Raw*>(weight + (first ? e + a.rot / 2 : at) * ES), w);
 #pragma unroll
             for (int i = 0; i < VEC; i += 4) {
                 const float4 c4 = *reinterpret_cast<const float4*>(cs + at + i);
                 const float4 s4 = *reinterpret_cast<const float4*>(cs + a.rot / 2 + at + i);
-                c[i] = c4.x, c[i + 1] = c4.y, c[i + 2] = c4.z, c[i + 3] = c4.w;
-                s[i] = sign * s4.x, s[i + 1] = sign * s4.y, s[i + 2] = sign * s4.z, s[i + 3] = sign * s4.w;
+                fx[i] *= c4.x, fx[i + 1] *= c4.y, fx[i + 2] *= c4.z, fx[i + 3] *= c4.w;
+                fy[i] = sign * s4.x * w[i], fy[i + 1] = sign * s4.y * w[i + 1];
+                fy[i + 2] = sign * s4.z * w[i + 2], fy[i + 3] = sign * s4.w * w[i + 3];
             }
             pair = first ? lane + a.rot / (2 * VEC) : lane - a.rot / (2 * VEC);
         }
     }
-    Raw wq = Q::zero(), wk = Q::zero();
-    if (a.q_weight) wq = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.q_weight) + e * ES);
-    if (a.k_weight) wk = *reinterpret_cast<const Raw*>(static_cast<const char*>(a.k_weight) + e * ES);
-    const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
-    char* key = static_cast<char*>(a.kv.key) + (page * a.kv.key_page + row * a.kv.key_token) * ES;
-    char* value = static_cast<char*>(a.kv.value) + (page * a.kv.value_page + row * a.kv.value_token) * ES;
 #pragma unroll
     for (int r = 0; r < kRopeRounds; ++r) {
-        const int h = h0 + r * HPW;
-        if (h - sub >= heads) break;  // the same for the whole warp
+        if (h0 - sub + r * HPW >= heads) break;  // the same for the whole warp
         float x[VEC], y[VEC];
         Q::wide(raw[r], x);
-        float ss = 0.0f;
+        if (INTERLEAVED) {
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) ss = fmaf(x[i], x[i], ss);
+            for (int i = 0; i < VEC; ++i) y[i] = x[i ^ 1];
+        } else {
+            Q::wide(shfl_raw(raw[r], pair), y);
+        }
+        float inv = 1.0f;
+        if (weight) {
+            float ss = 0.0f;
 #pragma unroll
-        for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const bool is_q = h < a.Hq;
-        if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
-            float w[VEC];
-            Q::wide(is_q ? wq : wk, w);
-            const float inv = rsqrtf(ss * (1.0f / D) + a.eps);
+            for (int i = 0; i < VEC; ++i) ss = fmaf(x[i], x[i], ss);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] *= inv * w[i];
+            for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            inv = rsqrtf(ss * (1.0f / D) + a.eps);
         }
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) y[i] = INTERLEAVED ? x[i ^ 1] : __shfl_sync(0xffffffffu, x[i], pair);
-        if (e < a.rot) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) x[i] = fmaf(x[i], c[i], y[i] * s[i]);
+        for (int i = 0; i < VEC; ++i) {
+            const float z = x[i] * fx[i];
+            x[i] = (turns ? fmaf(y[i], fy[i], z) : z) * inv;  // (what does not turn has no pair: 0 * inf is none of it)
         }
-        if (h >= heads) continue;
-        if (is_q)
-            *reinterpret_cast<Raw*>(q_out + (h * a.o_head + e) * ES) = Q::narrow(x);
-        else if (h < a.Hq + a.H)
-            *reinterpret_cast<Raw*>(key + ((h - a.Hq) * a.kv.key_head + e) * ES) = Q::narrow(x);
-        else
-            *reinterpret_cast<Raw*>(value + ((h - a.Hq - a.H) * a.kv.value_head + e) * ES) = raw[r];
+        if (h0 + r * HPW < heads) *reinterpret_cast<Raw*>(out + r * HPW * out_head * ES) = Q::narrow(x);
     }
 }
 
 template <int DT, int D, int VEC, bool I>
 static cudaError_t launch_rope_t(const RopeArgs& a, cudaStream_t s) {
-    const int runs = (a.Hq + 2 * a.H + rope_heads<D, VEC>() - 1) / rope_heads<D, VEC>();
+    constexpr int heads = rope_heads<D, VEC>();
+    const int runs = (a.Hq + heads - 1) / heads + 2 * ((a.H + heads - 1) / heads);
     const int64_t warps = a.tokens * runs, per = kRopeThreads / 32;
     return launch_dependent(rope_kernel<DT, D, VEC, I>, dim3((unsigned)((warps + per - 1) / per)), dim3(kRopeThreads), 0, s,
                             a);
