@@ -1,20 +1,24 @@
 // logprobs.cu -- log probabilities of given tokens with rank, entropy and the
 // top alternatives, in one pass over each row's logits.
 //
-// With a running reference m (the largest logit so far), c = log2(e)/T and
+// With a running reference m (a logit met so far; a new one when a logit lies
+// more than kLpSlack log2 units above it, which after a thread's first vector is
+// rare, so the lanes of a warp keep together), c = log2(e)/T and
 // d = (l - m) c, a thread keeps Z = sum 2^d and W = sum 2^d d; a new reference m'
 // with D = (m - m') c turns them into 2^D Z and 2^D (W + D Z).  Then, in log2 units,
 //   log p(t) = (l_t - m) c - log2 Z,   H = log2 Z - W / Z.
 // The difference is taken before the product, so that logits near the type's
 // lowest value (a common mask) neither overflow nor lose their order.
 // The rank counts l > l_t, and l = l_t at smaller ids.
-// Top alternatives: the k-th largest of the threads' own maxima bounds the row's
-// k-th largest from below, so the stream needs nothing but each thread's
-// maximum; afterwards only the stripes of the k threads at or above the bound
-// are read again (from L2), and the few logits found there are ranked.  Keys are
-// (logit, -id) in 64 bits, all different, so ties need no care.
+// Top alternatives: the k-th largest of the maxima of 128 groups of four threads
+// bounds the row's k-th largest from below, so the stream needs nothing but each
+// thread's maximum and where it was; afterwards only the stripes of the k groups at
+// or above the bound are read again (from L2), and the few logits found there are
+// ranked.  Keys are (logit, -id) in 64 bits, all different, so ties need no care.
 // A row is cut into segments where there are fewer rows than SMs; the last CTA of
 // a row joins them.
+#include <cuda_bf16.h>
+
 #include "cache_kernels.h"
 #include "rheo_device.cuh"
 #include "rheo_kernels.h"
@@ -25,7 +29,9 @@ constexpr int kLpThreads = 512;
 constexpr int kLpWarps = kLpThreads / 32;
 constexpr int kLpBatch = 4;       // vectors in flight a thread
 constexpr int kLpCand = 2048;     // candidates ranked at a time
+constexpr int kLpGroups = kLpThreads / 4;
 constexpr int kLpMaxSegments = kLpCand / kMaxTop;
+constexpr float kLpSlack = 24.0f;       // log2 units that a logit may lie above the reference
 constexpr float kLpFloor = -10000.0f;  // 2^floor = 0: keeps (-inf) * 0 out of W
 
 struct LpSums {
@@ -46,13 +52,53 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     return r;
 }
 
-// The next float below x; NaN for -inf.
-__device__ __forceinline__ float below(float x) {
-    if (x == -INFINITY) return __uint_as_float(0x7FC00000u);
-    if (x == 0.0f) return __uint_as_float(0x80000001u);
-    const uint32_t u = __float_as_uint(x);
-    return __uint_as_float(u & 0x80000000u ? u + 1 : u - 1);
+// Counts logits above a cut.  The cut for vectors before the token's is the type's
+// next value below its logit, so that equal ones count there; NaN for -inf, above
+// which (unordered) everything counts.
+__device__ __forceinline__ uint32_t below_bits(uint32_t u, uint32_t sign, uint32_t neg_inf, uint32_t nan) {
+    if (u == neg_inf) return nan;
+    if ((u & ~sign) == 0) return sign | 1u;  // either zero
+    return u & sign ? u + 1 : u - 1;
 }
+template <int DT> struct LpAbove;
+template <> struct LpAbove<0> {
+    unsigned long long n = 0ull;
+    __device__ static __forceinline__ uint32_t cut(float l, bool before) {
+        const uint32_t u = __float_as_uint(l);
+        return before ? below_bits(u, 0x80000000u, 0xFF800000u, 0x7FC00000u) : u;
+    }
+    __device__ static __forceinline__ float one(uint32_t l, uint32_t cut) {
+        float r;
+        asm("set.gtu.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(l)), "f"(__uint_as_float(cut)));
+        return r;
+    }
+    __device__ __forceinline__ void add(const uint4& x, uint32_t cut) {
+        n = f2_add(n, f2_add(f2_pack(one(x.x, cut), one(x.y, cut)), f2_pack(one(x.z, cut), one(x.w, cut))));
+    }
+    __device__ __forceinline__ void flush(int& count) {
+        count += (int)f2_fold(n);
+        n = 0ull;
+    }
+};
+template <> struct LpAbove<1> {
+    __nv_bfloat162 n = __floats2bfloat162_rn(0.0f, 0.0f);  // whole numbers to 256
+    __device__ static __forceinline__ uint32_t cut(float l, bool before) {
+        const uint32_t h = __float_as_uint(l) >> 16, u = before ? below_bits(h, 0x8000u, 0xFF80u, 0x7FC0u) : h;
+        return u | (u << 16);
+    }
+    __device__ static __forceinline__ __nv_bfloat162 two(uint32_t l, uint32_t cut) {
+        uint32_t r;
+        asm("set.gtu.bf16x2.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(l), "r"(cut));
+        return *reinterpret_cast<const __nv_bfloat162*>(&r);
+    }
+    __device__ __forceinline__ void add(const uint4& x, uint32_t cut) {
+        n = __hadd2(n, __hadd2(__hadd2(two(x.x, cut), two(x.y, cut)), __hadd2(two(x.z, cut), two(x.w, cut))));
+    }
+    __device__ __forceinline__ void flush(int& count) {
+        count += (int)(__low2float(n) + __high2float(n));
+        n = __floats2bfloat162_rn(0.0f, 0.0f);
+    }
+};
 
 // Larger for larger logits, then for smaller ids; 0 for -inf.
 __device__ __forceinline__ unsigned long long lp_key(float v, int id) {
@@ -62,15 +108,46 @@ __device__ __forceinline__ unsigned long long lp_key(float v, int id) {
 __device__ __forceinline__ int lp_id(unsigned long long key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
 __device__ __forceinline__ float lp_value(unsigned long long key) { return Elem<0>::value_of_key((uint32_t)(key >> 32)); }
 
+// The largest (NaN if there is one) and the smallest logit of a vector.
+template <int DT> struct LpVec;
+template <> struct LpVec<0> {
+    __device__ static __forceinline__ float largest(const uint4& x) {
+        return max_nan(max_nan(__uint_as_float(x.x), __uint_as_float(x.y)), max_nan(__uint_as_float(x.z), __uint_as_float(x.w)));
+    }
+    __device__ static __forceinline__ float smallest(const uint4& x) {
+        return fminf(fminf(__uint_as_float(x.x), __uint_as_float(x.y)), fminf(__uint_as_float(x.z), __uint_as_float(x.w)));
+    }
+};
+template <> struct LpVec<1> {
+    __device__ static __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static __forceinline__ uint32_t min2(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("min.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    __device__ static __forceinline__ float largest(const uint4& x) {
+        const uint32_t r = max2(max2(x.x, x.y), max2(x.z, x.w));
+        return max_nan(bf_lo(r), bf_hi(r));
+    }
+    __device__ static __forceinline__ float smallest(const uint4& x) {
+        const uint32_t r = min2(min2(x.x, x.y), min2(x.z, x.w));
+        return fminf(bf_lo(r), bf_hi(r));
+    }
+};
+
 struct LpShared {
     unsigned long long cand[kLpCand];
-    unsigned long long best[kLpThreads];
+    unsigned long long best[kLpGroups];
     unsigned long long top[kMaxTop];
     unsigned long long red[kLpWarps];
     LpSums sums[kLpWarps];
     int count[kLpWarps];
-    int stripe[kMaxTop];
-    int n_stripe, n_cand, last;
+    int group[kMaxTop];
+    int n_group, n_cand, last;
     unsigned long long floor;
 };
 
@@ -131,58 +208,74 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
     const float c = fminf(1.4426950408889634f / T, 3.0e38f);
     const char* row = a.logits + r * a.row_stride_bytes;
     const float lt = tk >= 0 ? E::value(E::load_scalar(row, tk)) : INFINITY;
-    const float lt_below = tk >= 0 ? below(lt) : INFINITY;
     const int tv = tk >= 0 ? tk / VEC : -1;  // the vector that holds the token
     const int vectors = (V + VEC - 1) / VEC;
     const int v0 = (int)((int64_t)seg * vectors / a.segments), v1 = (int)((int64_t)(seg + 1) * vectors / a.segments);
 
-    LpSums s{-INFINITY, 0.0f, 0.0f};
-    int mv = -1, count = 0;  // the vector in which the reference was met first
-    for (int base = v0 + tid; base < v1; base += kLpThreads * kLpBatch) {
-        uint4 x[kLpBatch];
+    float m = -INFINITY, mx = -INFINITY;       // reference, largest logit
+    unsigned long long z2 = 0ull, w2 = 0ull;   // sums of the even and of the odd elements
+    int mv = -1, count = 0;                    // the vector in which the largest was met first
+    const unsigned long long c2 = f2_pack(c, c);
+    LpAbove<DT> above;
+    const uint32_t before = LpAbove<DT>::cut(lt, true), after = LpAbove<DT>::cut(lt, false);
+    auto take = [&](const uint4& x, int v) {
+        const float vm = LpVec<DT>::largest(x), vn = LpVec<DT>::smallest(x);
+        mv = vm > mx ? v : mv;
+        mx = max_nan(mx, vm);
+        if (!((vm - m) * c <= kLpSlack) && vm > -INFINITY) {
+            const float d = fmaxf((m - vm) * c, kLpFloor), f = fast_exp2(d);
+            const unsigned long long f2 = f2_pack(f, f), d2 = f2_pack(d, d);
+            w2 = f2_mul(f2, f2_fma(d2, z2, w2));
+            z2 = f2_mul(f2, z2);
+            m = vm;
+        }
+        if (m > -INFINITY || m != m) {  // nothing but -inf so far adds nothing
+            const unsigned long long m2 = f2_pack(-m, -m);
+            if ((vn - m) * c > kLpFloor) {
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const unsigned long long d =
+                        f2_mul(f2_add(f2_pack(E::value(E::raw(x, e)), E::value(E::raw(x, e + 1))), m2), c2);
+                    const unsigned long long p = f2_exp2(d);
+                    z2 = f2_add(z2, p);
+                    w2 = f2_fma(p, d, w2);
+                }
+            } else {
+                // logits so far below the reference (masked ones) that 0 * d may not be 0
+#pragma unroll
+                for (int e = 0; e < VEC; e += 2) {
+                    const float d0 = max_nan((E::value(E::raw(x, e)) - m) * c, kLpFloor);
+                    const float d1 = max_nan((E::value(E::raw(x, e + 1)) - m) * c, kLpFloor);
+                    const unsigned long long d = f2_pack(d0, d1), p = f2_exp2(d);
+                    z2 = f2_add(z2, p);
+                    w2 = f2_fma(p, d, w2);
+                }
+            }
+        }
+        above.add(x, v < tv ? before : after);
+        if (v == tv) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) count += E::value(E::raw(x, e)) == lt && v * VEC + e < tk;
+        }
+    };
+    // a batch is taken while the next one is on its way
+    uint4 now[kLpBatch], next[kLpBatch];
+    auto fetch = [&](uint4 (&x)[kLpBatch], int base) {
 #pragma unroll
         for (int u = 0; u < kLpBatch; ++u)
             if (base + u * kLpThreads < v1) x[u] = load_vec<DT, ALIGNED>(row, (int64_t)(base + u * kLpThreads) * VEC, V);
+    };
+    fetch(now, v0 + tid);
+    for (int base = v0 + tid; base < v1; base += kLpThreads * kLpBatch) {
+        fetch(next, base + kLpThreads * kLpBatch);
 #pragma unroll
-        for (int u = 0; u < kLpBatch; ++u) {
-            const int v = base + u * kLpThreads;
-            if (v >= v1) break;
-            float l[VEC], vm = -INFINITY;
+        for (int u = 0; u < kLpBatch; ++u)
+            if (base + u * kLpThreads < v1) take(now[u], base + u * kLpThreads);
+        above.flush(count);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                l[e] = E::value(E::raw(x[u], e));
-                vm = max_nan(vm, l[e]);
-            }
-            if (!(vm <= s.m)) {
-                const float d = fmaxf((s.m - vm) * c, kLpFloor), f = fast_exp2(d);
-                s.w = f * (s.w + d * s.z);
-                s.z *= f;
-                s.m = vm;
-                mv = v;
-            }
-            if (s.m == -INFINITY) {
-                // nothing but -inf so far: it adds nothing to the sums
-                if (tk >= 0)
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        count += v == tv ? (l[e] == lt && v * VEC + e < tk) : v < tv ? !(l[e] <= lt_below) : 0;
-                continue;
-            }
-            const float cut = v < tv ? lt_below : lt;
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float d = max_nan((l[e] - s.m) * c, kLpFloor), p = fast_exp2(d);
-                s.z += p;
-                s.w = fmaf(p, d, s.w);
-                count += !(l[e] <= cut);
-            }
-            if (v == tv)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) count += l[e] == lt && v * VEC + e < tk;
-        }
+        for (int u = 0; u < kLpBatch; ++u) now[u] = next[u];
     }
-
-    const float mx = s.m;  // this thread's largest logit
+    LpSums s{m, f2_fold(z2), f2_fold(w2)};
 
     // sums and count over the block
 #pragma unroll
@@ -197,41 +290,44 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
         sm.count[warp] = count;
     }
     if (k > 0) {
-        unsigned long long key = 0ull;
-        if (mv >= 0 && mx > -INFINITY) {
-            const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)mv * VEC, V);
-            int id = -1;
+        // no larger than the key of the thread's first largest logit
+        unsigned long long key = mv >= 0 && mx > -INFINITY ? lp_key(mx, mv * VEC + VEC - 1) : 0ull;
 #pragma unroll
-            for (int e = VEC - 1; e >= 0; --e)
-                if (E::value(E::raw(x, e)) == mx) id = mv * VEC + e;
-            key = lp_key(mx, id);
+        for (int o = 1; o < 4; o <<= 1) {
+            const unsigned long long y = __shfl_xor_sync(0xffffffffu, key, o);
+            key = y > key ? y : key;
         }
-        sm.best[tid] = key;
+        if ((tid & 3) == 0) sm.best[tid >> 2] = key;
         if (tid == 0) {
-            sm.n_stripe = sm.n_cand = 0;
+            sm.n_group = sm.n_cand = 0;
             sm.floor = 1ull;
         }
         __syncthreads();
-        if (key != 0ull) {
-            int above = 0;
+        if (tid < kLpGroups && (key = sm.best[tid]) != 0ull) {
+            int above_me = 0;
 #pragma unroll 8
-            for (int j = 0; j < kLpThreads; ++j) above += sm.best[j] > key;
-            if (above < k) sm.stripe[atomicAdd(&sm.n_stripe, 1)] = tid;
-            if (above == k - 1) sm.floor = key;
+            for (int j = 0; j < kLpGroups; ++j) above_me += sm.best[j] > key;
+            if (above_me < k) sm.group[atomicAdd(&sm.n_group, 1)] = tid;
+            if (above_me == k - 1) sm.floor = key;
         }
         __syncthreads();
         const unsigned long long floor = sm.floor;
-        const int n_stripe = sm.n_stripe;
-        for (int q = warp; q < n_stripe; q += kLpWarps) {
-            for (int v = v0 + sm.stripe[q] + lane * kLpThreads; v < v1; v += 32 * kLpThreads) {
-                const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
+        // vectors of the groups' stripes, as one list over the block
+        const int deep = (v1 - v0 + kLpThreads - 1) / kLpThreads, total = sm.n_group * deep * 4;
+        auto vector_of = [&](int i) {
+            const int g = i / (deep * 4), r = i - g * deep * 4;
+            return v0 + sm.group[g] * 4 + (r & 3) + (r >> 2) * kLpThreads;
+        };
+        for (int i = tid; i < total; i += kLpThreads) {
+            const int v = vector_of(i);
+            if (v >= v1) continue;
+            const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
-                    if (y >= floor) {
-                        const int at = atomicAdd(&sm.n_cand, 1);
-                        if (at < kLpCand) sm.cand[at] = y;
-                    }
+            for (int e = 0; e < VEC; ++e) {
+                const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
+                if (y >= floor) {
+                    const int at = atomicAdd(&sm.n_cand, 1);
+                    if (at < kLpCand) sm.cand[at] = y;
                 }
             }
         }
@@ -244,15 +340,16 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
             unsigned long long last = ~0ull;
             for (int round = 0; round < k; ++round) {
                 unsigned long long top = 0ull;
-                for (int q = warp; q < n_stripe; q += kLpWarps)
-                    for (int v = v0 + sm.stripe[q] + lane * kLpThreads; v < v1; v += 32 * kLpThreads) {
-                        const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
+                for (int i = tid; i < total; i += kLpThreads) {
+                    const int v = vector_of(i);
+                    if (v >= v1) continue;
+                    const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
-                            if (y < last && y > top) top = y;
-                        }
+                    for (int e = 0; e < VEC; ++e) {
+                        const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
+                        if (y < last && y > top) top = y;
                     }
+                }
                 top = warp_max_u64(top);
                 if (lane == 0) sm.red[warp] = top;
                 __syncthreads();
