@@ -27,7 +27,7 @@ namespace rheo {
 
 constexpr int kLpThreads = 512;
 constexpr int kLpWarps = kLpThreads / 32;
-constexpr int kLpBatch = 4;       // vectors in flight a thread
+constexpr int kLpBatch = 2;       // vectors of a thread in work, and as many on their way
 constexpr int kLpCand = 2048;     // candidates ranked at a time
 constexpr int kLpGroups = kLpThreads / 4;
 constexpr int kLpMaxSegments = kLpCand / kMaxTop;
@@ -312,25 +312,31 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
         }
         __syncthreads();
         const unsigned long long floor = sm.floor;
-        // vectors of the groups' stripes, as one list over the block
-        const int deep = (v1 - v0 + kLpThreads - 1) / kLpThreads, total = sm.n_group * deep * 4;
-        auto vector_of = [&](int i) {
-            const int g = i / (deep * 4), r = i - g * deep * 4;
-            return v0 + sm.group[g] * 4 + (r & 3) + (r >> 2) * kLpThreads;
-        };
-        for (int i = tid; i < total; i += kLpThreads) {
-            const int v = vector_of(i);
-            if (v >= v1) continue;
-            const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
+        const int n_group = sm.n_group;
+        // a group's stripes by a warp: four neighbouring vectors a quarter of eight lanes, four rounds under way
+        auto each = [&](auto&& f) {
+            constexpr int step = 8 * kLpThreads;
+            for (int q = warp; q < n_group; q += kLpWarps) {
+                for (int v = v0 + sm.group[q] * 4 + (lane & 3) + (lane >> 2) * kLpThreads; v < v1; v += 4 * step) {
+                    uint4 x[4];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
-                if (y >= floor) {
-                    const int at = atomicAdd(&sm.n_cand, 1);
-                    if (at < kLpCand) sm.cand[at] = y;
+                    for (int u = 0; u < 4; ++u)
+                        if (v + u * step < v1) x[u] = load_vec<DT, ALIGNED>(row, (int64_t)(v + u * step) * VEC, V);
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        if (v + u * step < v1)
+#pragma unroll
+                            for (int e = 0; e < VEC; ++e)
+                                f(lp_key(E::value(E::raw(x[u], e)), (v + u * step) * VEC + e));
                 }
             }
-        }
+        };
+        each([&](unsigned long long y) {
+            if (y >= floor) {
+                const int at = atomicAdd(&sm.n_cand, 1);
+                if (at < kLpCand) sm.cand[at] = y;
+            }
+        });
         __syncthreads();
         const int n = sm.n_cand;
         if (n <= kLpCand) {
@@ -340,16 +346,9 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
             unsigned long long last = ~0ull;
             for (int round = 0; round < k; ++round) {
                 unsigned long long top = 0ull;
-                for (int i = tid; i < total; i += kLpThreads) {
-                    const int v = vector_of(i);
-                    if (v >= v1) continue;
-                    const uint4 x = load_vec<DT, ALIGNED>(row, (int64_t)v * VEC, V);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        const unsigned long long y = lp_key(E::value(E::raw(x, e)), v * VEC + e);
-                        if (y < last && y > top) top = y;
-                    }
-                }
+                each([&](unsigned long long y) {
+                    if (y < last && y > top) top = y;
+                });
                 top = warp_max_u64(top);
                 if (lane == 0) sm.red[warp] = top;
                 __syncthreads();
@@ -425,11 +424,12 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
     }
 }
 
-// CTAs a row: all SMs share the rows when there are few, with two full batches a
-// thread at least.
+// CTAs a row: about two an SM in all, so that one reads while the other ranks, with
+// four vectors a thread at least (144 rows of 151,936 in bf16: 33.8, 24.4, 32.7 us
+// with one, two, three an SM; two vectors in work at a time: 27.1 us with four).
 int logprob_segments(int rows, int vocab, int dtype, int sms) {
     const int vec = dtype == 1 ? 8 : 4, vectors = (vocab + vec - 1) / vec;
-    int n = sms / rows, most = vectors / (2 * kLpThreads);
+    int n = 2 * sms / rows, most = vectors / (4 * kLpThreads);
     n = n < most ? n : most;
     n = n < kLpMaxSegments ? n : kLpMaxSegments;
     return n < 1 ? 1 : n;
