@@ -390,8 +390,7 @@ def status(cfg: Config, ws: Workspace, stream=None) -> int:
     """Synchronise the stream, return and clear the device status word."""
     st = ctypes.c_int32()
     _check(lib().rheo_get_status(ctypes.byref(cfg.c()), ws.ptr(), _stream(stream), ctypes.byref(st)),
-           "rheo_get_status", "rheo_cache_sizes", "rheo_scratch_init", "rheo_scratch_status", "rheo_cache_reserve",
-           "rheo_qk_norm_rope", "rheo_tree_attend", "rheo_cache_commit", "rheo_logprob_sizes", "rheo_token_logprobs")
+           "rheo_get_status")
     return st.value
 
 
