@@ -1,9 +1,8 @@
 // logprobs.cu -- log probabilities of given tokens with rank, entropy and the
 // top alternatives, in one pass over each row's logits.
 //
-// With a running reference m (a logit met so far; a new one when a logit lies
-// more than kLpSlack log2 units above it, which after a thread's first vector is
-// rare, so the lanes of a warp keep together), c = log2(e)/T and
+// With a running reference m (the largest logit that the thread's warp has met: one
+// for all its lanes, so that it moves a handful of times a row), c = log2(e)/T and
 // d = (l - m) c, a thread keeps Z = sum 2^d and W = sum 2^d d; a new reference m'
 // with D = (m - m') c turns them into 2^D Z and 2^D (W + D Z).  Then, in log2 units,
 //   log p(t) = (l_t - m) c - log2 Z,   H = log2 Z - W / Z.
@@ -31,7 +30,6 @@ constexpr int kLpBatch = 2;       // vectors of a thread in work, and as many on
 constexpr int kLpCand = 2048;     // candidates ranked at a time
 constexpr int kLpGroups = kLpThreads / 4;
 constexpr int kLpMaxSegments = kLpCand / kMaxTop;
-constexpr float kLpSlack = 24.0f;       // log2 units that a logit may lie above the reference
 constexpr float kLpFloor = -10000.0f;  // 2^floor = 0: keeps (-inf) * 0 out of W
 
 struct LpSums {
@@ -219,15 +217,19 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
     LpAbove<DT> above;
     const uint32_t before = LpAbove<DT>::cut(lt, true), after = LpAbove<DT>::cut(lt, false);
     auto take = [&](const uint4& x, int v) {
+        const int own_tv = v < v1 ? tv : -1;
         const float vm = LpVec<DT>::largest(x), vn = LpVec<DT>::smallest(x);
         mv = vm > mx ? v : mv;
         mx = max_nan(mx, vm);
-        if (!((vm - m) * c <= kLpSlack) && vm > -INFINITY) {
-            const float d = fmaxf((m - vm) * c, kLpFloor), f = fast_exp2(d);
+        if (__any_sync(0xffffffffu, !(vm <= m))) {
+            float top = max_nan(m, vm);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+            const float d = fmaxf((m - top) * c, kLpFloor), f = fast_exp2(d);
             const unsigned long long f2 = f2_pack(f, f), d2 = f2_pack(d, d);
             w2 = f2_mul(f2, f2_fma(d2, z2, w2));
             z2 = f2_mul(f2, z2);
-            m = vm;
+            m = top;
         }
         if (m > -INFINITY || m != m) {  // nothing but -inf so far adds nothing
             const unsigned long long m2 = f2_pack(-m, -m);
@@ -252,25 +254,28 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
                 }
             }
         }
-        above.add(x, v < tv ? before : after);
-        if (v == tv) {
+        above.add(x, v < own_tv ? before : after);
+        if (v == own_tv) {
 #pragma unroll
             for (int e = 0; e < VEC; ++e) count += E::value(E::raw(x, e)) == lt && v * VEC + e < tk;
         }
     };
+    // (lanes past the segment take an empty vector, which no cut but NaN counts)
     // a batch is taken while the next one is on its way
     uint4 now[kLpBatch], next[kLpBatch];
+    const uint32_t low = DT == 1 ? 0xFF80FF80u : 0xFF800000u;
+    const uint4 none = make_uint4(low, low, low, low);  // -inf: adds nothing
     auto fetch = [&](uint4 (&x)[kLpBatch], int base) {
 #pragma unroll
         for (int u = 0; u < kLpBatch; ++u)
-            if (base + u * kLpThreads < v1) x[u] = load_vec<DT, ALIGNED>(row, (int64_t)(base + u * kLpThreads) * VEC, V);
+            x[u] = base + u * kLpThreads < v1 ? load_vec<DT, ALIGNED>(row, (int64_t)(base + u * kLpThreads) * VEC, V) : none;
     };
     fetch(now, v0 + tid);
-    for (int base = v0 + tid; base < v1; base += kLpThreads * kLpBatch) {
-        fetch(next, base + kLpThreads * kLpBatch);
+    for (int base = v0 + warp * 32; base < v1; base += kLpThreads * kLpBatch) {  // the same for the whole warp
+        fetch(next, base + lane + kLpThreads * kLpBatch);
 #pragma unroll
         for (int u = 0; u < kLpBatch; ++u)
-            if (base + u * kLpThreads < v1) take(now[u], base + u * kLpThreads);
+            if (base + u * kLpThreads < v1) take(now[u], base + u * kLpThreads + lane);
         above.flush(count);
 #pragma unroll
         for (int u = 0; u < kLpBatch; ++u) now[u] = next[u];
