@@ -301,8 +301,9 @@ typedef struct {
     int32_t* n_free;       /* [1]                                           */
 } rheo_pages;
 
-/* Keys and values of one layer.  Strides in elements; a token's D elements are
- * contiguous.  Pointers and strides (in bytes) are multiples of 16. */
+/* Keys and values of one layer.  Strides in elements, positive and below 2^38; a
+ * token's D elements are contiguous.  Pointers and strides (in bytes) are
+ * multiples of 16; the stride of a dimension of one is not looked at. */
 typedef struct {
     void* key;
     void* value;

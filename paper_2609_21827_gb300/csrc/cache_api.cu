@@ -48,11 +48,14 @@ int page_shift(int page_size) {
     return s;
 }
 
-bool kv_ok(const rheo_kv* kv, int es) {
+bool kv_ok(const rheo_kv* kv, const rheo_cache_config& c) {
     if (!kv || !kv->key || !kv->value || !aligned16(kv->key) || !aligned16(kv->value)) return false;
-    for (int64_t s : {kv->key_page, kv->key_head, kv->key_token, kv->value_page, kv->value_head, kv->value_token})
-        if (s * es % 16 != 0) return false;
-    return true;
+    // a dimension of one has no stride
+    const auto fits = [&](int64_t s, int n) {
+        return n == 1 || (s > 0 && s < (int64_t)1 << 38 && s * elem_bytes(c.dtype) % 16 == 0);
+    };
+    return fits(kv->key_page, c.pages) && fits(kv->key_head, c.kv_heads) && fits(kv->key_token, c.page_size) &&
+           fits(kv->value_page, c.pages) && fits(kv->value_head, c.kv_heads) && fits(kv->value_token, c.page_size);
 }
 
 // The status word comes first in every scratch buffer.
@@ -176,7 +179,7 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
                                  int64_t q_out_head, void* scratch, rheo_stream_t stream) {
     if (!valid(cfg) || !in || !in->q || !in->k || !in->v || !slot || !position || !q_out || !scratch) return RHEO_EINVAL;
     const int es = elem_bytes(cfg->dtype);
-    if (!kv_ok(kv, es)) return RHEO_EINVAL;
+    if (!kv_ok(kv, *cfg)) return RHEO_EINVAL;
     if (rot < 0 || rot > cfg->head_dim || rot % 8 != 0 || (rot > 0 && (!cos_sin || max_position < 1))) return RHEO_EINVAL;
     if (!(eps >= 0.0f) || (interleaved != 0 && interleaved != 1)) return RHEO_EINVAL;
     for (const void* p : {in->q, in->k, in->v, q_weight, k_weight, (const void*)cos_sin, (const void*)q_out})
@@ -215,7 +218,7 @@ extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_
                                 const uint8_t* mask, float scale, void* scratch, rheo_stream_t stream) {
     if (!valid(cfg) || !io || !io->q || !io->out || !block_table || !ctx_len || !scratch) return RHEO_EINVAL;
     const int es = elem_bytes(cfg->dtype);
-    if (!kv_ok(kv, es) || !aligned16(io->q) || !aligned16(io->out)) return RHEO_EINVAL;
+    if (!kv_ok(kv, *cfg) || !aligned16(io->q) || !aligned16(io->out)) return RHEO_EINVAL;
     for (int64_t s : {io->q_batch, io->q_token, io->q_head, io->out_batch, io->out_token, io->out_head})
         if (s * es % 16 != 0) return RHEO_EINVAL;
     if (!(scale > -INFINITY && scale < INFINITY)) return RHEO_EINVAL;
@@ -246,7 +249,8 @@ extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_
     a.part_ml = at<float>(scratch, L.part_ml);
     a.join = at<int4>(scratch, L.join);
     a.status = at<unsigned>(scratch, L.status);
-    return code(launch_attend(a, cfg->dtype == RHEO_BF16 ? 1 : 0, (cudaStream_t)stream));
+    const cudaError_t e = launch_attend(a, cfg->dtype == RHEO_BF16 ? 1 : 0, (cudaStream_t)stream);
+    return e == cudaErrorInvalidValue ? RHEO_EINVAL : code(e);  // a cache that no tensor map describes
 }
 
 extern "C" int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, const rheo_kv* kv, int64_t key_layer,
@@ -257,7 +261,7 @@ extern "C" int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, c
         depth < 1 || depth > 128 || !next_len || next_len == ctx_len || !scratch)
         return RHEO_EINVAL;
     const int es = elem_bytes(cfg->dtype);
-    if (!kv_ok(kv, es) || key_layer * es % 16 != 0 || value_layer * es % 16 != 0) return RHEO_EINVAL;
+    if (!kv_ok(kv, *cfg) || key_layer * es % 16 != 0 || value_layer * es % 16 != 0) return RHEO_EINVAL;
     const CacheLayout L = cache_layout(*cfg);
     CommitArgs a{};
     a.B = cfg->batch;

@@ -140,3 +140,11 @@ def test_tensors_on_the_host_are_refused():
     lc = rheo.LogprobConfig(rows=2, vocab=10)
     with pytest.raises(rheo.RheoError):
         rheo.token_logprobs(lc, torch.zeros((2, 10)), torch.zeros(2, dtype=torch.int32), None, None)
+
+
+@pytest.mark.parametrize("kw", [dict(key_head=0), dict(value_page=0), dict(key_token=-64), dict(value_head=2 ** 39)])
+def test_cache_strides_out_of_range_are_rejected(lib, kw):
+    """A head that is broadcast (stride 0), negative strides and strides past the range."""
+    c = rheo.CacheConfig(**BASE)
+    io = rheo._AttendIO(A, A, 0, *[64] * 6)
+    assert lib.rheo_tree_attend(c._ref, ctypes.byref(io), _kv(**kw), A, A, None, None, 0.1, A, None) == rheo.RHEO_EINVAL
