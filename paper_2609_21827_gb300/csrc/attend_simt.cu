@@ -6,6 +6,10 @@
 // log2 units, p = 2^(s - m), O = 2^(m_old - m) O + p V.  Half a warp owns R/16
 // rows, so the row statistics are four shuffles and p passes through shared
 // memory without a block barrier.
+// Four trees of up to 17 tokens over up to 733 places (8 query, 4 key/value heads of
+// 64): 18 us with the join, 0.18 TB/s: bound by dependent latencies (lengths, table, keys, two
+// products, join), as its few bytes come from L2.  The fp32 units, because tf32
+// products would round what an fp32 cache is kept for.
 #include <cuda_bf16.h>
 
 #include <type_traits>
@@ -237,6 +241,9 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
 // Joins the parts of an item that several CTAs summed, in the order of its keys.  A
 // thread takes eight columns of a row; neighbouring threads take neighbouring
 // rows, as the parts lie.  Grid (CTAs of the sums, pieces of 256 threads).
+// A second launch, and not the last CTA of an item, because that one alone would
+// read up to 2.4 MB of sums (61 tokens, 19 parts) at one SM's rate; spread over all SMs
+// they come from L2 in about 3 us.
 template <int DT, int D>
 __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a) {
     grid_dependency_begin();

@@ -10,7 +10,7 @@
 namespace rheo {
 
 // ---------------------------------------------------------------------------
-// reserve.  One launch of up to one CTA per SM.  Every CTA derives the whole
+// reserve.  One launch of up to two CTAs per SM.  Every CTA derives the whole
 // plan itself: pages to give back and to take of all B requests (three ints a
 // request, read from L2), and their exclusive prefix sums in shared memory.
 // From these each request's pages follow without any order between CTAs: the
@@ -20,10 +20,25 @@ namespace rheo {
 // sums and read from that request's row.  Released and taken entries never
 // overlap, so the tables may be updated in place; the counts, which every CTA
 // reads, are written by the last CTA to have read them (a ticket).
-// Latency bound: three dependent rounds of loads, a scan and the stores.
+// Latency bound: three dependent rounds of loads, a scan and the stores.  One
+// request takes less than the 6 us of a call from Python; 256 requests of 129 tokens into new tables take 7.4 us (10.8 with one CTA
+// an SM).
 // ---------------------------------------------------------------------------
 constexpr int kReserveThreads = 256;
 constexpr int kReserveBad = (int)0x80000000u;  // mark of a request that keeps what it holds
+
+// A thread's share of a copy: places at, at + step, ... below `to`, four loads under way.
+__device__ __forceinline__ void copy_ints(int32_t* out, const int32_t* in, int64_t at, int64_t to, int64_t step) {
+    for (; at < to; at += 4 * step) {
+        int32_t x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (at + i * step < to) x[i] = in[at + i * step];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (at + i * step < to) out[at + i * step] = x[i];
+    }
+}
 
 // Inclusive sums of both components over the block.
 __device__ __forceinline__ int2 block_scan_pair(int2 v, int2* warp_sums) {
@@ -131,12 +146,11 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(const ReserveA
         const int take = served ? want : 0;
         const int32_t* in = a.before.block_table + row;
         int32_t* out = a.after.block_table + row;
-        if (a.in_place) {
-            for (int j = own + tid; j < own + take; j += kReserveThreads) out[j] = taken(b, j - own);
-        } else {
-            for (int j = tid; j < a.max_pages; j += kReserveThreads)
-                out[j] = (j >= own && j < own + take) ? taken(b, j - own) : in[j];
+        if (!a.in_place) {
+            copy_ints(out, in, tid, own, kReserveThreads);
+            copy_ints(out, in, own + take + tid, a.max_pages, kReserveThreads);
         }
+        for (int j = own + tid; j < own + take; j += kReserveThreads) out[j] = taken(b, j - own);
         for (int r = tid; r < back; r += kReserveThreads) {
             const int at = free0 + back_at[b] + r;
             if (at < a.pages) a.after.free_list[at] = in[own - back + r];
@@ -160,10 +174,11 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(const ReserveA
             a.position[(int64_t)b * a.T + t] = pos;
         }
     }
-    if (!a.in_place)
-        for (int64_t i = (int64_t)blockIdx.x * kReserveThreads + tid; i < a.pages;
-             i += (int64_t)gridDim.x * kReserveThreads)
-            if (i < free0 || i >= have) a.after.free_list[i] = a.before.free_list[i];
+    if (!a.in_place) {
+        const int64_t at = (int64_t)blockIdx.x * kReserveThreads + tid, step = (int64_t)gridDim.x * kReserveThreads;
+        copy_ints(a.after.free_list, a.before.free_list, at, free0, step);
+        copy_ints(a.after.free_list, a.before.free_list, have + at, a.pages, step);
+    }
 
     if (s_last) {
         // every CTA has its copy of the counts: they may change now
@@ -188,55 +203,64 @@ __global__ void __launch_bounds__(kReserveThreads) reserve_kernel(const ReserveA
 
 cudaError_t launch_reserve(const ReserveArgs& a, int sms, cudaStream_t s) {
     const size_t smem = sizeof(int) * (3 * (size_t)a.B + 2);
-    cudaError_t err =
-        cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(64 * 1024));
-    if (err != cudaSuccess) return err;
-    return launch_dependent(reserve_kernel, dim3(a.B < sms ? a.B : sms), dim3(kReserveThreads), smem, s, a);
+    if (smem > 48 * 1024) {
+        const cudaError_t err = cudaFuncSetAttribute(reserve_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (err != cudaSuccess) return err;
+    }
+    return launch_dependent(reserve_kernel, dim3(a.B < 2 * sms ? a.B : 2 * sms), dim3(kReserveThreads), smem, s, a);
 }
 
 // ---------------------------------------------------------------------------
-// qk_norm_rope.  A warp takes one token and a run of its query heads, its key heads
-// or its value heads.  A lane holds 16 bytes of a head (VEC elements; 8 bytes where
-// the rotated part does not divide into pieces of 16), so 16 lanes hold a bf16 head
-// of 128.  The loads of the run are issued first, before the token's slot and
-// position have come.  With w the weights, c and s the turn, x an element and y its
-// pair, the result is (x (w c) + y (w' s)) / rms(x): the two factors of a lane's
-// elements are made once for the run, the sum of squares is a butterfly over the
-// head's lanes, and the pair is in the same lane (interleaved) or rot / (2 VEC)
-// lanes away (a shuffle of the raw elements).  HBM bound: each input and output
-// element crosses once.
+// qk_norm_rope.  An item is one token and a run of its query heads, its key heads
+// or its value heads; a warp takes items at a stride of all warps of the grid, and
+// has the next one's slot and position on their way while it works on one.  A lane
+// holds 16 bytes of a head (VEC elements; 8 bytes where the rotated part does not
+// divide into pieces of 16), so 16 lanes hold a bf16 head of 128.  The loads of a
+// run are issued first.  With w the weights, c and s the turn, x an element and y its
+// pair, the result is (x (w c) + y (w' s)) / rms(x), in packed fp32 arithmetic: the
+// two factors of a lane's elements are made once for the run, the sum of squares is
+// a butterfly over the head's lanes, and the pair is in the same lane (interleaved) or
+// rot / (2 VEC) lanes away (a shuffle of the raw elements).
+// HBM bound: each input and output element crosses once.  33,024 tokens of 32 query
+// and 8 key/value heads of 128 in bf16 take 140 us, 5.8 TB/s; what counts is bytes under way: 153, 149
+// and 155 us with 8 (spills), 6 and 5 CTAs an SM; one item a warp 154; runs of 16
+// heads with the next loads under way 158 to 185 (fewer warps); two loads a lane 176.
 // ---------------------------------------------------------------------------
 constexpr int kRopeThreads = 128;
+constexpr int kRopeCtas = 7;  // resident on an SM
+
+using F2 = unsigned long long;  // two floats for the packed fp32 instructions
+__device__ __forceinline__ float f2_lo(F2 x) { return __uint_as_float((uint32_t)x); }
+__device__ __forceinline__ float f2_hi(F2 x) { return __uint_as_float((uint32_t)(x >> 32)); }
+__device__ __forceinline__ F2 f2_swap(F2 x) { return f2_pack(f2_hi(x), f2_lo(x)); }
 
 template <int DT, int VEC> struct Piece;  // VEC neighbouring elements
 template <> struct Piece<0, 4> {
     using Raw = float4;
-    __device__ static __forceinline__ void wide(float4 r, float (&x)[4]) { x[0] = r.x, x[1] = r.y, x[2] = r.z, x[3] = r.w; }
-    __device__ static __forceinline__ float4 narrow(const float (&x)[4]) { return make_float4(x[0], x[1], x[2], x[3]); }
+    __device__ static __forceinline__ void wide(float4 r, F2 (&x)[2]) { x[0] = f2_pack(r.x, r.y), x[1] = f2_pack(r.z, r.w); }
+    __device__ static __forceinline__ float4 narrow(const F2 (&x)[2]) {
+        return make_float4(f2_lo(x[0]), f2_hi(x[0]), f2_lo(x[1]), f2_hi(x[1]));
+    }
     __device__ static __forceinline__ float4 zero() { return make_float4(0, 0, 0, 0); }
 };
-__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&x);
+__device__ __forceinline__ F2 bf16_wide(uint32_t x) { return f2_pack(bf_lo(x), bf_hi(x)); }
+__device__ __forceinline__ uint32_t bf16_narrow(F2 x) {
+    const __nv_bfloat162 y = __floats2bfloat162_rn(f2_lo(x), f2_hi(x));
+    return *reinterpret_cast<const uint32_t*>(&y);
 }
 template <> struct Piece<1, 4> {
     using Raw = uint2;
-    __device__ static __forceinline__ void wide(uint2 r, float (&x)[4]) {
-        x[0] = bf_lo(r.x), x[1] = bf_hi(r.x), x[2] = bf_lo(r.y), x[3] = bf_hi(r.y);
-    }
-    __device__ static __forceinline__ uint2 narrow(const float (&x)[4]) {
-        return make_uint2(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]));
-    }
+    __device__ static __forceinline__ void wide(uint2 r, F2 (&x)[2]) { x[0] = bf16_wide(r.x), x[1] = bf16_wide(r.y); }
+    __device__ static __forceinline__ uint2 narrow(const F2 (&x)[2]) { return make_uint2(bf16_narrow(x[0]), bf16_narrow(x[1])); }
     __device__ static __forceinline__ uint2 zero() { return make_uint2(0, 0); }
 };
 template <> struct Piece<1, 8> {
     using Raw = uint4;
-    __device__ static __forceinline__ void wide(uint4 r, float (&x)[8]) {
-        x[0] = bf_lo(r.x), x[1] = bf_hi(r.x), x[2] = bf_lo(r.y), x[3] = bf_hi(r.y);
-        x[4] = bf_lo(r.z), x[5] = bf_hi(r.z), x[6] = bf_lo(r.w), x[7] = bf_hi(r.w);
+    __device__ static __forceinline__ void wide(uint4 r, F2 (&x)[4]) {
+        x[0] = bf16_wide(r.x), x[1] = bf16_wide(r.y), x[2] = bf16_wide(r.z), x[3] = bf16_wide(r.w);
     }
-    __device__ static __forceinline__ uint4 narrow(const float (&x)[8]) {
-        return make_uint4(bf16_pair(x[0], x[1]), bf16_pair(x[2], x[3]), bf16_pair(x[4], x[5]), bf16_pair(x[6], x[7]));
+    __device__ static __forceinline__ uint4 narrow(const F2 (&x)[4]) {
+        return make_uint4(bf16_narrow(x[0]), bf16_narrow(x[1]), bf16_narrow(x[2]), bf16_narrow(x[3]));
     }
     __device__ static __forceinline__ uint4 zero() { return make_uint4(0, 0, 0, 0); }
 };
@@ -255,7 +279,7 @@ __device__ __forceinline__ float4 shfl_raw(float4 x, int from) {
 }
 
 template <int DT, int D, int VEC, bool INTERLEAVED>
-__global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
+__global__ void __launch_bounds__(kRopeThreads, kRopeCtas) rope_kernel(const RopeArgs a) {
     grid_dependency_begin();
     using Q = Piece<DT, VEC>;
     using Raw = typename Q::Raw;
@@ -263,136 +287,159 @@ __global__ void __launch_bounds__(kRopeThreads) rope_kernel(const RopeArgs a) {
     constexpr int ES = DT == 1 ? 2 : 4;
     const int lane = threadIdx.x & 31, ci = lane & (LPH - 1), sub = lane / LPH, e = ci * VEC;
     const int q_runs = (a.Hq + HEADS - 1) / HEADS, kv_runs = (a.H + HEADS - 1) / HEADS, runs = q_runs + 2 * kv_runs;
+
+    // items (token, run) at a stride of all warps, advanced without a division
     const int64_t item = (int64_t)blockIdx.x * (kRopeThreads / 32) + (threadIdx.x >> 5);
-    const int64_t token = item / runs;
-    if (token >= a.tokens) return;
-    int run = (int)(item - token * runs);
-    const int64_t b = token / a.T, t = token - b * a.T;
-    const int64_t slot = a.slot[token];
-    const int pos = a.position[token];
-
-    // which: 0 queries, 1 keys, 2 values; the same for the whole warp
-    const int which = run < q_runs ? 0 : run < q_runs + kv_runs ? 1 : 2;
-    if (which == 1) run -= q_runs;
-    if (which == 2) run -= q_runs + kv_runs;
-    const int h0 = run * HEADS + sub, heads = which == 0 ? a.Hq : a.H;
-    const char* in = static_cast<const char*>(which == 0 ? a.in.q : which == 1 ? a.in.k : a.in.v);
-    const int64_t in_batch = which == 0 ? a.in.q_batch : which == 1 ? a.in.k_batch : a.in.v_batch;
-    const int64_t in_token = which == 0 ? a.in.q_token : which == 1 ? a.in.k_token : a.in.v_token;
-    const int64_t in_head = which == 0 ? a.in.q_head : which == 1 ? a.in.k_head : a.in.v_head;
-    in += (b * in_batch + t * in_token + h0 * in_head + e) * ES;
-    Raw raw[kRopeRounds];
-#pragma unroll
-    for (int r = 0; r < kRopeRounds; ++r)
-        raw[r] = h0 + r * HPW < heads ? *reinterpret_cast<const Raw*>(in + r * HPW * in_head * ES) : Q::zero();
-
-    const bool inside = slot < a.slots && (a.rot == 0 || (pos >= 0 && pos < a.max_position));
-    if (slot >= 0 && !inside && lane == 0) atomicOr(a.status, kStBadIndex);
-    const bool live = slot >= 0 && inside;
-    char* out;
-    int64_t out_head;
-    if (which == 0) {
-        out = static_cast<char*>(a.q_out) + (b * a.o_batch + t * a.o_token) * ES;
-        out_head = a.o_head;
-    } else {
-        if (!live) return;
-        const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
-        out = static_cast<char*>(which == 1 ? a.kv.key : a.kv.value) +
-              (page * (which == 1 ? a.kv.key_page : a.kv.value_page) + row * (which == 1 ? a.kv.key_token : a.kv.value_token)) * ES;
-        out_head = which == 1 ? a.kv.key_head : a.kv.value_head;
+    const int64_t stride = (int64_t)gridDim.x * (kRopeThreads / 32), skip = stride / runs;
+    const int skip_run = (int)(stride - skip * runs), skip_t = (int)(skip % a.T), skip_b = (int)(skip / a.T);
+    const int64_t first_token = item / runs;
+    int at = (int)(item - first_token * runs), t = (int)(first_token % a.T), b = (int)(first_token / a.T);
+    int64_t slot_ahead = -1;
+    int pos_ahead = 0;
+    if (b < a.B) {
+        slot_ahead = a.slot[first_token];
+        pos_ahead = a.position[first_token];
     }
-    out += (h0 * out_head + e) * ES;
-    if (which == 2 || !live) {
+    while (b < a.B) {
+        const int64_t slot = slot_ahead;
+        const int pos = pos_ahead;
+        // which: 0 queries, 1 keys, 2 values; the same for the whole warp
+        const int which = at < q_runs ? 0 : at < q_runs + kv_runs ? 1 : 2;
+        const int run = which == 0 ? at : which == 1 ? at - q_runs : at - q_runs - kv_runs;
+        const int h0 = run * HEADS + sub, heads = which == 0 ? a.Hq : a.H;
+        const char* in = static_cast<const char*>(which == 0 ? a.in.q : which == 1 ? a.in.k : a.in.v);
+        const int64_t in_batch = which == 0 ? a.in.q_batch : which == 1 ? a.in.k_batch : a.in.v_batch;
+        const int64_t in_token = which == 0 ? a.in.q_token : which == 1 ? a.in.k_token : a.in.v_token;
+        const int64_t in_head = which == 0 ? a.in.q_head : which == 1 ? a.in.k_head : a.in.v_head;
+        in += (b * in_batch + t * in_token + h0 * in_head + e) * ES;
+        Raw raw[kRopeRounds];
 #pragma unroll
         for (int r = 0; r < kRopeRounds; ++r)
-            if (h0 + r * HPW < heads) *reinterpret_cast<Raw*>(out + r * HPW * out_head * ES) = live ? raw[r] : Q::zero();
-        return;
-    }
+            raw[r] = h0 + r * HPW < heads ? *reinterpret_cast<const Raw*>(in + r * HPW * in_head * ES) : Q::zero();
+        char* const q_out = static_cast<char*>(a.q_out) + (b * a.o_batch + t * a.o_token) * ES;
 
-    // factors of an element and of its pair
-    const char* weight = static_cast<const char*>(which == 0 ? a.q_weight : a.k_weight);
-    float fx[VEC], fy[VEC];
-    int pair = lane;  // the lane that holds the pairs of this lane's elements
+        at += skip_run;
+        const int carry = at >= runs;
+        if (carry) at -= runs;
+        t += skip_t + carry;
+        b += skip_b;
+        if (t >= a.T) t -= a.T, ++b;
+        if (b < a.B) {
+            const int64_t token = (int64_t)b * a.T + t;
+            slot_ahead = a.slot[token];
+            pos_ahead = a.position[token];
+        }
+
+        const bool inside = slot < a.slots && (a.rot == 0 || (pos >= 0 && pos < a.max_position));
+        if (slot >= 0 && !inside && lane == 0) atomicOr(a.status, kStBadIndex);
+        const bool live = slot >= 0 && inside;
+        char* out = q_out;
+        int64_t out_head = a.o_head;
+        if (which != 0) {
+            if (!live) continue;
+            const int64_t page = slot >> a.page_shift, row = slot & ((1 << a.page_shift) - 1);
+            out = static_cast<char*>(which == 1 ? a.kv.key : a.kv.value) +
+                  (page * (which == 1 ? a.kv.key_page : a.kv.value_page) +
+                   row * (which == 1 ? a.kv.key_token : a.kv.value_token)) * ES;
+            out_head = which == 1 ? a.kv.key_head : a.kv.value_head;
+        }
+        out += (h0 * out_head + e) * ES;
+        if (which == 2 || !live) {
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) fx[i] = 1.0f, fy[i] = 0.0f;
-    const bool turns = e < a.rot;
-    if (weight) Q::wide(*reinterpret_cast<const Raw*>(weight + e * ES), fx);
-    if (turns) {
-        const float* cs = a.cos_sin + (int64_t)pos * a.rot;
-        if (INTERLEAVED) {
+            for (int r = 0; r < kRopeRounds; ++r)
+                if (h0 + r * HPW < heads) *reinterpret_cast<Raw*>(out + r * HPW * out_head * ES) = live ? raw[r] : Q::zero();
+            continue;
+        }
+
+        // factors of an element and of its pair
+        const char* weight = static_cast<const char*>(which == 0 ? a.q_weight : a.k_weight);
+        F2 fx[VEC / 2], fy[VEC / 2];
+        int pair = lane;  // the lane that holds the pairs of this lane's elements
 #pragma unroll
-            for (int i = 0; i < VEC; i += 4) {
-                const float2 c2 = *reinterpret_cast<const float2*>(cs + (e + i) / 2);
-                const float2 s2 = *reinterpret_cast<const float2*>(cs + a.rot / 2 + (e + i) / 2);
-                fy[i] = -s2.x * fx[i + 1], fy[i + 1] = s2.x * fx[i];
-                fy[i + 2] = -s2.y * fx[i + 3], fy[i + 3] = s2.y * fx[i + 2];
-                fx[i] *= c2.x, fx[i + 1] *= c2.x, fx[i + 2] *= c2.y, fx[i + 3] *= c2.y;
+        for (int i = 0; i < VEC / 2; ++i) fx[i] = f2_pack(1.0f, 1.0f), fy[i] = 0ull;
+        const bool turns = e < a.rot;
+        if (weight) Q::wide(*reinterpret_cast<const Raw*>(weight + e * ES), fx);
+        if (turns) {
+            const float* cs = a.cos_sin + (int64_t)pos * a.rot;
+            if (INTERLEAVED) {
+#pragma unroll
+                for (int i = 0; i < VEC / 2; i += 2) {
+                    const float2 c2 = *reinterpret_cast<const float2*>(cs + e / 2 + i);
+                    const float2 s2 = *reinterpret_cast<const float2*>(cs + a.rot / 2 + e / 2 + i);
+                    fy[i] = f2_mul(f2_pack(-s2.x, s2.x), f2_swap(fx[i]));
+                    fy[i + 1] = f2_mul(f2_pack(-s2.y, s2.y), f2_swap(fx[i + 1]));
+                    fx[i] = f2_mul(fx[i], f2_pack(c2.x, c2.x));
+                    fx[i + 1] = f2_mul(fx[i + 1], f2_pack(c2.y, c2.y));
+                }
+            } else {
+                const bool first = e < a.rot / 2;
+                const int from = first ? e : e - a.rot / 2;
+                const float sign = first ? -1.0f : 1.0f;
+                F2 w[VEC / 2];
+#pragma unroll
+                for (int i = 0; i < VEC / 2; ++i) w[i] = f2_pack(1.0f, 1.0f);
+                if (weight) Q::wide(*reinterpret_cast<const Raw*>(weight + (first ? e + a.rot / 2 : from) * ES), w);
+#pragma unroll
+                for (int i = 0; i < VEC / 2; i += 2) {
+                    const float4 c4 = *reinterpret_cast<const float4*>(cs + from + 2 * i);
+                    const float4 s4 = *reinterpret_cast<const float4*>(cs + a.rot / 2 + from + 2 * i);
+                    fx[i] = f2_mul(fx[i], f2_pack(c4.x, c4.y)), fx[i + 1] = f2_mul(fx[i + 1], f2_pack(c4.z, c4.w));
+                    fy[i] = f2_mul(f2_pack(sign * s4.x, sign * s4.y), w[i]);
+                    fy[i + 1] = f2_mul(f2_pack(sign * s4.z, sign * s4.w), w[i + 1]);
+                }
+                pair = first ? lane + a.rot / (2 * VEC) : lane - a.rot / (2 * VEC);
             }
-        } else {
-            const bool first = e < a.rot / 2;
-            const int at = first ? e : e - a.rot / 2;
-            const float sign = first ? -1.0f : 1.0f;
-            float w[VEC];
+        }
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) w[i] = 1.0f;
-            if (weight) Q::wide(*reinterpret_cast<const Raw*>(weight + (first ? e + a.rot / 2 : at) * ES), w);
+        for (int r = 0; r < kRopeRounds; ++r) {
+            if (h0 - sub + r * HPW >= heads) break;  // the same for the whole warp
+            F2 x[VEC / 2], y[VEC / 2];
+            Q::wide(raw[r], x);
+            // what does not turn has no pair: zeros, as 0 * inf is none of it
+            if (INTERLEAVED) {
 #pragma unroll
-            for (int i = 0; i < VEC; i += 4) {
-                const float4 c4 = *reinterpret_cast<const float4*>(cs + at + i);
-                const float4 s4 = *reinterpret_cast<const float4*>(cs + a.rot / 2 + at + i);
-                fx[i] *= c4.x, fx[i + 1] *= c4.y, fx[i + 2] *= c4.z, fx[i + 3] *= c4.w;
-                fy[i] = sign * s4.x * w[i], fy[i + 1] = sign * s4.y * w[i + 1];
-                fy[i + 2] = sign * s4.z * w[i + 2], fy[i + 3] = sign * s4.w * w[i + 3];
+                for (int i = 0; i < VEC / 2; ++i) y[i] = turns ? f2_swap(x[i]) : 0ull;
+            } else {
+                const Raw other = shfl_raw(raw[r], pair);
+                Q::wide(turns ? other : Q::zero(), y);
             }
-            pair = first ? lane + a.rot / (2 * VEC) : lane - a.rot / (2 * VEC);
+            F2 inv = f2_pack(1.0f, 1.0f);
+            if (weight) {
+                F2 squares = f2_mul(x[0], x[0]);
+#pragma unroll
+                for (int i = 1; i < VEC / 2; ++i) squares = f2_fma(x[i], x[i], squares);
+                float ss = f2_fold(squares);
+#pragma unroll
+                for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+                ss = rsqrtf(ss * (1.0f / D) + a.eps);
+                inv = f2_pack(ss, ss);
+            }
+#pragma unroll
+            for (int i = 0; i < VEC / 2; ++i) x[i] = f2_mul(f2_fma(y[i], fy[i], f2_mul(x[i], fx[i])), inv);
+            if (h0 + r * HPW < heads) *reinterpret_cast<Raw*>(out + r * HPW * out_head * ES) = Q::narrow(x);
         }
-    }
-#pragma unroll
-    for (int r = 0; r < kRopeRounds; ++r) {
-        if (h0 - sub + r * HPW >= heads) break;  // the same for the whole warp
-        float x[VEC], y[VEC];
-        Q::wide(raw[r], x);
-        if (INTERLEAVED) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) y[i] = x[i ^ 1];
-        } else {
-            Q::wide(shfl_raw(raw[r], pair), y);
-        }
-        float inv = 1.0f;
-        if (weight) {
-            float ss = 0.0f;
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) ss = fmaf(x[i], x[i], ss);
-#pragma unroll
-            for (int o = LPH / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-            inv = rsqrtf(ss * (1.0f / D) + a.eps);
-        }
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            const float z = x[i] * fx[i];
-            x[i] = (turns ? fmaf(y[i], fy[i], z) : z) * inv;  // (what does not turn has no pair: 0 * inf is none of it)
-        }
-        if (h0 + r * HPW < heads) *reinterpret_cast<Raw*>(out + r * HPW * out_head * ES) = Q::narrow(x);
     }
 }
 
 template <int DT, int D, int VEC, bool I>
-static cudaError_t launch_rope_t(const RopeArgs& a, cudaStream_t s) {
+static cudaError_t launch_rope_t(const RopeArgs& a, int sms, cudaStream_t s) {
     constexpr int heads = rope_heads<D, VEC>();
     const int runs = (a.Hq + heads - 1) / heads + 2 * ((a.H + heads - 1) / heads);
-    const int64_t warps = a.tokens * runs, per = kRopeThreads / 32;
-    return launch_dependent(rope_kernel<DT, D, VEC, I>, dim3((unsigned)((warps + per - 1) / per)), dim3(kRopeThreads), 0, s,
-                            a);
+    const int64_t per = kRopeThreads / 32, ctas = ((int64_t)a.B * a.T * runs + per - 1) / per, most = (int64_t)sms * kRopeCtas;
+    return launch_dependent(rope_kernel<DT, D, VEC, I>, dim3((unsigned)(ctas < most ? ctas : most)), dim3(kRopeThreads), 0,
+                            s, a);
 }
-template <int DT, int D, int VEC> static cudaError_t launch_rope_i(const RopeArgs& a, bool interleaved, cudaStream_t s) {
-    return interleaved ? launch_rope_t<DT, D, VEC, true>(a, s) : launch_rope_t<DT, D, VEC, false>(a, s);
+template <int DT, int D, int VEC>
+static cudaError_t launch_rope_i(const RopeArgs& a, bool interleaved, int sms, cudaStream_t s) {
+    return interleaved ? launch_rope_t<DT, D, VEC, true>(a, sms, s) : launch_rope_t<DT, D, VEC, false>(a, sms, s);
 }
 
-cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, cudaStream_t s) {
-    if (dtype == 0) return D == 128 ? launch_rope_i<0, 128, 4>(a, interleaved, s) : launch_rope_i<0, 64, 4>(a, interleaved, s);
+cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, int sms, cudaStream_t s) {
+    const bool wide = D == 128;
+    if (dtype == 0) return wide ? launch_rope_i<0, 128, 4>(a, interleaved, sms, s) : launch_rope_i<0, 64, 4>(a, interleaved, sms, s);
     if (a.rot % 16 == 0)
-        return D == 128 ? launch_rope_i<1, 128, 8>(a, interleaved, s) : launch_rope_i<1, 64, 8>(a, interleaved, s);
-    return D == 128 ? launch_rope_i<1, 128, 4>(a, interleaved, s) : launch_rope_i<1, 64, 4>(a, interleaved, s);
+        return wide ? launch_rope_i<1, 128, 8>(a, interleaved, sms, s) : launch_rope_i<1, 64, 8>(a, interleaved, sms, s);
+    return wide ? launch_rope_i<1, 128, 4>(a, interleaved, sms, s) : launch_rope_i<1, 64, 4>(a, interleaved, sms, s);
 }
 
 // ---------------------------------------------------------------------------
@@ -401,7 +448,8 @@ cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, c
 // order and node k lies at or behind place k+1, so a batch of loads followed by
 // its stores never overwrites a line that a later batch reads.  Lines already
 // in place are left alone.  The bytes are few: bound by launch and by two
-// dependent rounds of loads (path, table), then HBM.
+// dependent rounds of loads (path, table), then HBM.  A path of six in 32 layers,
+// and 64 paths in 16 layers (25 MB): under 9 us each from Python, which the call bounds.
 // ---------------------------------------------------------------------------
 constexpr int kCommitThreads = 256;
 constexpr int kCommitBatch = 8;

@@ -189,7 +189,7 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
         if (s * es % 16 != 0) return RHEO_EINVAL;
     const CacheLayout L = cache_layout(*cfg);
     RopeArgs a{};
-    a.tokens = (int64_t)cfg->batch * cfg->tokens;
+    a.B = cfg->batch;
     a.T = cfg->tokens;
     a.Hq = cfg->q_heads;
     a.H = cfg->kv_heads;
@@ -210,7 +210,8 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
     a.o_token = q_out_token;
     a.o_head = q_out_head;
     a.status = at<unsigned>(scratch, L.status);
-    return code(launch_rope(a, cfg->dtype == RHEO_BF16 ? 1 : 0, cfg->head_dim, interleaved != 0, (cudaStream_t)stream));
+    return code(launch_rope(a, cfg->dtype == RHEO_BF16 ? 1 : 0, cfg->head_dim, interleaved != 0, multiprocessors(),
+                            (cudaStream_t)stream));
 }
 
 extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, const rheo_kv* kv,

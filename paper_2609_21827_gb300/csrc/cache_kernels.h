@@ -27,8 +27,7 @@ struct ReserveArgs {
 };
 
 struct RopeArgs {
-    int64_t tokens;           // B * T
-    int T, Hq, H, rot, max_position, page_shift;
+    int B, T, Hq, H, rot, max_position, page_shift;
     int64_t slots;            // pages * page_size
     rheo_qkv in;
     const void* q_weight;
@@ -90,7 +89,7 @@ struct LogprobArgs {
 };
 
 cudaError_t launch_reserve(const ReserveArgs& a, int sms, cudaStream_t s);
-cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, cudaStream_t s);
+cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, int sms, cudaStream_t s);
 cudaError_t launch_commit(const CommitArgs& a, int line_bytes, cudaStream_t s);
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s);

@@ -529,7 +529,7 @@ def _want_strided(x: torch.Tensor, name: str, dtype, shape) -> tuple:
 
 
 class _Buffers:
-    """Tensors whose checked pointers are kept until one of them is replaced."""
+    """Tensors that are checked again when one of them is replaced or has moved."""
 
     _held = None
 
@@ -537,8 +537,8 @@ class _Buffers:
         object.__setattr__(self, name, value)
         object.__setattr__(self, "_held", None)
 
-    def _keep(self, cfg, made):
-        object.__setattr__(self, "_held", (cfg, made))
+    def _keep(self, cfg, at, made):
+        object.__setattr__(self, "_held", (cfg, at, made))
         return made
 
 
@@ -560,13 +560,14 @@ class Pages(_Buffers):
 
     def c(self, cfg: CacheConfig) -> _Pages:
         held = self._held
-        if held is not None and held[0] is cfg:
-            return held[1]
+        at = (self.block_table.data_ptr(), self.n_pages.data_ptr(), self.free_list.data_ptr(), self.n_free.data_ptr())
+        if held is not None and held[0] is cfg and held[1] == at:
+            return held[2]
         i32 = torch.int32
-        return self._keep(cfg, _Pages(_want(self.block_table, "block_table", i32, cfg._table),
-                                      _want(self.n_pages, "n_pages", i32, cfg._one),
-                                      _want(self.free_list, "free_list", i32, (cfg.pages,)),
-                                      _want(self.n_free, "n_free", i32, (1,))))
+        return self._keep(cfg, at, _Pages(_want(self.block_table, "block_table", i32, cfg._table),
+                                          _want(self.n_pages, "n_pages", i32, cfg._one),
+                                          _want(self.free_list, "free_list", i32, (cfg.pages,)),
+                                          _want(self.n_free, "n_free", i32, (1,))))
 
 
 class CachePlan(_Buffers):
@@ -579,10 +580,12 @@ class CachePlan(_Buffers):
 
     def ptrs(self, cfg: CacheConfig) -> tuple:
         held = self._held
-        if held is not None and held[0] is cfg:
-            return held[1]
-        return self._keep(cfg, (_want(self.slot, "slot", torch.int64, cfg._each),
-                                _want(self.position, "position", torch.int32, cfg._each)))
+        at = (self.slot.data_ptr(), self.position.data_ptr())
+        if held is not None and held[0] is cfg and held[1] == at:
+            return at
+        _want(self.slot, "slot", torch.int64, cfg._each)
+        _want(self.position, "position", torch.int32, cfg._each)
+        return self._keep(cfg, at, at)
 
 
 def make_cache(cfg: CacheConfig, layers: int = 1, device="cuda"):
@@ -622,7 +625,7 @@ def qk_norm_rope(cfg: CacheConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     qp, qs = _want_strided(q, "q", dt, cfg._q)
     kp, ks = _want_strided(k, "k", dt, cfg._k)
     vp, vs = _want_strided(v, "v", dt, cfg._k)
-    op, os_ = _want_strided(q_out, "q_out", dt, cfg._q)
+    op, os_ = (qp, qs) if q_out is q else _want_strided(q_out, "q_out", dt, cfg._q)
     if op == qp and os_ != qs:
         raise RheoError("q_out on q's memory needs q's strides")
     most = rot = table = 0
@@ -688,10 +691,12 @@ class Logprobs(_Buffers):
 
     def c(self, cfg: LogprobConfig) -> _Logprobs:
         held = self._held
-        if held is not None and held[0] is cfg:
-            return held[1]
+        at = (self.logprob.data_ptr(), self.rank.data_ptr(), self.entropy.data_ptr(), self.top_ids.data_ptr(),
+              self.top_logprobs.data_ptr())
+        if held is not None and held[0] is cfg and held[1] == at:
+            return held[2]
         R, k, f32, i32 = cfg.rows, cfg.top, torch.float32, torch.int32
-        return self._keep(cfg, _Logprobs(
+        return self._keep(cfg, at, _Logprobs(
             _want(self.logprob, "logprob", f32, (R,)), _want(self.rank, "rank", i32, (R,)),
             _want(self.entropy, "entropy", f32, (R,)), _want(self.top_ids, "top_ids", i32, (R, k)),
             _want(self.top_logprobs, "top_logprobs", f32, (R, k))))

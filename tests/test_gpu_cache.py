@@ -119,6 +119,23 @@ def test_reserve_from_an_empty_pool_cycle_by_cycle():
         ctx = [min(c + (1 + (cycle + b) % 4 if new[b] else 0), 120) for b, c in enumerate(ctx)]
 
 
+def test_tables_that_have_moved_are_found_again():
+    """Storage exchanged under a tensor that an earlier call has seen."""
+    cfg = _cfg(batch=1, tokens=4, pages=8, max_pages=4)
+    pages, plan, ws = rheo.Pages(cfg), rheo.CachePlan(cfg), rheo.CacheWorkspace(cfg)
+    rheo.cache_reserve(cfg, _i32([0]), pages, plan, ws)
+    old, other = pages.block_table.clone(), torch.full((1, 4), 5, dtype=torch.int32, device="cuda")
+    kept = pages.block_table.untyped_storage()  # not freed, so that the new one lies elsewhere
+    pages.block_table.data = other
+    plan.slot.data = torch.zeros_like(plan.slot)
+    rheo.cache_reserve(cfg, _i32([4]), pages, plan, ws)
+    assert plan.slot.tolist() == [[5 * 16 + 4 + t for t in range(4)]] and old.tolist() != other.tolist()
+    pages.block_table.data = torch.zeros((1, 3), dtype=torch.int32, device="cuda")
+    with pytest.raises(rheo.RheoError):
+        rheo.cache_reserve(cfg, _i32([4]), pages, plan, ws)
+    assert kept.nbytes() and rheo.scratch_status(ws) == 0
+
+
 # ---------------------------------------------------------------- qk_norm_rope
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
