@@ -7,7 +7,7 @@
 // rows, so the row statistics are four shuffles and p passes through shared
 // memory without a block barrier.
 // Four trees of up to 17 tokens over up to 733 places (8 query, 4 key/value heads of
-// 64): 18 us with the join, 0.18 TB/s: bound by dependent latencies (lengths, table, keys, two
+// 64): 15.8 us with the join, 0.2 TB/s: bound by dependent latencies (lengths, table, keys, two
 // products, join), as its few bytes come from L2.  The fp32 units, because tf32
 // products would round what an fp32 cache is kept for.
 #include <cuda_bf16.h>
@@ -241,9 +241,14 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
 // Joins the parts of an item that several CTAs summed, in the order of its keys.  A
 // thread takes eight columns of a row; neighbouring threads take neighbouring
 // rows, as the parts lie.  Grid (CTAs of the sums, pieces of 256 threads).
-// A second launch, and not the last CTA of an item, because that one alone would
-// read up to 2.4 MB of sums (61 tokens, 19 parts) at one SM's rate; spread over all SMs
-// they come from L2 in about 3 us.
+// One pass: the parts' references are not known beforehand, so the sums follow the
+// largest so far, four parts at a time.
+// A second launch, although it costs 2 to 3 us: the last warp to add a part (a ticket an
+// item) joining its rows was slower even where they are few (17.0 us for 15.8 with four short fp32
+// trees, 23.2 for 19.9 with one token over 16,000), as what one warp reads
+// is on its way for longer, and the last CTA alone would read up to 2.4 MB.
+constexpr int kJoinBatch = 4;  // parts under way
+
 template <int DT, int D>
 __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a) {
     grid_dependency_begin();
@@ -255,30 +260,43 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const AttendArgs a) {
     const int h = rec.y / groups, row = rec.y % groups * a.item_rows + r;
     if (row >= rows) return;
     const int t = row / a.G, head = h * a.G + row % a.G;
-    const auto ml = [&](int s) {
-        return *reinterpret_cast<const float2*>(a.part_ml + (attend_part(blockIdx.x + s, s == 0) * a.part_rows + r) * 2);
-    };
-    float m = -INFINITY;
-#pragma unroll 8
-    for (int s = 0; s < segments; ++s) m = fmaxf(m, ml(s).x);
-    const float ref = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll 4
-    for (int s = 0; s < segments; ++s) {
-        const float2 y = ml(s);
-        const float w = fast_exp2(y.x - ref);
-        const float4* po = reinterpret_cast<const float4*>(a.part_o) +
-                           attend_part_at(a, attend_part(blockIdx.x + s, s == 0), r, 2 * c8);
-        const float4 u = po[0], v = po[a.part_rows];
-        l += w * y.y;
-        x[0] += w * u.x;
-        x[1] += w * u.y;
-        x[2] += w * u.z;
-        x[3] += w * u.w;
-        x[4] += w * v.x;
-        x[5] += w * v.y;
-        x[6] += w * v.z;
-        x[7] += w * v.w;
+    float m = -INFINITY, l = 0.0f, x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    for (int s0 = 0; s0 < segments; s0 += kJoinBatch) {
+        float2 ml[kJoinBatch];
+        float4 u[kJoinBatch], v[kJoinBatch];
+#pragma unroll
+        for (int k = 0; k < kJoinBatch; ++k) {
+            ml[k] = make_float2(-INFINITY, 0.0f);
+            u[k] = v[k] = make_float4(0, 0, 0, 0);
+            if (s0 + k < segments) {
+                const int64_t part = attend_part(blockIdx.x + s0 + k, s0 + k == 0);
+                const float4* po = reinterpret_cast<const float4*>(a.part_o) + attend_part_at(a, part, r, 2 * c8);
+                ml[k] = *reinterpret_cast<const float2*>(a.part_ml + (part * a.part_rows + r) * 2);
+                u[k] = po[0];
+                v[k] = po[a.part_rows];
+            }
+        }
+        float top = m;
+#pragma unroll
+        for (int k = 0; k < kJoinBatch; ++k) top = fmaxf(top, ml[k].x);
+        const float ref = top == -INFINITY ? 0.0f : top, f = fast_exp2(m - ref);
+        m = top;
+        l *= f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] *= f;
+#pragma unroll
+        for (int k = 0; k < kJoinBatch; ++k) {
+            const float w = fast_exp2(ml[k].x - ref);
+            l += w * ml[k].y;
+            x[0] += w * u[k].x;
+            x[1] += w * u[k].y;
+            x[2] += w * u[k].z;
+            x[3] += w * u[k].w;
+            x[4] += w * v[k].x;
+            x[5] += w * v[k].y;
+            x[6] += w * v[k].z;
+            x[7] += w * v[k].w;
+        }
     }
     const float inv = 1.0f / l;
 #pragma unroll

@@ -145,13 +145,14 @@ def lib():
 
 # The current stream's handle without a Stream object (3 us less a call), where this build of torch has it.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
     if _raw_stream is not None:
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_device())
     return torch.cuda.current_stream().cuda_stream
 
 
