@@ -20,9 +20,9 @@ namespace rheo {
 // sums and read from that request's row.  Released and taken entries never
 // overlap, so the tables may be updated in place; the counts, which every CTA
 // reads, are written by the last CTA to have read them (a ticket).
-// Latency bound: three dependent rounds of loads, a scan and the stores.  One
-// request takes less than the 6 us of a call from Python; 256 requests of 129 tokens into new tables take 7.4 us (10.8 with one CTA
-// an SM).
+// Latency bound: three dependent rounds of loads, a scan and the stores.  256
+// requests of 129 tokens into new tables take 6.6 us from Python, which the call
+// bounds as it does for one request (10.3 with one CTA an SM and a load at a time).
 // ---------------------------------------------------------------------------
 constexpr int kReserveThreads = 256;
 constexpr int kReserveBad = (int)0x80000000u;  // mark of a request that keeps what it holds
