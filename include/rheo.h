@@ -340,7 +340,8 @@ int rheo_cache_reserve(const rheo_cache_config* cfg, const int32_t* ctx_len, con
 
 /* Queries, keys and values of the B*T new tokens of one layer; strides in
  * elements (token: from t to t+1, batch: from b to b+1), D contiguous.
- * Pointers and strides (in bytes) are multiples of 16. */
+ * Pointers and strides (in bytes) are multiples of 16; here and in
+ * rheo_tree_attend the stride of a dimension of one is not looked at. */
 typedef struct {
     const void* q;
     const void* k;

@@ -58,6 +58,13 @@ bool kv_ok(const rheo_kv* kv, const rheo_cache_config& c) {
            fits(kv->value_page, c.pages) && fits(kv->value_head, c.kv_heads) && fits(kv->value_token, c.page_size);
 }
 
+// Strides [batch][token][head] of queries, keys, values or outputs.
+bool rows_ok(const rheo_cache_config& c, int64_t batch, int64_t token, int64_t head, int heads) {
+    const int es = elem_bytes(c.dtype);
+    return (c.batch == 1 || batch * es % 16 == 0) && (c.tokens == 1 || token * es % 16 == 0) &&
+           (heads == 1 || head * es % 16 == 0);
+}
+
 // The status word comes first in every scratch buffer.
 struct CacheLayout {
     size_t status, ticket, join, part_ml, part_o, total;
@@ -178,15 +185,16 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
                                  const rheo_kv* kv, void* q_out, int64_t q_out_batch, int64_t q_out_token,
                                  int64_t q_out_head, void* scratch, rheo_stream_t stream) {
     if (!valid(cfg) || !in || !in->q || !in->k || !in->v || !slot || !position || !q_out || !scratch) return RHEO_EINVAL;
-    const int es = elem_bytes(cfg->dtype);
     if (!kv_ok(kv, *cfg)) return RHEO_EINVAL;
     if (rot < 0 || rot > cfg->head_dim || rot % 8 != 0 || (rot > 0 && (!cos_sin || max_position < 1))) return RHEO_EINVAL;
     if (!(eps >= 0.0f) || (interleaved != 0 && interleaved != 1)) return RHEO_EINVAL;
     for (const void* p : {in->q, in->k, in->v, q_weight, k_weight, (const void*)cos_sin, (const void*)q_out})
         if (!aligned16(p)) return RHEO_EINVAL;
-    for (int64_t s : {in->q_batch, in->q_token, in->q_head, in->k_batch, in->k_token, in->k_head, in->v_batch,
-                      in->v_token, in->v_head, q_out_batch, q_out_token, q_out_head})
-        if (s * es % 16 != 0) return RHEO_EINVAL;
+    if (!rows_ok(*cfg, in->q_batch, in->q_token, in->q_head, cfg->q_heads) ||
+        !rows_ok(*cfg, in->k_batch, in->k_token, in->k_head, cfg->kv_heads) ||
+        !rows_ok(*cfg, in->v_batch, in->v_token, in->v_head, cfg->kv_heads) ||
+        !rows_ok(*cfg, q_out_batch, q_out_token, q_out_head, cfg->q_heads))
+        return RHEO_EINVAL;
     const CacheLayout L = cache_layout(*cfg);
     RopeArgs a{};
     a.B = cfg->batch;
@@ -218,10 +226,10 @@ extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_
                                 const int32_t* block_table, const int32_t* ctx_len, const int32_t* new_len,
                                 const uint8_t* mask, float scale, void* scratch, rheo_stream_t stream) {
     if (!valid(cfg) || !io || !io->q || !io->out || !block_table || !ctx_len || !scratch) return RHEO_EINVAL;
-    const int es = elem_bytes(cfg->dtype);
     if (!kv_ok(kv, *cfg) || !aligned16(io->q) || !aligned16(io->out)) return RHEO_EINVAL;
-    for (int64_t s : {io->q_batch, io->q_token, io->q_head, io->out_batch, io->out_token, io->out_head})
-        if (s * es % 16 != 0) return RHEO_EINVAL;
+    if (!rows_ok(*cfg, io->q_batch, io->q_token, io->q_head, cfg->q_heads) ||
+        !rows_ok(*cfg, io->out_batch, io->out_token, io->out_head, cfg->q_heads))
+        return RHEO_EINVAL;
     if (!(scale > -INFINITY && scale < INFINITY)) return RHEO_EINVAL;
     const CacheLayout L = cache_layout(*cfg);
     AttendArgs a{};

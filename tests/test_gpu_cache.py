@@ -284,3 +284,21 @@ def test_commit_flags_broken_paths_and_leaves_them():
         k0[:, p1, :, r1], v0[:, p1, :, r1] = k0[:, p0, :, r0].clone(), v0[:, p0, :, r0].clone()
     assert torch.equal(key, k0) and torch.equal(value, v0)
     assert nxt.tolist() == [10, 10, 10, 10, 14, -3, 60]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_strides_of_dimensions_of_one_do_not_count(dtype):
+    """One request, one token, one head: torch may give these dimensions any stride."""
+    cfg = _cfg(batch=1, tokens=1, pages=2, max_pages=2, q_heads=1, kv_heads=1, dtype=dtype)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    dt, D = cfg.torch_dtype, cfg.head_dim
+    odd = lambda: torch.randn(D, generator=g, device="cuda").to(dt).as_strided((1, 1, 1, D), (7, 5, 3, 1))  # noqa: E731
+    q, k, v = odd(), odd(), odd()
+    key, value = rheo.make_cache(cfg, 1)
+    pages, plan, ws = rheo.Pages(cfg), rheo.CachePlan(cfg), rheo.CacheWorkspace(cfg)
+    rheo.cache_reserve(cfg, _i32([0]), pages, plan, ws)
+    q_out, out = torch.zeros((1, 1, 1, D), dtype=dt, device="cuda"), torch.zeros(D, dtype=dt, device="cuda")
+    rheo.qk_norm_rope(cfg, q, k, v, None, None, None, plan, key[0], value[0], q_out, ws)
+    rheo.tree_attend(cfg, q, key[0], value[0], pages, _i32([0]), out.as_strided((1, 1, 1, D), (9, 9, 9, 1)), ws)
+    assert rheo.scratch_status(ws) == 0
+    assert torch.equal(q_out.flatten(), q.flatten()) and torch.equal(out, v.flatten())
