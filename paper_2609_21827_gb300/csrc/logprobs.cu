@@ -17,8 +17,9 @@
 // A row is cut into segments where there are fewer rows than SMs; the last CTA of
 // a row joins them.
 // 144 rows of 151,936 in bf16 take 26.7 us (1.6 TB/s; their loads alone 13.5), 576 rows 70
-// us (2.5 TB/s), four rows of 1,024 6 us with the call.  Bound by instructions (16 an element for the maximum, two
-// sums and the count) and, with few rows, by the ranking at a row's end.
+// us (2.5 TB/s), four rows of 1,024 6 us with the call.  288 rows: 19 instructions an
+// element (maximum, two sums, count, and the ends of rows), issue slots 53 % busy: a CTA
+// reads while the other one of its SM ranks.
 #include <cuda_bf16.h>
 
 #include "cache_kernels.h"
