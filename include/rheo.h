@@ -267,7 +267,9 @@ int rheo_get_status(const rheo_config* cfg, void* workspace, rheo_stream_t strea
  * at the top (the caller owns every buffer, no allocation, asynchronous, host
  * checks before any launch).  Their scratch buffers are zeroed once by
  * rheo_scratch_init, and again after a call whose status was not zero; calls
- * that may overlap in time need a scratch buffer each.
+ * that may overlap in time need a scratch buffer each.  Otherwise one buffer
+ * serves any of the functions here and rheo_token_logprobs, in any order and for
+ * every configuration that asks for no more bytes than it has.
  *
  * Tokens.  A call handles up to T = cfg.tokens new tokens of each of B
  * requests; request b has ctx_len[b] cached tokens (positions 0 .. ctx-1) and
@@ -429,6 +431,7 @@ typedef struct {
     float* top_logprobs;  /* [R,top] their log probabilities; -inf where the id is -1   */
 } rheo_logprobs;
 
+/* Scratch bytes of rheo_token_logprobs: the same for every configuration. */
 int rheo_logprob_sizes(const rheo_logprob_config* cfg, size_t* scratch_bytes);
 
 /* Row i reads logits row row_index[i] (NULL: i; [R] int32), of logit_rows rows

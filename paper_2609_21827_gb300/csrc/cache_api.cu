@@ -65,23 +65,27 @@ bool rows_ok(const rheo_cache_config& c, int64_t batch, int64_t token, int64_t h
            (heads == 1 || head * es % 16 == 0);
 }
 
-// The status word comes first in every scratch buffer.
+// What a call has to find at zero comes first and lies at the same places in every
+// scratch buffer: the status word, the ticket of the tables and the tickets of the
+// log probabilities' rows.  What a call leaves behind (parts, join records) lies
+// behind that, so one buffer serves any of the functions at any sizes, in any order.
+constexpr size_t kStatusAt = 0, kTicketAt = 256, kRowTicketsAt = 512;
+constexpr size_t kPartsAt = (kRowTicketsAt + sizeof(unsigned) * kLogprobCutRows + 255) / 256 * 256;
+
 struct CacheLayout {
-    size_t status, ticket, join, part_ml, part_o, total;
+    size_t join, part_ml, part_o, total;
 };
 
 CacheLayout cache_layout(const rheo_cache_config& c) {
     const int G = c.q_heads / c.kv_heads;
     const size_t ctas = kAttendCtas, rows = attend_part_rows(c.dtype, c.tokens, G);
     CacheLayout L{};
-    size_t o = 0;
+    size_t o = kPartsAt;
     auto take = [&](size_t bytes) {
         const size_t at = o;
         o = up256(o + bytes);
         return at;
     };
-    L.status = take(sizeof(unsigned));
-    L.ticket = take(sizeof(unsigned));
     L.join = take(sizeof(int4) * ctas);
     L.part_ml = take(2 * ctas * rows * 2 * sizeof(float));
     L.part_o = take(2 * ctas * rows * c.head_dim * sizeof(float));
@@ -89,27 +93,10 @@ CacheLayout cache_layout(const rheo_cache_config& c) {
     return L;
 }
 
-struct LogprobLayout {
-    size_t status, ticket, part, keys, total;
-    int segments;
-};
-
-LogprobLayout logprob_layout(const rheo_logprob_config& c) {
-    LogprobLayout L{};
-    L.segments = logprob_segments(c.rows, c.vocab, c.dtype, 152);
-    size_t o = 0;
-    auto take = [&](size_t bytes) {
-        const size_t at = o;
-        o = up256(o + bytes);
-        return at;
-    };
-    L.status = take(sizeof(unsigned));
-    L.ticket = take(sizeof(unsigned) * (size_t)c.rows);
-    L.part = take(sizeof(float) * 4 * (size_t)c.rows * L.segments);
-    L.keys = take(sizeof(unsigned long long) * kMaxTop * (size_t)c.rows * L.segments);
-    L.total = o;
-    return L;
-}
+// Rows that are not cut leave no parts, so the sizes do not depend on the configuration.
+constexpr size_t kLogprobPartAt = kPartsAt;
+constexpr size_t kLogprobKeysAt = (kLogprobPartAt + sizeof(float) * 4 * kLogprobParts + 255) / 256 * 256;
+constexpr size_t kLogprobBytes = kLogprobKeysAt + sizeof(unsigned long long) * kMaxTop * kLogprobParts;
 
 template <class T> T* at(void* p, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(p) + off); }
 int code(cudaError_t e) { return e == cudaSuccess ? RHEO_OK : RHEO_ELAUNCH; }
@@ -127,7 +114,7 @@ extern "C" int rheo_cache_sizes(const rheo_cache_config* cfg, size_t* scratch_by
 
 extern "C" int rheo_logprob_sizes(const rheo_logprob_config* cfg, size_t* scratch_bytes) {
     if (!valid(cfg)) return RHEO_EINVAL;
-    if (scratch_bytes) *scratch_bytes = logprob_layout(*cfg).total;
+    if (scratch_bytes) *scratch_bytes = kLogprobBytes;
     return RHEO_OK;
 }
 
@@ -159,7 +146,6 @@ extern "C" int rheo_cache_reserve(const rheo_cache_config* cfg, const int32_t* c
         same += x[i] == y[i];
     }
     if (same != 0 && same != 4) return RHEO_EINVAL;
-    const CacheLayout L = cache_layout(*cfg);
     ReserveArgs a{};
     a.B = cfg->batch;
     a.T = cfg->tokens;
@@ -174,8 +160,8 @@ extern "C" int rheo_cache_reserve(const rheo_cache_config* cfg, const int32_t* c
     a.after = *after;
     a.slot = slot;
     a.position = position;
-    a.status = at<unsigned>(scratch, L.status);
-    a.ticket = at<unsigned>(scratch, L.ticket);
+    a.status = at<unsigned>(scratch, kStatusAt);
+    a.ticket = at<unsigned>(scratch, kTicketAt);
     return code(launch_reserve(a, multiprocessors(), (cudaStream_t)stream));
 }
 
@@ -195,7 +181,6 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
         !rows_ok(*cfg, in->v_batch, in->v_token, in->v_head, cfg->kv_heads) ||
         !rows_ok(*cfg, q_out_batch, q_out_token, q_out_head, cfg->q_heads))
         return RHEO_EINVAL;
-    const CacheLayout L = cache_layout(*cfg);
     RopeArgs a{};
     a.B = cfg->batch;
     a.T = cfg->tokens;
@@ -217,7 +202,7 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
     a.o_batch = q_out_batch;
     a.o_token = q_out_token;
     a.o_head = q_out_head;
-    a.status = at<unsigned>(scratch, L.status);
+    a.status = at<unsigned>(scratch, kStatusAt);
     return code(launch_rope(a, cfg->dtype == RHEO_BF16 ? 1 : 0, cfg->head_dim, interleaved != 0, multiprocessors(),
                             (cudaStream_t)stream));
 }
@@ -257,7 +242,7 @@ extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_
     a.part_o = at<float>(scratch, L.part_o);
     a.part_ml = at<float>(scratch, L.part_ml);
     a.join = at<int4>(scratch, L.join);
-    a.status = at<unsigned>(scratch, L.status);
+    a.status = at<unsigned>(scratch, kStatusAt);
     const cudaError_t e = launch_attend(a, cfg->dtype == RHEO_BF16 ? 1 : 0, (cudaStream_t)stream);
     return e == cudaErrorInvalidValue ? RHEO_EINVAL : code(e);  // a cache that no tensor map describes
 }
@@ -271,7 +256,6 @@ extern "C" int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, c
         return RHEO_EINVAL;
     const int es = elem_bytes(cfg->dtype);
     if (!kv_ok(kv, *cfg) || key_layer * es % 16 != 0 || value_layer * es % 16 != 0) return RHEO_EINVAL;
-    const CacheLayout L = cache_layout(*cfg);
     CommitArgs a{};
     a.B = cfg->batch;
     a.T = cfg->tokens;
@@ -290,7 +274,7 @@ extern "C" int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, c
     a.accepted_len = accepted_len;
     a.accepted_nodes = accepted_nodes;
     a.next_len = next_len;
-    a.status = at<unsigned>(scratch, L.status);
+    a.status = at<unsigned>(scratch, kStatusAt);
     return code(launch_commit(a, cfg->head_dim * es, (cudaStream_t)stream));
 }
 
@@ -304,13 +288,12 @@ extern "C" int rheo_token_logprobs(const rheo_logprob_config* cfg, const void* l
     if (cfg->top > 0 && (!out->top_ids || !out->top_logprobs)) return RHEO_EINVAL;
     const int es = elem_bytes(cfg->dtype);
     if ((uintptr_t)logits % es != 0) return RHEO_EINVAL;
-    const LogprobLayout L = logprob_layout(*cfg);
     LogprobArgs a{};
     a.R = cfg->rows;
     a.V = cfg->vocab;
     a.k = cfg->top;
     a.per_t = cfg->rows_per_temperature;
-    a.segments = L.segments;
+    a.segments = logprob_segments(cfg->rows, cfg->vocab, cfg->dtype);
     a.logits = static_cast<const char*>(logits);
     a.row_stride_bytes = row_stride * es;
     a.logit_rows = logit_rows;
@@ -318,10 +301,10 @@ extern "C" int rheo_token_logprobs(const rheo_logprob_config* cfg, const void* l
     a.token = token;
     a.temperature = temperature;
     a.out = *out;
-    a.status = at<unsigned>(scratch, L.status);
-    a.ticket = at<unsigned>(scratch, L.ticket);
-    a.part = at<float>(scratch, L.part);
-    a.part_key = at<unsigned long long>(scratch, L.keys);
+    a.status = at<unsigned>(scratch, kStatusAt);
+    a.ticket = at<unsigned>(scratch, kRowTicketsAt);
+    a.part = at<float>(scratch, kLogprobPartAt);
+    a.part_key = at<unsigned long long>(scratch, kLogprobKeysAt);
     return code(launch_logprobs(a, cfg->dtype == RHEO_BF16 ? 1 : 0, aligned16(logits) && a.row_stride_bytes % 16 == 0,
                                 (cudaStream_t)stream));
 }

@@ -83,8 +83,8 @@ struct LogprobArgs {
     const float* temperature;
     rheo_logprobs out;
     unsigned* status;
-    unsigned* ticket;              // [R]
-    float* part;                   // [R * segments][4] reference, sum, weighted sum, count (bits)
+    unsigned* ticket;              // [R], where segments > 1
+    float* part;                   // [R * segments][4] reference, sum, weighted sum, count (bits); where segments > 1
     unsigned long long* part_key;  // [R * segments][kMaxTop]
 };
 
@@ -98,7 +98,10 @@ int attend_part_rows(int dtype, int T, int G);
 int attend_lead(int dtype);
 int attend_least(int dtype);
 constexpr int kAttendCtas = 152;  // one a multiprocessor
+// Rows of logits are cut into segments where two CTAs a multiprocessor leave each of them at least two.
+constexpr int kLogprobParts = 2 * 152;
+constexpr int kLogprobCutRows = kLogprobParts / 2;
 cudaError_t launch_logprobs(const LogprobArgs& a, int dtype, bool aligned, cudaStream_t s);
-int logprob_segments(int rows, int vocab, int dtype, int sms);
+int logprob_segments(int rows, int vocab, int dtype);
 
 }  // namespace rheo

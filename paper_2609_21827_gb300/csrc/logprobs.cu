@@ -437,9 +437,9 @@ __global__ void __launch_bounds__(kLpThreads) logprob_kernel(const LogprobArgs a
 // four vectors a thread at least (144 rows of 151,936 in bf16: 33.8, 24.4, 32.7 us
 // with one, two, three an SM, measured with a reference per thread, which took 2 us
 // less than the warp's and was less exact for peaked rows).
-int logprob_segments(int rows, int vocab, int dtype, int sms) {
+int logprob_segments(int rows, int vocab, int dtype) {
     const int vec = dtype == 1 ? 8 : 4, vectors = (vocab + vec - 1) / vec;
-    int n = 2 * sms / rows, most = vectors / (4 * kLpThreads);
+    int n = kLogprobParts / rows, most = vectors / (4 * kLpThreads);
     n = n < most ? n : most;
     n = n < kLpMaxSegments ? n : kLpMaxSegments;
     return n < 1 ? 1 : n;
