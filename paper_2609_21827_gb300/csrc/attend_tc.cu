@@ -611,7 +611,8 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
             if (whole) {
                 if (a.io.lse) a.io.lse[((int64_t)w.b * a.T + t) * a.H * a.G + head] = attend_lse(m, ll);
             } else {
-                *reinterpret_cast<float2*>(a.part_ml + (part * a.part_rows + r_in) * 2) = make_float2(m, ll);
+                // a row past the request's tokens follows its query, whatever that holds: its reference is not kept
+                *reinterpret_cast<float2*>(a.part_ml + (part * a.part_rows + r_in) * 2) = make_float2(live ? m : -INFINITY, ll);
             }
         }
         if (!whole && w.tile == 0 && threadIdx.x == 0)
