@@ -405,7 +405,8 @@ int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, con
  *   accepted_nodes [B,depth] int32 as rheo_verify writes it: ascending, entry k
  *   in k+1 .. T-1.  A path that breaks this is not moved and its next_len is
  *   ctx_len (RHEO_STATUS_BAD_INDEX); so for a bad length (RHEO_STATUS_BAD_LENGTH).
- * next_len [B] int32, not the buffer of ctx_len.  depth <= 128. */
+ * next_len [B] int32, which shares no memory with ctx_len, accepted_len,
+ * accepted_nodes or block_table (RHEO_EINVAL).  depth <= 128. */
 int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, const rheo_kv* kv, int64_t key_layer,
                       int64_t value_layer, const int32_t* block_table, const int32_t* ctx_len,
                       const int32_t* accepted_len, const int32_t* accepted_nodes, int32_t depth, int32_t* next_len,

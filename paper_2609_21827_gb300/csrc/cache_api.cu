@@ -48,6 +48,12 @@ int page_shift(int page_size) {
     return s;
 }
 
+// Whether n values of 4 bytes at p and m at q have none in common.
+bool apart(const void* p, int64_t n, const void* q, int64_t m) {
+    const uintptr_t x = (uintptr_t)p, y = (uintptr_t)q;
+    return x + 4 * (uintptr_t)n <= y || y + 4 * (uintptr_t)m <= x;
+}
+
 bool kv_ok(const rheo_kv* kv, const rheo_cache_config& c) {
     if (!kv || !kv->key || !kv->value || !aligned16(kv->key) || !aligned16(kv->value)) return false;
     // a dimension of one has no stride
@@ -252,7 +258,12 @@ extern "C" int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, c
                                  const int32_t* accepted_len, const int32_t* accepted_nodes, int32_t depth,
                                  int32_t* next_len, void* scratch, rheo_stream_t stream) {
     if (!valid(cfg) || layers < 1 || layers > 4096 || !block_table || !ctx_len || !accepted_len || !accepted_nodes ||
-        depth < 1 || depth > 128 || !next_len || next_len == ctx_len || !scratch)
+        depth < 1 || depth > 128 || !next_len || !scratch)
+        return RHEO_EINVAL;
+    // a request's first CTA writes next_len while its others still read these
+    const int64_t B = cfg->batch;
+    if (!apart(next_len, B, ctx_len, B) || !apart(next_len, B, accepted_len, B) ||
+        !apart(next_len, B, accepted_nodes, B * depth) || !apart(next_len, B, block_table, B * cfg->max_pages))
         return RHEO_EINVAL;
     const int es = elem_bytes(cfg->dtype);
     if (!kv_ok(kv, *cfg) || key_layer * es % 16 != 0 || value_layer * es % 16 != 0) return RHEO_EINVAL;

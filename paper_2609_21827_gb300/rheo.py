@@ -664,7 +664,7 @@ def cache_commit(cfg: CacheConfig, key_cache: torch.Tensor, value_cache: torch.T
                  ctx_len: torch.Tensor, accepted_len: torch.Tensor, accepted_nodes: torch.Tensor,
                  next_len: torch.Tensor, ws: CacheWorkspace, stream=None) -> None:
     """rheo_cache_commit: the accepted path's lines move behind the root in caches [layers, pages, kv_heads,
-    page_size, D]; next_len = ctx_len + 1 + accepted_len (another tensor than ctx_len)."""
+    page_size, D]; next_len = ctx_len + 1 + accepted_len (a tensor apart from the other ones)."""
     i32 = torch.int32
     if key_cache.dim() != 5 or accepted_nodes.dim() != 2:
         raise RheoError("caches [layers, pages, kv_heads, page_size, D] and accepted_nodes [B, depth] are wanted")
