@@ -342,8 +342,11 @@ int rheo_cache_reserve(const rheo_cache_config* cfg, const int32_t* ctx_len, con
 
 /* Queries, keys and values of the B*T new tokens of one layer; strides in
  * elements (token: from t to t+1, batch: from b to b+1), D contiguous.
- * Pointers and strides (in bytes) are multiples of 16; here and in
- * rheo_tree_attend the stride of a dimension of one is not looked at. */
+ * Pointers and strides (in bytes) are multiples of 16, strides lie between -2^38
+ * and 2^38, and those of an output (q_out; out of rheo_tree_attend) keep its rows
+ * apart: from the smallest on, each is at least what the dimensions before it
+ * span.  Here and in rheo_tree_attend the stride of a dimension of one is not
+ * looked at. */
 typedef struct {
     const void* q;
     const void* k;
@@ -380,8 +383,8 @@ int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* in, const vo
  * sums in fp32).  What a token does not see does not reach its output, NaN and
  * infinities included.  A token that sees nothing, and every t >= new_len, gets
  * out = 0 and lse = -inf.
- *   q, out [B,T,q_heads,D] with strides in elements (batch, token, head), D
- *   contiguous, pointers and strides (in bytes) multiples of 16;
+ *   q, out [B,T,q_heads,D] with strides in elements (batch, token, head) and
+ *   pointers as rheo_qkv's, D contiguous;
  *   lse [B,T,q_heads] fp32, may be NULL.
  * A request with a bad length (RHEO_STATUS_BAD_LENGTH) gets out = 0, lse = -inf;
  * a bad page in the table (RHEO_STATUS_BAD_INDEX) reads as zeros. */
@@ -399,8 +402,8 @@ int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, con
 
 /* After verification: the keys and values of the accepted path move to the
  * positions behind the root, in `layers` layers (layer l at kv->key + l *
- * key_layer elements, kv->value + l * value_layer).  For k = 0 .. accepted_len-1:
- * position ctx_len + accepted_nodes[b][k] -> ctx_len + k + 1; next_len = ctx_len
+ * key_layer elements, kv->value + l * value_layer; strides like rheo_kv's).  For
+ * k = 0 .. accepted_len-1: position ctx_len + accepted_nodes[b][k] -> ctx_len + k + 1; next_len = ctx_len
  * + 1 + accepted_len (the root and the path; the bonus token is the next root).
  *   accepted_nodes [B,depth] int32 as rheo_verify writes it: ascending, entry k
  *   in k+1 .. T-1.  A path that breaks this is not moved and its next_len is

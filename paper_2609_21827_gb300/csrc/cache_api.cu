@@ -3,7 +3,9 @@
 // scratch layout and launches on the caller's stream.
 #include <cuda_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
+#include <cstdlib>
 
 #include "cache_kernels.h"
 #include "rheo.h"
@@ -54,12 +56,15 @@ bool apart(const void* p, int64_t n, const void* q, int64_t m) {
     return x + 4 * (uintptr_t)n <= y || y + 4 * (uintptr_t)m <= x;
 }
 
+// A stride of n > 1 places, in elements: whole 16-byte pieces and below 2^38 (a dimension of one has none).
+constexpr int64_t kStrideEnd = (int64_t)1 << 38;
+bool stride_ok(int64_t s, int64_t n, int es) {
+    return n == 1 || (s > -kStrideEnd && s < kStrideEnd && s * es % 16 == 0);
+}
+
 bool kv_ok(const rheo_kv* kv, const rheo_cache_config& c) {
     if (!kv || !kv->key || !kv->value || !aligned16(kv->key) || !aligned16(kv->value)) return false;
-    // a dimension of one has no stride
-    const auto fits = [&](int64_t s, int n) {
-        return n == 1 || (s > 0 && s < (int64_t)1 << 38 && s * elem_bytes(c.dtype) % 16 == 0);
-    };
+    const auto fits = [&](int64_t s, int n) { return n == 1 || (s > 0 && stride_ok(s, n, elem_bytes(c.dtype))); };
     return fits(kv->key_page, c.pages) && fits(kv->key_head, c.kv_heads) && fits(kv->key_token, c.page_size) &&
            fits(kv->value_page, c.pages) && fits(kv->value_head, c.kv_heads) && fits(kv->value_token, c.page_size);
 }
@@ -67,8 +72,22 @@ bool kv_ok(const rheo_kv* kv, const rheo_cache_config& c) {
 // Strides [batch][token][head] of queries, keys, values or outputs.
 bool rows_ok(const rheo_cache_config& c, int64_t batch, int64_t token, int64_t head, int heads) {
     const int es = elem_bytes(c.dtype);
-    return (c.batch == 1 || batch * es % 16 == 0) && (c.tokens == 1 || token * es % 16 == 0) &&
-           (heads == 1 || head * es % 16 == 0);
+    return stride_ok(batch, c.batch, es) && stride_ok(token, c.tokens, es) && stride_ok(head, heads, es);
+}
+
+// The same of an output, whose rows share no element: from the smallest stride on, each is at least what the
+// dimensions before it span.
+bool out_rows_ok(const rheo_cache_config& c, int64_t batch, int64_t token, int64_t head, int heads) {
+    if (!rows_ok(c, batch, token, head, heads)) return false;
+    struct { int64_t stride, n; } d[3] = {{std::abs(batch), c.batch}, {std::abs(token), c.tokens}, {std::abs(head), heads}};
+    std::sort(d, d + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+    int64_t span = c.head_dim;
+    for (const auto& x : d) {
+        if (x.n == 1) continue;
+        if (x.stride < span) return false;
+        span += (x.n - 1) * x.stride;
+    }
+    return true;
 }
 
 // What a call has to find at zero comes first and lies at the same places in every
@@ -185,7 +204,7 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
     if (!rows_ok(*cfg, in->q_batch, in->q_token, in->q_head, cfg->q_heads) ||
         !rows_ok(*cfg, in->k_batch, in->k_token, in->k_head, cfg->kv_heads) ||
         !rows_ok(*cfg, in->v_batch, in->v_token, in->v_head, cfg->kv_heads) ||
-        !rows_ok(*cfg, q_out_batch, q_out_token, q_out_head, cfg->q_heads))
+        !out_rows_ok(*cfg, q_out_batch, q_out_token, q_out_head, cfg->q_heads))
         return RHEO_EINVAL;
     RopeArgs a{};
     a.B = cfg->batch;
@@ -219,7 +238,7 @@ extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_
     if (!valid(cfg) || !io || !io->q || !io->out || !block_table || !ctx_len || !scratch) return RHEO_EINVAL;
     if (!kv_ok(kv, *cfg) || !aligned16(io->q) || !aligned16(io->out)) return RHEO_EINVAL;
     if (!rows_ok(*cfg, io->q_batch, io->q_token, io->q_head, cfg->q_heads) ||
-        !rows_ok(*cfg, io->out_batch, io->out_token, io->out_head, cfg->q_heads))
+        !out_rows_ok(*cfg, io->out_batch, io->out_token, io->out_head, cfg->q_heads))
         return RHEO_EINVAL;
     if (!(scale > -INFINITY && scale < INFINITY)) return RHEO_EINVAL;
     const CacheLayout L = cache_layout(*cfg);
@@ -266,7 +285,9 @@ extern "C" int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, c
         !apart(next_len, B, accepted_nodes, B * depth) || !apart(next_len, B, block_table, B * cfg->max_pages))
         return RHEO_EINVAL;
     const int es = elem_bytes(cfg->dtype);
-    if (!kv_ok(kv, *cfg) || key_layer * es % 16 != 0 || value_layer * es % 16 != 0) return RHEO_EINVAL;
+    if (!kv_ok(kv, *cfg)) return RHEO_EINVAL;
+    for (const int64_t s : {key_layer, value_layer})
+        if (!stride_ok(s, 2, es) || (layers > 1 && s <= 0)) return RHEO_EINVAL;
     CommitArgs a{};
     a.B = cfg->batch;
     a.T = cfg->tokens;
