@@ -431,8 +431,8 @@ class CacheConfig:
         B, T, H, D = self.batch, self.tokens, self.kv_heads, self.head_dim
         for name, value in (("torch_dtype", torch_dtype), ("_c", c), ("_ref", ctypes.byref(c)), ("_bytes", None),
                             ("_one", (B,)), ("_each", (B, T)), ("_table", (B, self.max_pages)),
-                            ("_q", (B, T, self.q_heads, D)), ("_k", (B, T, H, D)), ("_lse", (B, T, self.q_heads)),
-                            ("_mask", (B, T, T)), ("_pool", (self.pages, H, self.page_size, D))):
+                            ("_free", (self.pages,)), ("_q", (B, T, self.q_heads, D)), ("_k", (B, T, H, D)),
+                            ("_lse", (B, T, self.q_heads)), ("_mask", (B, T, T)), ("_pool", (self.pages, H, self.page_size, D))):
             object.__setattr__(self, name, value)
 
     def scratch_bytes(self) -> int:
@@ -457,7 +457,7 @@ class LogprobConfig:
         code, torch_dtype = _dtype_of(self.dtype)
         c = _LogprobConfig(self.rows, self.vocab, self.top, code, self.rows_per_temperature)
         for name, value in (("torch_dtype", torch_dtype), ("_c", c), ("_ref", ctypes.byref(c)), ("_bytes", None),
-                            ("_rows", (self.rows,)),
+                            ("_rows", (self.rows,)), ("_top", (self.rows, self.top)),
                             ("_groups", (-(-self.rows // max(self.rows_per_temperature, 1)),))):
             object.__setattr__(self, name, value)
 
@@ -529,21 +529,7 @@ def _want_strided(x: torch.Tensor, name: str, dtype, shape) -> tuple:
     return x.data_ptr(), st
 
 
-class _Buffers:
-    """Tensors that are checked again when one of them is replaced or has moved."""
-
-    _held = None
-
-    def __setattr__(self, name, value):
-        object.__setattr__(self, name, value)
-        object.__setattr__(self, "_held", None)
-
-    def _keep(self, cfg, at, made):
-        object.__setattr__(self, "_held", (cfg, at, made))
-        return made
-
-
-class Pages(_Buffers):
+class Pages:
     """Pages of the requests and the stack of free ones.  Without arguments every page is free
     (page 0 on top); given tensors are used as they are."""
 
@@ -559,19 +545,16 @@ class Pages(_Buffers):
             n_free = torch.full((1,), cfg.pages, dtype=i32, device=device)
         self.block_table, self.n_pages, self.free_list, self.n_free = block_table, n_pages, free_list, n_free
 
+    def table(self, cfg: CacheConfig) -> int:
+        return _want(self.block_table, "block_table", torch.int32, cfg._table)
+
     def c(self, cfg: CacheConfig) -> _Pages:
-        held = self._held
-        at = (self.block_table.data_ptr(), self.n_pages.data_ptr(), self.free_list.data_ptr(), self.n_free.data_ptr())
-        if held is not None and held[0] is cfg and held[1] == at:
-            return held[2]
         i32 = torch.int32
-        return self._keep(cfg, at, _Pages(_want(self.block_table, "block_table", i32, cfg._table),
-                                          _want(self.n_pages, "n_pages", i32, cfg._one),
-                                          _want(self.free_list, "free_list", i32, (cfg.pages,)),
-                                          _want(self.n_free, "n_free", i32, (1,))))
+        return _Pages(self.table(cfg), _want(self.n_pages, "n_pages", i32, cfg._one),
+                      _want(self.free_list, "free_list", i32, cfg._free), _want(self.n_free, "n_free", i32, (1,)))
 
 
-class CachePlan(_Buffers):
+class CachePlan:
     """Slots [B, T] (int64) and positions [B, T] (int32) of a call's new tokens."""
 
     def __init__(self, cfg: CacheConfig, device="cuda", slot=None, position=None):
@@ -580,13 +563,8 @@ class CachePlan(_Buffers):
         self.position = torch.full(shape, -1, dtype=torch.int32, device=device) if position is None else position
 
     def ptrs(self, cfg: CacheConfig) -> tuple:
-        held = self._held
-        at = (self.slot.data_ptr(), self.position.data_ptr())
-        if held is not None and held[0] is cfg and held[1] == at:
-            return at
-        _want(self.slot, "slot", torch.int64, cfg._each)
-        _want(self.position, "position", torch.int32, cfg._each)
-        return self._keep(cfg, at, at)
+        return (_want(self.slot, "slot", torch.int64, cfg._each),
+                _want(self.position, "position", torch.int32, cfg._each))
 
 
 def make_cache(cfg: CacheConfig, layers: int = 1, device="cuda"):
@@ -655,7 +633,7 @@ def tree_attend(cfg: CacheConfig, q: torch.Tensor, key_cache: torch.Tensor, valu
     io = _AttendIO(qp, op, _want_opt(lse, "lse", torch.float32, cfg._lse), qs[0], qs[1], qs[2], os_[0], os_[1], os_[2])
     kv = _kv(cfg, key_cache, value_cache)
     _check(lib().rheo_tree_attend(
-        cfg._ref, io, kv, pages.c(cfg).block_table, _want(ctx_len, "ctx_len", i32, cfg._one),
+        cfg._ref, io, kv, pages.table(cfg), _want(ctx_len, "ctx_len", i32, cfg._one),
         _want_opt(new_len, "new_len", i32, cfg._one), _want_opt(mask, "mask", torch.uint8, cfg._mask),
         cfg.head_dim ** -0.5 if scale is None else scale, ws.of(cfg), _stream(stream)), "rheo_tree_attend")
 
@@ -673,13 +651,13 @@ def cache_commit(cfg: CacheConfig, key_cache: torch.Tensor, value_cache: torch.T
     kp, ks = _want_strided(key_cache, "key cache", cfg.torch_dtype, shape)
     vp, vs = _want_strided(value_cache, "value cache", cfg.torch_dtype, shape)
     _check(lib().rheo_cache_commit(
-        cfg._ref, layers, _KV(kp, vp, ks[1], ks[2], ks[3], vs[1], vs[2], vs[3]), ks[0], vs[0], pages.c(cfg).block_table,
+        cfg._ref, layers, _KV(kp, vp, ks[1], ks[2], ks[3], vs[1], vs[2], vs[3]), ks[0], vs[0], pages.table(cfg),
         _want(ctx_len, "ctx_len", i32, cfg._one), _want(accepted_len, "accepted_len", i32, cfg._one),
         _want(accepted_nodes, "accepted_nodes", i32, (cfg.batch, depth)), depth,
         _want(next_len, "next_len", i32, cfg._one), ws.of(cfg), _stream(stream)), "rheo_cache_commit")
 
 
-class Logprobs(_Buffers):
+class Logprobs:
     """Outputs of token_logprobs."""
 
     def __init__(self, cfg: LogprobConfig, device="cuda"):
@@ -691,16 +669,10 @@ class Logprobs(_Buffers):
         self.top_logprobs = torch.zeros((R, k), dtype=torch.float32, device=device)
 
     def c(self, cfg: LogprobConfig) -> _Logprobs:
-        held = self._held
-        at = (self.logprob.data_ptr(), self.rank.data_ptr(), self.entropy.data_ptr(), self.top_ids.data_ptr(),
-              self.top_logprobs.data_ptr())
-        if held is not None and held[0] is cfg and held[1] == at:
-            return held[2]
-        R, k, f32, i32 = cfg.rows, cfg.top, torch.float32, torch.int32
-        return self._keep(cfg, at, _Logprobs(
-            _want(self.logprob, "logprob", f32, (R,)), _want(self.rank, "rank", i32, (R,)),
-            _want(self.entropy, "entropy", f32, (R,)), _want(self.top_ids, "top_ids", i32, (R, k)),
-            _want(self.top_logprobs, "top_logprobs", f32, (R, k))))
+        f32, i32, rows, top = torch.float32, torch.int32, cfg._rows, cfg._top
+        return _Logprobs(_want(self.logprob, "logprob", f32, rows), _want(self.rank, "rank", i32, rows),
+                         _want(self.entropy, "entropy", f32, rows), _want(self.top_ids, "top_ids", i32, top),
+                         _want(self.top_logprobs, "top_logprobs", f32, top))
 
 
 def token_logprobs(cfg: LogprobConfig, logits: torch.Tensor, tokens: torch.Tensor, out: Logprobs,
