@@ -17,8 +17,11 @@
 //   !PAIR:  up to 128 rows (single tokens, short chains): stream 0 takes the
 //           first 64 keys of every tile, stream 1 the others, and their sums are
 //           joined at the end.
-// Whoever waits at a barrier meets each of its phases in turn: a parity tells a
-// phase only from its neighbours.
+// A parity tells a phase only from its neighbours, so a phase may be waited for only
+// when the one before it has ended.  The loading and issuing warps meet every phase of
+// their barriers in turn, the softmax groups those of the scores, the queries and the
+// items' starts.  The groups skip phases of pv_done and of full_v: what has ended by
+// then is said at these waits.
 // The reference m of a row follows its largest score only when that has grown by
 // more than kSlack in log2 units: then O is multiplied in place (rare after the
 // first tiles); until then p <= 2^kSlack, which bf16 and the fp32 sums hold with
@@ -50,6 +53,7 @@ namespace {
 
 constexpr int kTile = 128;                   // keys a tile: what is loaded at a time
 constexpr int kSub = 64;                     // keys of a score product: half a tile
+constexpr int kScores = 2;                   // score buffers of a stream
 constexpr int kTcThreads = 12 * 32;
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
@@ -66,11 +70,13 @@ template <int D, bool PAIR> struct TcShape {
     // Tensor memory: stream s has two buffers of scores at columns 128 s and 128 s + 64, whose first 32 columns take
     // the weights (bf16 pairs), and its sums at kO + s D.
     static constexpr int kO = 256;
+    // A softmax group that waits for the values of tile u knows that those of tile u - 2 have come (at clean()).
+    static_assert(kV >= kScores);
 };
 
 struct TcControl {
     unsigned long long full_k[5], empty_k[5], full_v[5], empty_v[5];
-    unsigned long long s_full[2][2], p_ready[2][2], pv_done[2][2], drained[2], q_ready, q_taken, all_sync;
+    unsigned long long s_full[2][kScores], p_ready[2][kScores], pv_done[2][kScores], drained[2], q_ready, q_taken, all_sync;
     uint32_t tmem;
     int abort;
     int any_odd;          // some drafted value is not finite
@@ -333,6 +339,11 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         // Values of the tile at place k0 (tile u of this CTA) before a product of this stream reads them: nothing behind
         // the request's places, and no element that is not finite among the drafted tokens'.  PAIR: a thread a line;
         // !PAIR: the stream's half of the lines, two threads a line.
+        // Called with a product of this stream's scores at hand, the only waits for full_v here, and not for each tile.  The
+        // phase before, tile u - kV, has ended: these scores were issued after the stream's product with the values two
+        // products ago (its buffer), which read tile u - 2 or a later one if it is of this item; if it is of an earlier
+        // one, u - 2 is too, and stream 0, which reads every tile, has waited for that item's last product before this
+        // item began.  The phase after needs this stream's product with tile u, which waits for what follows here.
         auto clean = [&](int k0, uint32_t u) -> bool {
             if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) return false;
             constexpr int pieces = PAIR ? D / 8 : D / 16;
@@ -434,7 +445,8 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                     } else {
                         const bool grow = top > m + kSlack || (m == -INFINITY && top > m);
                         if (__any_sync(0xffffffffu, grow)) {
-                            // the sums so far move to the new reference
+                            // the sums so far move to the new reference; the phase before of the last product's barrier has
+                            // ended, as these scores were issued after the product before that one, and products end in order
                             if (!bar_wait(&c.pv_done[st][buf ^ 1], ((products - 1) / 2) & 1, c)) return;
                             tc_fence_after();
                             const float f = !grow || m == -INFINITY ? 1.0f : fast_exp2(m - top);
@@ -483,7 +495,8 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         tile0 += n;
 
         // ---- the item's sums
-        // both buffers' last products
+        // both buffers' last products (the last scores were issued after the product before them, so the phases before
+        // these have ended)
         if (mine > 0) {
             const uint32_t x = products - 1;
             if (x > 0 && !bar_wait(&c.pv_done[st][(x - 1) & 1], ((x - 1) / 2) & 1, c)) return;
