@@ -403,8 +403,9 @@ int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, con
 /* After verification: the keys and values of the accepted path move to the
  * positions behind the root, in `layers` layers (layer l at kv->key + l *
  * key_layer elements, kv->value + l * value_layer; strides like rheo_kv's).  For
- * k = 0 .. accepted_len-1: position ctx_len + accepted_nodes[b][k] -> ctx_len + k + 1; next_len = ctx_len
- * + 1 + accepted_len (the root and the path; the bonus token is the next root).
+ * k = 0 .. accepted_len-1: position ctx_len + accepted_nodes[b][k] -> ctx_len + k
+ * + 1; next_len = ctx_len + 1 + accepted_len (the root and the path; the bonus
+ * token is the next root).
  *   accepted_nodes [B,depth] int32 as rheo_verify writes it: ascending, entry k
  *   in k+1 .. T-1.  A path that breaks this is not moved and its next_len is
  *   ctx_len (RHEO_STATUS_BAD_INDEX); so for a bad length (RHEO_STATUS_BAD_LENGTH).

@@ -7,7 +7,7 @@
 // rows, so the row statistics are four shuffles and p passes through shared
 // memory without a block barrier.
 // Four trees of up to 17 tokens over up to 733 places (8 query, 4 key/value heads of
-// 64): 15.1 us with the join, 0.2 TB/s: bound by dependent latencies (lengths, table, keys, two
+// 64): 15 to 17.5 us with the join, 0.2 TB/s: bound by dependent latencies (lengths, table, keys, two
 // products, join), as its few bytes come from L2.  The fp32 units, because tf32
 // products would round what an fp32 cache is kept for.
 #include <cuda_bf16.h>

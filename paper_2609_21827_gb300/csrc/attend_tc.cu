@@ -34,12 +34,12 @@
 // rows that do see such a token get the element added at the end.
 //
 // What bounds it.  32 single tokens, 32 query and 8 key/value heads of 128, contexts
-// to 16,201: 166 us, 6.4 TB/s (94 % of a copy's rate).  64 trees of 61 tokens over
-// contexts to 8,101: 244 to 256 us, 4.6 TB/s, 1.0 PFLOP/s: 64 keys of 256 rows need
-// 1,400 cycles of HBM, 1,280 of shared memory (the queries are read again for each
-// score product), 1,050 of the tensor cores and 800 of issue slots, and take 1,970,
-// the chain of a softmax warp's steps.  One tree of 61 over 1,911: 19 us with the
-// join, dependent latencies.  Measured against this layout: keys in
+// to 16,201: 166 to 169 us, 6.3 TB/s (93 % of a copy's rate).  64 trees of 61 tokens over
+// contexts to 8,101: 241 to 264 us on several GB300s, 4.4 to 4.9 TB/s, 1.0 to 1.1
+// PFLOP/s: 64 keys of 256 rows need 1,400 cycles of HBM, 1,280 of shared memory (the
+// queries are read again for each score product), 1,050 of the tensor cores and 800 of
+// issue slots, and take 1,970, the chain of a softmax warp's steps.  One tree of 61 over
+// 1,911: 19 us with the join, dependent latencies.  Measured against this layout: keys in
 // units of 64 in the rings 185 / 389 / 29 us where this took 193 / 367 / 24, scores of
 // 128 keys at a time (no second buffer) 196 / 404 / 23.
 #include <cuda.h>

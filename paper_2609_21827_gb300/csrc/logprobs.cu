@@ -16,8 +16,8 @@
 // ranked.  Keys are (logit, -id) in 64 bits, all different, so ties need no care.
 // A row is cut into segments where there are fewer rows than SMs; the last CTA of
 // a row joins them.
-// 144 rows of 151,936 in bf16 take 26.7 us (1.6 TB/s; their loads alone 13.5), 576 rows 70
-// us (2.5 TB/s), four rows of 1,024 6 us with the call.  288 rows: 19 instructions an
+// 144 rows of 151,936 in bf16 take 26.6 us (1.6 TB/s; their loads alone 13.5), 576 rows 71
+// us (2.5 TB/s), four rows of 1,024 5.7 us in a captured graph.  288 rows: 19.5 instructions an
 // element (maximum, two sums, count, and the ends of rows), issue slots 53 % busy: a CTA
 // reads while the other one of its SM ranks.
 #include <cuda_bf16.h>
