@@ -105,7 +105,8 @@ def test_the_functions_in_turn_on_one_buffer(dtype):
     """Tables, attention that leaves parts of split items, and log probabilities that leave parts of cut rows."""
     cfg = rheo.CacheConfig(batch=4, tokens=40, pages=160, page_size=64, max_pages=64, q_heads=4, kv_heads=2, head_dim=64, dtype=dtype)
     ws = rheo.CacheWorkspace(cfg)
-    for i, (R, ctx, T) in enumerate([(10, [3000, 41], 40), (100, [1000, 900, 800, 700], 9), (152, [3500], 1), (3, [2000, 2], 17)]):
+    turns = [(10, [3000, 41], 40), (100, [1000, 900, 800, 700], 9), (152, [3500], 1), (3, [2000, 2], 17)]
+    for i, (R, ctx, T) in enumerate(turns):
         _attend(ws, dtype, ctx, T, i)
         _check_rows(_logits(R, dtype, i), ws, dtype)
         _reserve(ws, [3, 40, 17, 90][: 1 + i])
