@@ -79,10 +79,12 @@ bool rows_ok(const rheo_cache_config& c, int64_t batch, int64_t token, int64_t h
 // dimensions before it span.
 bool out_rows_ok(const rheo_cache_config& c, int64_t batch, int64_t token, int64_t head, int heads) {
     if (!rows_ok(c, batch, token, head, heads)) return false;
-    struct { int64_t stride, n; } d[3] = {{std::abs(batch), c.batch}, {std::abs(token), c.tokens}, {std::abs(head), heads}};
-    std::sort(d, d + 3, [](const auto& x, const auto& y) { return x.stride < y.stride; });
+    struct Dim { int64_t stride, n; };
+    const auto dim = [](int64_t s, int64_t n) { return Dim{n == 1 ? 0 : std::abs(s), n}; };
+    Dim d[3] = {dim(batch, c.batch), dim(token, c.tokens), dim(head, heads)};
+    std::sort(d, d + 3, [](const Dim& x, const Dim& y) { return x.stride < y.stride; });
     int64_t span = c.head_dim;
-    for (const auto& x : d) {
+    for (const Dim& x : d) {
         if (x.n == 1) continue;
         if (x.stride < span) return false;
         span += (x.n - 1) * x.stride;
