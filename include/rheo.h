@@ -58,7 +58,8 @@ enum {
     RHEO_STATUS_INTERNAL = 8,        /* broken invariant (e.g. prune not ancestor-closed) */
     RHEO_STATUS_BAD_LENGTH = 16,     /* a negative length, or one past the block table */
     RHEO_STATUS_NO_PAGES = 32,       /* the pool has no page left for a request       */
-    RHEO_STATUS_BAD_INDEX = 64       /* a page, slot, position, row or token out of range */
+    RHEO_STATUS_BAD_INDEX = 64,      /* a page, slot, position, row or token out of range */
+    RHEO_STATUS_BAD_VALUE = 128      /* a number that 4 bits cannot stand for: NaN, infinite, past the largest scale */
 };
 
 /* Problem size.  K = deterministic slots per pool (pool = K+1), 0 <= m <= K,
@@ -450,6 +451,91 @@ int rheo_logprob_sizes(const rheo_logprob_config* cfg, size_t* scratch_bytes);
 int rheo_token_logprobs(const rheo_logprob_config* cfg, const void* logits, int64_t row_stride, int64_t logit_rows,
                         const int32_t* row_index, const int32_t* token, const float* temperature,
                         const rheo_logprobs* out, void* scratch, rheo_stream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Long contexts: attention limited to a window, and caches held in 4 bits.  The
+ * definitions are ours; rules, scratch buffers and errors as above.
+ *
+ * Window.  New token t of request b has position pos = C + depth[b][t] behind C
+ * cached tokens (depth [B,T] int32: the pruned tree's depths, as
+ * rheo_cache_reserve takes them; NULL: t; values outside 0 .. T-1 count as the
+ * nearest), a cached token its place.  With window > 0, a token sees of what
+ * rheo_tree_attend shows it the tokens whose position is below `sinks`, or above
+ * pos - window (its own and the window - 1 before).  window 0: all; sinks is not looked at. */
+typedef struct {
+    int32_t window;        /* positions, the token's own among them; 0: no limit */
+    int32_t sinks;         /* first positions that stay visible                  */
+    const int32_t* depth;
+} rheo_window;
+
+/* rheo_tree_attend with a window.  Pages that lie wholly outside what the call's
+ * tokens may see (past the sinks, and before the window of a token at depth 0) are
+ * not read, nor are their entries of the table. */
+int rheo_window_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, const rheo_kv* kv,
+                       const int32_t* block_table, const int32_t* ctx_len, const int32_t* new_len, const uint8_t* mask,
+                       const rheo_window* window, float scale, void* scratch, rheo_stream_t stream);
+
+/* A cache in two parts.  A request's first tokens lie in pages held in 4 bits, the
+ * others in 16 bits, as above: n4[b] = packed pages, then ctx_len[b] tokens in the
+ * pages of block_table.  ctx_len, slots and the block table count from the first
+ * token in 16 bits, so reserve, qk_norm_rope and commit serve that part as it is;
+ * positions are places plus n4[b] * page_size (rheo_cache_reserve: add that to
+ * depth).  `packed_cfg` is cfg but for pages and max_pages, which are the packed
+ * pool's; its tables are a rheo_pages like the others, so rheo_cache_reserve
+ * with packed_cfg, ctx_len = n4[b] * page_size and new_len = 0 takes back the
+ * packed pages of a request that ended (ctx_len 0).  bf16 caches only.
+ *
+ * A packed page holds the keys and values of page_size tokens of one head in
+ * rheo_packed_sizes() bytes: 4-bit numbers n = -7 .. 7, for keys with a scale s for
+ * each channel over min(page_size, 32) tokens, for values with one for each
+ * token over 32 channels.  s is the smallest (1 + m/8) 2^e (m 0..7, e -19 .. 12) with 7 s >=
+ * the largest magnitude, n = x / s rounded to the nearest, halves away from zero.  n s is
+ * exact in bf16.  Magnitudes past 53760 and infinities count as 53760, NaN as 0
+ * (RHEO_STATUS_BAD_VALUE). */
+typedef struct {
+    uint8_t* data;       /* of one layer; 16-byte aligned                        */
+    int64_t page, head;  /* strides in bytes: positive multiples of 16 below 2^39 (that of
+                            a dimension of one is not looked at); a page of a head is contiguous */
+} rheo_packed;
+
+/* Bytes of a packed page of one head. */
+int rheo_packed_sizes(const rheo_cache_config* packed_cfg, int64_t* page_bytes);
+
+/* Packs whole pages, in `layers` layers (layer l at kv->key + l * key_layer elements,
+ * kv->value + l * value_layer, packed->data + l * packed_layer bytes).  Of request b the
+ * first k = max(0, floor((ctx_len[b] - keep) / page_size)) pages: their numbers go
+ * to k packed pages from the top of the packed stack, which follow the request's packed
+ * ones in its table; their pages go onto the 16-bit stack, both in order of request, then of
+ * place; the others move to the front of the block table; ctx_out = ctx_len - k * page_size.
+ * A request whose pages the packed stack cannot give packs none, and neither does any
+ * behind it that would (RHEO_STATUS_NO_PAGES); nor one with a bad length: ctx_len
+ * negative or past the pages that it holds, more packed pages than max_pages
+ * (RHEO_STATUS_BAD_LENGTH).  A page of the tables out of its pool is not read or written
+ * (RHEO_STATUS_BAD_INDEX); the tables change as if it were.
+ * before, before4, ctx_len and after, after4, ctx_out are the same nine buffers (in place),
+ * or share no memory; entries that hold no page keep their value (from before).
+ * keep >= 0, layers 1..4096. */
+int rheo_cache_pack(const rheo_cache_config* cfg, const rheo_cache_config* packed_cfg, int32_t layers, const rheo_kv* kv,
+                    int64_t key_layer, int64_t value_layer, const rheo_packed* packed, int64_t packed_layer, int32_t keep,
+                    const rheo_pages* before, const rheo_pages* before4, const int32_t* ctx_len, const rheo_pages* after,
+                    const rheo_pages* after4, int32_t* ctx_out, void* scratch, rheo_stream_t stream);
+
+/* Packed pages src[i] back to pages dst[i] of the 16-bit cache, i = 0 .. n-1, in every
+ * layer.  An entry with a -1 is left out, and so is one out of its pool
+ * (RHEO_STATUS_BAD_INDEX).  The pages of dst are distinct.  n >= 0. */
+int rheo_cache_unpack(const rheo_cache_config* cfg, const rheo_cache_config* packed_cfg, int32_t layers,
+                      const rheo_packed* packed, int64_t packed_layer, const rheo_kv* kv, int64_t key_layer,
+                      int64_t value_layer, int32_t n, const int32_t* src, const int32_t* dst, void* scratch,
+                      rheo_stream_t stream);
+
+/* rheo_tree_attend and rheo_window_attend over both parts: request b's cached tokens are
+ * the n4[b] pages of packed_table ([B, packed_cfg->max_pages]), then ctx_len[b] tokens in 16
+ * bits.  window may be NULL.  A bad n4 (RHEO_STATUS_BAD_LENGTH) gives out = 0, lse = -inf.
+ * (cfg->max_pages + packed_cfg->max_pages) * page_size <= 2^30. */
+int rheo_packed_attend(const rheo_cache_config* cfg, const rheo_cache_config* packed_cfg, const rheo_attend_io* io,
+                       const rheo_kv* kv, const int32_t* block_table, const int32_t* ctx_len, const int32_t* new_len,
+                       const rheo_packed* packed, const int32_t* packed_table, const int32_t* n4, const uint8_t* mask,
+                       const rheo_window* window, float scale, void* scratch, rheo_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -39,7 +39,8 @@ template <int D, int R> struct SimtSmem {
     float p[R][kSimtTile + 4];
 };
 
-template <int D, int R>
+// LONG: tokens see what their window shows them, and an item walks the tiles that one of its own may see.
+template <int D, int R, bool LONG>
 __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const AttendArgs a) {
     grid_dependency_begin();
     extern __shared__ __align__(16) unsigned char raw_smem[];
@@ -47,9 +48,14 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
     __shared__ AttendCut cut_s;
     constexpr int RT = R / 16, DJ = D / 64, ES = 4;
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
-    const int rows = a.T * a.G, groups = (rows + R - 1) / R, per = a.H * groups;
+    const int rows = a.T * a.G, groups = (rows + R - 1) / R, per = LONG ? a.H : a.H * groups;
     if (tid < 32) {
-        const AttendCut c = attend_cut<kSimtTile>(a, per, blockIdx.x);
+        AttendCut c;
+        if constexpr (LONG)
+            c = attend_cut_over(a, a.B * groups, per, blockIdx.x,
+                                [&](int i) { return LongItem<kSimtTile>(a, i / groups, i % groups * R, R).n; });
+        else
+            c = attend_cut<kSimtTile>(a, per, blockIdx.x);
         if (tid == 0) cut_s = c;
     }
     __syncthreads();
@@ -57,19 +63,28 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
     if (tid == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
 
     for (AttendWalk<kSimtTile> walk(cut); walk.more(); walk.next(per)) {
-        const int b = walk.b;
-        const AttendSpan span = attend_span(a, b);
+        const int b = LONG ? walk.b / groups : walk.b, group = LONG ? walk.b % groups : walk.item % groups, r0 = group * R;
+        LongItem<kSimtTile> it;
+        AttendSpan span;
+        if constexpr (LONG) {
+            it = LongItem<kSimtTile>(a, b, r0, R);
+            span = AttendSpan{it.s.ctx, it.s.add, it.s.bad};
+            walk.open_tiles(it.n);
+        } else {
+            span = attend_span(a, b);
+            walk.open(span.len());
+        }
         if (span.bad && tid == 0) atomicOr(a.status, kStBadLength);
         const int len = span.len();
-        walk.open(len);
-        const int tile = walk.tile, n = walk.n, h = walk.item / groups, r0 = (walk.item % groups) * R;
+        const int tile = walk.tile, n = walk.n, h = LONG ? walk.item : walk.item / groups;
+        auto place_of = [&](int i) { return (LONG ? it.number(i) : i) * kSimtTile; };  // of the item's i-th tile
         const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
 
         auto load = [&](int tl, int buf) {
             constexpr int C = D * ES / 16;  // 16-byte pieces of a line
             for (int i = tid; i < kSimtTile * C; i += kSimtThreads) {
-                const int kr = i / C, c = i % C, l = tl * kSimtTile + kr;
-                bool ok = l < len;
+                const int kr = i / C, c = i % C, l = place_of(tl) + kr;
+                bool ok = l < len && (!LONG || it.wanted(l, 1));
                 int64_t page = 0;
                 if (ok) {
                     page = table[l >> a.page_shift];
@@ -112,7 +127,7 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
             for (int d = 0; d < DJ * 4; ++d) o[i][d] = 0.0f;
         }
         for (int q = 0; q < n; ++q) {
-            const int buf = q & 1, k0 = (tile + q) * kSimtTile;
+            const int buf = q & 1, k0 = place_of(tile + q);
             if (q + 1 < n) load(tile + q + 1, buf ^ 1);
             if (q + 1 < n) cp_async_wait<1>();
             else cp_async_wait<0>();
@@ -136,17 +151,20 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
                         s[i][j] += qq.x * kk[j].x + qq.y * kk[j].y + qq.z * kk[j].z + qq.w * kk[j].w;
                 }
             }
-            const bool tail = k0 + kSimtTile > span.ctx;  // places that not every token sees
+            // places that not every token sees
+            const bool tail = k0 + kSimtTile > span.ctx || (LONG && k0 < it.lo_most);
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
                 const int row = r0 + ty * RT + i, t = row / a.G;
                 const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + min(t, a.T - 1)) * a.T : nullptr;
+                const int first = LONG && tail && t < span.add ? long_first(a, it.s, long_depth(a, b, t)) : 0;
                 unsigned hidden = 0;
                 float top = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     s[i][j] *= a.scale_log2;
-                    if (tail && !(t < span.add && attend_sees(span, mrow, t, k0 + tx + 16 * j))) {
+                    const int l0 = k0 + tx + 16 * j;
+                    if (tail && !(t < span.add && (LONG ? it.sees(a, b, mrow, t, first, l0) : attend_sees(span, mrow, t, l0)))) {
                         s[i][j] = -INFINITY;
                         hidden |= 1u << j;
                     }
@@ -234,7 +252,7 @@ __global__ void __launch_bounds__(kSimtThreads, 1) attend_simt_kernel(const Atte
             if (a.io.lse && tx == 0) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m[i], ll);
         }
         if (!whole && tile == 0 && tid == 0)
-            a.join[blockIdx.x] = make_int4(b, walk.item, walk.segments(cut, blockIdx.x), 0);
+            a.join[blockIdx.x] = make_int4(b, h * groups + group, walk.segments(cut, blockIdx.x), 0);
     }
 }
 
@@ -341,25 +359,32 @@ template <int DT, int D> static cudaError_t launch_join(const AttendArgs& a, cud
     return launch_dependent(attend_join_kernel<DT, D>, dim3(a.ctas, (a.part_rows * (D / 8) + 255) / 256), dim3(256), 0, s, a);
 }
 
-template <int D, int R> static cudaError_t launch_simt(const AttendArgs& a, cudaStream_t s) {
+template <int D, int R, bool LONG> static cudaError_t launch_simt(const AttendArgs& a, cudaStream_t s) {
     const size_t smem = sizeof(SimtSmem<D, R>);
-    cudaError_t err = cudaFuncSetAttribute(attend_simt_kernel<D, R>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    cudaError_t err = cudaFuncSetAttribute(attend_simt_kernel<D, R, LONG>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                            (int)smem);
     if (err != cudaSuccess) return err;
-    return launch_dependent(attend_simt_kernel<D, R>, dim3(a.ctas), dim3(kSimtThreads), smem, s, a);
+    return launch_dependent(attend_simt_kernel<D, R, LONG>, dim3(a.ctas), dim3(kSimtThreads), smem, s, a);
+}
+template <bool LONG> static cudaError_t launch_simt_of(const AttendArgs& a, cudaStream_t s) {
+    if (a.item_rows == 16) return a.D == 64 ? launch_simt<64, 16, LONG>(a, s) : launch_simt<128, 16, LONG>(a, s);
+    return a.D == 64 ? launch_simt<64, 64, LONG>(a, s) : launch_simt<128, 64, LONG>(a, s);
+}
+
+cudaError_t launch_attend_join(const AttendArgs& a, int dtype, cudaStream_t s) {
+    if (dtype == 1) return a.D == 64 ? launch_join<1, 64>(a, s) : launch_join<1, 128>(a, s);
+    return a.D == 64 ? launch_join<0, 64>(a, s) : launch_join<0, 128>(a, s);
 }
 
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s) {
-    cudaError_t err;
-    if (dtype == 1) {
-        err = launch_attend_tc(a, s);
-        if (err != cudaSuccess) return err;
-        return a.D == 64 ? launch_join<1, 64>(a, s) : launch_join<1, 128>(a, s);
-    }
-    if (a.item_rows == 16) err = a.D == 64 ? launch_simt<64, 16>(a, s) : launch_simt<128, 16>(a, s);
-    else err = a.D == 64 ? launch_simt<64, 64>(a, s) : launch_simt<128, 64>(a, s);
-    if (err != cudaSuccess) return err;
-    return a.D == 64 ? launch_join<0, 64>(a, s) : launch_join<0, 128>(a, s);
+    const cudaError_t err = dtype == 1 ? launch_attend_tc(a, s) : launch_simt_of<false>(a, s);
+    return err != cudaSuccess ? err : launch_attend_join(a, dtype, s);
+}
+
+cudaError_t launch_window_attend(const AttendArgs& a, int dtype, cudaStream_t s) {
+    if (dtype == 1) return launch_packed_attend(a, s);
+    const cudaError_t err = launch_simt_of<true>(a, s);
+    return err != cudaSuccess ? err : launch_attend_join(a, dtype, s);
 }
 
 }  // namespace rheo

@@ -6,8 +6,10 @@
 #include <algorithm>
 #include <cstdint>
 #include <cstdlib>
+#include <initializer_list>
 
 #include "cache_kernels.h"
+#include "packed.cuh"
 #include "rheo.h"
 #include "rheo_device.cuh"
 #include "rheo_kernels.h"
@@ -128,6 +130,92 @@ constexpr size_t kLogprobBytes = kLogprobKeysAt + sizeof(unsigned long long) * k
 template <class T> T* at(void* p, size_t off) { return reinterpret_cast<T*>(static_cast<char*>(p) + off); }
 int code(cudaError_t e) { return e == cudaSuccess ? RHEO_OK : RHEO_ELAUNCH; }
 
+// What the attention functions have in common.
+bool attend_ok(const rheo_cache_config* cfg, const rheo_attend_io* io, const rheo_kv* kv, const int32_t* block_table,
+               const int32_t* ctx_len, float scale, const void* scratch) {
+    if (!valid(cfg) || !io || !io->q || !io->out || !block_table || !ctx_len || !scratch) return false;
+    if (!kv_ok(kv, *cfg) || !aligned16(io->q) || !aligned16(io->out)) return false;
+    if (!rows_ok(*cfg, io->q_batch, io->q_token, io->q_head, cfg->q_heads) ||
+        !out_rows_ok(*cfg, io->out_batch, io->out_token, io->out_head, cfg->q_heads))
+        return false;
+    return scale > -INFINITY && scale < INFINITY;
+}
+
+AttendArgs attend_args(const rheo_cache_config& c, const rheo_attend_io& io, const rheo_kv& kv, const int32_t* block_table,
+                       const int32_t* ctx_len, const int32_t* new_len, const uint8_t* mask, float scale, void* scratch) {
+    const CacheLayout L = cache_layout(c);
+    AttendArgs a{};
+    a.B = c.batch;
+    a.T = c.tokens;
+    a.H = c.kv_heads;
+    a.G = c.q_heads / c.kv_heads;
+    a.D = c.head_dim;
+    a.P = c.page_size;
+    a.page_shift = page_shift(c.page_size);
+    a.pages = c.pages;
+    a.max_pages = c.max_pages;
+    a.ctas = kAttendCtas;
+    a.lead = attend_lead(c.dtype);
+    a.least = attend_least(c.dtype);
+    a.item_rows = attend_item_rows(c.dtype, a.T, a.G);
+    a.part_rows = attend_part_rows(c.dtype, a.T, a.G);
+    a.io = io;
+    a.kv = kv;
+    a.block_table = block_table;
+    a.ctx_len = ctx_len;
+    a.new_len = new_len;
+    a.mask = mask;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.part_o = at<float>(scratch, L.part_o);
+    a.part_ml = at<float>(scratch, L.part_ml);
+    a.join = at<int4>(scratch, L.join);
+    a.status = at<unsigned>(scratch, kStatusAt);
+    return a;
+}
+
+bool window_ok(const rheo_window& w) { return w.window >= 0 && w.sinks >= 0; }
+void set_window(AttendArgs& a, const rheo_window& w) {
+    a.window = w.window;
+    a.sinks = w.sinks;
+    a.depth = w.depth;
+}
+
+// The packed pool's configuration beside the 16-bit cache's.
+bool packed_cfg_ok(const rheo_cache_config* c, const rheo_cache_config* p) {
+    return valid(c) && valid(p) && c->dtype == RHEO_BF16 && p->dtype == RHEO_BF16 && c->batch == p->batch &&
+           c->page_size == p->page_size && c->kv_heads == p->kv_heads && c->q_heads == p->q_heads &&
+           c->head_dim == p->head_dim && c->tokens == p->tokens;
+}
+constexpr int64_t kPackedStrideEnd = (int64_t)1 << 39;
+bool packed_stride_ok(int64_t s, int64_t n) { return n == 1 || (s > 0 && s < kPackedStrideEnd && s % 16 == 0); }
+bool packed_ok(const rheo_packed* p, const rheo_cache_config& c) {
+    return p && p->data && aligned16(p->data) && packed_stride_ok(p->page, c.pages) && packed_stride_ok(p->head, c.kv_heads);
+}
+// Layers: their strides, and the last layer's place within 64 bits.
+bool layers_ok(int32_t layers, int64_t key_layer, int64_t value_layer, int64_t packed_layer) {
+    if (layers < 1 || layers > 4096) return false;
+    if (layers == 1) return true;
+    return key_layer > 0 && value_layer > 0 && stride_ok(key_layer, 2, 2) && stride_ok(value_layer, 2, 2) &&
+           packed_stride_ok(packed_layer, 2);
+}
+// A layout that is written: heads, tokens, pages and layers share no memory.  (Spans reach past 64 bits.)
+struct Span {
+    int64_t stride, n;
+};
+bool spans_apart(int64_t line, std::initializer_list<Span> dims) {
+    Span d[4];
+    int k = 0;
+    for (const Span& x : dims)
+        if (x.n > 1) d[k++] = x;
+    std::sort(d, d + k, [](const Span& x, const Span& y) { return x.stride < y.stride; });
+    __int128 span = line;
+    for (int i = 0; i < k; ++i) {
+        if (d[i].stride < span) return false;
+        span += (__int128)(d[i].n - 1) * d[i].stride;
+    }
+    return true;
+}
+
 }  // namespace
 }  // namespace rheo
 
@@ -237,41 +325,134 @@ extern "C" int rheo_qk_norm_rope(const rheo_cache_config* cfg, const rheo_qkv* i
 extern "C" int rheo_tree_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, const rheo_kv* kv,
                                 const int32_t* block_table, const int32_t* ctx_len, const int32_t* new_len,
                                 const uint8_t* mask, float scale, void* scratch, rheo_stream_t stream) {
-    if (!valid(cfg) || !io || !io->q || !io->out || !block_table || !ctx_len || !scratch) return RHEO_EINVAL;
-    if (!kv_ok(kv, *cfg) || !aligned16(io->q) || !aligned16(io->out)) return RHEO_EINVAL;
-    if (!rows_ok(*cfg, io->q_batch, io->q_token, io->q_head, cfg->q_heads) ||
-        !out_rows_ok(*cfg, io->out_batch, io->out_token, io->out_head, cfg->q_heads))
-        return RHEO_EINVAL;
-    if (!(scale > -INFINITY && scale < INFINITY)) return RHEO_EINVAL;
-    const CacheLayout L = cache_layout(*cfg);
-    AttendArgs a{};
-    a.B = cfg->batch;
-    a.T = cfg->tokens;
-    a.H = cfg->kv_heads;
-    a.G = cfg->q_heads / cfg->kv_heads;
-    a.D = cfg->head_dim;
-    a.P = cfg->page_size;
-    a.page_shift = page_shift(cfg->page_size);
-    a.pages = cfg->pages;
-    a.max_pages = cfg->max_pages;
-    a.ctas = kAttendCtas;
-    a.lead = attend_lead(cfg->dtype);
-    a.least = attend_least(cfg->dtype);
-    a.item_rows = attend_item_rows(cfg->dtype, a.T, a.G);
-    a.part_rows = attend_part_rows(cfg->dtype, a.T, a.G);
-    a.io = *io;
-    a.kv = *kv;
-    a.block_table = block_table;
-    a.ctx_len = ctx_len;
-    a.new_len = new_len;
-    a.mask = mask;
-    a.scale_log2 = scale * 1.4426950408889634f;
-    a.part_o = at<float>(scratch, L.part_o);
-    a.part_ml = at<float>(scratch, L.part_ml);
-    a.join = at<int4>(scratch, L.join);
-    a.status = at<unsigned>(scratch, kStatusAt);
+    if (!attend_ok(cfg, io, kv, block_table, ctx_len, scale, scratch)) return RHEO_EINVAL;
+    const AttendArgs a = attend_args(*cfg, *io, *kv, block_table, ctx_len, new_len, mask, scale, scratch);
     const cudaError_t e = launch_attend(a, cfg->dtype == RHEO_BF16 ? 1 : 0, (cudaStream_t)stream);
     return e == cudaErrorInvalidValue ? RHEO_EINVAL : code(e);  // a cache that no tensor map describes
+}
+
+extern "C" int rheo_window_attend(const rheo_cache_config* cfg, const rheo_attend_io* io, const rheo_kv* kv,
+                                  const int32_t* block_table, const int32_t* ctx_len, const int32_t* new_len,
+                                  const uint8_t* mask, const rheo_window* window, float scale, void* scratch,
+                                  rheo_stream_t stream) {
+    if (!attend_ok(cfg, io, kv, block_table, ctx_len, scale, scratch) || !window || !window_ok(*window)) return RHEO_EINVAL;
+    AttendArgs a = attend_args(*cfg, *io, *kv, block_table, ctx_len, new_len, mask, scale, scratch);
+    set_window(a, *window);
+    const cudaError_t e = launch_window_attend(a, cfg->dtype == RHEO_BF16 ? 1 : 0, (cudaStream_t)stream);
+    return e == cudaErrorInvalidValue ? RHEO_EINVAL : code(e);  // a cache that no tensor map describes
+}
+
+extern "C" int rheo_packed_sizes(const rheo_cache_config* packed_cfg, int64_t* page_bytes) {
+    if (!valid(packed_cfg) || packed_cfg->dtype != RHEO_BF16) return RHEO_EINVAL;
+    if (page_bytes) *page_bytes = packed_page_bytes(packed_cfg->page_size, packed_cfg->head_dim);
+    return RHEO_OK;
+}
+
+extern "C" int rheo_packed_attend(const rheo_cache_config* cfg, const rheo_cache_config* packed_cfg,
+                                  const rheo_attend_io* io, const rheo_kv* kv, const int32_t* block_table,
+                                  const int32_t* ctx_len, const int32_t* new_len, const rheo_packed* packed,
+                                  const int32_t* packed_table, const int32_t* n4, const uint8_t* mask,
+                                  const rheo_window* window, float scale, void* scratch, rheo_stream_t stream) {
+    if (!attend_ok(cfg, io, kv, block_table, ctx_len, scale, scratch) || !packed_cfg_ok(cfg, packed_cfg)) return RHEO_EINVAL;
+    if (!packed_ok(packed, *packed_cfg) || !packed_table || !n4 || (window && !window_ok(*window))) return RHEO_EINVAL;
+    if (((int64_t)cfg->max_pages + packed_cfg->max_pages) * cfg->page_size > (int64_t)1 << 30) return RHEO_EINVAL;
+    AttendArgs a = attend_args(*cfg, *io, *kv, block_table, ctx_len, new_len, mask, scale, scratch);
+    if (window) set_window(a, *window);
+    a.packed = *packed;
+    a.table4 = packed_table;
+    a.n_pages4 = n4;
+    a.pages4 = packed_cfg->pages;
+    a.max_pages4 = packed_cfg->max_pages;
+    const cudaError_t e = launch_packed_attend(a, (cudaStream_t)stream);
+    return e == cudaErrorInvalidValue ? RHEO_EINVAL : code(e);
+}
+
+extern "C" int rheo_cache_pack(const rheo_cache_config* cfg, const rheo_cache_config* packed_cfg, int32_t layers,
+                               const rheo_kv* kv, int64_t key_layer, int64_t value_layer, const rheo_packed* packed,
+                               int64_t packed_layer, int32_t keep, const rheo_pages* before, const rheo_pages* before4,
+                               const int32_t* ctx_len, const rheo_pages* after, const rheo_pages* after4,
+                               int32_t* ctx_out, void* scratch, rheo_stream_t stream) {
+    if (!packed_cfg_ok(cfg, packed_cfg) || !kv_ok(kv, *cfg) || !packed_ok(packed, *packed_cfg)) return RHEO_EINVAL;
+    if (!layers_ok(layers, key_layer, value_layer, packed_layer) || keep < 0 || !before || !before4 || !ctx_len || !after ||
+        !after4 || !ctx_out || !scratch)
+        return RHEO_EINVAL;
+    const int64_t page_bytes = packed_page_bytes(packed_cfg->page_size, packed_cfg->head_dim);
+    if (!spans_apart(page_bytes, {{packed->page, packed_cfg->pages}, {packed->head, cfg->kv_heads}, {packed_layer, layers}}))
+        return RHEO_EINVAL;
+    const int64_t B = cfg->batch;
+    const int64_t n[9] = {B * cfg->max_pages, B, cfg->pages, 1, B * packed_cfg->max_pages, B, packed_cfg->pages, 1, B};
+    const int32_t* x[9] = {before->block_table,  before->n_pages,  before->free_list,  before->n_free, before4->block_table,
+                           before4->n_pages, before4->free_list, before4->n_free, ctx_len};
+    const int32_t* y[9] = {after->block_table,  after->n_pages,  after->free_list,  after->n_free, after4->block_table,
+                           after4->n_pages, after4->free_list, after4->n_free, ctx_out};
+    int same = 0;
+    for (int i = 0; i < 9; ++i) {
+        if (!x[i] || !y[i]) return RHEO_EINVAL;
+        same += x[i] == y[i];
+    }
+    if (same != 0 && same != 9) return RHEO_EINVAL;
+    for (int i = 0; i < 9; ++i)
+        for (int j = 0; j < 9; ++j) {
+            if (i != j && (!apart(y[i], n[i], y[j], n[j]))) return RHEO_EINVAL;
+            if (same == 0 && !apart(y[i], n[i], x[j], n[j])) return RHEO_EINVAL;
+        }
+    PackArgs a{};
+    a.B = cfg->batch;
+    a.H = cfg->kv_heads;
+    a.D = cfg->head_dim;
+    a.P = cfg->page_size;
+    a.pages = cfg->pages;
+    a.max_pages = cfg->max_pages;
+    a.pages4 = packed_cfg->pages;
+    a.max_pages4 = packed_cfg->max_pages;
+    a.layers = layers;
+    a.keep = keep;
+    a.in_place = same == 9;
+    a.kv = *kv;
+    a.key_layer = key_layer;
+    a.value_layer = value_layer;
+    a.packed = *packed;
+    a.packed_layer = packed_layer;
+    a.before = *before;
+    a.before4 = *before4;
+    a.after = *after;
+    a.after4 = *after4;
+    a.ctx_len = ctx_len;
+    a.ctx_out = ctx_out;
+    a.plan = at<int32_t>(scratch, kPartsAt);
+    a.status = at<unsigned>(scratch, kStatusAt);
+    return code(launch_pack(a, multiprocessors(), (cudaStream_t)stream));
+}
+
+extern "C" int rheo_cache_unpack(const rheo_cache_config* cfg, const rheo_cache_config* packed_cfg, int32_t layers,
+                                 const rheo_packed* packed, int64_t packed_layer, const rheo_kv* kv, int64_t key_layer,
+                                 int64_t value_layer, int32_t n, const int32_t* src, const int32_t* dst, void* scratch,
+                                 rheo_stream_t stream) {
+    if (!packed_cfg_ok(cfg, packed_cfg) || !kv_ok(kv, *cfg) || !packed_ok(packed, *packed_cfg)) return RHEO_EINVAL;
+    if (!layers_ok(layers, key_layer, value_layer, packed_layer) || n < 0 || (n > 0 && (!src || !dst)) || !scratch)
+        return RHEO_EINVAL;
+    const int64_t P = cfg->page_size, D = cfg->head_dim;
+    if (!spans_apart(D, {{kv->key_page, cfg->pages}, {kv->key_head, cfg->kv_heads}, {kv->key_token, P}, {key_layer, layers}}) ||
+        !spans_apart(D, {{kv->value_page, cfg->pages}, {kv->value_head, cfg->kv_heads}, {kv->value_token, P}, {value_layer, layers}}))
+        return RHEO_EINVAL;
+    if (n == 0) return RHEO_OK;
+    UnpackArgs a{};
+    a.H = cfg->kv_heads;
+    a.D = cfg->head_dim;
+    a.P = cfg->page_size;
+    a.pages = cfg->pages;
+    a.pages4 = packed_cfg->pages;
+    a.layers = layers;
+    a.n = n;
+    a.kv = *kv;
+    a.key_layer = key_layer;
+    a.value_layer = value_layer;
+    a.packed = *packed;
+    a.packed_layer = packed_layer;
+    a.src = src;
+    a.dst = dst;
+    a.status = at<unsigned>(scratch, kStatusAt);
+    return code(launch_unpack(a, multiprocessors(), (cudaStream_t)stream));
 }
 
 extern "C" int rheo_cache_commit(const rheo_cache_config* cfg, int32_t layers, const rheo_kv* kv, int64_t key_layer,

@@ -54,6 +54,30 @@ struct CommitArgs {
     unsigned* status;
 };
 
+struct PackArgs {
+    int B, H, D, P, pages, max_pages, pages4, max_pages4, layers, keep, in_place;
+    rheo_kv kv;
+    int64_t key_layer, value_layer;
+    rheo_packed packed;
+    int64_t packed_layer;
+    rheo_pages before, before4, after, after4;
+    const int32_t* ctx_len;
+    int32_t* ctx_out;
+    int32_t* plan;            // [B + 3] pages packed before each request, then the heights of both stacks
+    unsigned* status;
+};
+
+struct UnpackArgs {
+    int H, D, P, pages, pages4, layers, n;
+    rheo_kv kv;
+    int64_t key_layer, value_layer;
+    rheo_packed packed;
+    int64_t packed_layer;
+    const int32_t* src;
+    const int32_t* dst;
+    unsigned* status;
+};
+
 struct AttendArgs {
     int B, T, H, G, D, P, page_shift, pages, max_pages;
     int ctas;                 // CTAs that share the tiles
@@ -72,6 +96,13 @@ struct AttendArgs {
     float* part_ml;           // [2 * ctas][part_rows][2] running maximum (log2 units) and sum
     int4* join;               // [ctas] the item that a CTA begins and others go on with: request, item, segments
     unsigned* status;
+    // windows and packed pages (rheo_window_attend, rheo_packed_attend)
+    int window, sinks;        // 0: no window
+    const int32_t* depth;     // or null: t
+    rheo_packed packed;       // data null: none
+    const int32_t* table4;
+    const int32_t* n_pages4;
+    int pages4, max_pages4;
 };
 
 struct LogprobArgs {
@@ -91,7 +122,12 @@ struct LogprobArgs {
 cudaError_t launch_reserve(const ReserveArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_rope(const RopeArgs& a, int dtype, int D, bool interleaved, int sms, cudaStream_t s);
 cudaError_t launch_commit(const CommitArgs& a, int line_bytes, cudaStream_t s);
+cudaError_t launch_pack(const PackArgs& a, int sms, cudaStream_t s);
+cudaError_t launch_unpack(const UnpackArgs& a, int sms, cudaStream_t s);
 cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_window_attend(const AttendArgs& a, int dtype, cudaStream_t s);
+cudaError_t launch_packed_attend(const AttendArgs& a, cudaStream_t s);
+cudaError_t launch_attend_join(const AttendArgs& a, int dtype, cudaStream_t s);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s);
 int attend_item_rows(int dtype, int T, int G);
 int attend_part_rows(int dtype, int T, int G);

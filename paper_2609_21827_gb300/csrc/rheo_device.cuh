@@ -39,6 +39,7 @@ enum : uint32_t {
     kStBadLength = 16u,
     kStNoPages = 32u,
     kStBadIndex = 64u,
+    kStBadValue = 128u,
 };
 
 enum : int { kTagSample = 1, kTagVerify = 2, kTagResidual = 3 };

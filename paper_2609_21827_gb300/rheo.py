@@ -18,13 +18,14 @@ RHEO_F32, RHEO_BF16 = 0, 1
 RHEO_OK, RHEO_EINVAL, RHEO_ELAUNCH, RHEO_ETOOLARGE = 0, -1, -2, -3
 VERIFY_RHEO, VERIFY_RRSW, VERIFY_ONEHOT = 0, 1, 2
 STATUS_BAD_LOGIT, STATUS_EMPTY_ROW, STATUS_BAD_TEMPERATURE, STATUS_INTERNAL = 1, 2, 4, 8
-STATUS_BAD_LENGTH, STATUS_NO_PAGES, STATUS_BAD_INDEX = 16, 32, 64
+STATUS_BAD_LENGTH, STATUS_NO_PAGES, STATUS_BAD_INDEX, STATUS_BAD_VALUE = 16, 32, 64, 128
 SLOT_ROOT, SLOT_LEAD, SLOT_SAMPLED, SLOT_FILL = 0, 1, 2, 3
 
 EXPORTS = ("rheo_sizes", "rheo_workspace_init", "rheo_expand", "rheo_prune", "rheo_verify", "rheo_verify_static",
            "rheo_tree_attention", "rheo_verify_variant", "rheo_verify_full",
            "rheo_get_status", "rheo_cache_sizes", "rheo_scratch_init", "rheo_scratch_status", "rheo_cache_reserve",
-           "rheo_qk_norm_rope", "rheo_tree_attend", "rheo_cache_commit", "rheo_logprob_sizes", "rheo_token_logprobs")
+           "rheo_qk_norm_rope", "rheo_tree_attend", "rheo_cache_commit", "rheo_logprob_sizes", "rheo_token_logprobs",
+           "rheo_window_attend", "rheo_packed_sizes", "rheo_cache_pack", "rheo_cache_unpack", "rheo_packed_attend")
 
 
 class RheoError(RuntimeError):
@@ -91,6 +92,14 @@ class _Logprobs(ctypes.Structure):
     _fields_ = [(n, _VP) for n in ("logprob", "rank", "entropy", "top_ids", "top_logprobs")]
 
 
+class _Window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32), ("depth", _VP)]
+
+
+class _Packed(ctypes.Structure):
+    _fields_ = [("data", _VP), ("page", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -137,6 +146,13 @@ def lib():
         L.rheo_logprob_sizes.argtypes = [ctypes.POINTER(_LogprobConfig), ctypes.POINTER(ctypes.c_size_t)]
         L.rheo_token_logprobs.argtypes = [ctypes.POINTER(_LogprobConfig), _VP, i64, i64, _VP, _VP, _VP,
                                           ctypes.POINTER(_Logprobs), _VP, _VP]
+        W, P4 = ctypes.POINTER(_Window), ctypes.POINTER(_Packed)
+        L.rheo_window_attend.argtypes = [K, ctypes.POINTER(_AttendIO), KV, _VP, _VP, _VP, _VP, W, f32, _VP, _VP]
+        L.rheo_packed_sizes.argtypes = [K, ctypes.POINTER(i64)]
+        L.rheo_cache_pack.argtypes = [K, K, i32, KV, i64, i64, P4, i64, i32, PG, PG, _VP, PG, PG, _VP, _VP, _VP]
+        L.rheo_cache_unpack.argtypes = [K, K, i32, P4, i64, KV, i64, i64, i32, _VP, _VP, _VP, _VP]
+        L.rheo_packed_attend.argtypes = [K, K, ctypes.POINTER(_AttendIO), KV, _VP, _VP, _VP, P4, _VP, _VP, _VP, W, f32, _VP,
+                                         _VP]
         for name in EXPORTS:
             getattr(L, name).restype = ctypes.c_int
         _lib = L
@@ -694,3 +710,110 @@ def token_logprobs(cfg: LogprobConfig, logits: torch.Tensor, tokens: torch.Tenso
         cfg._ref, p, max(st[0], V) if n == 1 else st[0], n, _want_opt(rows, "rows", i32, cfg._rows),
         _want(tokens, "tokens", i32, cfg._rows), _want_opt(temperature, "temperature", torch.float32, cfg._groups),
         out.c(cfg), ws.of(cfg), _stream(stream)), "rheo_token_logprobs")
+
+
+# ---------------------------------------------------------------------------
+# Long contexts: attention limited to a window, and caches held in 4 bits (include/rheo.h
+# has the definitions).  A packed pool has a CacheConfig of its own, the cache's but for
+# pages and max_pages, and Pages like any other.
+# ---------------------------------------------------------------------------
+
+def packed_page_bytes(packed_cfg: CacheConfig) -> int:
+    """Bytes of a packed page of one head."""
+    n = ctypes.c_int64()
+    _check(lib().rheo_packed_sizes(packed_cfg._ref, ctypes.byref(n)), "rheo_packed_sizes")
+    return n.value
+
+
+def make_packed(packed_cfg: CacheConfig, layers: int = 1, device="cuda") -> torch.Tensor:
+    """Packed pages [layers, pages, kv_heads, bytes] (uint8), unwritten ones zero."""
+    return torch.zeros((layers, packed_cfg.pages, packed_cfg.kv_heads, packed_page_bytes(packed_cfg)), dtype=torch.uint8,
+                       device=device)
+
+
+def _packed_shape(packed_cfg: CacheConfig) -> tuple:
+    shape = getattr(packed_cfg, "_packed", None)
+    if shape is None:
+        shape = (packed_cfg.pages, packed_cfg.kv_heads, packed_page_bytes(packed_cfg))
+        object.__setattr__(packed_cfg, "_packed", shape)
+    return shape
+
+
+def _window(cfg: CacheConfig, window: int, sinks: int, depth) -> _Window:
+    return _Window(window, sinks, _want_opt(depth, "depth", torch.int32, cfg._each))
+
+
+def _attend_io(cfg: CacheConfig, q: torch.Tensor, out: torch.Tensor, lse) -> _AttendIO:
+    qp, qs = _want_strided(q, "q", cfg.torch_dtype, cfg._q)
+    op, os_ = _want_strided(out, "out", cfg.torch_dtype, cfg._q)
+    return _AttendIO(qp, op, _want_opt(lse, "lse", torch.float32, cfg._lse), qs[0], qs[1], qs[2], os_[0], os_[1], os_[2])
+
+
+def window_attend(cfg: CacheConfig, q: torch.Tensor, key_cache: torch.Tensor, value_cache: torch.Tensor, pages: Pages,
+                  ctx_len: torch.Tensor, out: torch.Tensor, ws: CacheWorkspace, window: int, sinks: int = 0,
+                  depth: torch.Tensor = None, new_len: torch.Tensor = None, mask: torch.Tensor = None,
+                  lse: torch.Tensor = None, scale: float = None, stream=None) -> None:
+    """rheo_window_attend: tree_attend in which a token sees the last `window` positions (its own among them; 0: all) and
+    the first `sinks`; depth [B, T] int32, the new tokens' depths as tree_attention writes them (None: 0, 1, ...)."""
+    i32 = torch.int32
+    _check(lib().rheo_window_attend(
+        cfg._ref, _attend_io(cfg, q, out, lse), _kv(cfg, key_cache, value_cache), pages.table(cfg),
+        _want(ctx_len, "ctx_len", i32, cfg._one), _want_opt(new_len, "new_len", i32, cfg._one),
+        _want_opt(mask, "mask", torch.uint8, cfg._mask), _window(cfg, window, sinks, depth),
+        cfg.head_dim ** -0.5 if scale is None else scale, ws.of(cfg), _stream(stream)), "rheo_window_attend")
+
+
+def packed_attend(cfg: CacheConfig, packed_cfg: CacheConfig, q: torch.Tensor, key_cache: torch.Tensor,
+                  value_cache: torch.Tensor, pages: Pages, ctx_len: torch.Tensor, packed: torch.Tensor, packed_pages: Pages,
+                  out: torch.Tensor, ws: CacheWorkspace, window: int = 0, sinks: int = 0, depth: torch.Tensor = None,
+                  new_len: torch.Tensor = None, mask: torch.Tensor = None, lse: torch.Tensor = None, scale: float = None,
+                  stream=None) -> None:
+    """rheo_packed_attend: attention over packed_pages.n_pages packed pages a request (packed [pages, kv_heads, bytes], one
+    layer) and the ctx_len tokens in 16 bits behind them; the window as in window_attend (0: none)."""
+    i32 = torch.int32
+    pp, ps = _want_strided(packed, "packed", torch.uint8, _packed_shape(packed_cfg))
+    _check(lib().rheo_packed_attend(
+        cfg._ref, packed_cfg._ref, _attend_io(cfg, q, out, lse), _kv(cfg, key_cache, value_cache), pages.table(cfg),
+        _want(ctx_len, "ctx_len", i32, cfg._one), _want_opt(new_len, "new_len", i32, cfg._one), _Packed(pp, ps[0], ps[1]),
+        packed_pages.table(packed_cfg), _want(packed_pages.n_pages, "n_pages", i32, packed_cfg._one),
+        _want_opt(mask, "mask", torch.uint8, cfg._mask), _window(cfg, window, sinks, depth),
+        cfg.head_dim ** -0.5 if scale is None else scale, ws.of(cfg), _stream(stream)), "rheo_packed_attend")
+
+
+def _layers(cfg: CacheConfig, packed_cfg: CacheConfig, key_cache, value_cache, packed) -> tuple:
+    """Layers, key and value caches [layers, pages, kv_heads, page_size, D] and packed pages with their layers' strides."""
+    if key_cache.dim() != 5 or packed.dim() != 4:
+        raise RheoError("caches [layers, pages, kv_heads, page_size, D] and packed pages [layers, pages, kv_heads, bytes] "
+                        "are wanted")
+    n = key_cache.shape[0]
+    kp, ks = _want_strided(key_cache, "key cache", cfg.torch_dtype, (n,) + cfg._pool)
+    vp, vs = _want_strided(value_cache, "value cache", cfg.torch_dtype, (n,) + cfg._pool)
+    pp, ps = _want_strided(packed, "packed", torch.uint8, (n,) + _packed_shape(packed_cfg))
+    return n, _KV(kp, vp, ks[1], ks[2], ks[3], vs[1], vs[2], vs[3]), ks[0], vs[0], _Packed(pp, ps[1], ps[2]), ps[0]
+
+
+def cache_pack(cfg: CacheConfig, packed_cfg: CacheConfig, key_cache: torch.Tensor, value_cache: torch.Tensor,
+               packed: torch.Tensor, pages: Pages, packed_pages: Pages, ctx_len: torch.Tensor, ws: CacheWorkspace,
+               keep: int = 0, out: tuple = None, stream=None) -> None:
+    """rheo_cache_pack: whole pages of the caches [layers, pages, kv_heads, page_size, D] go into 4 bits, all but the last
+    `keep` tokens of a request.  pages, packed_pages and ctx_len are updated in place, or stay as they are and
+    out = (Pages, Pages, ctx_len) receives the new state."""
+    n, kv, kl, vl, p4, pl = _layers(cfg, packed_cfg, key_cache, value_cache, packed)
+    before, before4, ctx = pages.c(cfg), packed_pages.c(packed_cfg), _want(ctx_len, "ctx_len", torch.int32, cfg._one)
+    after, after4, ctx_out = (before, before4, ctx) if out is None else (
+        out[0].c(cfg), out[1].c(packed_cfg), _want(out[2], "ctx_len of out", torch.int32, cfg._one))
+    _check(lib().rheo_cache_pack(cfg._ref, packed_cfg._ref, n, kv, kl, vl, p4, pl, keep, before, before4, ctx, after, after4,
+                                 ctx_out, ws.of(cfg), _stream(stream)), "rheo_cache_pack")
+
+
+def cache_unpack(cfg: CacheConfig, packed_cfg: CacheConfig, packed: torch.Tensor, key_cache: torch.Tensor,
+                 value_cache: torch.Tensor, src: torch.Tensor, dst: torch.Tensor, ws: CacheWorkspace, stream=None) -> None:
+    """rheo_cache_unpack: packed pages src [n] int32 back to pages dst [n] of the caches, in every layer; -1 leaves an
+    entry out."""
+    n, kv, kl, vl, p4, pl = _layers(cfg, packed_cfg, key_cache, value_cache, packed)
+    if src.dim() != 1:
+        raise RheoError("src: [n] is wanted")
+    shape = tuple(src.shape)
+    _check(lib().rheo_cache_unpack(cfg._ref, packed_cfg._ref, n, p4, pl, kv, kl, vl, shape[0],
+                                   _want(src, "src", torch.int32, shape), _want(dst, "dst", torch.int32, shape), ws.of(cfg),
+                                   _stream(stream)), "rheo_cache_unpack")
