@@ -194,6 +194,7 @@ template <int TILE> struct LongItem {
     int ns, w0, n;     // tiles of the sinks, first one of the window, all of the item
     int lo, lo_most;   // first place of the window of any of the item's tokens, and the last such first place
     int sinks;         // places below it are seen whatever the window (0 without one)
+    int sinks_end;     // where the sinks' tiles end: at the last sink, if the window begins behind them
     __device__ __forceinline__ LongItem() {}
     // Rows r0 .. r0 + count - 1 of request b's (token, query head) pairs.
     __device__ __forceinline__ LongItem(const AttendArgs& a, int b, int r0, int count) {
@@ -202,7 +203,7 @@ template <int TILE> struct LongItem {
         const int t0 = r0 / a.G, t1 = min((min(r0 + count, a.T * a.G) - 1) / a.G, s.add - 1);
         ns = n = 1;
         w0 = sinks = 0;
-        lo = lo_most = INT32_MAX;
+        lo = lo_most = sinks_end = INT32_MAX;
         if (t0 >= s.add) return;  // no row is of a token: one tile, of which nothing is seen or read
         lo = lo_most = 0;
         const int hi = a.mask ? s.len() : s.ctx + t1 + 1;
@@ -213,7 +214,9 @@ template <int TILE> struct LongItem {
             sinks = a.sinks;
             if (sinks > 0) ns = index(min(sinks, hi) - 1) + 1;
         }
-        w0 = max(ns, index(min(lo, hi - 1)));
+        const int from = index(min(lo, hi - 1));
+        w0 = max(ns, from);
+        sinks_end = from >= ns ? sinks : INT32_MAX;
         n = ns + index(hi - 1) + 1 - w0;
     }
     __device__ __forceinline__ int index(int place) const {
@@ -223,7 +226,8 @@ template <int TILE> struct LongItem {
     __device__ __forceinline__ bool is_packed(int number) const { return number < np; }
     __device__ __forceinline__ int begin(int number) const { return number < np ? number * TILE : s.pk + (number - np) * TILE; }
     __device__ __forceinline__ int end(int number) const {
-        return number < np ? min(number * TILE + TILE, s.pk) : min(s.pk + (number - np + 1) * TILE, s.len());
+        const int e = number < np ? min(number * TILE + TILE, s.pk) : min(s.pk + (number - np + 1) * TILE, s.len());
+        return number < ns ? min(e, sinks_end) : e;
     }
     __device__ __forceinline__ int packed_tiles() const { return np <= ns ? np : ns + max(0, min(np, w0 - ns + n) - w0); }
     // whether some token of the item may see one of `count` places from `place` on

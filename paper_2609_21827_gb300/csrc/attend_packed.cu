@@ -494,6 +494,10 @@ template <int D, int NT> cudaError_t launch_few(const AttendArgs& a, cudaStream_
 cudaError_t launch_packed_attend(const AttendArgs& in, cudaStream_t s) {
     AttendArgs a = in;
     const int rows = a.T * a.G;
+    if (rows > 16) {
+        const cudaError_t err = launch_packed_tc(a, s);
+        return err != cudaSuccess ? err : launch_attend_join(a, 1, s);
+    }
     const bool one = rows <= 8;
     a.item_rows = one ? 8 : 16;
     a.part_rows = a.item_rows;

@@ -382,8 +382,7 @@ cudaError_t launch_attend(const AttendArgs& a, int dtype, cudaStream_t s) {
 }
 
 cudaError_t launch_window_attend(const AttendArgs& a, int dtype, cudaStream_t s) {
-    if (dtype == 1) return launch_packed_attend(a, s);
-    const cudaError_t err = launch_simt_of<true>(a, s);
+    const cudaError_t err = dtype == 1 ? launch_window_tc(a, s) : launch_simt_of<true>(a, s);
     return err != cudaSuccess ? err : launch_attend_join(a, dtype, s);
 }
 

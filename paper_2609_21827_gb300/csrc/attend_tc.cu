@@ -46,6 +46,7 @@
 #include <cuda_bf16.h>
 
 #include "attend.cuh"
+#include "packed.cuh"
 #include "rheo_kernels.h"
 
 namespace rheo {
@@ -54,7 +55,11 @@ namespace {
 constexpr int kTile = 128;                   // keys a tile: what is loaded at a time
 constexpr int kSub = 64;                     // keys of a score product: half a tile
 constexpr int kScores = 2;                   // score buffers of a stream
-constexpr int kTcThreads = 12 * 32;
+constexpr int kTcThreads = 12 * 32, kTcPackedThreads = 16 * 32;
+__host__ __device__ constexpr int tc_threads(int kind) { return kind == 2 ? kTcPackedThreads : kTcThreads; }
+// Registers a thread where sixteen warps share them: softmax groups, warps that load and issue, warps that expand packed tiles.
+constexpr int kSoftmaxRegs = 168, kIssueRegs = 72, kExpandRegs = 104, kPackedLaunchRegs = 128;
+static_assert(2 * kSoftmaxRegs + kIssueRegs + kExpandRegs <= 4 * kPackedLaunchRegs);
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
 constexpr int kDrainLimit = 1 << 16;         // and of a drain after that
@@ -215,10 +220,57 @@ __device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap* map, i
         : "memory");
 }
 
-// Score products of tile `tile` of an item of `len` places: the second half only where it has a place.
-__device__ __forceinline__ int tc_subs(int len, int tile) { return len - tile * kTile > kSub ? 2 : 1; }
-
 using TcWalk = AttendWalk<kTile>;
+
+// kWhole: a class is a request, and an item walks all its places.  kWindow, kPacked: classes and tiles of LongItem.
+enum { kWhole, kWindow, kPacked };
+
+// One item: request, key/value head, first query row, lengths (ctx: all cached tokens), and its tiles.
+template <int KIND> struct TcItem {
+    int b, h, r0;
+    AttendSpan s;
+    LongItem<kTile> it;
+    __device__ __forceinline__ TcItem() {}
+    __device__ __forceinline__ TcItem(const AttendArgs& a, int cls, int item, int groups, int item_rows) {
+        if constexpr (KIND == kWhole) {
+            b = cls;
+            h = item / groups;
+            r0 = item % groups * item_rows;
+            s = attend_span(a, b);
+        } else {
+            b = cls / groups;
+            h = item;
+            r0 = cls % groups * item_rows;
+            it = LongItem<kTile>(a, b, r0, item_rows);
+            s = AttendSpan{it.s.ctx, it.s.add, it.s.bad};
+        }
+    }
+    __device__ __forceinline__ void open(TcWalk& w) const {
+        if constexpr (KIND == kWhole) w.open(s.len());
+        else w.open_tiles(it.n);
+    }
+    // of the item's i-th tile
+    __device__ __forceinline__ int begin(int i) const { return KIND == kWhole ? i * kTile : it.begin(it.number(i)); }
+    __device__ __forceinline__ int end(int i) const { return KIND == kWhole ? s.len() : it.end(it.number(i)); }
+    __device__ __forceinline__ bool packed(int i) const { return KIND == kPacked && it.is_packed(it.number(i)); }
+    // score products: the second half only where it has a place
+    __device__ __forceinline__ int subs(int i) const { return end(i) - begin(i) > kSub ? 2 : 1; }
+    // LONG: whether a tile of 16 bits has places that not all of the item's tokens see (or nobody).  chain: they see all
+    // drafted tokens up to the first of them.
+    __device__ __forceinline__ bool unclear(bool chain, int place, int end, int G) const {
+        return place + kTile > min(end, chain ? s.ctx + r0 / G + 1 : s.ctx) || place < it.lo_most;
+    }
+    // Whether some of n tiles from the i-th on has a second half: only the last ones of the sinks and of both parts may lack it.
+    __device__ __forceinline__ bool second(int i, int n) const {
+        if constexpr (KIND == kWhole) return n > 1 || subs(i) == 2;
+        bool any = false;
+        for (int k = 0; k < min(n, 4); ++k) any |= subs(i + k) == 2;
+        return any;
+    }
+};
+template <int KIND> __device__ __forceinline__ int tc_per(const AttendArgs& a, int groups) {
+    return KIND == kWhole ? a.H * groups : a.H;
+}
 
 __device__ __forceinline__ float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 
@@ -249,18 +301,24 @@ __device__ __forceinline__ void tc_queries(const AttendArgs& a, int b, int h, in
 
 // Which of the 64 places from the j0-th drafted token on the tokens tt0 .. t_last see, a vote a word; the lane of token t
 // keeps its words.  TOKENS at a time, so that as many loads are under way.
-template <int TOKENS>
-__device__ __forceinline__ void tc_votes(const AttendArgs& a, const AttendSpan& span, int b, int j0, int tt0, int t_last, int t,
+template <int TOKENS, int KIND>
+__device__ __forceinline__ void tc_votes(const AttendArgs& a, const TcItem<KIND>& item, int j0, int tt0, int t_last, int t,
                                          uint32_t (&words)[2]) {
-    const int lane = threadIdx.x & 31;
+    const int lane = threadIdx.x & 31, b = item.b;
+    const AttendSpan span = item.s;
     for (int tt = tt0; tt <= t_last; tt += TOKENS) {
         bool sees[TOKENS][2];
 #pragma unroll
         for (int u = 0; u < TOKENS; ++u) {
-            const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + min(tt + u, t_last)) * a.T : nullptr;
+            const int tok = min(tt + u, t_last);
+            const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + tok) * a.T : nullptr;
+            const int first = KIND == kWhole ? 0 : long_first(a, item.it.s, long_depth(a, b, tok));
 #pragma unroll
-            for (int v = 0; v < 2; ++v)
-                sees[u][v] = tt + u < span.add && attend_sees(span, mrow, tt + u, span.ctx + j0 + 32 * v + lane);
+            for (int v = 0; v < 2; ++v) {
+                const int place = span.ctx + j0 + 32 * v + lane;
+                if constexpr (KIND == kWhole) sees[u][v] = tt + u < span.add && attend_sees(span, mrow, tt + u, place);
+                else sees[u][v] = tt + u < span.add && place >= span.ctx && item.it.sees(a, b, mrow, tt + u, first, place);
+            }
         }
 #pragma unroll
         for (int u = 0; u < TOKENS; ++u)
@@ -272,13 +330,18 @@ __device__ __forceinline__ void tc_votes(const AttendArgs& a, const AttendSpan& 
     }
 }
 
+// The n lowest of 64 bits.
+__device__ __forceinline__ unsigned long long low_bits(int n) {
+    return n >= 64 ? ~0ull : n <= 0 ? 0ull : (1ull << n) - 1;
+}
+
 // The softmax group of stream `st`.
-template <int D, bool PAIR>
+template <int D, bool PAIR, int KIND>
 __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, char* q_smem, char* v_ring, char* merge, int st) {
     using S = TcShape<D, PAIR>;
     const int tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
-              per = a.H * groups;
+              per = tc_per<KIND>(a, groups);
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t t_s = c.tmem + lanes + st * 128, t_o = c.tmem + lanes + S::kO + st * D;
     const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);  // above 0, so that hidden places stay at -inf
@@ -291,22 +354,22 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         return bar_wait(&c.all_sync, syncs++ & 1, c);
     };
     // queries of an item: each stream's group fetches its own rows (PAIR), or stream 0's all of them
-    auto fetch = [&](int b, int item) {
-        const int h = item / groups, first = item % groups * item_rows + (PAIR ? st * 128 : 0);
-        tc_queries<D>(a, b, h, first, min(128, rows - first), q_smem + (PAIR ? st * S::kQ : 0), tid, 128);
+    auto fetch = [&](const TcItem<KIND>& x) {
+        const int first = x.r0 + (PAIR ? st * 128 : 0);
+        tc_queries<D>(a, x.b, x.h, first, min(128, rows - first), q_smem + (PAIR ? st * S::kQ : 0), tid, 128);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     TcWalk w(c.cut);
-    AttendSpan next_span{0, 0, false};
+    TcItem<KIND> next;
     if (w.more()) {
-        next_span = attend_span(a, w.b);
-        if (PAIR || st == 0) fetch(w.b, w.item);
+        next = TcItem<KIND>(a, w.b, w.item, groups, item_rows);
+        if (PAIR || st == 0) fetch(next);
     }
     while (w.more()) {
-        const AttendSpan span = next_span;
-        const int len = span.len();
-        w.open(len);
-        const int n = w.n, h = w.item / groups, r0 = w.item % groups * item_rows;
+        const TcItem<KIND> item = next;
+        const AttendSpan span = item.s;
+        item.open(w);
+        const int n = w.n, b = item.b, h = item.h, r0 = item.r0;
         if (span.bad && threadIdx.x == 0) atomicOr(a.status, kStBadLength);
         if (!sync_all()) return;  // both streams are through with the last item
         // and the scores' warp has seen its start (it has to meet every phase of q_ready)
@@ -318,22 +381,32 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         tc_fence_before();
         bar_arrive_warp(&c.q_ready);
         const bool last = w.last();
-        const int next_b = w.item + 1 == per ? w.b + 1 : w.b, next_item = w.item + 1 == per ? 0 : w.item + 1;
-        if (!last) next_span = attend_span(a, next_b);
+        if (!last)
+            next = TcItem<KIND>(a, w.item + 1 == per ? w.b + 1 : w.b, w.item + 1 == per ? 0 : w.item + 1, groups, item_rows);
         ++items;
 
         const int row = r0 + (PAIR ? st * 128 : 0) + tid, t = row / a.G;
         const bool live = row < rows && t < span.add;
         const bool warp_live = __any_sync(0xffffffffu, live);
         const bool stream_live = PAIR ? r0 + st * 128 < rows : true;
-        if (PAIR && !stream_live && !last) fetch(next_b, next_item);
-        if (a.T <= 64 && (w.b != seen_b || r0 != seen_r0) && warp_live) {
+        if (PAIR && !stream_live && !last) fetch(next);
+        const int t_first = (row - lane) / a.G, t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);  // of the warp
+        // LONG: what a row sees is places [first, upto) and those below the sinks' end, without a mask and depths of its own
+        // also among the drafted tokens; the warp's rows all see places [all_from, all_to)
+        const bool chain = KIND != kWhole && !a.mask && (!a.depth || !a.window);
+        int first = 0, upto = 0, all_from = 0, all_to = 0;
+        if constexpr (KIND != kWhole) {
+            if (live) first = long_first(a, item.it.s, long_depth(a, b, t));
+            upto = chain ? span.ctx + t + 1 : span.ctx;
+            all_to = chain ? span.ctx + t_first + 1 : span.ctx;
+            all_from = a.depth ? item.it.lo_most : long_first(a, item.it.s, t_last);
+        }
+        if (a.T <= 64 && !chain && (b != seen_b || r0 != seen_r0) && warp_live) {
             // which drafted tokens the row sees: once for all heads of a request
             uint32_t x[2] = {0u, 0u};
-            const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
-            tc_votes<8>(a, span, w.b, 0, (row - lane) / a.G, t_last, t, x);
+            tc_votes<8>(a, item, 0, t_first, t_last, t, x);
             seen = ((unsigned long long)x[1] << 32) | x[0];
-            seen_b = w.b;
+            seen_b = b;
             seen_r0 = r0;
         }
         // Values of the tile at place k0 (tile u of this CTA) before a product of this stream reads them: nothing behind
@@ -344,7 +417,8 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         // products ago (its buffer), which read tile u - 2 or a later one if it is of this item; if it is of an earlier
         // one, u - 2 is too, and stream 0, which reads every tile, has waited for that item's last product before this
         // item began.  The phase after needs this stream's product with tile u, which waits for what follows here.
-        auto clean = [&](int k0, uint32_t u) -> bool {
+        // LONG: nothing that no token of the item sees, and no element that is not finite where some may not see the place.
+        auto clean = [&](int k0, int end, uint32_t u) -> bool {
             if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) return false;
             constexpr int pieces = PAIR ? D / 8 : D / 16;
             const int r = PAIR ? tid : st * kSub + tid / 2, p0 = PAIR ? 0 : tid % 2 * pieces, place = k0 + r;
@@ -353,10 +427,10 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 const int p = p0 + i;
                 return reinterpret_cast<uint4*>(line + (p >> 3) * 16384 + (((p & 7) ^ (r & 7)) << 4));
             };
-            if (place >= len) {
+            if (place >= end || (KIND != kWhole && !item.it.wanted(place, 1))) {
 #pragma unroll
                 for (int i = 0; i < pieces; ++i) *piece(i) = make_uint4(0, 0, 0, 0);
-            } else if (place >= span.ctx) {
+            } else if (place >= span.ctx || (KIND != kWhole && place < item.it.lo_most)) {
                 // 0 * v summed over the line is NaN exactly if some element is not finite
                 const __nv_bfloat162 zero = __floats2bfloat162_rn(0.0f, 0.0f);
                 __nv_bfloat162 acc = zero;
@@ -370,7 +444,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 }
                 if (!(__low2float(acc) == 0.0f && __high2float(acc) == 0.0f)) {
                     const int j = place - span.ctx;
-                    atomicOr(&c.odd[j >> 5], 1u << (j & 31));
+                    if (KIND == kWhole) atomicOr(&c.odd[j >> 5], 1u << (j & 31));
                     c.any_odd = 1;
                     __threadfence_block();  // the other stream's group finds either the elements or the mark
 #pragma unroll 1
@@ -387,12 +461,30 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         float m = -INFINITY, l = 0.0f;
         int mine = 0;  // score products of this stream in this item so far
         for (int q = 0; q < n && stream_live; ++q) {
-            const int tile_k0 = (w.tile + q) * kTile, subs = tc_subs(len, w.tile + q);
+            const int tile_k0 = item.begin(w.tile + q), end = item.end(w.tile + q), subs = item.subs(w.tile + q);
+            // places that not all of the item's tokens see, in 16 bits
+            const bool to_clean = KIND == kWhole ? tile_k0 + kTile > span.ctx
+                                                 : !item.packed(w.tile + q) && item.unclear(chain, tile_k0, end, a.G);
             for (int sub = PAIR ? 0 : st; sub < subs; sub += PAIR ? 1 : 2) {
                 const int k0 = tile_k0 + sub * kSub;
-                const bool tail = k0 + kSub > span.ctx;
+                const bool tail = KIND == kWhole ? k0 + kSub > span.ctx : k0 + kSub > min(end, all_to) || k0 < all_from;
                 uint32_t vis[2] = {0xffffffffu, 0xffffffffu};
-                if (tail && warp_live) {
+                if (KIND != kWhole && tail && warp_live) {
+                    unsigned long long x = low_bits(min(end, upto) - k0) & (~low_bits(first - k0) | low_bits(item.it.sinks - k0));
+                    const int off = k0 - span.ctx;
+                    if (!chain && off > -kSub && !item.packed(w.tile + q)) {
+                        // drafted tokens by the mask, their depths and the window
+                        if (a.T <= 64) {
+                            x |= off >= 0 ? (off < 64 ? seen >> off : 0ull) : seen << -off;
+                        } else {
+                            uint32_t y[2] = {0u, 0u};
+                            tc_votes<8>(a, item, off, t_first, t_last, t, y);
+                            x |= ((unsigned long long)y[1] << 32) | y[0];
+                        }
+                    }
+                    vis[0] = (uint32_t)x;
+                    vis[1] = (uint32_t)(x >> 32);
+                } else if (tail && warp_live) {
                     if (a.T <= 64) {
                         // seen: bit j is drafted token j; bits below it are the cached places
                         const int off = k0 - span.ctx;
@@ -401,15 +493,14 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                         vis[0] = (uint32_t)x;
                         vis[1] = (uint32_t)(x >> 32);
                     } else {
-                        const int t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);
-                        tc_votes<8>(a, span, w.b, k0 - span.ctx, (row - lane) / a.G, t_last, t, vis);
+                        tc_votes<8>(a, item, k0 - span.ctx, t_first, t_last, t, vis);
                     }
                 }
                 const uint32_t buf = products & 1, t_b = t_s + 64 * buf;
                 if (!bar_wait(&c.s_full[st][buf], (products / 2) & 1, c)) return;
                 tc_fence_after();
                 // the item's last scores are there: this stream's queries have been read
-                if (PAIR && q == n - 1 && sub == subs - 1 && !last) fetch(next_b, next_item);
+                if (PAIR && q == n - 1 && sub == subs - 1 && !last) fetch(next);
                 __syncwarp();
                 if (warp_live) {
                     uint32_t s[2][32];
@@ -483,8 +574,8 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                     l += f2_fold(f2_add(f2_add(sum[0], sum[1]), f2_add(sum[2], sum[3])));
                     tc_wait_st();
                 }
-                if ((!PAIR || sub == 0) && tile_k0 + kTile > span.ctx) {
-                    if (!clean(tile_k0, tile0 + q)) return;
+                if ((!PAIR || sub == 0) && to_clean) {
+                    if (!clean(tile_k0, end, tile0 + q)) return;
                 }
                 tc_fence_before();
                 bar_arrive_warp(&c.p_ready[st][buf]);
@@ -506,7 +597,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         const bool whole = n == w.all;
         const int64_t part = attend_part(blockIdx.x, w.tile == 0);
         const int r_in = (PAIR ? st * 128 : 0) + tid, head = h * a.G + row - t * a.G;
-        const bool both = !PAIR && (n > 1 || tc_subs(len, w.tile) == 2);  // stream 1 has a share of the sums
+        const bool both = !PAIR && item.second(w.tile, n);               // stream 1 has a share of the sums
         float f0 = 1.0f, f1 = 0.0f;                                      // the weights of the two streams
         int columns = D;             // that the streams exchange at a time
         const int kept = PAIR ? 128 : min(128, (rows + 31) / 32 * 32);  // rows of an item, to whole warps
@@ -516,7 +607,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         } else if (!PAIR && st == 1) {
             columns = 0;
         }
-        if (!PAIR && !both && st == 0 && !last) fetch(next_b, next_item);
+        if (!PAIR && !both && st == 0 && !last) fetch(next);
         float4* pass = reinterpret_cast<float4*>(merge);  // [columns / 4][kept]
         float ll = live ? l : 0.0f;
         for (int d0 = 0; d0 < D && columns > 0; d0 += columns) {
@@ -536,7 +627,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 }
                 if (!sync_all()) return;
                 if (st == 0 && d0 == 0) {
-                    if (!last) fetch(next_b, next_item);  // both streams are through with the queries
+                    if (!last) fetch(next);  // both streams are through with the queries
                     const float2 x = c.ml[tid];
                     const float mm = fmaxf(m, x.x), ref = mm == -INFINITY ? 0.0f : mm;
                     f0 = fast_exp2(m - ref);
@@ -575,28 +666,39 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                         for (int i = 0; i < 32; ++i) o[i] = 0.0f;
                     }
                     if (odd && live) {
-                        // drafted values that are not finite, for the rows that see them
-                        const uint8_t* mrow = a.mask ? a.mask + ((int64_t)w.b * a.T + t) * a.T : nullptr;
-                        for (int word = 0; word < (span.add + 31) / 32; ++word) {
-                            for (uint32_t bits = c.odd[word]; bits; bits &= bits - 1) {
-                                const int j = word * 32 + __ffs(bits) - 1, x = span.ctx + j;
-                                if (!(mrow ? mrow[j] != 0 : j <= t)) continue;
-                                const int64_t page = a.block_table[(int64_t)w.b * a.max_pages + (x >> a.page_shift)];
-                                if (page < 0 || page >= a.pages) continue;
-                                const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.kv.value) +
-                                                         page * a.kv.value_page + h * a.kv.value_head +
-                                                         (x & (a.P - 1)) * a.kv.value_token + d;
+                        // values that are not finite, for the rows that see their places
+                        const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + t) * a.T : nullptr;
+                        auto add_odd = [&](int x) {  // place x in the pages of 16 bits
+                            const int64_t page = a.block_table[(int64_t)b * a.max_pages + (x >> a.page_shift)];
+                            if (page < 0 || page >= a.pages) return;
+                            const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(a.kv.value) + page * a.kv.value_page +
+                                                     h * a.kv.value_head + (x & (a.P - 1)) * a.kv.value_token + d;
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) {
-                                    const float y = __bfloat162float(v[i]);
-                                    if (!(fabsf(y) < INFINITY)) o[i] += y;
+                            for (int i = 0; i < 32; ++i) {
+                                const float y = __bfloat162float(v[i]);
+                                if (!(fabsf(y) < INFINITY)) o[i] += y;
+                            }
+                        };
+                        if constexpr (KIND == kWhole) {
+                            for (int word = 0; word < (span.add + 31) / 32; ++word) {
+                                for (uint32_t bits = c.odd[word]; bits; bits &= bits - 1) {
+                                    const int j = word * 32 + __ffs(bits) - 1;
+                                    if (mrow ? mrow[j] != 0 : j <= t) add_odd(span.ctx + j);
                                 }
+                            }
+                        } else {
+                            for (int i = w.tile; i < w.tile + n; ++i) {
+                                if (item.packed(i) || !item.unclear(chain, item.begin(i), item.end(i), a.G)) continue;
+                                for (int l0 = item.begin(i); l0 < item.end(i); ++l0)
+                                    if ((l0 >= span.ctx || l0 < item.it.lo_most) && item.it.wanted(l0, 1) &&
+                                        item.it.sees(a, b, mrow, t, first, l0))
+                                        add_odd(l0 - item.it.s.pk);
                             }
                         }
                     }
                     // (no lane leaves the iteration early: the next one begins with a warp-wide load)
                     if (row < rows && whole) {
-                        uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.io.out) + w.b * a.io.out_batch +
+                        uint4* out = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(a.io.out) + b * a.io.out_batch +
                                                               t * a.io.out_token + head * a.io.out_head + d);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
@@ -622,39 +724,44 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         }
         if ((PAIR || st == 0) && row < rows) {
             if (whole) {
-                if (a.io.lse) a.io.lse[((int64_t)w.b * a.T + t) * a.H * a.G + head] = attend_lse(m, ll);
+                if (a.io.lse) a.io.lse[((int64_t)b * a.T + t) * a.H * a.G + head] = attend_lse(m, ll);
             } else {
                 // a row past the request's tokens follows its query, whatever that holds: its reference is not kept
                 *reinterpret_cast<float2*>(a.part_ml + (part * a.part_rows + r_in) * 2) = make_float2(live ? m : -INFINITY, ll);
             }
         }
         if (!whole && w.tile == 0 && threadIdx.x == 0)
-            a.join[blockIdx.x] = make_int4(w.b, w.item, w.segments(c.cut, blockIdx.x), 0);
+            a.join[blockIdx.x] = make_int4(b, h * groups + r0 / item_rows, w.segments(c.cut, blockIdx.x), 0);
         w.next(per);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Key tiles, or value tiles, into their ring: lane = (page, half) of a tile.
-template <int D, bool PAIR, int SLOTS>
+template <int D, bool PAIR, int SLOTS, int KIND>
 __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const CUtensorMap* map, char* ring,
                                         unsigned long long* full, unsigned long long* empty, bool report) {
     using S = TcShape<D, PAIR>;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
-              per = a.H * groups;
+              per = tc_per<KIND>(a, groups);
     const int boxes = kTile / a.P * S::kHalves;
     const int pi = lane / S::kHalves, half = lane % S::kHalves;
     uint32_t u = 0;
     for (TcWalk w(c.cut); w.more();) {
-        const int len = attend_span(a, w.b).len(), h = w.item / groups;
-        w.open(len);
+        const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);
+        const int h = item.h;
+        item.open(w);
         const int n = w.n;
-        const int32_t* table = a.block_table + (int64_t)w.b * a.max_pages;
+        const int32_t* table = a.block_table + (int64_t)item.b * a.max_pages;
+        // whether a token may see some of this lane's places of the tile, which begin at l0
+        auto wants = [&](int i, int& l0) {
+            l0 = item.begin(i) + pi * a.P;
+            return lane < boxes && l0 < item.end(i) && (KIND == kWhole || (!item.packed(i) && item.it.wanted(l0, a.P)));
+        };
         auto page_of = [&](int q) {
-            const int l0 = (w.tile + q) * kTile + pi * a.P;
-            int page = a.pages;  // past the pool: reads as zeros
-            if (q < n && lane < boxes && l0 < len) page = table[l0 >> a.page_shift];
+            int page = a.pages, l0;  // past the pool: reads as zeros
+            if (q < n && wants(w.tile + q, l0)) page = table[(KIND == kWhole ? l0 : l0 - item.it.s.pk) >> a.page_shift];
             return page;
         };
         int page = page_of(0);
@@ -662,6 +769,11 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
             const int next = page_of(q + 1);
             const int slot = u % SLOTS;
             if (u >= SLOTS && !bar_wait(&empty[slot], (u / SLOTS - 1) & 1, c)) goto out;
+            if (item.packed(w.tile + q)) {  // tc_expand's
+                if (lane == 0) bar_arrive(&full[slot]);
+                page = next;
+                continue;
+            }
             if (lane == 0) bar_expect(&full[slot], S::kUnit);
             __syncwarp();
             if (page < 0 || page > a.pages) {
@@ -669,7 +781,8 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
                 page = a.pages;
             }
             if (lane < boxes) {
-                if (report && page == a.pages && (w.tile + q) * kTile + pi * a.P < len) atomicOr(a.status, kStBadIndex);
+                int l0;
+                if (report && page == a.pages && wants(w.tile + q, l0)) atomicOr(a.status, kStBadIndex);
                 tma_tile(smem_u32(ring + slot * S::kUnit + half * 16384 + pi * a.P * 128), map, half * 64, h, page, &full[slot]);
             }
             page = next;
@@ -701,25 +814,25 @@ template <bool PAIR> __device__ __forceinline__ bool tc_has(int st, int sub, int
 }
 
 // The score products of both streams, tile after tile.
-template <int D, bool PAIR>
+template <int D, bool PAIR, int KIND>
 __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, char* q_smem, char* k_ring) {
     using S = TcShape<D, PAIR>;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
-              per = a.H * groups;
+              per = tc_per<KIND>(a, groups);
     const uint32_t t_s = uniform(c.tmem), q_at = uniform(smem_u32(q_smem)), ring = uniform(smem_u32(k_ring));
     uint32_t items = 0, done[2] = {0, 0};
     TcSlot<S::kK> at;
     for (TcWalk w(c.cut); w.more(); ++items) {
-        const int len = attend_span(a, w.b).len();
-        w.open(len);
+        const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);
+        item.open(w);
         const int n = w.n;
-        const bool second = PAIR && w.item % groups * item_rows + 128 < rows;  // stream 1 has rows
+        const bool second = PAIR && item.r0 + 128 < rows;  // stream 1 has rows
         if (!bar_wait(&c.q_ready, items & 1, c)) goto out;
         tc_fence_after();
         if (lane == 0) bar_arrive(&c.q_taken);
         for (int q = 0; q < n; ++q, at.next()) {
-            const int subs = tc_subs(len, w.tile + q);
+            const int subs = item.subs(w.tile + q);
             if (!bar_wait(&c.full_k[at.slot], at.parity, c)) goto out;
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub)
@@ -758,21 +871,23 @@ out:
 }
 
 // The products of weights and values of both streams.
-template <int D, bool PAIR>
+template <int D, bool PAIR, int KIND>
 __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char* v_ring) {
     using S = TcShape<D, PAIR>;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
-              per = a.H * groups;
+              per = tc_per<KIND>(a, groups);
     const uint32_t t_s = uniform(c.tmem), ring = uniform(smem_u32(v_ring));
     uint32_t done[2] = {0, 0};
     TcSlot<S::kV> at;
     for (TcWalk w(c.cut); w.more();) {
-        const int len = attend_span(a, w.b).len();
-        w.open(len);
+        const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);
+        item.open(w);
         const int n = w.n;
-        const bool second = PAIR && w.item % groups * item_rows + 128 < rows;
+        const bool second = PAIR && item.r0 + 128 < rows;
+        uint32_t begun[2] = {0, 0};
         for (int q = 0; q < n; ++q, at.next()) {
-            const int subs = tc_subs(len, w.tile + q);
+            const int subs = item.subs(w.tile + q);
+            const bool packed = item.packed(w.tile + q);
             if (!bar_wait(&c.full_v[at.slot], at.parity, c)) goto out;
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub)
@@ -783,14 +898,22 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
                     if (!bar_wait(&c.p_ready[st][buf], (done[st] / 2) & 1, c)) goto out;
                     ++done[st];
                     tc_fence_after();
-                    const uint32_t v_at = uniform(ring + at.slot * S::kUnit) + sub * kSub * 128;
+                    // 16 bits: a line a token, the halves' lines one behind the other; packed: a line a channel, a half of
+                    // the tokens behind the other
+                    const uint32_t v_at = uniform(ring + at.slot * S::kUnit) + sub * (packed ? D : kSub) * 128;
                     const uint32_t p_at = uniform(t_s + st * 128 + 64 * buf);
-                    const bool add = uniform((PAIR ? sub > 0 : 0) | q);  // the first of an item starts the sums
+                    const bool add = KIND == kWhole ? uniform((PAIR ? sub > 0 : 0) | q) : uniform(begun[st]);  // the first of an item starts the sums
+                    begun[st] = 1;
                     if (elect_one()) {
 #pragma unroll
-                        for (int i = 0; i < kSub / 16; ++i)
-                            mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024),
-                                   mma_desc(D, true), i > 0 || add);
+                        for (int i = 0; i < kSub / 16; ++i) {
+                            if (KIND == kPacked && packed)
+                                mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * 32, 16, 1024),
+                                       mma_desc(D, false), i > 0 || add);
+                            else
+                                mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024),
+                                       mma_desc(D, true), i > 0 || add);
+                        }
                         tc_commit(&c.pv_done[st][buf]);
                     }
                     __syncwarp();
@@ -807,8 +930,95 @@ out:
     bar_wait<true>(&c.drained[1], 0, c);
 }
 
-template <int D, bool PAIR>
-__global__ void __launch_bounds__(kTcThreads, 1)
+// Packed tiles into both rings, as the products read them: warps 0, 1 of four the keys (a line a token), 2, 3 the values (a
+// line a channel, so that the tokens, whose pairs share a word, lie side by side).  A warp takes every second
+// pair of patches of 32 tokens and 32 channels; lanes of even r take the first patch of a pair first, the others the second,
+// which keeps the stores of eight lanes in different banks.
+template <int D, bool PAIR, int SLOTS, bool KEYS>
+__device__ __forceinline__ void tc_expand(const AttendArgs& a, TcControl& c, char* ring, unsigned long long* full,
+                                          unsigned long long* empty) {
+    using S = TcShape<D, PAIR>;
+    const int lane = threadIdx.x & 31, r = lane >> 2, t4 = lane & 3, half = threadIdx.x >> 5 & 1;
+    const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
+              per = tc_per<kPacked>(a, groups);
+    const int N = packed_tokens(a.P), block_bytes = packed_block_bytes(N, D);
+    constexpr int X = D / 32, kPatches = 4 * X / 2;  // of a warp
+    // the lane's place in a block, its first patch of 32 channels
+    const int sub_block = N == 16 ? (KEYS ? r >> 2 : t4 >> 1) : 0;
+    const int code_at = KEYS ? ((N == 16 ? r & 3 : r) * 4 + t4) * 16
+                             : N * D / 2 + (r * (N / 8) + (N == 16 ? t4 & 1 : t4)) * 16;
+    const int scale_at = KEYS ? N * D + 8 * t4 : N * D + D + 8 * (N == 16 ? t4 & 1 : t4);
+    uint32_t u = 0;
+    for (TcWalk w(c.cut); w.more(); w.next(per)) {
+        const TcItem<kPacked> item(a, w.b, w.item, groups, item_rows);
+        item.open(w);
+        const int32_t* table = a.table4 + (int64_t)item.b * a.max_pages4;
+        for (int q = 0; q < w.n; ++q, ++u) {
+            const int slot = u % SLOTS;
+            const bool packed = item.packed(w.tile + q);
+            uint4 words[kPatches];
+            uint2 scales[kPatches];
+            if (packed) {
+                // where the tile's runs of 32 tokens lie: the lane's block of each
+                const int k0 = item.begin(w.tile + q);
+                const uint8_t* block[4];
+#pragma unroll
+                for (int run = 0; run < 4; ++run) {
+                    const int place = k0 + 32 * run + 16 * sub_block;
+                    block[run] = nullptr;
+                    if (place >= item.it.s.pk || !item.it.wanted(place, N)) continue;
+                    const int page = table[place >> a.page_shift];
+                    if (page < 0 || page >= a.pages4) {
+                        if (KEYS) atomicOr(a.status, kStBadIndex);
+                        continue;
+                    }
+                    block[run] = a.packed.data + page * a.packed.page + item.h * a.packed.head + (place & (a.P - 1)) / N * block_bytes;
+                }
+#pragma unroll
+                for (int i = 0; i < kPatches; ++i) {
+                    // pair i / 2 of this warp; keys: neighbouring channels, values: neighbouring tokens
+                    const int pair = 2 * (i / 2) + half, second = (i ^ r) & 1;
+                    const int x = KEYS ? 2 * (pair % (X / 2)) + second : pair % X;
+                    const int i2 = i / 2;  // (constant places in `block`, whatever `half` is)
+                    const uint8_t* at = !KEYS    ? (second ? block[2 * (2 * i2 / X) + 1] : block[2 * (2 * i2 / X)])
+                                        : X == 4 ? block[i2]
+                                                 : (half ? block[(2 * i2 + 1) % 4] : block[2 * i2 % 4]);
+                    words[i] = make_uint4(kPackedZero, kPackedZero, kPackedZero, kPackedZero);
+                    scales[i] = make_uint2(0, 0);
+                    if (at) {
+                        words[i] = *reinterpret_cast<const uint4*>(at + code_at + N * 16 * x);
+                        scales[i] = *reinterpret_cast<const uint2*>(at + scale_at + (KEYS ? 32 : N) * x);
+                    }
+                }
+            }
+            if (u >= SLOTS && !bar_wait(&empty[slot], (u / SLOTS - 1) & 1, c)) return;
+            if (packed) {
+                char* tile = ring + slot * S::kUnit;
+#pragma unroll
+                for (int i = 0; i < kPatches; ++i) {
+                    const int pair = 2 * (i / 2) + half, second = (i ^ r) & 1;
+                    const int run = KEYS ? pair / (X / 2) : 2 * (pair / X) + second;
+                    const int x = KEYS ? 2 * (pair % (X / 2)) + second : pair % X;
+                    uint32_t s[4], o[4], d[4][4];
+                    packed_scales(scales[i], s, o);
+                    packed_words(words[i], s, o, d);
+                    // rows: the run's tokens, or the patch's channels; octets of the other
+                    const int row0 = 32 * (KEYS ? run : x) + 8 * (r >> 1) + (r & 1), octet = 4 * (KEYS ? x : run) + t4;
+                    char* line = tile + (octet >> 3) * (KEYS ? 16384 : D * 128) + row0 * 128;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<uint4*>(line + 256 * k + (((octet & 7) ^ ((row0 + 2 * k) & 7)) << 4)) =
+                            make_uint4(d[k][0], d[k][1], d[k][2], d[k][3]);
+                }
+                fence_async();
+            }
+            bar_arrive_warp(&full[slot]);
+        }
+    }
+}
+
+template <int D, bool PAIR, int KIND>
+__global__ void __launch_bounds__(tc_threads(KIND), 1)
     attend_tc_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap key, const __grid_constant__ CUtensorMap value) {
     using S = TcShape<D, PAIR>;
     extern __shared__ char raw[];
@@ -820,12 +1030,13 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     TcControl& c = *reinterpret_cast<TcControl*>(merge + S::kMerge);
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
+        constexpr int fill = KIND == kPacked ? 3 : 1;  // the loading warp, and two that expand
         for (int i = 0; i < S::kK; ++i) {
-            bar_init(&c.full_k[i], 1);
+            bar_init(&c.full_k[i], fill);
             bar_init(&c.empty_k[i], 1);
         }
         for (int i = 0; i < S::kV; ++i) {
-            bar_init(&c.full_v[i], 1);
+            bar_init(&c.full_v[i], fill);
             bar_init(&c.empty_v[i], 1);
         }
         for (int i = 0; i < 2; ++i) {
@@ -850,19 +1061,34 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (warp == 9) {
-        const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128;
-        const AttendCut cut = attend_cut<kTile>(a, a.H * ((rows + item_rows - 1) / item_rows), blockIdx.x);
+        const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows;
+        AttendCut cut;
+        if constexpr (KIND == kWhole)
+            cut = attend_cut<kTile>(a, a.H * groups, blockIdx.x);
+        else
+            cut = attend_cut_over(a, a.B * groups, a.H, blockIdx.x, [&](int i) {
+                return LongItem<kTile>(a, i / groups, i % groups * item_rows, item_rows).n;
+            });
         if ((threadIdx.x & 31) == 0) c.cut = cut;
     }
     if (threadIdx.x == 0) a.join[blockIdx.x] = make_int4(0, 0, 0, 0);
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp < 8) tc_softmax<D, PAIR>(a, c, q_smem, v_ring, merge, warp >> 2);
-    else if (warp == 8) tc_load<D, PAIR, S::kK>(a, c, &key, k_ring, c.full_k, c.empty_k, true);
-    else if (warp == 11) tc_load<D, PAIR, S::kV>(a, c, &value, v_ring, c.full_v, c.empty_v, false);
-    else if (warp == 9) tc_scores<D, PAIR>(a, c, q_smem, k_ring);
-    else tc_sums<D, PAIR>(a, c, v_ring);
+    if (warp < 8) {
+        if (KIND == kPacked) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+        tc_softmax<D, PAIR, KIND>(a, c, q_smem, v_ring, merge, warp >> 2);
+    } else if (warp < 12) {
+        if (KIND == kPacked) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
+        if (warp == 8) tc_load<D, PAIR, S::kK, KIND>(a, c, &key, k_ring, c.full_k, c.empty_k, true);
+        else if (warp == 11) tc_load<D, PAIR, S::kV, KIND>(a, c, &value, v_ring, c.full_v, c.empty_v, false);
+        else if (warp == 9) tc_scores<D, PAIR, KIND>(a, c, q_smem, k_ring);
+        else tc_sums<D, PAIR, KIND>(a, c, v_ring);
+    } else if constexpr (KIND == kPacked) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExpandRegs));
+        if (warp < 14) tc_expand<D, PAIR, S::kK, true>(a, c, k_ring, c.full_k, c.empty_k);
+        else tc_expand<D, PAIR, S::kV, false>(a, c, v_ring, c.full_v, c.empty_v);
+    }
     tc_fence_before();
     __syncthreads();
     if (warp == 8) {
@@ -902,7 +1128,7 @@ bool encode(CUtensorMap* map, const AttendArgs& a, void* base, int64_t page, int
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool PAIR> cudaError_t launch_tc(const AttendArgs& a, cudaStream_t s) {
+template <int D, bool PAIR, int KIND> cudaError_t launch_tc(const AttendArgs& a, cudaStream_t s) {
     CUtensorMap key, value;
     if (!encode_fn()) return cudaErrorNotSupported;
     if (!encode(&key, a, a.kv.key, a.kv.key_page, a.kv.key_head, a.kv.key_token) ||
@@ -910,17 +1136,29 @@ template <int D, bool PAIR> cudaError_t launch_tc(const AttendArgs& a, cudaStrea
         return cudaErrorInvalidValue;
     constexpr size_t smem = tc_smem_bytes<D, PAIR>();
     static_assert(smem <= 227 * 1024);
-    cudaError_t err = cudaFuncSetAttribute(attend_tc_kernel<D, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (KIND == kPacked) {
+        // the groups' registers are taken from what the block was launched with: less would leave a group waiting
+        static const int regs = [] {
+            cudaFuncAttributes f;
+            return cudaFuncGetAttributes(&f, attend_tc_kernel<D, PAIR, KIND>) == cudaSuccess ? f.numRegs : 0;
+        }();
+        if (regs < kPackedLaunchRegs) return cudaErrorNotSupported;
+    }
+    cudaError_t err = cudaFuncSetAttribute(attend_tc_kernel<D, PAIR, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (err != cudaSuccess) return err;
-    return launch_dependent(attend_tc_kernel<D, PAIR>, dim3(a.ctas), dim3(kTcThreads), smem, s, a, key, value);
+    return launch_dependent(attend_tc_kernel<D, PAIR, KIND>, dim3(a.ctas), dim3(tc_threads(KIND)), smem, s, a, key, value);
+}
+
+template <int KIND> cudaError_t launch_tc_kind(const AttendArgs& a, cudaStream_t s) {
+    const bool pair = (int64_t)a.T * a.G > 128;
+    if (a.D == 64) return pair ? launch_tc<64, true, KIND>(a, s) : launch_tc<64, false, KIND>(a, s);
+    return pair ? launch_tc<128, true, KIND>(a, s) : launch_tc<128, false, KIND>(a, s);
 }
 
 }  // namespace
 
-cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s) {
-    const bool pair = (int64_t)a.T * a.G > 128;
-    if (a.D == 64) return pair ? launch_tc<64, true>(a, s) : launch_tc<64, false>(a, s);
-    return pair ? launch_tc<128, true>(a, s) : launch_tc<128, false>(a, s);
-}
+cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s) { return launch_tc_kind<kWhole>(a, s); }
+cudaError_t launch_window_tc(const AttendArgs& a, cudaStream_t s) { return launch_tc_kind<kWindow>(a, s); }
+cudaError_t launch_packed_tc(const AttendArgs& a, cudaStream_t s) { return launch_tc_kind<kPacked>(a, s); }
 
 }  // namespace rheo

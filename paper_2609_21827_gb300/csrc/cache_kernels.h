@@ -129,6 +129,8 @@ cudaError_t launch_window_attend(const AttendArgs& a, int dtype, cudaStream_t s)
 cudaError_t launch_packed_attend(const AttendArgs& a, cudaStream_t s);
 cudaError_t launch_attend_join(const AttendArgs& a, int dtype, cudaStream_t s);
 cudaError_t launch_attend_tc(const AttendArgs& a, cudaStream_t s);
+cudaError_t launch_window_tc(const AttendArgs& a, cudaStream_t s);
+cudaError_t launch_packed_tc(const AttendArgs& a, cudaStream_t s);
 int attend_item_rows(int dtype, int T, int G);
 int attend_part_rows(int dtype, int T, int G);
 int attend_lead(int dtype);
