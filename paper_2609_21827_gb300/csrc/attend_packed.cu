@@ -2,10 +2,11 @@
 // ones behind them.
 //
 // An item is up to 8 NT query rows (token, head of the key/value head) of a request and
-// its tiles of 32 places.  A CTA an SM; one warp copies packed blocks into a ring of
-// shared memory (one bulk copy each, a page of a head is contiguous), the others take
-// every kWarps-th tile, each with running maxima, sums and outputs of its own, and are
-// joined in shared memory at the item's end.
+// its tiles of 32 places.  A CTA is four warps, of which each takes every fourth tile, with running maxima,
+// sums and outputs of its own; they are joined in shared memory at the item's end.  Three or four
+// CTAs an SM, so that the others have work where one begins or ends an item.  A warp looks
+// up 32 of its packed tiles at a time (a lane each) and has the next one copied (a bulk copy, as a
+// block is contiguous) while it works on one.
 // Both products are taken with the cache as the first operand of m16n8k16, so
 // that the few query rows fill its 8 columns: S^T = K Q^T (16 places x 8 rows), O^T = V^T P^T
 // (16 channels x 8 rows).  A lane's 16 bytes of a packed block are four rows of that
@@ -28,14 +29,17 @@ namespace rheo {
 namespace {
 
 constexpr int kTile = 32;            // places a tile
-constexpr int kSlots = 32;           // of the ring
+constexpr int kWarps = 4;            // of a CTA
+constexpr int kThreads = 32 * kWarps;
+constexpr int kSlots = 2;            // of a warp
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 22;  // polls of a wait before the kernel gives up
 
+// CTAs an SM: 16 rows of 128 channels need more than 128 registers a thread.
+constexpr int few_per_sm(int D, int NT) { return NT == 2 && D == 128 ? 3 : 4; }
+
 template <int D, int NT> struct Few {
-    // Warps that take tiles: with the copying one 16, which leaves a thread 128 registers, or 8.
-    static constexpr int kWarps = NT == 1 ? 15 : 7;
-    static constexpr int kThreads = 32 * (kWarps + 1);
+    static constexpr int kPerSm = few_per_sm(D, NT);
     static constexpr int kX = D / 32;
     static constexpr int kRows = 8 * NT;
     static constexpr int kSlot = packed_block_bytes(16, D) * 2;  // the larger of one block of 32 tokens and two of 16
@@ -45,10 +49,10 @@ template <int D, int NT> struct Few {
 
 template <int D, int NT> struct FewSmem {
     using F = Few<D, NT>;
-    alignas(16) unsigned char ring[kSlots][F::kSlot];
-    float o[F::kWarps][F::kRows * F::kLine];
-    float2 ml[F::kWarps][F::kRows];
-    unsigned long long full[kSlots], empty[kSlots];
+    alignas(16) unsigned char slot[kWarps][kSlots][F::kSlot];
+    float o[kWarps][F::kRows * F::kLine];
+    float2 ml[kWarps][F::kRows];
+    unsigned long long full[kWarps][kSlots];
     AttendCut cut;
     int abort;
     int odd[2];  // some value that is not finite was left out, of items in turn
@@ -57,9 +61,6 @@ template <int D, int NT> struct FewSmem {
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void bar_init(unsigned long long* b, int count) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(unsigned long long* b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
 }
 __device__ __forceinline__ void bar_expect(unsigned long long* b, int bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(b)), "r"(bytes) : "memory");
@@ -88,7 +89,7 @@ __device__ __forceinline__ void bulk_copy(void* dst, const void* src, int bytes,
                  : "memory");
 }
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
@@ -117,78 +118,16 @@ __device__ __forceinline__ void feed(float (&c0)[4], float (&c1)[4], const uint3
 }
 __device__ __forceinline__ int quad_row(int r, int i) { return 8 * (r >> 1) + (r & 1) + 2 * i; }
 
-// Copies the packed tiles of this CTA's items into the ring, in order; lane = tile of 32 at a time.
-template <int D, int NT> __device__ __forceinline__ void few_load(const AttendArgs& a, FewSmem<D, NT>& sm) {
-    using F = Few<D, NT>;
-    const int lane = threadIdx.x & 31, N = packed_tokens(a.P), block_bytes = packed_block_bytes(N, D), blocks = kTile / N;
-    const int rows = a.T * a.G, groups = (rows + F::kRows - 1) / F::kRows;
-    uint32_t u = 0;
-    bool fine = true;
-    for (AttendWalk<kTile> w(sm.cut); w.more() && fine; w.next(a.H)) {
-        const int b = w.b / groups, r0 = w.b % groups * F::kRows;
-        const LongItem<kTile> it(a, b, r0, F::kRows);
-        w.open_tiles(it.n);
-        const int to = min(w.tile + w.n, it.packed_tiles());
-        const int32_t* table = a.table4 + (int64_t)b * a.max_pages4;
-        for (int i0 = w.tile; i0 < to && fine; i0 += 32) {
-            // this lane's tile: where its blocks lie (null: not wanted, or a bad page)
-            const uint8_t* src[2] = {nullptr, nullptr};
-            if (i0 + lane < to) {
-                const int place = it.begin(it.number(i0 + lane));
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = place + k * N;
-                    if (k >= blocks || at >= it.s.pk || !it.wanted(at, N)) continue;
-                    const int page = table[at >> a.page_shift];
-                    if (page < 0 || page >= a.pages4) {
-                        atomicOr(a.status, kStBadIndex);
-                        continue;
-                    }
-                    src[k] = a.packed.data + page * a.packed.page + w.item * a.packed.head + (at & (a.P - 1)) / N * block_bytes;
-                }
-            }
-            const uint32_t gone = __ballot_sync(0xffffffffu, !src[0] || (blocks == 2 && !src[1]));
-            const int count = min(32, to - i0);
-            for (int l = 0; l < count; ++l, ++u) {
-                const uint32_t slot = u % kSlots;
-                if (u >= kSlots && !bar_wait(&sm.empty[slot], (u / kSlots - 1) & 1, &sm.abort)) {
-                    fine = false;
-                    break;
-                }
-                if ((gone >> l) & 1) {  // blocks that are not there are zeros
-                    const uint32_t has = __shfl_sync(0xffffffffu, (src[0] ? 1 : 0) | (src[1] ? 2 : 0), l);
-                    for (int k = 0; k < blocks; ++k)
-                        for (int j = lane * 16; !((has >> k) & 1) && j < block_bytes; j += 512)
-                            *reinterpret_cast<uint4*>(&sm.ring[slot][k * block_bytes + j]) =
-                                make_uint4(kPackedZero, kPackedZero, kPackedZero, kPackedZero);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
-                if (lane == l) {
-                    bar_expect(&sm.full[slot], ((src[0] ? 1 : 0) + (src[1] ? 1 : 0)) * block_bytes);
-                    if (src[0]) bulk_copy(&sm.ring[slot][0], src[0], block_bytes, &sm.full[slot]);
-                    if (src[1]) bulk_copy(&sm.ring[slot][block_bytes], src[1], block_bytes, &sm.full[slot]);
-                }
-                __syncwarp();
-            }
-        }
-    }
-    // no copy is in flight when the CTA ends
-    for (uint32_t x = u > kSlots ? u - kSlots : 0; x < u; ++x) bar_wait<true>(&sm.full[x % kSlots], (x / kSlots) & 1, &sm.abort);
-}
-
 template <int D, int NT>
-__global__ void __launch_bounds__(Few<D, NT>::kThreads, 1) packed_few_kernel(const AttendArgs a) {
+__global__ void __launch_bounds__(kThreads, Few<D, NT>::kPerSm) packed_few_kernel(const AttendArgs a) {
     using F = Few<D, NT>;
     extern __shared__ __align__(128) unsigned char raw_smem[];
     FewSmem<D, NT>& sm = *reinterpret_cast<FewSmem<D, NT>*>(raw_smem);
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, r = lane >> 2, t4 = lane & 3;
+    const int tid = threadIdx.x, lane = tid & 31, r = lane >> 2, t4 = lane & 3;
+    const int warp = __shfl_sync(0xffffffffu, tid >> 5, 0);  // (known to be the same in all lanes)
     const int rows = a.T * a.G, groups = (rows + F::kRows - 1) / F::kRows;
     if (tid == 0) {
-        for (int i = 0; i < kSlots; ++i) {
-            bar_init(&sm.full[i], 1);
-            bar_init(&sm.empty[i], 1);
-        }
+        for (int i = 0; i < kWarps * kSlots; ++i) bar_init(&sm.full[0][i], 1);
         sm.abort = sm.odd[0] = sm.odd[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -203,19 +142,33 @@ __global__ void __launch_bounds__(Few<D, NT>::kThreads, 1) packed_few_kernel(con
         }
     }
     __syncthreads();
-    if (warp == F::kWarps) {
-        few_load<D, NT>(a, sm);
-        return;
-    }
-    auto sync = [] { asm volatile("bar.sync 1, %0;" ::"n"(32 * F::kWarps) : "memory"); };
-
     const int N = packed_tokens(a.P), block_bytes = packed_block_bytes(N, D);
     // where this lane's pieces of a tile lie: its keys' block and its values' one (two blocks of 16 tokens, or the same of 32)
     const int k_block = N == 16 ? (r >> 2) * block_bytes : 0, v_block = N == 16 ? (t4 >> 1) * block_bytes : 0;
     const int k_at = k_block + ((N == 16 ? r & 3 : r) * 4 + t4) * 16, k_step = N * 16;  // from 32 channels to the next
     const int v_at = v_block + N * D / 2 + (r * (N / 8) + (N == 16 ? t4 & 1 : t4)) * 16, v_step = N * 16;
     const int ks_at = k_block + N * D + 8 * t4, vs_at = v_block + N * D + D + 8 * (N == 16 ? t4 & 1 : t4);
-    uint32_t seq = 0, seq4 = 0, items = 0;  // tiles, packed tiles, items of this CTA before the item at hand
+    const int blocks = kTile / N;
+    uint32_t items = 0, ahead = 0, done = 0;  // items, copies begun and waited for; the k-th copy goes to slot k % kSlots
+    // Copies of one tile's blocks, which lie at src0 and src1 (of 32 tokens: one); 0: not there, zeros
+    auto copy = [&](unsigned long long src0, unsigned long long src1) {
+        const uint32_t k = ahead++ % kSlots;
+        unsigned char* to = sm.slot[warp][k];
+        if (src0 == 0 || (blocks == 2 && src1 == 0)) {
+            for (int z = 0; z < blocks; ++z)
+                for (int j = lane * 16; (z == 0 ? src0 : src1) == 0 && j < block_bytes; j += 512)
+                    *reinterpret_cast<uint4*>(to + z * block_bytes + j) = make_uint4(kPackedZero, kPackedZero, kPackedZero, kPackedZero);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        }
+        __syncwarp();
+        if (lane == 0) {
+            const int n0 = src0 != 0, n1 = blocks == 2 && src1 != 0;
+            bar_expect(&sm.full[warp][k], (n0 + n1) * block_bytes);
+            if (n0) bulk_copy(to, reinterpret_cast<const void*>(src0), block_bytes, &sm.full[warp][k]);
+            if (n1) bulk_copy(to + block_bytes, reinterpret_cast<const void*>(src1), block_bytes, &sm.full[warp][k]);
+        }
+        __syncwarp();
+    };
 
     for (AttendWalk<kTile> w(sm.cut); w.more(); w.next(a.H)) {
         const int b = w.b / groups, g = w.b % groups, h = w.item, r0 = g * F::kRows;
@@ -224,6 +177,39 @@ __global__ void __launch_bounds__(Few<D, NT>::kThreads, 1) packed_few_kernel(con
         if (it.s.bad && tid == 0) atomicOr(a.status, kStBadLength);
         const int to = w.tile + w.n, packed_to = min(to, it.packed_tiles());
         const int32_t* table = a.block_table + (int64_t)b * a.max_pages;
+
+        // this warp's tiles: every kWarps-th from `at` on; the packed ones come first
+        const int at = w.tile + warp;
+        const bool mine = at < to;
+        const int turns = at < packed_to ? (packed_to - at + kWarps - 1) / kWarps : 0;
+        unsigned long long src[2] = {0, 0};  // where this lane's one of 32 packed tiles lies
+        int asked = 0;                       // packed tiles of this item whose copies have begun
+        auto copy_next = [&] {
+            if (asked >= turns) return;
+            if (asked % 32 == 0) {
+                const int i = at + (asked + lane) * kWarps;
+                src[0] = src[1] = 0;
+                if (i < packed_to) {
+                    const int place = it.number(i) * kTile;
+                    const int32_t* table4 = a.table4 + (int64_t)b * a.max_pages4;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int l0 = place + k * N;
+                        if (k >= blocks || l0 >= it.s.pk || !it.wanted(l0, N)) continue;
+                        const int page = table4[l0 >> a.page_shift];
+                        if (page < 0 || page >= a.pages4) atomicOr(a.status, kStBadIndex);
+                        else
+                            src[k] = (unsigned long long)(a.packed.data + page * a.packed.page + h * a.packed.head +
+                                                          (l0 & (a.P - 1)) / N * block_bytes);
+                    }
+                }
+                __syncwarp();
+            }
+            const unsigned long long src0 = __shfl_sync(0xffffffffu, src[0], asked & 31);
+            copy(src0, blocks == 2 ? __shfl_sync(0xffffffffu, src[1], asked & 31) : 0);
+            ++asked;
+        };
+        for (int k = 0; k < kSlots; ++k) copy_next();
 
         // queries: column r of the products
         uint32_t q[NT][F::kX][4];
@@ -261,82 +247,33 @@ __global__ void __launch_bounds__(Few<D, NT>::kThreads, 1) packed_few_kernel(con
 #pragma unroll
                 for (int k = 0; k < 8; ++k) o[n][x][k / 4][k % 4] = 0.0f;
         }
-        bool mine = false;
-        for (int i = w.tile + (int)((warp + F::kWarps - seq % F::kWarps) % F::kWarps); i < to; i += F::kWarps) {
-            mine = true;
-            const int number = it.number(i), place = it.begin(number), end = it.end(number);
-            const bool packed = i < packed_to;
-            const uint32_t u = seq4 + (i - w.tile), slot = u % kSlots;
-            const unsigned char* ring = sm.ring[slot];
-            float s[NT][2][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) s[n][k / 4][k % 4] = 0.0f;
-            const char* near_value[4];  // 16 bits: this lane's places' values; null where there is none to read
-            if (packed) {
-                bar_wait(&sm.full[slot], (u / kSlots) & 1, &sm.abort);  // (where it fails the results do not count)
-#pragma unroll
-                for (int x = 0; x < F::kX; ++x) {
-                    uint32_t sc[4], so[4], d[4][4];
-                    packed_scales(*reinterpret_cast<const uint2*>(ring + ks_at + 32 * x), sc, so);
-                    packed_words(*reinterpret_cast<const uint4*>(ring + k_at + k_step * x), sc, so, d);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) feed(s[n][0], s[n][1], d, q[n][x]);
-                }
-            } else {
-                const char* key[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int l0 = place + quad_row(r, k), x = l0 - it.s.pk;
-                    key[k] = near_value[k] = nullptr;
-                    if (l0 >= end || !it.wanted(l0, 1)) continue;
-                    const int page = table[x >> a.page_shift];
-                    if (page < 0 || page >= a.pages) {
-                        atomicOr(a.status, kStBadIndex);
-                        continue;
-                    }
-                    key[k] = static_cast<const char*>(a.kv.key) +
-                             (page * a.kv.key_page + h * a.kv.key_head + (x & (a.P - 1)) * a.kv.key_token + 8 * t4) * 2;
-                    near_value[k] = static_cast<const char*>(a.kv.value) +
-                                    (page * a.kv.value_page + h * a.kv.value_head + (x & (a.P - 1)) * a.kv.value_token + 8 * t4) * 2;
-                }
-                __syncwarp();
-#pragma unroll
-                for (int x = 0; x < F::kX; ++x) {
-                    uint32_t d[4][4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint4 y = make_uint4(0, 0, 0, 0);
-                        if (key[k]) y = *reinterpret_cast<const uint4*>(key[k] + 64 * x);
-                        d[k][0] = y.x, d[k][1] = y.y, d[k][2] = y.z, d[k][3] = y.w;
-                    }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) feed(s[n][0], s[n][1], d, q[n][x]);
-                }
-            }
-            // s[n][k / 2][2 (k % 2) + e]: place f(r, k), row 8 n + 2 t4 + e
-            const bool masked = place + kTile > min(end, it.s.ctx) || place < it.lo_most;
-            uint32_t p[NT][4];
+        // Scores (of places f(r, k), rows 8 n + 2 t4 + e at s[n][k / 2][2 (k % 2) + e]) to weights, the second operand of the
+        // values' product.
+        auto weigh = [&](float (&s)[NT][2][4], uint32_t (&p)[NT][4], int place, int end, bool masked) {
             bool grow = false;
             float top[NT][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    top[n][e] = -INFINITY;
+                for (int k = 0; k < 8; ++k) s[n][k / 4][k % 4] *= a.scale_log2;
+            if (masked) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        float& y = s[n][k / 2][2 * (k % 2) + e];
-                        y *= a.scale_log2;
-                        if (masked) {
-                            const int l0 = place + quad_row(r, k), t = token[n][e];
-                            const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + max(t, 0)) * a.T : nullptr;
-                            if (t < 0 || l0 >= end || !it.sees(a, b, mrow, t, first[n][e], l0)) y = -INFINITY;
-                        }
-                        top[n][e] = fmaxf(top[n][e], y);
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int l0 = place + quad_row(r, k / 2), t = token[n][k % 2];
+                        const uint8_t* mrow = a.mask ? a.mask + ((int64_t)b * a.T + max(t, 0)) * a.T : nullptr;
+                        if (t < 0 || l0 >= end || !it.sees(a, b, mrow, t, first[n][k % 2], l0)) s[n][k / 4][k % 4] = -INFINITY;
                     }
-                    grow |= top[n][e] > m[n][e] + kSlack || (m[n][e] == -INFINITY && top[n][e] > m[n][e]);
+                __syncwarp();
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    top[n][e] = fmaxf(fmaxf(s[n][0][e], s[n][0][2 + e]), fmaxf(s[n][1][e], s[n][1][2 + e]));
+                    // (a reference of -inf: the comparison holds for anything above it)
+                    grow |= top[n][e] > m[n][e] + kSlack;
                 }
             if (__any_sync(0xffffffffu, grow)) {
 #pragma unroll
@@ -366,41 +303,106 @@ __global__ void __launch_bounds__(Few<D, NT>::kThreads, 1) packed_few_kernel(con
                     p[n][k] = transposed(pack_bf16(p0, p1));
                 }
             }
-            if (packed) {
+        };
+        // ---- in 16 bits: first, as their loads wait for one another
+        for (int i = at + turns * kWarps; i < to; i += kWarps) {
+            const int number = it.number(i), place = it.begin(number), end = it.end(number);
+            const bool masked = place + kTile > min(end, it.s.ctx) || place < it.lo_most;
+            int page[4];  // of this lane's places; -1 where there is none to read
 #pragma unroll
-                for (int x = 0; x < F::kX; ++x) {
-                    uint32_t sc[4], so[4], d[4][4];
-                    packed_scales(*reinterpret_cast<const uint2*>(ring + vs_at + N * x), sc, so);
-                    packed_words(*reinterpret_cast<const uint4*>(ring + v_at + v_step * x), sc, so, d);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) feed(o[n][x][0], o[n][x][1], d, p[n]);
-                }
-                __syncwarp();
-                if (lane == 0) bar_arrive(&sm.empty[slot]);
-            } else {
-                bool odd = false;
-#pragma unroll
-                for (int x = 0; x < F::kX; ++x) {
-                    uint32_t d[4][4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        uint4 y = make_uint4(0, 0, 0, 0);
-                        if (near_value[k]) y = *reinterpret_cast<const uint4*>(near_value[k] + 64 * x);
-                        if (masked) {
-                            const uint32_t z[4] = {odd_mask(y.x), odd_mask(y.y), odd_mask(y.z), odd_mask(y.w)};
-                            odd |= (z[0] | z[1] | z[2] | z[3]) != 0;
-                            y = make_uint4(y.x & ~z[0], y.y & ~z[1], y.z & ~z[2], y.w & ~z[3]);
-                        }
-                        d[0][k] = transposed(y.x), d[1][k] = transposed(y.y), d[2][k] = transposed(y.z), d[3][k] = transposed(y.w);
-                    }
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) feed(o[n][x][0], o[n][x][1], d, p[n]);
-                }
-                if (odd) sm.odd[items & 1] = 1;
+            for (int k = 0; k < 4; ++k) {
+                const int l0 = place + quad_row(r, k);
+                page[k] = l0 < end && it.wanted(l0, 1) ? table[(l0 - it.s.pk) >> a.page_shift] : -1;
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int l0 = place + quad_row(r, k);
+                if (l0 < end && it.wanted(l0, 1) && (page[k] < 0 || page[k] >= a.pages)) {
+                    atomicOr(a.status, kStBadIndex);
+                    page[k] = -1;
+                }
+            }
+            __syncwarp();
+            // 32 channels of the places' lines (a load under a condition would wait for the one before: what is not there is
+            // read from page 0)
+            auto line = [&](const void* base, int64_t page_stride, int64_t head_stride, int64_t token_stride, int k, int x) {
+                const int row = (place + quad_row(r, k) - it.s.pk) & (a.P - 1);
+                const uint4 y = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(base) +
+                                                                max(page[k], 0) * page_stride + h * head_stride +
+                                                                row * token_stride + 8 * t4 + 32 * x);
+                return page[k] < 0 ? make_uint4(0, 0, 0, 0) : y;
+            };
+            float s[NT][2][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s[n][k / 4][k % 4] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < F::kX; ++x) {
+                uint32_t d[4][4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const uint4 y = line(a.kv.key, a.kv.key_page, a.kv.key_head, a.kv.key_token, k, x);
+                    d[k][0] = y.x, d[k][1] = y.y, d[k][2] = y.z, d[k][3] = y.w;
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) feed(s[n][0], s[n][1], d, q[n][x]);
+            }
+            uint32_t p[NT][4];
+            weigh(s, p, place, end, masked);
+            bool odd = false;
+#pragma unroll
+            for (int x = 0; x < F::kX; ++x) {
+                uint32_t d[4][4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint4 y = line(a.kv.value, a.kv.value_page, a.kv.value_head, a.kv.value_token, k, x);
+                    if (masked) {
+                        const uint32_t z[4] = {odd_mask(y.x), odd_mask(y.y), odd_mask(y.z), odd_mask(y.w)};
+                        odd |= (z[0] | z[1] | z[2] | z[3]) != 0;
+                        y = make_uint4(y.x & ~z[0], y.y & ~z[1], y.z & ~z[2], y.w & ~z[3]);
+                    }
+                    d[0][k] = transposed(y.x), d[1][k] = transposed(y.y), d[2][k] = transposed(y.z), d[3][k] = transposed(y.w);
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) feed(o[n][x][0], o[n][x][1], d, p[n]);
+            }
+            if (odd) sm.odd[items & 1] = 1;
         }
-        seq += w.n;
-        seq4 += max(0, packed_to - w.tile);
+
+        // ---- packed
+        for (int i = at; i < packed_to; i += kWarps) {
+            const int number = it.number(i), place = number * kTile;
+            const uint32_t k = done % kSlots;
+            const unsigned char* from = sm.slot[warp][k];
+            bar_wait(&sm.full[warp][k], (done / kSlots) & 1, &sm.abort);  // (where it fails the results do not count)
+            float s[NT][2][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int z = 0; z < 8; ++z) s[n][z / 4][z % 4] = 0.0f;
+#pragma unroll
+            for (int x = 0; x < F::kX; ++x) {
+                uint32_t sc[4], so[4], d[4][4];
+                packed_scales(*reinterpret_cast<const uint2*>(from + ks_at + 32 * x), sc, so);
+                packed_words(*reinterpret_cast<const uint4*>(from + k_at + k_step * x), sc, so, d);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) feed(s[n][0], s[n][1], d, q[n][x]);
+            }
+            uint32_t p[NT][4];
+            weigh(s, p, place, it.end(number), place + kTile > it.s.pk || place < it.lo_most);
+#pragma unroll
+            for (int x = 0; x < F::kX; ++x) {
+                uint32_t sc[4], so[4], d[4][4];
+                packed_scales(*reinterpret_cast<const uint2*>(from + vs_at + N * x), sc, so);
+                packed_words(*reinterpret_cast<const uint4*>(from + v_at + v_step * x), sc, so, d);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) feed(o[n][x][0], o[n][x][1], d, p[n]);
+            }
+            ++done;
+            __syncwarp();
+            copy_next();
+        }
 
         // ---- the item's sums: every warp's into shared memory, then a thread four columns of a row
 #pragma unroll
@@ -418,25 +420,24 @@ __global__ void __launch_bounds__(Few<D, NT>::kThreads, 1) packed_few_kernel(con
                         for (int k = 0; k < 4; ++k) to_row[32 * x + quad_row(r, k)] = o[n][x][k / 2][2 * (k % 2) + e];
                 }
             }
-        sync();
+        __syncthreads();
         const bool left_out = *(volatile int*)&sm.odd[items & 1] != 0;
         if (tid == 0) sm.odd[~items & 1] = 0;  // the next item's, read last before the sums of this one
         ++items;
         const bool whole = w.n == w.all;
         const int64_t part = attend_part(blockIdx.x, w.tile == 0);
-        const int filled = min((int)F::kWarps, w.n);  // warps that had a tile: seq - w.n .. on
-        for (int k = tid; k < F::kRows * (D / 4); k += 32 * F::kWarps) {
+        const int filled = min((int)kWarps, w.n);
+        for (int k = tid; k < F::kRows * (D / 4); k += kThreads) {
             const int rr = k / (D / 4), c4 = k % (D / 4), row = r0 + rr, t = row / a.G, head = h * a.G + row - t * a.G;
             if (row >= rows) continue;
             float mm = -INFINITY, ll = 0.0f, y[4] = {0, 0, 0, 0};
-            for (int z = 0; z < filled; ++z) mm = fmaxf(mm, sm.ml[(seq - w.n + z) % F::kWarps][rr].x);
+            for (int z = 0; z < filled; ++z) mm = fmaxf(mm, sm.ml[z][rr].x);
             const float ref = mm == -INFINITY ? 0.0f : mm;
             for (int z = 0; z < filled; ++z) {
-                const int from = (seq - w.n + z) % F::kWarps;
-                const float2 x = sm.ml[from][rr];
+                const float2 x = sm.ml[z][rr];
                 const float f = fast_exp2(x.x - ref);
                 ll += f * x.y;
-                const float* src = &sm.o[from][rr * F::kLine + 4 * c4];
+                const float* src = &sm.o[z][rr * F::kLine + 4 * c4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) y[e] += f * src[e];
             }
@@ -476,17 +477,19 @@ __global__ void __launch_bounds__(Few<D, NT>::kThreads, 1) packed_few_kernel(con
         }
         if (!whole && w.tile == 0 && tid == 0)
             a.join[blockIdx.x] = make_int4(b, h * groups + g, w.segments(sm.cut, blockIdx.x), 0);
-        sync();
+        __syncthreads();
     }
+    // no copy is in flight when the CTA ends (all have been waited for, but where a wait failed)
+    for (; done < ahead; ++done) bar_wait<true>(&sm.full[warp][done % kSlots], (done / kSlots) & 1, &sm.abort);
     if (tid == 0 && *(volatile int*)&sm.abort) atomicOr(a.status, kStInternal);
 }
 
 template <int D, int NT> cudaError_t launch_few(const AttendArgs& a, cudaStream_t s) {
     constexpr size_t smem = sizeof(FewSmem<D, NT>);
-    static_assert(smem <= 227 * 1024);
+    static_assert((smem + 1024) * Few<D, NT>::kPerSm <= 228 * 1024);
     const cudaError_t err = cudaFuncSetAttribute(packed_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (err != cudaSuccess) return err;
-    return launch_dependent(packed_few_kernel<D, NT>, dim3(a.ctas), dim3(Few<D, NT>::kThreads), smem, s, a);
+    return launch_dependent(packed_few_kernel<D, NT>, dim3(a.ctas), dim3(kThreads), smem, s, a);
 }
 
 }  // namespace
@@ -494,14 +497,15 @@ template <int D, int NT> cudaError_t launch_few(const AttendArgs& a, cudaStream_
 cudaError_t launch_packed_attend(const AttendArgs& in, cudaStream_t s) {
     AttendArgs a = in;
     const int rows = a.T * a.G;
-    if (rows > 16) {
+    if (rows > kFewRows) {
         const cudaError_t err = launch_packed_tc(a, s);
         return err != cudaSuccess ? err : launch_attend_join(a, 1, s);
     }
     const bool one = rows <= 8;
     a.item_rows = one ? 8 : 16;
     a.part_rows = a.item_rows;
-    a.lead = 8;
+    a.ctas = kAttendCtas * few_per_sm(a.D, one ? 1 : 2);
+    a.lead = 24;
     a.least = 16;
     const cudaError_t err = a.D == 64 ? (one ? launch_few<64, 1>(a, s) : launch_few<64, 2>(a, s))
                                       : (one ? launch_few<128, 1>(a, s) : launch_few<128, 2>(a, s));

@@ -58,17 +58,20 @@ constexpr int kScores = 2;                   // score buffers of a stream
 constexpr int kTcThreads = 12 * 32, kTcPackedThreads = 16 * 32;
 __host__ __device__ constexpr int tc_threads(int kind) { return kind == 2 ? kTcPackedThreads : kTcThreads; }
 // Registers a thread where sixteen warps share them: softmax groups, warps that load and issue, warps that expand packed tiles.
-constexpr int kSoftmaxRegs = 168, kIssueRegs = 72, kExpandRegs = 104, kPackedLaunchRegs = 128;
+constexpr int kSoftmaxRegs = 160, kIssueRegs = 80, kExpandRegs = 112, kPackedLaunchRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kExpandRegs <= 4 * kPackedLaunchRegs);
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
 constexpr int kDrainLimit = 1 << 16;         // and of a drain after that
 
-template <int D, bool PAIR> struct TcShape {
+template <int D, bool PAIR, int KIND> struct TcShape {
     static constexpr int kUnit = kTile * D * 2;  // bytes of a key or value tile
     static constexpr int kHalves = D / 64;       // 128-byte wide parts of a line
-    static constexpr int kK = D == 128 ? 2 : 5;  // slots of the key ring
-    static constexpr int kV = D == 128 ? 3 : 5;  // and of the value ring, which is read later
+    static constexpr int kK = D == 128 ? 2 : KIND == 2 ? 4 : 5;                   // slots of the key ring
+    static constexpr int kV = D == 128 ? (KIND == 2 ? 2 : 3) : KIND == 2 ? 4 : 5;  // and of the value ring, which is read later
+    // Packed tiles on their way: 64 places' codes and scales of the keys, or the values, a slot.
+    static constexpr int kRaw = KIND == 2 ? 3 : 0;
+    static constexpr int kRawUnit = 36 * D;  // four blocks of 16 tokens: the most
     static constexpr int kQ = 128 * D * 2;       // bytes of 128 rows of queries
     static constexpr int kQueries = PAIR ? 2 * kQ : kQ;
     static constexpr int kMerge = PAIR ? 0 : 16384;
@@ -81,6 +84,8 @@ template <int D, bool PAIR> struct TcShape {
 
 struct TcControl {
     unsigned long long full_k[5], empty_k[5], full_v[5], empty_v[5];
+    unsigned long long raw_full[2][3], raw_empty[2][3];  // keys, values
+    uint32_t raw_have[2][3];                            // which blocks are there
     unsigned long long s_full[2][kScores], p_ready[2][kScores], pv_done[2][kScores], drained[2], q_ready, q_taken, all_sync;
     uint32_t tmem;
     int abort;
@@ -90,9 +95,9 @@ struct TcControl {
     AttendCut cut;
 };
 
-template <int D, bool PAIR> constexpr size_t tc_smem_bytes() {
-    using S = TcShape<D, PAIR>;
-    return 1024 + S::kQueries + (size_t)(S::kK + S::kV) * S::kUnit + S::kMerge + sizeof(TcControl);
+template <int D, bool PAIR, int KIND> constexpr size_t tc_smem_bytes() {
+    using S = TcShape<D, PAIR, KIND>;
+    return 1024 + S::kQueries + (size_t)(S::kK + S::kV) * S::kUnit + S::kMerge + 2 * S::kRaw * S::kRawUnit + sizeof(TcControl);
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -231,6 +236,8 @@ template <int KIND> struct TcItem {
     AttendSpan s;
     LongItem<kTile> it;
     __device__ __forceinline__ TcItem() {}
+    __device__ __forceinline__ TcItem(int request, int item, int groups, int item_rows, const AttendSpan& span)
+        : b(request), h(item / groups), r0(item % groups * item_rows), s(span) {}
     __device__ __forceinline__ TcItem(const AttendArgs& a, int cls, int item, int groups, int item_rows) {
         if constexpr (KIND == kWhole) {
             b = cls;
@@ -255,10 +262,10 @@ template <int KIND> struct TcItem {
     __device__ __forceinline__ bool packed(int i) const { return KIND == kPacked && it.is_packed(it.number(i)); }
     // score products: the second half only where it has a place
     __device__ __forceinline__ int subs(int i) const { return end(i) - begin(i) > kSub ? 2 : 1; }
-    // LONG: whether a tile of 16 bits has places that not all of the item's tokens see (or nobody).  chain: they see all
-    // drafted tokens up to the first of them.
-    __device__ __forceinline__ bool unclear(bool chain, int place, int end, int G) const {
-        return place + kTile > min(end, chain ? s.ctx + r0 / G + 1 : s.ctx) || place < it.lo_most;
+    // LONG: whether a tile of 16 bits has places that not all of the item's tokens see (or nobody); of those from lo_most
+    // on they all see the ones below `upto`.
+    __device__ __forceinline__ bool unclear(int upto, int place, int end) const {
+        return place + kTile > min(end, upto) || place < it.lo_most;
     }
     // Whether some of n tiles from the i-th on has a second half: only the last ones of the sinks and of both parts may lack it.
     __device__ __forceinline__ bool second(int i, int n) const {
@@ -338,7 +345,7 @@ __device__ __forceinline__ unsigned long long low_bits(int n) {
 // The softmax group of stream `st`.
 template <int D, bool PAIR, int KIND>
 __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, char* q_smem, char* v_ring, char* merge, int st) {
-    using S = TcShape<D, PAIR>;
+    using S = TcShape<D, PAIR, KIND>;
     const int tid = threadIdx.x & 127, lane = tid & 31, warp = tid >> 5;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
@@ -354,19 +361,22 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         return bar_wait(&c.all_sync, syncs++ & 1, c);
     };
     // queries of an item: each stream's group fetches its own rows (PAIR), or stream 0's all of them
-    auto fetch = [&](const TcItem<KIND>& x) {
-        const int first = x.r0 + (PAIR ? st * 128 : 0);
-        tc_queries<D>(a, x.b, x.h, first, min(128, rows - first), q_smem + (PAIR ? st * S::kQ : 0), tid, 128);
+    auto fetch = [&](int cls, int item) {
+        const int h = KIND == kWhole ? item / groups : item, b = KIND == kWhole ? cls : cls / groups;
+        const int first = (KIND == kWhole ? item : cls) % groups * item_rows + (PAIR ? st * 128 : 0);
+        tc_queries<D>(a, b, h, first, min(128, rows - first), q_smem + (PAIR ? st * S::kQ : 0), tid, 128);
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
     TcWalk w(c.cut);
-    TcItem<KIND> next;
+    AttendSpan next_span{0, 0, false};
     if (w.more()) {
-        next = TcItem<KIND>(a, w.b, w.item, groups, item_rows);
-        if (PAIR || st == 0) fetch(next);
+        if (KIND == kWhole) next_span = attend_span(a, w.b);
+        if (PAIR || st == 0) fetch(w.b, w.item);
     }
     while (w.more()) {
-        const TcItem<KIND> item = next;
+        TcItem<KIND> item;
+        if constexpr (KIND == kWhole) item = TcItem<KIND>(w.b, w.item, groups, item_rows, next_span);
+        else item = TcItem<KIND>(a, w.b, w.item, groups, item_rows);
         const AttendSpan span = item.s;
         item.open(w);
         const int n = w.n, b = item.b, h = item.h, r0 = item.r0;
@@ -381,24 +391,25 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         tc_fence_before();
         bar_arrive_warp(&c.q_ready);
         const bool last = w.last();
-        if (!last)
-            next = TcItem<KIND>(a, w.item + 1 == per ? w.b + 1 : w.b, w.item + 1 == per ? 0 : w.item + 1, groups, item_rows);
+        const int next_b = w.item + 1 == per ? w.b + 1 : w.b, next_item = w.item + 1 == per ? 0 : w.item + 1;
+        if (KIND == kWhole && !last) next_span = attend_span(a, next_b);
         ++items;
 
         const int row = r0 + (PAIR ? st * 128 : 0) + tid, t = row / a.G;
         const bool live = row < rows && t < span.add;
         const bool warp_live = __any_sync(0xffffffffu, live);
         const bool stream_live = PAIR ? r0 + st * 128 < rows : true;
-        if (PAIR && !stream_live && !last) fetch(next);
+        if (PAIR && !stream_live && !last) fetch(next_b, next_item);
         const int t_first = (row - lane) / a.G, t_last = min(min(row - lane + 31, rows - 1) / a.G, a.T - 1);  // of the warp
         // LONG: what a row sees is places [first, upto) and those below the sinks' end, without a mask and depths of its own
         // also among the drafted tokens; the warp's rows all see places [all_from, all_to)
         const bool chain = KIND != kWhole && !a.mask && (!a.depth || !a.window);
-        int first = 0, upto = 0, all_from = 0, all_to = 0;
+        int first = 0, upto = 0, all_from = 0, all_to = 0, clear_to = 0;
         if constexpr (KIND != kWhole) {
             if (live) first = long_first(a, item.it.s, long_depth(a, b, t));
             upto = chain ? span.ctx + t + 1 : span.ctx;
             all_to = chain ? span.ctx + t_first + 1 : span.ctx;
+            clear_to = chain ? span.ctx + r0 / a.G + 1 : span.ctx;
             all_from = a.depth ? item.it.lo_most : long_first(a, item.it.s, t_last);
         }
         if (a.T <= 64 && !chain && (b != seen_b || r0 != seen_r0) && warp_live) {
@@ -464,7 +475,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
             const int tile_k0 = item.begin(w.tile + q), end = item.end(w.tile + q), subs = item.subs(w.tile + q);
             // places that not all of the item's tokens see, in 16 bits
             const bool to_clean = KIND == kWhole ? tile_k0 + kTile > span.ctx
-                                                 : !item.packed(w.tile + q) && item.unclear(chain, tile_k0, end, a.G);
+                                                 : !item.packed(w.tile + q) && item.unclear(clear_to, tile_k0, end);
             for (int sub = PAIR ? 0 : st; sub < subs; sub += PAIR ? 1 : 2) {
                 const int k0 = tile_k0 + sub * kSub;
                 const bool tail = KIND == kWhole ? k0 + kSub > span.ctx : k0 + kSub > min(end, all_to) || k0 < all_from;
@@ -500,7 +511,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 if (!bar_wait(&c.s_full[st][buf], (products / 2) & 1, c)) return;
                 tc_fence_after();
                 // the item's last scores are there: this stream's queries have been read
-                if (PAIR && q == n - 1 && sub == subs - 1 && !last) fetch(next);
+                if (PAIR && q == n - 1 && sub == subs - 1 && !last) fetch(next_b, next_item);
                 __syncwarp();
                 if (warp_live) {
                     uint32_t s[2][32];
@@ -607,7 +618,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         } else if (!PAIR && st == 1) {
             columns = 0;
         }
-        if (!PAIR && !both && st == 0 && !last) fetch(next);
+        if (!PAIR && !both && st == 0 && !last) fetch(next_b, next_item);
         float4* pass = reinterpret_cast<float4*>(merge);  // [columns / 4][kept]
         float ll = live ? l : 0.0f;
         for (int d0 = 0; d0 < D && columns > 0; d0 += columns) {
@@ -627,7 +638,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                 }
                 if (!sync_all()) return;
                 if (st == 0 && d0 == 0) {
-                    if (!last) fetch(next);  // both streams are through with the queries
+                    if (!last) fetch(next_b, next_item);  // both streams are through with the queries
                     const float2 x = c.ml[tid];
                     const float mm = fmaxf(m, x.x), ref = mm == -INFINITY ? 0.0f : mm;
                     f0 = fast_exp2(m - ref);
@@ -688,7 +699,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                             }
                         } else {
                             for (int i = w.tile; i < w.tile + n; ++i) {
-                                if (item.packed(i) || !item.unclear(chain, item.begin(i), item.end(i), a.G)) continue;
+                                if (item.packed(i) || !item.unclear(clear_to, item.begin(i), item.end(i))) continue;
                                 for (int l0 = item.begin(i); l0 < item.end(i); ++l0)
                                     if ((l0 >= span.ctx || l0 < item.it.lo_most) && item.it.wanted(l0, 1) &&
                                         item.it.sees(a, b, mrow, t, first, l0))
@@ -741,7 +752,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
 template <int D, bool PAIR, int SLOTS, int KIND>
 __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const CUtensorMap* map, char* ring,
                                         unsigned long long* full, unsigned long long* empty, bool report) {
-    using S = TcShape<D, PAIR>;
+    using S = TcShape<D, PAIR, KIND>;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
@@ -816,7 +827,7 @@ template <bool PAIR> __device__ __forceinline__ bool tc_has(int st, int sub, int
 // The score products of both streams, tile after tile.
 template <int D, bool PAIR, int KIND>
 __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, char* q_smem, char* k_ring) {
-    using S = TcShape<D, PAIR>;
+    using S = TcShape<D, PAIR, KIND>;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
@@ -873,7 +884,7 @@ out:
 // The products of weights and values of both streams.
 template <int D, bool PAIR, int KIND>
 __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char* v_ring) {
-    using S = TcShape<D, PAIR>;
+    using S = TcShape<D, PAIR, KIND>;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
     const uint32_t t_s = uniform(c.tmem), ring = uniform(smem_u32(v_ring));
@@ -887,7 +898,13 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
         uint32_t begun[2] = {0, 0};
         for (int q = 0; q < n; ++q, at.next()) {
             const int subs = item.subs(w.tile + q);
-            const bool packed = item.packed(w.tile + q);
+            // 16 bits: a line a token, the second half's lines behind the first's; packed: a line a channel, the second half of
+            // the tokens behind the first
+            const bool packed = KIND == kPacked && item.packed(w.tile + q);
+            const uint32_t half_bytes = KIND == kPacked ? uniform(packed ? D * 128 : kSub * 128) : kSub * 128;
+            const uint32_t step = KIND == kPacked ? uniform(packed ? 32 : 2048) : 2048;
+            const uint32_t lead = KIND == kPacked ? uniform(packed ? 16 : 16384) : 16384;
+            const uint32_t desc = KIND == kPacked ? uniform(packed ? mma_desc(D, false) : mma_desc(D, true)) : mma_desc(D, true);
             if (!bar_wait(&c.full_v[at.slot], at.parity, c)) goto out;
 #pragma unroll
             for (int sub = 0; sub < 2; ++sub)
@@ -898,22 +915,14 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
                     if (!bar_wait(&c.p_ready[st][buf], (done[st] / 2) & 1, c)) goto out;
                     ++done[st];
                     tc_fence_after();
-                    // 16 bits: a line a token, the halves' lines one behind the other; packed: a line a channel, a half of
-                    // the tokens behind the other
-                    const uint32_t v_at = uniform(ring + at.slot * S::kUnit) + sub * (packed ? D : kSub) * 128;
+                    const uint32_t v_at = uniform(ring + at.slot * S::kUnit) + sub * half_bytes;
                     const uint32_t p_at = uniform(t_s + st * 128 + 64 * buf);
                     const bool add = KIND == kWhole ? uniform((PAIR ? sub > 0 : 0) | q) : uniform(begun[st]);  // the first of an item starts the sums
                     begun[st] = 1;
                     if (elect_one()) {
 #pragma unroll
-                        for (int i = 0; i < kSub / 16; ++i) {
-                            if (KIND == kPacked && packed)
-                                mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * 32, 16, 1024),
-                                       mma_desc(D, false), i > 0 || add);
-                            else
-                                mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * 2048, 16384, 1024),
-                                       mma_desc(D, true), i > 0 || add);
-                        }
+                        for (int i = 0; i < kSub / 16; ++i)
+                            mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * step, lead, 1024), desc, i > 0 || add);
                         tc_commit(&c.pv_done[st][buf]);
                     }
                     __syncwarp();
@@ -930,104 +939,166 @@ out:
     bar_wait<true>(&c.drained[1], 0, c);
 }
 
-// Packed tiles into both rings, as the products read them: warps 0, 1 of four the keys (a line a token), 2, 3 the values (a
-// line a channel, so that the tokens, whose pairs share a word, lie side by side).  A warp takes every second
-// pair of patches of 32 tokens and 32 channels; lanes of even r take the first patch of a pair first, the others the second,
-// which keeps the stores of eight lanes in different banks.
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, int bytes, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
+}
+
+// Packed tiles into both rings, as the products read them: two warps the keys (a line a token), two the values (a
+// line a channel, so that the tokens, whose pairs share a word, lie side by side).  The first of two also has the packed
+// bytes copied, 64 places at a time and up to three such halves ahead, into slots that both read.  A warp
+// takes every second pair of patches of 32 tokens and 32 channels; lanes of even r take the first patch of a
+// pair first, the others the second, which keeps the stores of eight lanes in different banks.  (Packed words straight from HBM
+// into registers, all patches of a tile unrolled: the code was longer than what the instruction caches hold beside the others',
+// 64 trees of 61 tokens took 927 us.)
 template <int D, bool PAIR, int SLOTS, bool KEYS>
-__device__ __forceinline__ void tc_expand(const AttendArgs& a, TcControl& c, char* ring, unsigned long long* full,
+__device__ __forceinline__ void tc_expand(const AttendArgs& a, TcControl& c, char* ring, char* raw, unsigned long long* full,
                                           unsigned long long* empty) {
-    using S = TcShape<D, PAIR>;
+    using S = TcShape<D, PAIR, kPacked>;
+    constexpr int X = D / 32, which = KEYS ? 0 : 1;
+    constexpr int kRawScales = 32 * D;  // where a slot's scales lie, behind the codes
     const int lane = threadIdx.x & 31, r = lane >> 2, t4 = lane & 3, half = threadIdx.x >> 5 & 1;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<kPacked>(a, groups);
-    const int N = packed_tokens(a.P), block_bytes = packed_block_bytes(N, D);
-    constexpr int X = D / 32, kPatches = 4 * X / 2;  // of a warp
-    // the lane's place in a block, its first patch of 32 channels
-    const int sub_block = N == 16 ? (KEYS ? r >> 2 : t4 >> 1) : 0;
-    const int code_at = KEYS ? ((N == 16 ? r & 3 : r) * 4 + t4) * 16
-                             : N * D / 2 + (r * (N / 8) + (N == 16 ? t4 & 1 : t4)) * 16;
-    const int scale_at = KEYS ? N * D + 8 * t4 : N * D + D + 8 * (N == 16 ? t4 & 1 : t4);
-    uint32_t u = 0;
-    for (TcWalk w(c.cut); w.more(); w.next(per)) {
-        const TcItem<kPacked> item(a, w.b, w.item, groups, item_rows);
-        item.open(w);
-        const int32_t* table = a.table4 + (int64_t)item.b * a.max_pages4;
-        for (int q = 0; q < w.n; ++q, ++u) {
-            const int slot = u % SLOTS;
-            const bool packed = item.packed(w.tile + q);
-            uint4 words[kPatches];
-            uint2 scales[kPatches];
-            if (packed) {
-                // where the tile's runs of 32 tokens lie: the lane's block of each
-                const int k0 = item.begin(w.tile + q);
-                const uint8_t* block[4];
-#pragma unroll
-                for (int run = 0; run < 4; ++run) {
-                    const int place = k0 + 32 * run + 16 * sub_block;
-                    block[run] = nullptr;
-                    if (place >= item.it.s.pk || !item.it.wanted(place, N)) continue;
-                    const int page = table[place >> a.page_shift];
-                    if (page < 0 || page >= a.pages4) {
-                        if (KEYS) atomicOr(a.status, kStBadIndex);
-                        continue;
-                    }
-                    block[run] = a.packed.data + page * a.packed.page + item.h * a.packed.head + (place & (a.P - 1)) / N * block_bytes;
-                }
-#pragma unroll
-                for (int i = 0; i < kPatches; ++i) {
-                    // pair i / 2 of this warp; keys: neighbouring channels, values: neighbouring tokens
-                    const int pair = 2 * (i / 2) + half, second = (i ^ r) & 1;
-                    const int x = KEYS ? 2 * (pair % (X / 2)) + second : pair % X;
-                    const int i2 = i / 2;  // (constant places in `block`, whatever `half` is)
-                    const uint8_t* at = !KEYS    ? (second ? block[2 * (2 * i2 / X) + 1] : block[2 * (2 * i2 / X)])
-                                        : X == 4 ? block[i2]
-                                                 : (half ? block[(2 * i2 + 1) % 4] : block[2 * i2 % 4]);
-                    words[i] = make_uint4(kPackedZero, kPackedZero, kPackedZero, kPackedZero);
-                    scales[i] = make_uint2(0, 0);
-                    if (at) {
-                        words[i] = *reinterpret_cast<const uint4*>(at + code_at + N * 16 * x);
-                        scales[i] = *reinterpret_cast<const uint2*>(at + scale_at + (KEYS ? 32 : N) * x);
+    const int N = packed_tokens(a.P), codes = N * D / 2, marks = KEYS ? D : N * D / 32;  // bytes of a block's codes, scales
+    // the lane's place in the codes and scales of a run of 32 tokens (two blocks of 16, or one), its first patch of 32 channels
+    const int sub = N == 16 ? (KEYS ? r >> 2 : t4 >> 1) : 0, in_run = 32 / N;
+    const int code_at = sub * codes + (KEYS ? ((N == 16 ? r & 3 : r) * 4 + t4) * 16
+                                            : (r * (N / 8) + (N == 16 ? t4 & 1 : t4)) * 16);
+    const int scale_at = kRawScales + sub * marks + (KEYS ? 8 * t4 : 8 * (N == 16 ? t4 & 1 : t4));
+
+    // halves on their way, by the first warp: a walk of its own
+    TcWalk cw(c.cut);
+    TcItem<kPacked> ci;
+    int cq = 0, chalf = 0;
+    uint32_t copied = 0;
+    bool copying = half == 0 && cw.more();
+    if (copying) {
+        ci = TcItem<kPacked>(a, cw.b, cw.item, groups, item_rows);
+        ci.open(cw);
+    }
+    auto copy_next = [&]() -> bool {
+        while (copying) {
+            const int i = cw.tile + cq, k0 = ci.begin(i) + 64 * chalf;
+            const bool there = ci.packed(i);
+            const TcItem<kPacked> item = ci;
+            const int n4 = ci.it.end(ci.it.number(i));
+            // on to the next half
+            if (there && chalf == 0 && ci.subs(i) == 2) {
+                chalf = 1;
+            } else {
+                chalf = 0;
+                if (++cq >= cw.n || !there) {  // an item's packed tiles come first
+                    cw.next(per);
+                    cq = 0;
+                    copying = cw.more();
+                    if (copying) {
+                        ci = TcItem<kPacked>(a, cw.b, cw.item, groups, item_rows);
+                        ci.open(cw);
                     }
                 }
             }
-            if (u >= SLOTS && !bar_wait(&empty[slot], (u / SLOTS - 1) & 1, c)) return;
-            if (packed) {
-                char* tile = ring + slot * S::kUnit;
+            if (!there) continue;
+            const uint32_t slot = copied % S::kRaw;
+            const int place = k0 + lane * N;
+            const uint8_t* src = nullptr;
+            if (lane < 64 / N && place < n4 && item.it.wanted(place, N)) {
+                const int page = a.table4[(int64_t)item.b * a.max_pages4 + (place >> a.page_shift)];
+                if (page >= 0 && page < a.pages4)
+                    src = a.packed.data + page * a.packed.page + item.h * a.packed.head +
+                          (place & (a.P - 1)) / N * packed_block_bytes(N, D);
+                else if (KEYS)
+                    atomicOr(a.status, kStBadIndex);
+            }
+            const uint32_t have = __ballot_sync(0xffffffffu, src != nullptr);
+            if (copied >= S::kRaw && !bar_wait(&c.raw_empty[which][slot], (copied / S::kRaw - 1) & 1, c)) return false;
+            if (lane == 0) {
+                c.raw_have[which][slot] = have;
+                bar_expect(&c.raw_full[which][slot], __popc(have) * (codes + marks));
+            }
+            __syncwarp();
+            if (src) {
+                const uint32_t to = smem_u32(raw + slot * S::kRawUnit);
+                bulk_copy(to + lane * codes, src + (KEYS ? 0 : codes), codes, &c.raw_full[which][slot]);
+                bulk_copy(to + kRawScales + lane * marks, src + 2 * codes + (KEYS ? 0 : D), marks, &c.raw_full[which][slot]);
+            }
+            __syncwarp();
+            ++copied;
+            return true;
+        }
+        return true;
+    };
+    bool fine = true;
+    uint32_t u = 0, taken = 0;
+    for (TcWalk w(c.cut); w.more() && fine; w.next(per)) {
+        const TcItem<kPacked> item(a, w.b, w.item, groups, item_rows);
+        item.open(w);
+        for (int q = 0; q < w.n && fine; ++q, ++u) {
+            const int slot = u % SLOTS;
+            if (u >= SLOTS && !bar_wait(&empty[slot], (u / SLOTS - 1) & 1, c)) {
+                fine = false;
+                break;
+            }
+            if (item.packed(w.tile + q)) {
+                const int halves = item.subs(w.tile + q);
+                for (int hf = 0; hf < halves && fine; ++hf, ++taken) {
+                    const uint32_t rs = taken % S::kRaw;
+#pragma unroll 1
+                    while (copying && copied < taken + S::kRaw && fine) fine = copy_next();
+                    if (!bar_wait(&c.raw_full[which][rs], (taken / S::kRaw) & 1, c)) {
+                        fine = false;
+                        break;
+                    }
+                    const uint32_t have = c.raw_have[which][rs];
+                    const char* from = raw + rs * S::kRawUnit;
+                    char* tile = ring + slot * S::kUnit;
+#pragma unroll 1
+                    for (int i = 0; i < X; ++i) {
+                        // keys: neighbouring patches of channels, values: of tokens
+                        const int second = (i ^ r) & 1, pair = 2 * (i / 2) + half;
+                        const int run = KEYS ? pair / (X / 2) : second, x = KEYS ? 2 * (pair % (X / 2)) + second : pair;
+                        uint4 words = *reinterpret_cast<const uint4*>(from + run * in_run * codes + code_at + N * 16 * x);
+                        uint2 bytes = *reinterpret_cast<const uint2*>(from + run * in_run * marks + scale_at + (KEYS ? 32 : N) * x);
+                        if (!((have >> (run * in_run + sub)) & 1)) {
+                            words = make_uint4(kPackedZero, kPackedZero, kPackedZero, kPackedZero);
+                            bytes = make_uint2(0, 0);
+                        }
+                        uint32_t s[4], o[4], d[4][4];
+                        packed_scales(bytes, s, o);
+                        packed_words(words, s, o, d);
+                        // rows: the tile's tokens, or the channels; octets of the other
+                        const int row0 = (KEYS ? 64 * hf + 32 * run : 32 * x) + 8 * (r >> 1) + (r & 1);
+                        const int octet = KEYS ? 4 * x + t4 : 4 * run + t4;
+                        char* line = tile + (KEYS ? (octet >> 3) * 16384 : hf * D * 128) + row0 * 128;
 #pragma unroll
-                for (int i = 0; i < kPatches; ++i) {
-                    const int pair = 2 * (i / 2) + half, second = (i ^ r) & 1;
-                    const int run = KEYS ? pair / (X / 2) : 2 * (pair / X) + second;
-                    const int x = KEYS ? 2 * (pair % (X / 2)) + second : pair % X;
-                    uint32_t s[4], o[4], d[4][4];
-                    packed_scales(scales[i], s, o);
-                    packed_words(words[i], s, o, d);
-                    // rows: the run's tokens, or the patch's channels; octets of the other
-                    const int row0 = 32 * (KEYS ? run : x) + 8 * (r >> 1) + (r & 1), octet = 4 * (KEYS ? x : run) + t4;
-                    char* line = tile + (octet >> 3) * (KEYS ? 16384 : D * 128) + row0 * 128;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        *reinterpret_cast<uint4*>(line + 256 * k + (((octet & 7) ^ ((row0 + 2 * k) & 7)) << 4)) =
-                            make_uint4(d[k][0], d[k][1], d[k][2], d[k][3]);
+                        for (int k = 0; k < 4; ++k)
+                            *reinterpret_cast<uint4*>(line + 256 * k + (((octet & 7) ^ ((row0 + 2 * k) & 7)) << 4)) =
+                                make_uint4(d[k][0], d[k][1], d[k][2], d[k][3]);
+                    }
+                    bar_arrive_warp(&c.raw_empty[which][rs]);
                 }
                 fence_async();
             }
             bar_arrive_warp(&full[slot]);
         }
     }
+    // no copy is in flight when the CTA ends
+    for (; half == 0 && taken < copied; ++taken) bar_wait<true>(&c.raw_full[which][taken % S::kRaw], (taken / S::kRaw) & 1, c);
 }
 
 template <int D, bool PAIR, int KIND>
 __global__ void __launch_bounds__(tc_threads(KIND), 1)
     attend_tc_kernel(const AttendArgs a, const __grid_constant__ CUtensorMap key, const __grid_constant__ CUtensorMap value) {
-    using S = TcShape<D, PAIR>;
+    using S = TcShape<D, PAIR, KIND>;
     extern __shared__ char raw[];
     char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     char* q_smem = base;
     char* k_ring = q_smem + S::kQueries;
     char* v_ring = k_ring + S::kK * S::kUnit;
     char* merge = v_ring + S::kV * S::kUnit;
-    TcControl& c = *reinterpret_cast<TcControl*>(merge + S::kMerge);
+    char* raw_ring = merge + S::kMerge;
+    TcControl& c = *reinterpret_cast<TcControl*>(raw_ring + 2 * S::kRaw * S::kRawUnit);
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         constexpr int fill = KIND == kPacked ? 3 : 1;  // the loading warp, and two that expand
@@ -1038,6 +1109,10 @@ __global__ void __launch_bounds__(tc_threads(KIND), 1)
         for (int i = 0; i < S::kV; ++i) {
             bar_init(&c.full_v[i], fill);
             bar_init(&c.empty_v[i], 1);
+        }
+        for (int i = 0; i < 2 * S::kRaw; ++i) {
+            bar_init(&c.raw_full[i / 3][i % 3], 1);
+            bar_init(&c.raw_empty[i / 3][i % 3], 2);
         }
         for (int i = 0; i < 2; ++i) {
             for (int buf = 0; buf < 2; ++buf) {
@@ -1086,8 +1161,8 @@ __global__ void __launch_bounds__(tc_threads(KIND), 1)
         else tc_sums<D, PAIR, KIND>(a, c, v_ring);
     } else if constexpr (KIND == kPacked) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExpandRegs));
-        if (warp < 14) tc_expand<D, PAIR, S::kK, true>(a, c, k_ring, c.full_k, c.empty_k);
-        else tc_expand<D, PAIR, S::kV, false>(a, c, v_ring, c.full_v, c.empty_v);
+        if (warp < 14) tc_expand<D, PAIR, S::kK, true>(a, c, k_ring, raw_ring, c.full_k, c.empty_k);
+        else tc_expand<D, PAIR, S::kV, false>(a, c, v_ring, raw_ring + S::kRaw * S::kRawUnit, c.full_v, c.empty_v);
     }
     tc_fence_before();
     __syncthreads();
@@ -1134,7 +1209,7 @@ template <int D, bool PAIR, int KIND> cudaError_t launch_tc(const AttendArgs& a,
     if (!encode(&key, a, a.kv.key, a.kv.key_page, a.kv.key_head, a.kv.key_token) ||
         !encode(&value, a, a.kv.value, a.kv.value_page, a.kv.value_head, a.kv.value_token))
         return cudaErrorInvalidValue;
-    constexpr size_t smem = tc_smem_bytes<D, PAIR>();
+    constexpr size_t smem = tc_smem_bytes<D, PAIR, KIND>();
     static_assert(smem <= 227 * 1024);
     if (KIND == kPacked) {
         // the groups' registers are taken from what the block was launched with: less would leave a group waiting

@@ -107,7 +107,7 @@ struct CacheLayout {
 
 CacheLayout cache_layout(const rheo_cache_config& c) {
     const int G = c.q_heads / c.kv_heads;
-    const size_t ctas = kAttendCtas, rows = attend_part_rows(c.dtype, c.tokens, G);
+    const size_t ctas = attend_most_ctas(c.dtype, c.tokens, G), rows = attend_part_rows(c.dtype, c.tokens, G);
     CacheLayout L{};
     size_t o = kPartsAt;
     auto take = [&](size_t bytes) {
