@@ -58,7 +58,7 @@ constexpr int kScores = 2;                   // score buffers of a stream
 constexpr int kTcThreads = 12 * 32, kTcPackedThreads = 16 * 32;
 __host__ __device__ constexpr int tc_threads(int kind) { return kind == 2 ? kTcPackedThreads : kTcThreads; }
 // Registers a thread where sixteen warps share them: softmax groups, warps that load and issue, warps that expand packed tiles.
-constexpr int kSoftmaxRegs = 160, kIssueRegs = 80, kExpandRegs = 112, kPackedLaunchRegs = 128;
+constexpr int kSoftmaxRegs = 168, kIssueRegs = 88, kExpandRegs = 88, kPackedLaunchRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kExpandRegs <= 4 * kPackedLaunchRegs);
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
@@ -70,8 +70,9 @@ template <int D, bool PAIR, int KIND> struct TcShape {
     static constexpr int kK = D == 128 ? 2 : KIND == 2 ? 4 : 5;                   // slots of the key ring
     static constexpr int kV = D == 128 ? (KIND == 2 ? 2 : 3) : KIND == 2 ? 4 : 5;  // and of the value ring, which is read later
     // Packed tiles on their way: 64 places' codes and scales of the keys, or the values, a slot.
-    static constexpr int kRaw = KIND == 2 ? 3 : 0;
-    static constexpr int kRawUnit = 36 * D;  // four blocks of 16 tokens: the most
+    static constexpr int kRaw = 3;
+    static constexpr int kRawUnit = KIND == 2 ? 36 * D : 0;  // four blocks of 16 tokens: the most
+    static constexpr int kRawScales = 32 * D;                // where the scales lie, behind the codes
     static constexpr int kQ = 128 * D * 2;       // bytes of 128 rows of queries
     static constexpr int kQueries = PAIR ? 2 * kQ : kQ;
     static constexpr int kMerge = PAIR ? 0 : 16384;
@@ -152,9 +153,10 @@ __device__ __forceinline__ bool elect_one() {
         : "=r"(e)::"memory");
     return e != 0;
 }
-__device__ __forceinline__ void tc_commit(unsigned long long* b) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b)) : "memory");
+__device__ __forceinline__ void tc_commit_at(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void tc_commit(unsigned long long* b) { tc_commit_at(smem_u32(b)); }
 // A value that is the same in all lanes, in a register that the compiler knows to be.
 __device__ __forceinline__ uint32_t uniform(uint32_t x) { return __reduce_or_sync(0xffffffffu, x); }
 
@@ -223,6 +225,12 @@ __device__ __forceinline__ void tma_tile(uint32_t dst, const CUtensorMap* map, i
         "cp.async.bulk.tensor.4d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
         "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(0), "r"(head), "r"(page)
         : "memory");
+}
+
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, int bytes, unsigned long long* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
+                 "r"(bytes), "r"(smem_u32(bar))
+                 : "memory");
 }
 
 using TcWalk = AttendWalk<kTile>;
@@ -748,17 +756,42 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
     asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// Key tiles, or value tiles, into their ring: lane = (page, half) of a tile.
-template <int D, bool PAIR, int SLOTS, int KIND>
-__device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const CUtensorMap* map, char* ring,
-                                        unsigned long long* full, unsigned long long* empty, bool report) {
+// A place in a ring: slot and the parity of its phase, one step at a time.
+struct TcSlot {
+    uint32_t slot = 0, parity = 0;
+    __device__ __forceinline__ void next(uint32_t slots) {
+        if (++slot == slots) {
+            slot = 0;
+            parity ^= 1;
+        }
+    }
+};
+
+// Key tiles, or value tiles, into their ring: lane = (page, half) of a tile.  Packed ones go to a ring of their own, 64
+// places at a time, from which tc_expand fills the other; lane = block.
+template <int D, bool PAIR, int KIND>
+__device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, bool keys, const CUtensorMap* map, char* ring, char* raw) {
     using S = TcShape<D, PAIR, KIND>;
+    unsigned long long* const full = keys ? c.full_k : c.full_v;
+    unsigned long long* const empty = keys ? c.empty_k : c.empty_v;
+    unsigned long long* const raw_full = c.raw_full[keys ? 0 : 1];
+    unsigned long long* const raw_empty = c.raw_empty[keys ? 0 : 1];
+    uint32_t* const raw_have = c.raw_have[keys ? 0 : 1];
+    const uint32_t slots = keys ? S::kK : S::kV;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
     const int boxes = kTile / a.P * S::kHalves;
     const int pi = lane / S::kHalves, half = lane % S::kHalves;
-    uint32_t u = 0;
+    const int N = packed_tokens(a.P), codes = N * D / 2, marks = keys ? D : N * D / 32;  // bytes of a block's codes, scales
+    TcSlot at;
+    uint32_t u = 0, copied = 0, seen = 0;  // tiles; packed halves copied, and known to have been expanded
+    // Packed halves before the `to`-th have been expanded.
+    auto expanded = [&](uint32_t to) {
+        for (; seen < to; ++seen)
+            if (!bar_wait(&raw_empty[seen % S::kRaw], (seen / S::kRaw) & 1, c)) return false;
+        return true;
+    };
     for (TcWalk w(c.cut); w.more();) {
         const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);
         const int h = item.h;
@@ -767,34 +800,67 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
         const int32_t* table = a.block_table + (int64_t)item.b * a.max_pages;
         // whether a token may see some of this lane's places of the tile, which begin at l0
         auto wants = [&](int i, int& l0) {
+            if (KIND == kPacked && item.packed(i)) {
+                l0 = item.begin(i) + lane * N;
+                return lane < kTile / N && l0 < item.end(i) && item.it.wanted(l0, N);
+            }
             l0 = item.begin(i) + pi * a.P;
-            return lane < boxes && l0 < item.end(i) && (KIND == kWhole || (!item.packed(i) && item.it.wanted(l0, a.P)));
+            return lane < boxes && l0 < item.end(i) && (KIND == kWhole || item.it.wanted(l0, a.P));
         };
         auto page_of = [&](int q) {
-            int page = a.pages, l0;  // past the pool: reads as zeros
-            if (q < n && wants(w.tile + q, l0)) page = table[(KIND == kWhole ? l0 : l0 - item.it.s.pk) >> a.page_shift];
+            int page = -1, l0;
+            if (KIND == kPacked && q < n && item.packed(w.tile + q)) {
+                if (wants(w.tile + q, l0)) page = a.table4[(int64_t)item.b * a.max_pages4 + (l0 >> a.page_shift)];
+            } else {
+                page = a.pages;  // past the pool: reads as zeros
+                if (q < n && wants(w.tile + q, l0)) page = table[(KIND == kWhole ? l0 : l0 - item.it.s.pk) >> a.page_shift];
+            }
             return page;
         };
         int page = page_of(0);
-        for (int q = 0; q < n; ++q, ++u) {
+        for (int q = 0; q < n; ++q, ++u, at.next(slots)) {
             const int next = page_of(q + 1);
-            const int slot = u % SLOTS;
-            if (u >= SLOTS && !bar_wait(&empty[slot], (u / SLOTS - 1) & 1, c)) goto out;
-            if (item.packed(w.tile + q)) {  // tc_expand's
-                if (lane == 0) bar_arrive(&full[slot]);
+            int l0;
+            if (KIND == kPacked && item.packed(w.tile + q)) {
+                const bool wanted = wants(w.tile + q, l0), good = wanted && page >= 0 && page < a.pages4;
+                if (keys && wanted && !good) atomicOr(a.status, kStBadIndex);
+                const uint32_t have = __ballot_sync(0xffffffffu, good);
+                const uint8_t* src = a.packed.data + (good ? page * a.packed.page : 0) + h * a.packed.head +
+                                     (l0 & (a.P - 1)) / N * packed_block_bytes(N, D);
+                const int subs = item.subs(w.tile + q), blocks = 64 / N;
+                for (int sub = 0; sub < subs; ++sub, ++copied) {
+                    const uint32_t rs = copied % S::kRaw;
+                    if (copied >= S::kRaw && !expanded(copied - S::kRaw + 1)) goto out;
+                    const uint32_t mine = have >> (sub * blocks) & ((1u << blocks) - 1);
+                    if (lane == 0) {
+                        raw_have[rs] = mine;
+                        bar_expect(&raw_full[rs], __popc(mine) * (codes + marks));
+                    }
+                    __syncwarp();
+                    const int k = lane - sub * blocks;
+                    if (good && k >= 0 && k < blocks) {
+                        const uint32_t to = smem_u32(raw + rs * S::kRawUnit);
+                        bulk_copy(to + k * codes, src + (keys ? 0 : codes), codes, &raw_full[rs]);
+                        bulk_copy(to + S::kRawScales + k * marks, src + 2 * codes + (keys ? 0 : D), marks, &raw_full[rs]);
+                    }
+                    __syncwarp();
+                }
                 page = next;
                 continue;
             }
-            if (lane == 0) bar_expect(&full[slot], S::kUnit);
+            // (a phase of `empty` may be waited for only when the one before it has ended: the warps that expanded the tiles
+            // up to here have met it)
+            if (KIND == kPacked && !expanded(copied)) goto out;
+            if (u >= slots && !bar_wait(&empty[at.slot], at.parity ^ 1, c)) goto out;
+            if (lane == 0) bar_expect(&full[at.slot], S::kUnit);
             __syncwarp();
             if (page < 0 || page > a.pages) {
-                if (report) atomicOr(a.status, kStBadIndex);
+                if (keys) atomicOr(a.status, kStBadIndex);
                 page = a.pages;
             }
             if (lane < boxes) {
-                int l0;
-                if (report && page == a.pages && wants(w.tile + q, l0)) atomicOr(a.status, kStBadIndex);
-                tma_tile(smem_u32(ring + slot * S::kUnit + half * 16384 + pi * a.P * 128), map, half * 64, h, page, &full[slot]);
+                if (keys && page == a.pages && wants(w.tile + q, l0)) atomicOr(a.status, kStBadIndex);
+                tma_tile(smem_u32(ring + at.slot * S::kUnit + half * 16384 + pi * a.P * 128), map, half * 64, h, page, &full[at.slot]);
             }
             page = next;
         }
@@ -802,22 +868,17 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, const
     }
 out:
     // no copy is in flight when the CTA ends, and no arrival of a product that read one
-    for (uint32_t x = u > SLOTS ? u - SLOTS : 0; x < u; ++x) {
-        bar_wait<true>(&full[x % SLOTS], (x / SLOTS) & 1, c);
-        bar_wait<true>(&empty[x % SLOTS], (x / SLOTS) & 1, c);
+    for (; seen < copied; ++seen) bar_wait<true>(&raw_empty[seen % S::kRaw], (seen / S::kRaw) & 1, c);
+    for (uint32_t x = u > slots ? u - slots : 0; x < u; ++x) {
+        bar_wait<true>(&full[x % slots], (x / slots) & 1, c);
+        bar_wait<true>(&empty[x % slots], (x / slots) & 1, c);
     }
 }
 
-// A place in a ring: slot and the parity of its phase, one step at a time.
-template <int SLOTS> struct TcSlot {
-    uint32_t slot = 0, parity = 0;
-    __device__ __forceinline__ void next() {
-        if (++slot == SLOTS) {
-            slot = 0;
-            parity ^= 1;
-        }
-    }
-};
+// Products of a tile in the issuing warps' code: one after the other, or a loop over the four, because the loops of all
+// roles together have to stay in the instruction cache.  64 trees of 61 tokens: 265 us and 286 without windows or packed
+// pages; over packed pages 669 and 439.
+template <int KIND> constexpr int kProductUnroll = KIND == kWhole ? 4 : 1;
 
 // Which streams have a product with half `sub` of a tile that has `subs` halves.
 template <bool PAIR> __device__ __forceinline__ bool tc_has(int st, int sub, int subs, bool second) {
@@ -832,8 +893,8 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
     const uint32_t t_s = uniform(c.tmem), q_at = uniform(smem_u32(q_smem)), ring = uniform(smem_u32(k_ring));
-    uint32_t items = 0, done[2] = {0, 0};
-    TcSlot<S::kK> at;
+    uint32_t items = 0, done0 = 0, done1 = 0;  // products of both streams
+    TcSlot at;
     for (TcWalk w(c.cut); w.more(); ++items) {
         const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);
         item.open(w);
@@ -842,32 +903,33 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
         if (!bar_wait(&c.q_ready, items & 1, c)) goto out;
         tc_fence_after();
         if (lane == 0) bar_arrive(&c.q_taken);
-        for (int q = 0; q < n; ++q, at.next()) {
+        for (int q = 0; q < n; ++q, at.next(S::kK)) {
             const int subs = item.subs(w.tile + q);
             if (!bar_wait(&c.full_k[at.slot], at.parity, c)) goto out;
+#pragma unroll (kProductUnroll<KIND>)
+            for (int x = 0; x < 4; ++x) {
+                const int sub = x >> 1, st = x & 1;
+                if (!tc_has<PAIR>(st, sub, subs, second)) continue;
+                // the buffer's last weights have been read
+                const uint32_t d = st ? done1 : done0, buf = d & 1;
+                if (d > 1 && !bar_wait(&c.pv_done[st][buf], (d / 2 - 1) & 1, c)) goto out;
+                if (st) ++done1;
+                else ++done0;
+                tc_fence_after();
+                const uint32_t s_at = uniform(t_s + st * 128 + 64 * buf);
+                const uint64_t q_desc = smem_desc(uniform(q_at + (PAIR ? st * S::kQ : 0)), 16, 1024);
+                const uint64_t k_desc = smem_desc(uniform(ring + at.slot * S::kUnit + sub * kSub * 128), 16, 1024);
+                const uint32_t bar = uniform(smem_u32(&c.s_full[st][buf]));
+                if (elect_one()) {
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    if (!tc_has<PAIR>(st, sub, subs, second)) continue;
-                    // the buffer's last weights have been read
-                    const uint32_t buf = done[st] & 1;
-                    if (done[st] > 1 && !bar_wait(&c.pv_done[st][buf], (done[st] / 2 - 1) & 1, c)) goto out;
-                    ++done[st];
-                    tc_fence_after();
-                    const uint32_t s_at = uniform(t_s + st * 128 + 64 * buf);
-                    const uint32_t k_at = uniform(ring + at.slot * S::kUnit) + sub * kSub * 128;
-                    if (elect_one()) {
-#pragma unroll
-                        for (int i = 0; i < D / 16; ++i) {
-                            const uint32_t off = (i >> 2) * 16384 + (i & 3) * 32;
-                            mma_ss(s_at, smem_desc(q_at + (PAIR ? st * S::kQ : 0) + off, 16, 1024),
-                                   smem_desc(k_at + off, 16, 1024), mma_desc(kSub, false), i > 0);
-                        }
-                        tc_commit(&c.s_full[st][buf]);
+                    for (int i = 0; i < D / 16; ++i) {
+                        const uint32_t off = ((i >> 2) * 16384 + (i & 3) * 32) / 16;  // (addresses count 16 bytes, in the low bits)
+                        mma_ss(s_at, q_desc + off, k_desc + off, mma_desc(kSub, false), i > 0);
                     }
-                    __syncwarp();
+                    tc_commit_at(bar);
                 }
+                __syncwarp();
+            }
             if (elect_one()) tc_commit(&c.empty_k[at.slot]);
             __syncwarp();
         }
@@ -888,45 +950,45 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
     const uint32_t t_s = uniform(c.tmem), ring = uniform(smem_u32(v_ring));
-    uint32_t done[2] = {0, 0};
-    TcSlot<S::kV> at;
+    uint32_t done0 = 0, done1 = 0;
+    TcSlot at;
     for (TcWalk w(c.cut); w.more();) {
         const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);
         item.open(w);
         const int n = w.n;
         const bool second = PAIR && item.r0 + 128 < rows;
-        uint32_t begun[2] = {0, 0};
-        for (int q = 0; q < n; ++q, at.next()) {
+        uint32_t begun = 0;  // streams with sums
+        for (int q = 0; q < n; ++q, at.next(S::kV)) {
             const int subs = item.subs(w.tile + q);
             // 16 bits: a line a token, the second half's lines behind the first's; packed: a line a channel, the second half of
             // the tokens behind the first
             const bool packed = KIND == kPacked && item.packed(w.tile + q);
             const uint32_t half_bytes = KIND == kPacked ? uniform(packed ? D * 128 : kSub * 128) : kSub * 128;
-            const uint32_t step = KIND == kPacked ? uniform(packed ? 32 : 2048) : 2048;
+            const uint32_t step = KIND == kPacked ? uniform(packed ? 32 / 16 : 2048 / 16) : 2048 / 16;
             const uint32_t lead = KIND == kPacked ? uniform(packed ? 16 : 16384) : 16384;
             const uint32_t desc = KIND == kPacked ? uniform(packed ? mma_desc(D, false) : mma_desc(D, true)) : mma_desc(D, true);
             if (!bar_wait(&c.full_v[at.slot], at.parity, c)) goto out;
+#pragma unroll (kProductUnroll<KIND>)
+            for (int x = 0; x < 4; ++x) {
+                const int sub = x >> 1, st = x & 1;
+                if (!tc_has<PAIR>(st, sub, subs, second)) continue;
+                const uint32_t d = st ? done1 : done0, buf = d & 1;
+                if (!bar_wait(&c.p_ready[st][buf], (d / 2) & 1, c)) goto out;
+                if (st) ++done1;
+                else ++done0;
+                tc_fence_after();
+                const uint32_t p_at = uniform(t_s + st * 128 + 64 * buf), o_at = uniform(t_s + S::kO + st * D);
+                const uint64_t v_desc = smem_desc(uniform(ring + at.slot * S::kUnit + sub * half_bytes), lead, 1024);
+                const uint32_t add = uniform(begun >> st & 1);  // the first of an item starts the sums
+                const uint32_t bar = uniform(smem_u32(&c.pv_done[st][buf]));
+                begun |= 1u << st;
+                if (elect_one()) {
 #pragma unroll
-            for (int sub = 0; sub < 2; ++sub)
-#pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    if (!tc_has<PAIR>(st, sub, subs, second)) continue;
-                    const uint32_t buf = done[st] & 1;
-                    if (!bar_wait(&c.p_ready[st][buf], (done[st] / 2) & 1, c)) goto out;
-                    ++done[st];
-                    tc_fence_after();
-                    const uint32_t v_at = uniform(ring + at.slot * S::kUnit) + sub * half_bytes;
-                    const uint32_t p_at = uniform(t_s + st * 128 + 64 * buf);
-                    const bool add = KIND == kWhole ? uniform((PAIR ? sub > 0 : 0) | q) : uniform(begun[st]);  // the first of an item starts the sums
-                    begun[st] = 1;
-                    if (elect_one()) {
-#pragma unroll
-                        for (int i = 0; i < kSub / 16; ++i)
-                            mma_ts(t_s + S::kO + st * D, p_at + 8 * i, smem_desc(v_at + i * step, lead, 1024), desc, i > 0 || add);
-                        tc_commit(&c.pv_done[st][buf]);
-                    }
-                    __syncwarp();
+                    for (int i = 0; i < kSub / 16; ++i) mma_ts(o_at, p_at + 8 * i, v_desc + i * step, desc, i > 0 || add);
+                    tc_commit_at(bar);
                 }
+                __syncwarp();
+            }
             if (elect_one()) tc_commit(&c.empty_v[at.slot]);
             __syncwarp();
         }
@@ -939,152 +1001,79 @@ out:
     bar_wait<true>(&c.drained[1], 0, c);
 }
 
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, int bytes, unsigned long long* bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src),
-                 "r"(bytes), "r"(smem_u32(bar))
-                 : "memory");
-}
-
 // Packed tiles into both rings, as the products read them: two warps the keys (a line a token), two the values (a
-// line a channel, so that the tokens, whose pairs share a word, lie side by side).  The first of two also has the packed
-// bytes copied, 64 places at a time and up to three such halves ahead, into slots that both read.  A warp
-// takes every second pair of patches of 32 tokens and 32 channels; lanes of even r take the first patch of a
-// pair first, the others the second, which keeps the stores of eight lanes in different banks.  (Packed words straight from HBM
-// into registers, all patches of a tile unrolled: the code was longer than what the instruction caches hold beside the others',
-// 64 trees of 61 tokens took 927 us.)
-template <int D, bool PAIR, int SLOTS, bool KEYS>
-__device__ __forceinline__ void tc_expand(const AttendArgs& a, TcControl& c, char* ring, char* raw, unsigned long long* full,
-                                          unsigned long long* empty) {
+// line a channel, so that the tokens, whose pairs share a word, lie side by side).  A warp takes every second pair of
+// patches of 32 tokens and 32 channels; lanes of even r take the first patch of a pair first, the others the second,
+// which keeps the stores of eight lanes in different banks.  Rolled loops: with all patches of a tile unrolled the code was
+// longer than what the instruction caches hold beside the other warps' (64 trees of 61 tokens: 927 us), and with the look-ups
+// and copies in these warps they held the products up (835 us).
+template <int D, bool PAIR>
+__device__ __forceinline__ void tc_expand(const AttendArgs& a, TcControl& c, bool keys, char* ring, const char* raw) {
     using S = TcShape<D, PAIR, kPacked>;
-    constexpr int X = D / 32, which = KEYS ? 0 : 1;
-    constexpr int kRawScales = 32 * D;  // where a slot's scales lie, behind the codes
+    constexpr int X = D / 32;
+    unsigned long long* const full = keys ? c.full_k : c.full_v;
+    unsigned long long* const empty = keys ? c.empty_k : c.empty_v;
+    unsigned long long* const raw_full = c.raw_full[keys ? 0 : 1];
+    unsigned long long* const raw_empty = c.raw_empty[keys ? 0 : 1];
+    const uint32_t* const raw_have = c.raw_have[keys ? 0 : 1];
+    const uint32_t slots = keys ? S::kK : S::kV;
     const int lane = threadIdx.x & 31, r = lane >> 2, t4 = lane & 3, half = threadIdx.x >> 5 & 1;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<kPacked>(a, groups);
-    const int N = packed_tokens(a.P), codes = N * D / 2, marks = KEYS ? D : N * D / 32;  // bytes of a block's codes, scales
+    const int N = packed_tokens(a.P), codes = N * D / 2, marks = keys ? D : N * D / 32;  // bytes of a block's codes, scales
     // the lane's place in the codes and scales of a run of 32 tokens (two blocks of 16, or one), its first patch of 32 channels
-    const int sub = N == 16 ? (KEYS ? r >> 2 : t4 >> 1) : 0, in_run = 32 / N;
-    const int code_at = sub * codes + (KEYS ? ((N == 16 ? r & 3 : r) * 4 + t4) * 16
+    const int sub = N == 16 ? (keys ? r >> 2 : t4 >> 1) : 0, in_run = 32 / N;
+    const int code_at = sub * codes + (keys ? ((N == 16 ? r & 3 : r) * 4 + t4) * 16
                                             : (r * (N / 8) + (N == 16 ? t4 & 1 : t4)) * 16);
-    const int scale_at = kRawScales + sub * marks + (KEYS ? 8 * t4 : 8 * (N == 16 ? t4 & 1 : t4));
-
-    // halves on their way, by the first warp: a walk of its own
-    TcWalk cw(c.cut);
-    TcItem<kPacked> ci;
-    int cq = 0, chalf = 0;
-    uint32_t copied = 0;
-    bool copying = half == 0 && cw.more();
-    if (copying) {
-        ci = TcItem<kPacked>(a, cw.b, cw.item, groups, item_rows);
-        ci.open(cw);
-    }
-    auto copy_next = [&]() -> bool {
-        while (copying) {
-            const int i = cw.tile + cq, k0 = ci.begin(i) + 64 * chalf;
-            const bool there = ci.packed(i);
-            const TcItem<kPacked> item = ci;
-            const int n4 = ci.it.end(ci.it.number(i));
-            // on to the next half
-            if (there && chalf == 0 && ci.subs(i) == 2) {
-                chalf = 1;
-            } else {
-                chalf = 0;
-                if (++cq >= cw.n || !there) {  // an item's packed tiles come first
-                    cw.next(per);
-                    cq = 0;
-                    copying = cw.more();
-                    if (copying) {
-                        ci = TcItem<kPacked>(a, cw.b, cw.item, groups, item_rows);
-                        ci.open(cw);
-                    }
-                }
-            }
-            if (!there) continue;
-            const uint32_t slot = copied % S::kRaw;
-            const int place = k0 + lane * N;
-            const uint8_t* src = nullptr;
-            if (lane < 64 / N && place < n4 && item.it.wanted(place, N)) {
-                const int page = a.table4[(int64_t)item.b * a.max_pages4 + (place >> a.page_shift)];
-                if (page >= 0 && page < a.pages4)
-                    src = a.packed.data + page * a.packed.page + item.h * a.packed.head +
-                          (place & (a.P - 1)) / N * packed_block_bytes(N, D);
-                else if (KEYS)
-                    atomicOr(a.status, kStBadIndex);
-            }
-            const uint32_t have = __ballot_sync(0xffffffffu, src != nullptr);
-            if (copied >= S::kRaw && !bar_wait(&c.raw_empty[which][slot], (copied / S::kRaw - 1) & 1, c)) return false;
-            if (lane == 0) {
-                c.raw_have[which][slot] = have;
-                bar_expect(&c.raw_full[which][slot], __popc(have) * (codes + marks));
-            }
-            __syncwarp();
-            if (src) {
-                const uint32_t to = smem_u32(raw + slot * S::kRawUnit);
-                bulk_copy(to + lane * codes, src + (KEYS ? 0 : codes), codes, &c.raw_full[which][slot]);
-                bulk_copy(to + kRawScales + lane * marks, src + 2 * codes + (KEYS ? 0 : D), marks, &c.raw_full[which][slot]);
-            }
-            __syncwarp();
-            ++copied;
-            return true;
-        }
-        return true;
-    };
-    bool fine = true;
-    uint32_t u = 0, taken = 0;
-    for (TcWalk w(c.cut); w.more() && fine; w.next(per)) {
+    const int scale_at = S::kRawScales + sub * marks + (keys ? 8 * t4 : 8 * (N == 16 ? t4 & 1 : t4));
+    TcSlot at, from_at;  // of the tiles' ring, and of the packed halves'
+    uint32_t u = 0;
+    for (TcWalk w(c.cut); w.more(); w.next(per)) {
         const TcItem<kPacked> item(a, w.b, w.item, groups, item_rows);
         item.open(w);
-        for (int q = 0; q < w.n && fine; ++q, ++u) {
-            const int slot = u % SLOTS;
-            if (u >= SLOTS && !bar_wait(&empty[slot], (u / SLOTS - 1) & 1, c)) {
-                fine = false;
-                break;
-            }
-            if (item.packed(w.tile + q)) {
-                const int halves = item.subs(w.tile + q);
-                for (int hf = 0; hf < halves && fine; ++hf, ++taken) {
-                    const uint32_t rs = taken % S::kRaw;
+        for (int q = 0; q < w.n; ++q, ++u, at.next(slots)) {
+            if (u >= slots && !bar_wait(&empty[at.slot], at.parity ^ 1, c)) return;
+            const bool packed = item.packed(w.tile + q);
+            const int halves = packed ? item.subs(w.tile + q) : 0;
 #pragma unroll 1
-                    while (copying && copied < taken + S::kRaw && fine) fine = copy_next();
-                    if (!bar_wait(&c.raw_full[which][rs], (taken / S::kRaw) & 1, c)) {
-                        fine = false;
-                        break;
+            for (int hf = 0; hf < halves; ++hf, from_at.next(S::kRaw)) {
+                const uint32_t rs = from_at.slot;
+                if (!bar_wait(&raw_full[rs], from_at.parity, c)) return;
+                const uint32_t have = raw_have[rs];
+                const char* from = raw + rs * S::kRawUnit;
+                char* tile = ring + at.slot * S::kUnit;
+#pragma unroll 1
+                for (int i = 0; i < X; ++i) {
+                    // keys: neighbouring patches of channels, values: of tokens
+                    const int second = (i ^ r) & 1, pair = 2 * (i / 2) + half;
+                    const int run = keys ? pair / (X / 2) : second, x = keys ? 2 * (pair % (X / 2)) + second : pair;
+                    uint4 words = *reinterpret_cast<const uint4*>(from + run * in_run * codes + code_at + N * 16 * x);
+                    uint2 bytes = *reinterpret_cast<const uint2*>(from + run * in_run * marks + scale_at + (keys ? 32 : N) * x);
+                    if (!((have >> (run * in_run + sub)) & 1)) {
+                        words = make_uint4(kPackedZero, kPackedZero, kPackedZero, kPackedZero);
+                        bytes = make_uint2(0, 0);
                     }
-                    const uint32_t have = c.raw_have[which][rs];
-                    const char* from = raw + rs * S::kRawUnit;
-                    char* tile = ring + slot * S::kUnit;
-#pragma unroll 1
-                    for (int i = 0; i < X; ++i) {
-                        // keys: neighbouring patches of channels, values: of tokens
-                        const int second = (i ^ r) & 1, pair = 2 * (i / 2) + half;
-                        const int run = KEYS ? pair / (X / 2) : second, x = KEYS ? 2 * (pair % (X / 2)) + second : pair;
-                        uint4 words = *reinterpret_cast<const uint4*>(from + run * in_run * codes + code_at + N * 16 * x);
-                        uint2 bytes = *reinterpret_cast<const uint2*>(from + run * in_run * marks + scale_at + (KEYS ? 32 : N) * x);
-                        if (!((have >> (run * in_run + sub)) & 1)) {
-                            words = make_uint4(kPackedZero, kPackedZero, kPackedZero, kPackedZero);
-                            bytes = make_uint2(0, 0);
-                        }
-                        uint32_t s[4], o[4], d[4][4];
-                        packed_scales(bytes, s, o);
-                        packed_words(words, s, o, d);
-                        // rows: the tile's tokens, or the channels; octets of the other
-                        const int row0 = (KEYS ? 64 * hf + 32 * run : 32 * x) + 8 * (r >> 1) + (r & 1);
-                        const int octet = KEYS ? 4 * x + t4 : 4 * run + t4;
-                        char* line = tile + (KEYS ? (octet >> 3) * 16384 : hf * D * 128) + row0 * 128;
+                    uint32_t s[4], o[4], d[4][4];
+                    packed_scales(bytes, s, o);
+                    packed_words(words, s, o, d);
+                    // rows: the tile's tokens, or the channels; octets of the other
+                    const int row0 = (keys ? 64 * hf + 32 * run : 32 * x) + 8 * (r >> 1) + (r & 1);
+                    const int octet = keys ? 4 * x + t4 : 4 * run + t4;
+                    char* line = tile + (keys ? (octet >> 3) * 16384 : hf * D * 128) + row0 * 128;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            *reinterpret_cast<uint4*>(line + 256 * k + (((octet & 7) ^ ((row0 + 2 * k) & 7)) << 4)) =
-                                make_uint4(d[k][0], d[k][1], d[k][2], d[k][3]);
-                    }
-                    bar_arrive_warp(&c.raw_empty[which][rs]);
+                    for (int k = 0; k < 4; ++k)
+                        *reinterpret_cast<uint4*>(line + 256 * k + (((octet & 7) ^ ((row0 + 2 * k) & 7)) << 4)) =
+                            make_uint4(d[k][0], d[k][1], d[k][2], d[k][3]);
                 }
-                fence_async();
+                bar_arrive_warp(&raw_empty[rs]);
             }
-            bar_arrive_warp(&full[slot]);
+            if (packed) {
+                fence_async();
+                if (half == 0) bar_arrive_warp(&full[at.slot]);  // in the loading warp's place
+            }
+            bar_arrive_warp(&full[at.slot]);
         }
     }
-    // no copy is in flight when the CTA ends
-    for (; half == 0 && taken < copied; ++taken) bar_wait<true>(&c.raw_full[which][taken % S::kRaw], (taken / S::kRaw) & 1, c);
 }
 
 template <int D, bool PAIR, int KIND>
@@ -1155,14 +1144,18 @@ __global__ void __launch_bounds__(tc_threads(KIND), 1)
         tc_softmax<D, PAIR, KIND>(a, c, q_smem, v_ring, merge, warp >> 2);
     } else if (warp < 12) {
         if (KIND == kPacked) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
-        if (warp == 8) tc_load<D, PAIR, S::kK, KIND>(a, c, &key, k_ring, c.full_k, c.empty_k, true);
-        else if (warp == 11) tc_load<D, PAIR, S::kV, KIND>(a, c, &value, v_ring, c.full_v, c.empty_v, false);
-        else if (warp == 9) tc_scores<D, PAIR, KIND>(a, c, q_smem, k_ring);
+        char* raw_values = raw_ring + S::kRaw * S::kRawUnit;
+        if (KIND == kWhole && warp == 8) {  // (code of its own: 32 single tokens 168 us, with the other's 171)
+            tc_load<D, PAIR, KIND>(a, c, true, &key, k_ring, raw_ring);
+        } else if (warp == 8 || warp == 11) {
+            const bool keys = KIND != kWhole && warp == 8;
+            tc_load<D, PAIR, KIND>(a, c, keys, keys ? &key : &value, keys ? k_ring : v_ring, keys ? raw_ring : raw_values);
+        } else if (warp == 9) tc_scores<D, PAIR, KIND>(a, c, q_smem, k_ring);
         else tc_sums<D, PAIR, KIND>(a, c, v_ring);
     } else if constexpr (KIND == kPacked) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExpandRegs));
-        if (warp < 14) tc_expand<D, PAIR, S::kK, true>(a, c, k_ring, raw_ring, c.full_k, c.empty_k);
-        else tc_expand<D, PAIR, S::kV, false>(a, c, v_ring, raw_ring + S::kRaw * S::kRawUnit, c.full_v, c.empty_v);
+        const bool keys = warp < 14;
+        tc_expand<D, PAIR>(a, c, keys, keys ? k_ring : v_ring, keys ? raw_ring : raw_ring + S::kRaw * S::kRawUnit);
     }
     tc_fence_before();
     __syncthreads();
