@@ -58,7 +58,7 @@ constexpr int kScores = 2;                   // score buffers of a stream
 constexpr int kTcThreads = 12 * 32, kTcPackedThreads = 16 * 32;
 __host__ __device__ constexpr int tc_threads(int kind) { return kind == 2 ? kTcPackedThreads : kTcThreads; }
 // Registers a thread where sixteen warps share them: softmax groups, warps that load and issue, warps that expand packed tiles.
-constexpr int kSoftmaxRegs = 168, kIssueRegs = 88, kExpandRegs = 88, kPackedLaunchRegs = 128;
+constexpr int kSoftmaxRegs = 160, kIssueRegs = 96, kExpandRegs = 96, kPackedLaunchRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kExpandRegs <= 4 * kPackedLaunchRegs);
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
@@ -70,7 +70,7 @@ template <int D, bool PAIR, int KIND> struct TcShape {
     static constexpr int kK = D == 128 ? 2 : KIND == 2 ? 4 : 5;                   // slots of the key ring
     static constexpr int kV = D == 128 ? (KIND == 2 ? 2 : 3) : KIND == 2 ? 4 : 5;  // and of the value ring, which is read later
     // Packed tiles on their way: 64 places' codes and scales of the keys, or the values, a slot.
-    static constexpr int kRaw = 3;
+    static constexpr int kRawK = 4, kRawV = 3;
     static constexpr int kRawUnit = KIND == 2 ? 36 * D : 0;  // four blocks of 16 tokens: the most
     static constexpr int kRawScales = 32 * D;                // where the scales lie, behind the codes
     static constexpr int kQ = 128 * D * 2;       // bytes of 128 rows of queries
@@ -85,20 +85,24 @@ template <int D, bool PAIR, int KIND> struct TcShape {
 
 struct TcControl {
     unsigned long long full_k[5], empty_k[5], full_v[5], empty_v[5];
-    unsigned long long raw_full[2][3], raw_empty[2][3];  // keys, values
-    uint32_t raw_have[2][3];                            // which blocks are there
     unsigned long long s_full[2][kScores], p_ready[2][kScores], pv_done[2][kScores], drained[2], q_ready, q_taken, all_sync;
     uint32_t tmem;
     int abort;
     int any_odd;          // some drafted value is not finite
-    uint32_t odd[128];    // which drafted tokens'
+    union {
+        uint32_t odd[128];  // kWhole: which drafted tokens'
+        struct {            // kPacked: packed halves on their way, keys and values, and which of their blocks are there
+            unsigned long long raw_full[2][4], raw_empty[2][4];
+            uint32_t raw_have[2][4];
+        };
+    };
     float2 ml[128];       // !PAIR: stream 1's reference and sum, then the weights of both streams
     AttendCut cut;
 };
 
 template <int D, bool PAIR, int KIND> constexpr size_t tc_smem_bytes() {
     using S = TcShape<D, PAIR, KIND>;
-    return 1024 + S::kQueries + (size_t)(S::kK + S::kV) * S::kUnit + S::kMerge + 2 * S::kRaw * S::kRawUnit + sizeof(TcControl);
+    return 1024 + S::kQueries + (size_t)(S::kK + S::kV) * S::kUnit + S::kMerge + (S::kRawK + S::kRawV) * S::kRawUnit + sizeof(TcControl);
 }
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -392,7 +396,7 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         if (!sync_all()) return;  // both streams are through with the last item
         // and the scores' warp has seen its start (it has to meet every phase of q_ready)
         if (items > 0 && !bar_wait(&c.q_taken, (items - 1) & 1, c)) return;
-        if (threadIdx.x < 128) c.odd[threadIdx.x] = 0;
+        if (KIND == kWhole && threadIdx.x < 128) c.odd[threadIdx.x] = 0;
         if (threadIdx.x == 0) c.any_odd = 0;
         asm volatile("cp.async.wait_all;" ::: "memory");
         fence_async();
@@ -777,19 +781,24 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, bool 
     unsigned long long* const raw_full = c.raw_full[keys ? 0 : 1];
     unsigned long long* const raw_empty = c.raw_empty[keys ? 0 : 1];
     uint32_t* const raw_have = c.raw_have[keys ? 0 : 1];
-    const uint32_t slots = keys ? S::kK : S::kV;
+    const uint32_t slots = keys ? S::kK : S::kV, raws = keys ? S::kRawK : S::kRawV;
     const int lane = threadIdx.x & 31;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<KIND>(a, groups);
     const int boxes = kTile / a.P * S::kHalves;
     const int pi = lane / S::kHalves, half = lane % S::kHalves;
     const int N = packed_tokens(a.P), codes = N * D / 2, marks = keys ? D : N * D / 32;  // bytes of a block's codes, scales
+    // this lane's block of a packed tile: which half it is of, its place there, where it lies in its page
+    const int my_half = lane / (64 / N), my_place = lane % (64 / N);
+    const int my_block = (lane & (a.P / N - 1)) * packed_block_bytes(N, D) + (keys ? 0 : codes);
+    const int my_marks = 2 * codes + (keys ? 0 : D - codes);  // its scales behind its codes
+    const uint32_t raw_to = smem_u32(raw);
     TcSlot at;
     uint32_t u = 0, copied = 0, seen = 0;  // tiles; packed halves copied, and known to have been expanded
     // Packed halves before the `to`-th have been expanded.
     auto expanded = [&](uint32_t to) {
         for (; seen < to; ++seen)
-            if (!bar_wait(&raw_empty[seen % S::kRaw], (seen / S::kRaw) & 1, c)) return false;
+            if (!bar_wait(&raw_empty[seen % raws], (seen / raws) & 1, c)) return false;
         return true;
     };
     for (TcWalk w(c.cut); w.more();) {
@@ -825,26 +834,22 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, bool 
                 const bool wanted = wants(w.tile + q, l0), good = wanted && page >= 0 && page < a.pages4;
                 if (keys && wanted && !good) atomicOr(a.status, kStBadIndex);
                 const uint32_t have = __ballot_sync(0xffffffffu, good);
-                const uint8_t* src = a.packed.data + (good ? page * a.packed.page : 0) + h * a.packed.head +
-                                     (l0 & (a.P - 1)) / N * packed_block_bytes(N, D);
-                const int subs = item.subs(w.tile + q), blocks = 64 / N;
-                for (int sub = 0; sub < subs; ++sub, ++copied) {
-                    const uint32_t rs = copied % S::kRaw;
-                    if (copied >= S::kRaw && !expanded(copied - S::kRaw + 1)) goto out;
-                    const uint32_t mine = have >> (sub * blocks) & ((1u << blocks) - 1);
-                    if (lane == 0) {
-                        raw_have[rs] = mine;
-                        bar_expect(&raw_full[rs], __popc(mine) * (codes + marks));
-                    }
-                    __syncwarp();
-                    const int k = lane - sub * blocks;
-                    if (good && k >= 0 && k < blocks) {
-                        const uint32_t to = smem_u32(raw + rs * S::kRawUnit);
-                        bulk_copy(to + k * codes, src + (keys ? 0 : codes), codes, &raw_full[rs]);
-                        bulk_copy(to + S::kRawScales + k * marks, src + 2 * codes + (keys ? 0 : D), marks, &raw_full[rs]);
-                    }
-                    __syncwarp();
+                const uint32_t subs = item.subs(w.tile + q);
+                copied += subs;
+                if (copied > raws && !expanded(copied - raws)) goto out;
+                if (lane < subs) {
+                    const uint32_t mine = have >> (lane * (64 / N)) & ((1u << (64 / N)) - 1), rs = (copied - subs + lane) % raws;
+                    raw_have[rs] = mine;
+                    bar_expect(&raw_full[rs], __popc(mine) * (codes + marks));
                 }
+                __syncwarp();
+                if (good) {
+                    const uint32_t rs = (copied - subs + my_half) % raws, to = raw_to + rs * S::kRawUnit;
+                    const uint8_t* src = a.packed.data + page * a.packed.page + h * a.packed.head + my_block;
+                    bulk_copy(to + my_place * codes, src, codes, &raw_full[rs]);
+                    bulk_copy(to + S::kRawScales + my_place * marks, src + my_marks, marks, &raw_full[rs]);
+                }
+                __syncwarp();
                 page = next;
                 continue;
             }
@@ -868,7 +873,7 @@ __device__ __forceinline__ void tc_load(const AttendArgs& a, TcControl& c, bool 
     }
 out:
     // no copy is in flight when the CTA ends, and no arrival of a product that read one
-    for (; seen < copied; ++seen) bar_wait<true>(&raw_empty[seen % S::kRaw], (seen / S::kRaw) & 1, c);
+    for (; seen < copied; ++seen) bar_wait<true>(&raw_empty[seen % raws], (seen / raws) & 1, c);
     for (uint32_t x = u > slots ? u - slots : 0; x < u; ++x) {
         bar_wait<true>(&full[x % slots], (x / slots) & 1, c);
         bar_wait<true>(&empty[x % slots], (x / slots) & 1, c);
@@ -921,11 +926,13 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
                 const uint64_t k_desc = smem_desc(uniform(ring + at.slot * S::kUnit + sub * kSub * 128), 16, 1024);
                 const uint32_t bar = uniform(smem_u32(&c.s_full[st][buf]));
                 if (elect_one()) {
+#pragma unroll (KIND == kWhole ? D / 64 : 1)
+                    for (int z = 0; z < D / 64; ++z)
 #pragma unroll
-                    for (int i = 0; i < D / 16; ++i) {
-                        const uint32_t off = ((i >> 2) * 16384 + (i & 3) * 32) / 16;  // (addresses count 16 bytes, in the low bits)
-                        mma_ss(s_at, q_desc + off, k_desc + off, mma_desc(kSub, false), i > 0);
-                    }
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t off = (z * 16384 + i * 32) / 16;  // (addresses count 16 bytes, in the low bits)
+                            mma_ss(s_at, q_desc + off, k_desc + off, mma_desc(kSub, false), z + i > 0);
+                        }
                     tc_commit_at(bar);
                 }
                 __syncwarp();
@@ -1016,7 +1023,7 @@ __device__ __forceinline__ void tc_expand(const AttendArgs& a, TcControl& c, boo
     unsigned long long* const raw_full = c.raw_full[keys ? 0 : 1];
     unsigned long long* const raw_empty = c.raw_empty[keys ? 0 : 1];
     const uint32_t* const raw_have = c.raw_have[keys ? 0 : 1];
-    const uint32_t slots = keys ? S::kK : S::kV;
+    const uint32_t slots = keys ? S::kK : S::kV, raws = keys ? S::kRawK : S::kRawV;
     const int lane = threadIdx.x & 31, r = lane >> 2, t4 = lane & 3, half = threadIdx.x >> 5 & 1;
     const int rows = a.T * a.G, item_rows = PAIR ? 256 : 128, groups = (rows + item_rows - 1) / item_rows,
               per = tc_per<kPacked>(a, groups);
@@ -1036,7 +1043,7 @@ __device__ __forceinline__ void tc_expand(const AttendArgs& a, TcControl& c, boo
             const bool packed = item.packed(w.tile + q);
             const int halves = packed ? item.subs(w.tile + q) : 0;
 #pragma unroll 1
-            for (int hf = 0; hf < halves; ++hf, from_at.next(S::kRaw)) {
+            for (int hf = 0; hf < halves; ++hf, from_at.next(raws)) {
                 const uint32_t rs = from_at.slot;
                 if (!bar_wait(&raw_full[rs], from_at.parity, c)) return;
                 const uint32_t have = raw_have[rs];
@@ -1087,7 +1094,7 @@ __global__ void __launch_bounds__(tc_threads(KIND), 1)
     char* v_ring = k_ring + S::kK * S::kUnit;
     char* merge = v_ring + S::kV * S::kUnit;
     char* raw_ring = merge + S::kMerge;
-    TcControl& c = *reinterpret_cast<TcControl*>(raw_ring + 2 * S::kRaw * S::kRawUnit);
+    TcControl& c = *reinterpret_cast<TcControl*>(raw_ring + (S::kRawK + S::kRawV) * S::kRawUnit);
     const int warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) {
         constexpr int fill = KIND == kPacked ? 3 : 1;  // the loading warp, and two that expand
@@ -1099,9 +1106,9 @@ __global__ void __launch_bounds__(tc_threads(KIND), 1)
             bar_init(&c.full_v[i], fill);
             bar_init(&c.empty_v[i], 1);
         }
-        for (int i = 0; i < 2 * S::kRaw; ++i) {
-            bar_init(&c.raw_full[i / 3][i % 3], 1);
-            bar_init(&c.raw_empty[i / 3][i % 3], 2);
+        for (int i = 0; KIND == kPacked && i < 8; ++i) {
+            bar_init(&c.raw_full[i / 4][i % 4], 1);
+            bar_init(&c.raw_empty[i / 4][i % 4], 2);
         }
         for (int i = 0; i < 2; ++i) {
             for (int buf = 0; buf < 2; ++buf) {
@@ -1144,7 +1151,7 @@ __global__ void __launch_bounds__(tc_threads(KIND), 1)
         tc_softmax<D, PAIR, KIND>(a, c, q_smem, v_ring, merge, warp >> 2);
     } else if (warp < 12) {
         if (KIND == kPacked) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kIssueRegs));
-        char* raw_values = raw_ring + S::kRaw * S::kRawUnit;
+        char* raw_values = raw_ring + S::kRawK * S::kRawUnit;
         if (KIND == kWhole && warp == 8) {  // (code of its own: 32 single tokens 168 us, with the other's 171)
             tc_load<D, PAIR, KIND>(a, c, true, &key, k_ring, raw_ring);
         } else if (warp == 8 || warp == 11) {
@@ -1155,7 +1162,7 @@ __global__ void __launch_bounds__(tc_threads(KIND), 1)
     } else if constexpr (KIND == kPacked) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExpandRegs));
         const bool keys = warp < 14;
-        tc_expand<D, PAIR>(a, c, keys, keys ? k_ring : v_ring, keys ? raw_ring : raw_ring + S::kRaw * S::kRawUnit);
+        tc_expand<D, PAIR>(a, c, keys, keys ? k_ring : v_ring, keys ? raw_ring : raw_ring + S::kRawK * S::kRawUnit);
     }
     tc_fence_before();
     __syncthreads();
