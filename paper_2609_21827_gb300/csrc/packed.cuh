@@ -31,7 +31,7 @@ __host__ __device__ constexpr int packed_block_bytes(int N, int D) { return N * 
 __host__ __device__ constexpr int packed_page_bytes(int P, int D) {
     return P / packed_tokens(P) * packed_block_bytes(packed_tokens(P), D);
 }
-constexpr uint32_t kPackedZero = 0x88888888u;  // eight codes of 0
+constexpr uint32_t kPackedZero = 0x44444444u;  // eight codes of 0: n + 8 = 8 in each
 
 // The pairs of scales s and of -24 s of eight scale bytes.
 __device__ __forceinline__ void packed_scales(uint2 bytes, uint32_t (&s)[4], uint32_t (&c)[4]) {

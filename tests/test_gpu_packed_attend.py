@@ -195,6 +195,30 @@ def test_bad_lengths_and_pages_set_their_bits(T):
         assert torch.isfinite(out[2]).all()
 
 
+@pytest.mark.parametrize("P,D", [(16, 64), (16, 128), (32, 128), (128, 64)])
+@pytest.mark.parametrize("T", [1, 3, 40])
+def test_bad_pages_read_as_zeros(T, P, D):
+    """The same bits as over a page whose numbers are all 0 (n + 8 = 8: one bit of four, at bit 2 modulo 4)."""
+    p = _problem([20, 20, 20], None, T, 8, 2, D, P, n4=[5, 6, 5], seed=9)
+    table = p.table4.clone()
+    spare = table[1, 5].item()
+    zeros = p.data[spare].clone()
+    p.data[spare] = 0x44
+    p.held4.n_pages.copy_(i32([5, 5, 5]))
+    for at in (0, 3, 4):
+        p.table4.copy_(table)
+        p.table4[2, at] = spare
+        want = [x.clone() for x in p.run()]
+        assert rheo.scratch_status(p.ws) == 0
+        k, v = lr.unpack_pages(p.data[spare].cpu().numpy(), P, D)
+        assert not k.any() and not v.any() and zeros.any()
+        for wrong in (p.cfg4.pages, -1):
+            p.table4[2, at] = wrong
+            out, lse = p.run()
+            assert rheo.scratch_status(p.ws) == rheo.STATUS_BAD_INDEX
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+
+
 @pytest.mark.parametrize("T,G", [(1, 4), (49, 4)])
 def test_many_calls_one_after_the_other(T, G):
     ps = [_problem([7 * b for b in range(8)], None, T, 8 * G, 8, 128, 16, n4=[250 - 30 * b for b in range(8)], seed=20 + i)
