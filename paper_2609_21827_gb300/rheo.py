@@ -739,7 +739,15 @@ def _packed_shape(packed_cfg: CacheConfig) -> tuple:
     return shape
 
 
+def _count(x: int, name: str) -> int:
+    """A number of positions, which the library holds in 32 bits."""
+    if not 0 <= x < 1 << 31:
+        raise RheoError(f"{name}: 0 .. 2^31 - 1 is wanted, got {x}")
+    return x
+
+
 def _window(cfg: CacheConfig, window: int, sinks: int, depth) -> _Window:
+    _count(window, "window"), _count(sinks, "sinks")
     return _Window(window, sinks, _want_opt(depth, "depth", torch.int32, cfg._each))
 
 
@@ -798,6 +806,7 @@ def cache_pack(cfg: CacheConfig, packed_cfg: CacheConfig, key_cache: torch.Tenso
     """rheo_cache_pack: whole pages of the caches [layers, pages, kv_heads, page_size, D] go into 4 bits, all but the last
     `keep` tokens of a request.  pages, packed_pages and ctx_len are updated in place, or stay as they are and
     out = (Pages, Pages, ctx_len) receives the new state."""
+    _count(keep, "keep")
     n, kv, kl, vl, p4, pl = _layers(cfg, packed_cfg, key_cache, value_cache, packed)
     before, before4, ctx = pages.c(cfg), packed_pages.c(packed_cfg), _want(ctx_len, "ctx_len", torch.int32, cfg._one)
     after, after4, ctx_out = (before, before4, ctx) if out is None else (

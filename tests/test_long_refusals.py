@@ -189,3 +189,14 @@ def test_tensors_of_other_kinds_are_refused():
         rheo.cache_pack(c, c, pool[0], pool[0], torch.zeros((64, 2, 1120), dtype=torch.uint8), None, None, None, None)
     with pytest.raises(rheo.RheoError):
         rheo.cache_unpack(c, c, torch.zeros((1, 64, 2, 1120), dtype=torch.uint8), pool, pool, None, None, None)
+
+
+@pytest.mark.parametrize("wrong", [-1, 2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 32])
+def test_counts_past_32_bits(wrong):
+    """The binding does not hand over what 32 bits would turn into another number."""
+    c = _cfg()
+    for call in (lambda: rheo._window(c, wrong, 0, None), lambda: rheo._window(c, 1, wrong, None),
+                 lambda: rheo.cache_pack(c, c, None, None, None, None, None, None, None, keep=wrong)):
+        with pytest.raises(rheo.RheoError, match="2\\^31"):
+            call()
+    assert rheo._window(c, 2 ** 31 - 1, 2 ** 31 - 1, None).window == 2 ** 31 - 1
