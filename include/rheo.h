@@ -498,8 +498,9 @@ typedef struct {
                             a dimension of one is not looked at); a page of a head is contiguous */
 } rheo_packed;
 
-/* Bytes of a packed page of one head. */
-int rheo_packed_sizes(const rheo_cache_config* packed_cfg, int64_t* page_bytes);
+/* Bytes of a packed page of one head, and of the scratch of rheo_cache_pack, rheo_cache_unpack and rheo_packed_attend (at
+ * least rheo_cache_sizes', so that it serves the other cache functions too).  Either may be NULL. */
+int rheo_packed_sizes(const rheo_cache_config* packed_cfg, int64_t* page_bytes, size_t* scratch_bytes);
 
 /* Packs whole pages, in `layers` layers (layer l at kv->key + l * key_layer elements,
  * kv->value + l * value_layer, packed->data + l * packed_layer bytes).  Of request b the

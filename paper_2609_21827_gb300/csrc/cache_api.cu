@@ -105,9 +105,11 @@ struct CacheLayout {
     size_t join, part_ml, part_o, total;
 };
 
-CacheLayout cache_layout(const rheo_cache_config& c) {
+// packed: of the attention over packed pages, which asks for more, so that the other functions go on asking for no more
+// than a buffer of any configuration of fp32 or more rows has.
+CacheLayout cache_layout(const rheo_cache_config& c, bool packed) {
     const int G = c.q_heads / c.kv_heads;
-    const size_t ctas = attend_most_ctas(c.dtype, c.tokens, G), rows = attend_part_rows(c.dtype, c.tokens, G);
+    const size_t ctas = packed ? packed_attend_most_ctas(c.tokens, G) : kAttendCtas, rows = attend_part_rows(c.dtype, c.tokens, G);
     CacheLayout L{};
     size_t o = kPartsAt;
     auto take = [&](size_t bytes) {
@@ -142,8 +144,8 @@ bool attend_ok(const rheo_cache_config* cfg, const rheo_attend_io* io, const rhe
 }
 
 AttendArgs attend_args(const rheo_cache_config& c, const rheo_attend_io& io, const rheo_kv& kv, const int32_t* block_table,
-                       const int32_t* ctx_len, const int32_t* new_len, const uint8_t* mask, float scale, void* scratch) {
-    const CacheLayout L = cache_layout(c);
+                       const int32_t* ctx_len, const int32_t* new_len, const uint8_t* mask, float scale, void* scratch, bool packed = false) {
+    const CacheLayout L = cache_layout(c, packed);
     AttendArgs a{};
     a.B = c.batch;
     a.T = c.tokens;
@@ -223,7 +225,7 @@ using namespace rheo;
 
 extern "C" int rheo_cache_sizes(const rheo_cache_config* cfg, size_t* scratch_bytes) {
     if (!valid(cfg)) return RHEO_EINVAL;
-    if (scratch_bytes) *scratch_bytes = cache_layout(*cfg).total;
+    if (scratch_bytes) *scratch_bytes = cache_layout(*cfg, false).total;
     return RHEO_OK;
 }
 
@@ -342,9 +344,10 @@ extern "C" int rheo_window_attend(const rheo_cache_config* cfg, const rheo_atten
     return e == cudaErrorInvalidValue ? RHEO_EINVAL : code(e);  // a cache that no tensor map describes
 }
 
-extern "C" int rheo_packed_sizes(const rheo_cache_config* packed_cfg, int64_t* page_bytes) {
+extern "C" int rheo_packed_sizes(const rheo_cache_config* packed_cfg, int64_t* page_bytes, size_t* scratch_bytes) {
     if (!valid(packed_cfg) || packed_cfg->dtype != RHEO_BF16) return RHEO_EINVAL;
     if (page_bytes) *page_bytes = packed_page_bytes(packed_cfg->page_size, packed_cfg->head_dim);
+    if (scratch_bytes) *scratch_bytes = cache_layout(*packed_cfg, true).total;
     return RHEO_OK;
 }
 
@@ -356,7 +359,7 @@ extern "C" int rheo_packed_attend(const rheo_cache_config* cfg, const rheo_cache
     if (!attend_ok(cfg, io, kv, block_table, ctx_len, scale, scratch) || !packed_cfg_ok(cfg, packed_cfg)) return RHEO_EINVAL;
     if (!packed_ok(packed, *packed_cfg) || !packed_table || !n4 || (window && !window_ok(*window))) return RHEO_EINVAL;
     if (((int64_t)cfg->max_pages + packed_cfg->max_pages) * cfg->page_size > (int64_t)1 << 30) return RHEO_EINVAL;
-    AttendArgs a = attend_args(*cfg, *io, *kv, block_table, ctx_len, new_len, mask, scale, scratch);
+    AttendArgs a = attend_args(*cfg, *io, *kv, block_table, ctx_len, new_len, mask, scale, scratch, true);
     if (window) set_window(a, *window);
     a.packed = *packed;
     a.table4 = packed_table;

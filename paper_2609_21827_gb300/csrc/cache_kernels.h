@@ -137,10 +137,8 @@ int attend_lead(int dtype);
 int attend_least(int dtype);
 constexpr int kAttendCtas = 152;  // one a multiprocessor
 constexpr int kFewRows = 16;      // query rows of a key/value head up to which packed pages are read by small tiles
-// CTAs of any attention over this configuration: the small tiles' kernel runs up to four a multiprocessor.
-constexpr int attend_most_ctas(int dtype, int64_t T, int64_t G) {
-    return dtype == 1 && T * G <= kFewRows ? 4 * kAttendCtas : kAttendCtas;
-}
+// CTAs of the attention over packed pages: the small tiles' kernel runs up to four a multiprocessor.
+constexpr int packed_attend_most_ctas(int64_t T, int64_t G) { return T * G <= kFewRows ? 4 * kAttendCtas : kAttendCtas; }
 // Rows of logits are cut into segments where two CTAs a multiprocessor leave each of them at least two.
 constexpr int kLogprobParts = 2 * 152;
 constexpr int kLogprobCutRows = kLogprobParts / 2;

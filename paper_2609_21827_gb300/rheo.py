@@ -148,7 +148,7 @@ def lib():
                                           ctypes.POINTER(_Logprobs), _VP, _VP]
         W, P4 = ctypes.POINTER(_Window), ctypes.POINTER(_Packed)
         L.rheo_window_attend.argtypes = [K, ctypes.POINTER(_AttendIO), KV, _VP, _VP, _VP, _VP, W, f32, _VP, _VP]
-        L.rheo_packed_sizes.argtypes = [K, ctypes.POINTER(i64)]
+        L.rheo_packed_sizes.argtypes = [K, ctypes.POINTER(i64), ctypes.POINTER(ctypes.c_size_t)]
         L.rheo_cache_pack.argtypes = [K, K, i32, KV, i64, i64, P4, i64, i32, PG, PG, _VP, PG, PG, _VP, _VP, _VP]
         L.rheo_cache_unpack.argtypes = [K, K, i32, P4, i64, KV, i64, i64, i32, _VP, _VP, _VP, _VP]
         L.rheo_packed_attend.argtypes = [K, K, ctypes.POINTER(_AttendIO), KV, _VP, _VP, _VP, P4, _VP, _VP, _VP, W, f32, _VP,
@@ -445,7 +445,7 @@ class CacheConfig:
         c = _CacheConfig(self.batch, self.tokens, self.pages, self.page_size, self.max_pages, self.q_heads,
                          self.kv_heads, self.head_dim, code)
         B, T, H, D = self.batch, self.tokens, self.kv_heads, self.head_dim
-        for name, value in (("torch_dtype", torch_dtype), ("_c", c), ("_ref", ctypes.byref(c)), ("_bytes", None),
+        for name, value in (("torch_dtype", torch_dtype), ("_c", c), ("_ref", ctypes.byref(c)), ("_bytes", None), ("_bytes4", None),
                             ("_one", (B,)), ("_each", (B, T)), ("_table", (B, self.max_pages)),
                             ("_free", (self.pages,)), ("_q", (B, T, self.q_heads, D)), ("_k", (B, T, H, D)),
                             ("_lse", (B, T, self.q_heads)), ("_mask", (B, T, T)), ("_pool", (self.pages, H, self.page_size, D))):
@@ -457,6 +457,13 @@ class CacheConfig:
             _check(lib().rheo_cache_sizes(self._ref, ctypes.byref(n)), "rheo_cache_sizes")
             object.__setattr__(self, "_bytes", n.value)
         return self._bytes
+
+    def packed_scratch_bytes(self) -> int:
+        if self._bytes4 is None:
+            n = ctypes.c_size_t()
+            _check(lib().rheo_packed_sizes(self._ref, None, ctypes.byref(n)), "rheo_packed_sizes")
+            object.__setattr__(self, "_bytes4", n.value)
+        return self._bytes4
 
 
 @dataclass(frozen=True)
@@ -489,10 +496,14 @@ class _Scratch:
     """A scratch buffer, zeroed when made; one for each stream whose calls may overlap."""
 
     def __init__(self, cfg, device="cuda", stream=None):
-        self.nbytes = cfg.scratch_bytes()
+        self.nbytes = self._size(cfg)
         self.buf = torch.empty(self.nbytes, dtype=torch.uint8, device=device)
         self._ptr = self.buf.data_ptr()
         self.init(stream)
+
+    @staticmethod
+    def _size(cfg) -> int:
+        return cfg.scratch_bytes()
 
     def of(self, cfg) -> int:
         """The buffer's pointer, if it is large enough for cfg."""
@@ -508,7 +519,18 @@ class _Scratch:
 
 
 class CacheWorkspace(_Scratch):
-    pass
+    """For the functions over packed pages too, which only bf16 caches have and which ask for more."""
+
+    @staticmethod
+    def _size(cfg) -> int:
+        return cfg.packed_scratch_bytes() if cfg.dtype == "bf16" else cfg.scratch_bytes()
+
+    def of_packed(self, cfg) -> int:
+        """The buffer's pointer, if it is large enough for the functions over packed pages."""
+        wanted = cfg._bytes4 or cfg.packed_scratch_bytes()
+        if self.nbytes < wanted:
+            raise RheoError(f"the workspace holds {self.nbytes} bytes, {wanted} are wanted for packed pages")
+        return self._ptr
 
 
 class LogprobWorkspace(_Scratch):
@@ -721,7 +743,7 @@ def token_logprobs(cfg: LogprobConfig, logits: torch.Tensor, tokens: torch.Tenso
 def packed_page_bytes(packed_cfg: CacheConfig) -> int:
     """Bytes of a packed page of one head."""
     n = ctypes.c_int64()
-    _check(lib().rheo_packed_sizes(packed_cfg._ref, ctypes.byref(n)), "rheo_packed_sizes")
+    _check(lib().rheo_packed_sizes(packed_cfg._ref, ctypes.byref(n), None), "rheo_packed_sizes")
     return n.value
 
 
@@ -785,7 +807,7 @@ def packed_attend(cfg: CacheConfig, packed_cfg: CacheConfig, q: torch.Tensor, ke
         _want(ctx_len, "ctx_len", i32, cfg._one), _want_opt(new_len, "new_len", i32, cfg._one), _Packed(pp, ps[0], ps[1]),
         packed_pages.table(packed_cfg), _want(packed_pages.n_pages, "n_pages", i32, packed_cfg._one),
         _want_opt(mask, "mask", torch.uint8, cfg._mask), _window(cfg, window, sinks, depth),
-        cfg.head_dim ** -0.5 if scale is None else scale, ws.of(cfg), _stream(stream)), "rheo_packed_attend")
+        cfg.head_dim ** -0.5 if scale is None else scale, ws.of_packed(cfg), _stream(stream)), "rheo_packed_attend")
 
 
 def _layers(cfg: CacheConfig, packed_cfg: CacheConfig, key_cache, value_cache, packed) -> tuple:
@@ -812,7 +834,7 @@ def cache_pack(cfg: CacheConfig, packed_cfg: CacheConfig, key_cache: torch.Tenso
     after, after4, ctx_out = (before, before4, ctx) if out is None else (
         out[0].c(cfg), out[1].c(packed_cfg), _want(out[2], "ctx_len of out", torch.int32, cfg._one))
     _check(lib().rheo_cache_pack(cfg._ref, packed_cfg._ref, n, kv, kl, vl, p4, pl, keep, before, before4, ctx, after, after4,
-                                 ctx_out, ws.of(cfg), _stream(stream)), "rheo_cache_pack")
+                                 ctx_out, ws.of_packed(cfg), _stream(stream)), "rheo_cache_pack")
 
 
 def cache_unpack(cfg: CacheConfig, packed_cfg: CacheConfig, packed: torch.Tensor, key_cache: torch.Tensor,
@@ -824,5 +846,5 @@ def cache_unpack(cfg: CacheConfig, packed_cfg: CacheConfig, packed: torch.Tensor
         raise RheoError("src: [n] is wanted")
     shape = tuple(src.shape)
     _check(lib().rheo_cache_unpack(cfg._ref, packed_cfg._ref, n, p4, pl, kv, kl, vl, shape[0],
-                                   _want(src, "src", torch.int32, shape), _want(dst, "dst", torch.int32, shape), ws.of(cfg),
+                                   _want(src, "src", torch.int32, shape), _want(dst, "dst", torch.int32, shape), ws.of_packed(cfg),
                                    _stream(stream)), "rheo_cache_unpack")

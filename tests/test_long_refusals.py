@@ -200,3 +200,24 @@ def test_counts_past_32_bits(wrong):
         with pytest.raises(rheo.RheoError, match="2\\^31"):
             call()
     assert rheo._window(c, 2 ** 31 - 1, 2 ** 31 - 1, None).window == 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("T,Hq,H,more", [(1, 4, 2, True), (5, 4, 2, True), (8, 4, 2, True), (9, 4, 2, False), (129, 32, 8, False)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scratch_sizes(lib, T, Hq, H, more, D):
+    """Only the functions over packed pages ask for the parts of their small tiles; the others ask for no more than before, as
+    buffers made for other configurations serve them."""
+    c = _cfg(tokens=T, q_heads=Hq, kv_heads=H, head_dim=D)
+    rows = min(-(-T * Hq // H // 8) * 8, 128 if T * Hq // H <= 128 else 256)
+    parts = 2 * 152 * rows * (D + 2) * 4
+    assert parts < c.scratch_bytes() < parts + 8192
+    assert 4 * parts < c.packed_scratch_bytes() < 4 * parts + 16384 if more else c.packed_scratch_bytes() == c.scratch_bytes()
+    ws = rheo.CacheWorkspace.__new__(rheo.CacheWorkspace)
+    ws.nbytes, ws._ptr = c.scratch_bytes(), 1 << 20
+    assert ws.of(c) == 1 << 20
+    if more:
+        with pytest.raises(rheo.RheoError, match="packed"):
+            ws.of_packed(c)
+    ws.nbytes = rheo.CacheWorkspace._size(c)
+    assert ws.of(c) == ws.of_packed(c) == 1 << 20
+    assert rheo.CacheWorkspace._size(_cfg(dtype="f32")) == _cfg(dtype="f32").scratch_bytes()
