@@ -57,8 +57,9 @@ constexpr int kSub = 64;                     // keys of a score product: half a 
 constexpr int kScores = 2;                   // score buffers of a stream
 constexpr int kTcThreads = 12 * 32, kTcPackedThreads = 16 * 32;
 __host__ __device__ constexpr int tc_threads(int kind) { return kind == 2 ? kTcPackedThreads : kTcThreads; }
-// Registers a thread where sixteen warps share them: softmax groups, warps that load and issue, warps that expand packed tiles.
-constexpr int kSoftmaxRegs = 160, kIssueRegs = 96, kExpandRegs = 96, kPackedLaunchRegs = 128;
+// Registers a thread where sixteen warps share them: softmax groups, warps that load and issue, warps that expand packed
+// tiles.  64 trees of 61 tokens: 367, 341, 328 us with 160, 168, 176 for the softmax groups, 327 with 184 (the issuing warps spill).
+constexpr int kSoftmaxRegs = 176, kIssueRegs = 80, kExpandRegs = 80, kPackedLaunchRegs = 128;
 static_assert(2 * kSoftmaxRegs + kIssueRegs + kExpandRegs <= 4 * kPackedLaunchRegs);
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 23;          // polls of a wait before the kernel gives up
@@ -209,6 +210,7 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint
 __device__ __forceinline__ constexpr uint32_t mma_desc(int n, bool b_along_n) {
     return (1u << 4) | (1u << 7) | (1u << 10) | (b_along_n ? 1u << 16 : 0u) | ((uint32_t)(n >> 3) << 17) | (8u << 24);
 }
+constexpr uint32_t kNegateA = 1u << 13;
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t desc, bool add) {
     asm volatile(
         "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
@@ -364,7 +366,6 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
     const uint32_t lanes = (uint32_t)(warp * 32) << 16;
     const uint32_t t_s = c.tmem + lanes + st * 128, t_o = c.tmem + lanes + S::kO + st * D;
     const float sc = fmaxf(fabsf(a.scale_log2), 1e-30f);  // above 0, so that hidden places stay at -inf
-    const bool negative = a.scale_log2 < 0.0f;
     uint32_t items = 0, products = 0, syncs = 0, tile0 = 0;
     unsigned long long seen = 0;  // T <= 64: drafted tokens that this row sees, of request seen_b's rows from seen_r0
     int seen_b = -1, seen_r0 = -1;
@@ -530,12 +531,6 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                     tmem_ld32(s[0], t_b);
                     tmem_ld32(s[1], t_b + 32);
                     tc_wait_ld();
-                    if (negative) {
-#pragma unroll
-                        for (int v = 0; v < 2; ++v)
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) s[v][i] ^= 0x80000000u;
-                    }
                     if (tail) {
 #pragma unroll
                         for (int v = 0; v < 2; ++v)
@@ -880,10 +875,11 @@ out:
     }
 }
 
-// Products of a tile in the issuing warps' code: one after the other, or a loop over the four, because the loops of all
-// roles together have to stay in the instruction cache.  64 trees of 61 tokens: 265 us and 286 without windows or packed
-// pages; over packed pages 669 and 439.
-template <int KIND> constexpr int kProductUnroll = KIND == kWhole ? 4 : 1;
+// Products of a tile in the issuing warps' code: how many of the four stand one behind the other, the rest a loop, because
+// the loops of all roles together have to stay in the instruction cache.  64 trees of 61 tokens with 1, 2, 4: over packed
+// pages 388, 367 and 438 us, in windows 169, 163 and 158; 32 single tokens in a window, where a stream has one
+// half of a tile, 43.5, 45.2 and 45.7.
+template <int KIND, bool PAIR> constexpr int kProductUnroll = KIND == kWhole ? 4 : KIND == kPacked ? 2 : PAIR ? 4 : 1;
 
 // Which streams have a product with half `sub` of a tile that has `subs` halves.
 template <bool PAIR> __device__ __forceinline__ bool tc_has(int st, int sub, int subs, bool second) {
@@ -899,6 +895,9 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
               per = tc_per<KIND>(a, groups);
     const uint32_t t_s = uniform(c.tmem), q_at = uniform(smem_u32(q_smem)), ring = uniform(smem_u32(k_ring));
     uint32_t items = 0, done0 = 0, done1 = 0;  // products of both streams
+    // a scale below 0: of the queries' negatives (with the signs turned in the softmax groups, which need the room in the
+    // instruction cache, 64 trees in windows took 158 us, not 155, and two prompt pieces 111, not 107)
+    const uint32_t s_desc = uniform(mma_desc(kSub, false) | (a.scale_log2 < 0.0f ? kNegateA : 0u));
     TcSlot at;
     for (TcWalk w(c.cut); w.more(); ++items) {
         const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);
@@ -911,7 +910,7 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
         for (int q = 0; q < n; ++q, at.next(S::kK)) {
             const int subs = item.subs(w.tile + q);
             if (!bar_wait(&c.full_k[at.slot], at.parity, c)) goto out;
-#pragma unroll (kProductUnroll<KIND>)
+#pragma unroll (kProductUnroll<KIND, PAIR>)
             for (int x = 0; x < 4; ++x) {
                 const int sub = x >> 1, st = x & 1;
                 if (!tc_has<PAIR>(st, sub, subs, second)) continue;
@@ -931,7 +930,7 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const uint32_t off = (z * 16384 + i * 32) / 16;  // (addresses count 16 bytes, in the low bits)
-                            mma_ss(s_at, q_desc + off, k_desc + off, mma_desc(kSub, false), z + i > 0);
+                            mma_ss(s_at, q_desc + off, k_desc + off, s_desc, z + i > 0);
                         }
                     tc_commit_at(bar);
                 }
@@ -975,7 +974,7 @@ __device__ __forceinline__ void tc_sums(const AttendArgs& a, TcControl& c, char*
             const uint32_t lead = KIND == kPacked ? uniform(packed ? 16 : 16384) : 16384;
             const uint32_t desc = KIND == kPacked ? uniform(packed ? mma_desc(D, false) : mma_desc(D, true)) : mma_desc(D, true);
             if (!bar_wait(&c.full_v[at.slot], at.parity, c)) goto out;
-#pragma unroll (kProductUnroll<KIND>)
+#pragma unroll (kProductUnroll<KIND, PAIR>)
             for (int x = 0; x < 4; ++x) {
                 const int sub = x >> 1, st = x & 1;
                 if (!tc_has<PAIR>(st, sub, subs, second)) continue;
