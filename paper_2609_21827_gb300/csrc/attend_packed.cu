@@ -19,6 +19,12 @@
 // Places that a row does not see get -inf before the maximum.  16-bit values that are
 // not finite count as 0 where some row may not see their place (0 * inf would
 // spoil it) and are added at the item's end for the rows that see them.
+//
+// What bounds it: instructions.  32 single tokens, contexts to 16,201, 32 query and 8 key/value heads of 128: 75 us, 3.9 TB/s (57 %
+// of a copy's rate), some 1,000 instructions a warp and tile at 59 % of the issue slots, of which turning numbers into bf16 (a
+// shift, a logic operation and a multiply-add a pair, on pipes of half rate) takes more than half.  48 chains of three tokens, heads of 64, a window of
+// 8,192: 51 us.  With the tensor cores' kernel, whose tiles have 128 rows, these take 251 and 142 us.  (Over 16 bits alone that one
+// is quicker, as nothing is to be turned: 32 single tokens in a window of 1,024 take it 43 us, this one 53.)
 #include <cuda_bf16.h>
 
 #include "attend.cuh"
@@ -35,11 +41,12 @@ constexpr int kSlots = 2;            // of a warp
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 22;  // polls of a wait before the kernel gives up
 
-// CTAs an SM: 16 rows of 128 channels need more than 128 registers a thread.
-constexpr int few_per_sm(int D, int NT) { return NT == 2 && D == 128 ? 3 : 4; }
+// CTAs an SM: lines of 128 channels need more than 128 registers a thread (32 single tokens, contexts to 16,201: 76.8 us with
+// four, 75.6 with three).
+constexpr int few_per_sm(int D) { return D == 128 ? 3 : 4; }
 
 template <int D, int NT> struct Few {
-    static constexpr int kPerSm = few_per_sm(D, NT);
+    static constexpr int kPerSm = few_per_sm(D);
     static constexpr int kX = D / 32;
     static constexpr int kRows = 8 * NT;
     static constexpr int kSlot = packed_block_bytes(16, D) * 2;  // the larger of one block of 32 tokens and two of 16
@@ -504,7 +511,7 @@ cudaError_t launch_packed_attend(const AttendArgs& in, cudaStream_t s) {
     const bool one = rows <= 8;
     a.item_rows = one ? 8 : 16;
     a.part_rows = a.item_rows;
-    a.ctas = kAttendCtas * few_per_sm(a.D, one ? 1 : 2);
+    a.ctas = kAttendCtas * few_per_sm(a.D);
     // What an item's start and end cost in tiles (32 single tokens, contexts to 16,201: 99.7, 89.7, 80.7, 80.9 us with 6, 12,
     // 24, 32), and the tiles of a part at least where few items are cut by themselves (one token over 16,201: 28.1, 26.1,
     // 25.6 us with 4, 8, 16).

@@ -531,6 +531,12 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
                     tmem_ld32(s[0], t_b);
                     tmem_ld32(s[1], t_b + 32);
                     tc_wait_ld();
+                    if (KIND == kWhole && a.scale_log2 < 0.0f) {
+#pragma unroll
+                        for (int v = 0; v < 2; ++v)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) s[v][i] ^= 0x80000000u;
+                    }
                     if (tail) {
 #pragma unroll
                         for (int v = 0; v < 2; ++v)
@@ -895,9 +901,11 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
               per = tc_per<KIND>(a, groups);
     const uint32_t t_s = uniform(c.tmem), q_at = uniform(smem_u32(q_smem)), ring = uniform(smem_u32(k_ring));
     uint32_t items = 0, done0 = 0, done1 = 0;  // products of both streams
-    // a scale below 0: of the queries' negatives (with the signs turned in the softmax groups, which need the room in the
-    // instruction cache, 64 trees in windows took 158 us, not 155, and two prompt pieces 111, not 107)
-    const uint32_t s_desc = uniform(mma_desc(kSub, false) | (a.scale_log2 < 0.0f ? kNegateA : 0u));
+    // windows and packed pages: a scale below 0 turns the queries' signs here, not those of the scores in the softmax groups,
+    // which need the room in the instruction cache (64 trees in windows 158 us, two prompt pieces 111, so 155 and 107; without
+    // windows or packed pages 241 as it is, so 245)
+    const uint32_t s_desc =
+        KIND == kWhole ? mma_desc(kSub, false) : uniform(mma_desc(kSub, false) | (a.scale_log2 < 0.0f ? kNegateA : 0u));
     TcSlot at;
     for (TcWalk w(c.cut); w.more(); ++items) {
         const TcItem<KIND> item(a, w.b, w.item, groups, item_rows);

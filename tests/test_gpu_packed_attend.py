@@ -125,6 +125,17 @@ def test_large_scores_and_negative_scale():
         p.check()
 
 
+@pytest.mark.parametrize("T", [40, 80])
+@pytest.mark.parametrize("window", [0, 150])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scales_below_zero_with_many_rows(T, window, D):
+    """One stream of rows, and two."""
+    p = _problem([200, 3], None, T, 4, 2, D, 32, n4=[4, 9], seed=8, spread=8.0, window=window, sinks=5, tree=T == 40)
+    for scale in (-0.05, -1.0, 0.05):
+        p.scale = scale
+        p.check()
+
+
 @pytest.mark.parametrize("T,G", [(1, 4), (4, 4), (61, 4)])
 def test_scores_that_rise_along_the_context(T, G):
     """Scales grow page by page: the running maximum moves again and again."""

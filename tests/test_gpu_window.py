@@ -246,3 +246,12 @@ def test_many_calls_one_after_the_other(dtype, T, G):
     for p, (out, lse) in zip(ps, first):
         assert torch.equal(p.out, out) and torch.equal(p.lse, lse) and rheo.scratch_status(p.ws) == 0
     ps[2].check()
+
+
+@pytest.mark.parametrize("T", [30, 80])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scales_below_zero_with_many_rows(T, D):
+    p = _problem([500, 3, 129], None, T, 4, 2, D, 32, "bf16", window=150, sinks=5, tree=T == 30, seed=8, spread=8.0)
+    for scale in (-0.05, -1.0, 0.05):
+        p.scale = scale
+        p.check()
