@@ -136,7 +136,10 @@ int attend_part_rows(int dtype, int T, int G);
 int attend_lead(int dtype);
 int attend_least(int dtype);
 constexpr int kAttendCtas = 152;  // one a multiprocessor
-constexpr int kFewRows = 16;      // query rows of a key/value head up to which packed pages are read by small tiles
+// Query rows of a key/value head up to which packed pages are read by the small tiles, 8 or 16 at a time.  32 requests, contexts to
+// 8,201, 32 query and 8 key/value heads of 128, 20, 32, 48 and 64 rows: 110, 116, 174, 225 us; with the tensor cores' kernel
+// 156, 140, 149, 146.  (To 16,201, 16 rows: 105 and 249.)
+constexpr int kFewRows = 32;
 // CTAs of the attention over packed pages: the small tiles' kernel runs up to four a multiprocessor.
 constexpr int packed_attend_most_ctas(int64_t T, int64_t G) { return T * G <= kFewRows ? 4 * kAttendCtas : kAttendCtas; }
 // Rows of logits are cut into segments where two CTAs a multiprocessor leave each of them at least two.

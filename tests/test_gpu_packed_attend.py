@@ -49,6 +49,15 @@ def test_more_rows_than_an_item(T, Hq, H, D, tree):
     _problem([5, 0, 250], [T, T - 1, T // 2], T, Hq, H, D, 32, n4=[3, 7, 0], tree=tree, seed=T).check()
 
 
+@pytest.mark.parametrize("T,Hq,H", [(8, 4, 2), (9, 2, 1), (5, 8, 2), (16, 4, 2), (17, 4, 2), (31, 1, 1), (32, 2, 2), (33, 1, 1), (4, 8, 1)])
+@pytest.mark.parametrize("tree", [False, True])
+@pytest.mark.parametrize("window", [0, 70])
+def test_rows_where_the_tiles_change(T, Hq, H, tree, window):
+    """16 to 34 query rows of a head: one group of the small tiles, two, the tensor cores' tiles."""
+    _problem([5, 0, 250, 33], [T, T - 1, 1, T], T, Hq, H, 128 if T % 2 else 64, 32, n4=[3, 7, 0, 60], tree=tree, window=window,
+             sinks=3, seed=T).check()
+
+
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 5), (16, 0), (33, 1), (100, 70), (129, 40), (300, 3), (2 ** 31 - 1, 9)])
 @pytest.mark.parametrize("T", [1, 3, 40])
 @pytest.mark.parametrize("P", [16, 64])

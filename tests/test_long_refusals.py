@@ -202,7 +202,7 @@ def test_counts_past_32_bits(wrong):
     assert rheo._window(c, 2 ** 31 - 1, 2 ** 31 - 1, None).window == 2 ** 31 - 1
 
 
-@pytest.mark.parametrize("T,Hq,H,more", [(1, 4, 2, True), (5, 4, 2, True), (8, 4, 2, True), (9, 4, 2, False), (129, 32, 8, False)])
+@pytest.mark.parametrize("T,Hq,H,more", [(1, 4, 2, True), (5, 4, 2, True), (16, 4, 2, True), (17, 4, 2, False), (129, 32, 8, False)])
 @pytest.mark.parametrize("D", [64, 128])
 def test_scratch_sizes(lib, T, Hq, H, more, D):
     """Only the functions over packed pages ask for the parts of their small tiles; the others ask for no more than before, as
