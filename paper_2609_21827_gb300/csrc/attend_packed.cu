@@ -20,11 +20,12 @@
 // not finite count as 0 where some row may not see their place (0 * inf would
 // spoil it) and are added at the item's end for the rows that see them.
 //
-// What bounds it: instructions.  32 single tokens, contexts to 16,201, 32 query and 8 key/value heads of 128: 75 us, 3.9 TB/s (57 %
-// of a copy's rate), some 1,000 instructions a warp and tile at 59 % of the issue slots, of which turning numbers into bf16 (a
-// shift, a logic operation and a multiply-add a pair, on pipes of half rate) takes more than half.  48 chains of three tokens, heads of 64, a window of
-// 8,192: 51 us.  With the tensor cores' kernel, whose tiles have 128 rows, these take 251 and 142 us.  (Over 16 bits alone that one
-// is quicker, as nothing is to be turned: 32 single tokens in a window of 1,024 take it 43 us, this one 53.)
+// What bounds it: instructions.  32 single tokens, contexts to 16,201, 32 query and 8 key/value heads of 128: 75 us,
+// 3.9 TB/s (57 % of a copy's rate), some 1,000 instructions a warp and tile at 59 % of the issue slots, more than half of
+// which turn numbers into bf16 (a shift, a logic operation and a multiply-add a pair, on pipes of half rate).  48 chains
+// of three tokens, heads of 64, a window of 8,192: 51 us.  With the tensor cores' kernel, whose tiles have 128 rows, these
+// take 251 and 142 us.  (Over 16 bits alone that one is quicker, as nothing is to be turned: 32 single tokens in a window of
+// 1,024 take it 43 us, this one 53.)
 #include <cuda_bf16.h>
 
 #include "attend.cuh"

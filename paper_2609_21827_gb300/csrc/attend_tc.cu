@@ -42,6 +42,10 @@
 // 1,911: 19 us with the join, dependent latencies.  Measured against this layout: keys in
 // units of 64 in the rings 185 / 389 / 29 us where this took 193 / 367 / 24, scores of
 // 128 keys at a time (no second buffer) 196 / 404 / 23.
+// With windows: the 64 trees and 2,048 positions 155 us (floor 84), two prompt pieces of 2,000 tokens and 1,024 positions
+// 107 (33), 32 single tokens 43.5 (19): items of ten to twenty tiles, whose starts and ends take as long as four.  Over packed
+// pages the 64 trees take 326 us (floor 136, the products): tensor cores 31 %, issue slots 55 %, HBM 13 %; the softmax warps'
+// chain, and instruction fetch, as the roles' loops share the instruction cache.
 #include <cuda.h>
 #include <cuda_bf16.h>
 
