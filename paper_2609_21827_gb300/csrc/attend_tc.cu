@@ -84,7 +84,8 @@ template <int D, bool PAIR, int KIND> struct TcShape {
     // Tensor memory: stream s has two buffers of scores at columns 128 s and 128 s + 64, whose first 32 columns take
     // the weights (bf16 pairs), and its sums at kO + s D.
     static constexpr int kO = 256;
-    // A softmax group that waits for the values of tile u knows that those of tile u - 2 have come (at clean()).
+    // A softmax group that waits for the values of tile u knows that those of tile u - 2 have come (the reason is at clean(),
+    // and rests on the order of tc_scores).
     static_assert(kV >= kScores);
 };
 
@@ -441,10 +442,16 @@ __device__ __forceinline__ void tc_softmax(const AttendArgs& a, TcControl& c, ch
         // the request's places, and no element that is not finite among the drafted tokens'.  PAIR: a thread a line;
         // !PAIR: the stream's half of the lines, two threads a line.
         // Called with a product of this stream's scores at hand, the only waits for full_v here, and not for each tile.  The
-        // phase before, tile u - kV, has ended: these scores were issued after the stream's product with the values two
-        // products ago (its buffer), which read tile u - 2 or a later one if it is of this item; if it is of an earlier
-        // one, u - 2 is too, and stream 0, which reads every tile, has waited for that item's last product before this
-        // item began.  The phase after needs this stream's product with tile u, which waits for what follows here.
+        // phase before, tile u - kV, has ended:
+        // PAIR: a stream with rows has a product in every tile of the item, so its product two before this one (whose
+        // buffer these scores took: they were issued after it) read tile u - 2 or a later one, or is of an earlier item.
+        // !PAIR: stream 1 has no product in a tile without a second half, which LONG has in the middle of items (the last
+        // tiles of the sinks and of the packed part), so its product two before may be of tile u - 3 or u - 4.  Stream 0 has
+        // one in every tile, and tc_scores issues its scores of tile u before stream 1's: after stream 0's product with the
+        // values of tile u - 2, or of an earlier item's last tile.
+        // Where tile u - 2 is of an earlier item: stream 0, which reads every tile, has waited for that item's last product
+        // before this item began.
+        // The phase after needs this stream's product with tile u, which waits for what follows here.
         // LONG: nothing that no token of the item sees, and no element that is not finite where some may not see the place.
         auto clean = [&](int k0, int end, uint32_t u) -> bool {
             if (!bar_wait(&c.full_v[u % S::kV], (u / S::kV) & 1, c)) return false;
@@ -922,6 +929,7 @@ __device__ __forceinline__ void tc_scores(const AttendArgs& a, TcControl& c, cha
         for (int q = 0; q < n; ++q, at.next(S::kK)) {
             const int subs = item.subs(w.tile + q);
             if (!bar_wait(&c.full_k[at.slot], at.parity, c)) goto out;
+            // (stream 0's scores of a tile before stream 1's: stream 1's waits for values at clean() rest on it)
 #pragma unroll (kProductUnroll<KIND, PAIR>)
             for (int x = 0; x < 4; ++x) {
                 const int sub = x >> 1, st = x & 1;
