@@ -1,4 +1,6 @@
-"""Windows over packed pages where they meet other things: tiles of one half one behind the other."""
+"""Windows over packed pages where they meet other things: numbers that are not finite
+which some tokens see and others do not, trees of more than 64 tokens, tiles of one
+half one behind the other, and lengths that change between the replays of a graph."""
 import math
 
 import pytest
@@ -45,6 +47,58 @@ def _near(got, want, bound):
     return ((got.double() - want).abs() <= bound).all()
 
 
+# query rows of a head: the small tiles' one and two columns of eight, two groups of them, one stream, one, two
+ROWS = [(6, 1), (6, 2), (7, 4), (40, 1), (9, 8), (40, 4)]
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("T,G", ROWS)
+@pytest.mark.parametrize("tree", [False, True])
+def test_what_is_outside_a_tokens_window_does_not_reach_it(bad, T, G, tree):
+    """Lines behind the packed pages: seen by no token, by the first ones' windows, by all, and a drafted one.  Rows that
+    see none of them keep to the definition, the others are not finite."""
+    W, near, n4 = 90, [300, 40], [5, 9]
+    p = lr.Problem(rheo, near, None, T, 2 * G, 2, 128 if T % 2 else 64, 16, n4=n4, window=W, sinks=2, tree=tree, seed=T + G)
+    p.check()
+    o, w, e, el = _expected(p)
+    c, pk = p.ctx[0], n4[0] * 16
+    places = [pk + 3, c - W, c - W + 1, c - W + 2, c + T // 2]
+    for l in places:
+        _plant(p, 0, l, {slice(None, None, 3): bad}, {slice(1, None, 2): bad})
+    out, lse = p.run()
+    hit = _rows_that_see(p, 0, places)
+    assert rheo.scratch_status(p.ws) == 0 and hit.any() and (tree or not hit.all())
+    for b, clear in ((0, ~hit), (1, torch.ones_like(hit))):
+        assert _near(out[b][clear], o[b][clear], e[b][clear]) and _near(lse[b][clear], w[b][clear], el[b][clear])
+    assert not torch.isfinite(out[0][hit][..., 1::2]).any()
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("T,G", ROWS)
+@pytest.mark.parametrize("tree", [False, True])
+def test_values_that_are_not_finite_stay_in_their_columns(bad, T, G, tree):
+    """A cached value behind the packed pages that only the first tokens' windows reach, one that no token sees, and a
+    drafted one."""
+    W, n4 = 90, [5]
+    p = lr.Problem(rheo, [300], None, T, 2 * G, 2, 64 if T % 2 else 128, 16, n4=n4, window=W, tree=tree, seed=T)
+    p.check()
+    o, w, e, el = _expected(p)
+    c = p.ctx[0]
+    planted = {5: c - W + 1, 7: n4[0] * 16 + 1, 9: c + T // 2}
+    for d, l in planted.items():
+        _plant(p, 0, l, {}, {d: bad})
+    out, lse = p.run()
+    assert rheo.scratch_status(p.ws) == 0 and _near(lse, w, el)
+    for d, l in planted.items():
+        hit = _rows_that_see(p, 0, [l])
+        col = out[0][hit][..., d]
+        assert torch.isnan(col).all() if math.isnan(bad) else (col == bad).all()
+        assert _near(out[0][~hit][..., d], o[0][~hit][..., d], e[0][~hit][..., d])
+        assert hit.any() == (d != 7) and not hit.all()
+    keep = [d for d in range(p.cfg.head_dim) if d not in planted]
+    assert _near(out[..., keep], o[..., keep], e[..., keep])
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("T,G", [(10, 4), (40, 2), (20, 8)])
 def test_halves_of_tiles_one_behind_the_other(T, G, D):
@@ -67,3 +121,39 @@ def test_halves_of_tiles_one_behind_the_other(T, G, D):
         hit = _rows_that_see(p, b, [p.ctx[b] + T // 2])
         assert (out[b][hit][..., b % D] == math.inf).all() and hit.any()
         assert _near(out[b][~hit][..., b % D], o[b][~hit][..., b % D], e[b][~hit][..., b % D])
+
+
+@pytest.mark.parametrize("T,G,D", [(65, 1, 128), (129, 1, 64), (129, 2, 128), (300, 1, 64)])
+@pytest.mark.parametrize("window,sinks", [(3, 0), (1, 5), (70, 40), (6, 160), (200, 900), (5000, 2)])
+@pytest.mark.parametrize("with_depth", [True, False])
+def test_trees_of_more_than_64_tokens(T, G, D, window, sinks, with_depth):
+    """Nothing packed, parts of any length, drafted tokens across the tiles' halves; sinks that end in the packed
+    part, among the drafted tokens and behind them; positions by depth and by place."""
+    near, n4 = [0, 1, 63, 130, 250, 5], [0, 1, 7, 0, 3, 25]
+    p = lr.Problem(rheo, near, [T, T, T - 1, T, T // 2, 1], T, 2 * G, 2, D, 32 if T == 129 else 16, n4=n4, tree=True,
+                   window=window, sinks=sinks, with_depth=with_depth, seed=T + window)
+    p.check()
+
+
+@pytest.mark.parametrize("T,tree", [(1, False), (7, True), (30, True), (80, True)])
+def test_in_a_graph_with_lengths_that_change(T, tree):
+    p = lr.Problem(rheo, [100, 90], None, T, 8, 2, 64, 16, n4=[30, 60], window=120, sinks=7, tree=tree, seed=6)
+    near, held = i32(p.near), p.held4.n_pages
+    call = lambda: rheo.packed_attend(p.cfg, p.cfg4, p.q, p.key, p.value, p.held, near, p.data, p.held4, p.out, p.ws,  # noqa: E731
+                                      window=120, sinks=7, depth=p.depth, mask=p.mask, lse=p.lse, scale=p.scale)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for lens, packed in (([100, 90], [30, 60]), ([0, 3], [0, 1]), ([77, 0], [21, 59]), ([100, 90], [0, 60])):
+        near.copy_(i32(lens))
+        held.copy_(i32(packed))
+        p.out.fill_(3.0)
+        p.lse.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        p.near, p.n4, p.ctx = lens, packed, [c + 16 * n for c, n in zip(lens, packed)]
+        o, w, e, el = _expected(p)
+        assert _near(p.out, o, e) and _near(p.lse, w, el)
+    assert rheo.scratch_status(p.ws) == 0
