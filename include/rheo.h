@@ -499,7 +499,8 @@ typedef struct {
 } rheo_packed;
 
 /* Bytes of a packed page of one head, and of the scratch of rheo_cache_pack, rheo_cache_unpack and rheo_packed_attend (at
- * least rheo_cache_sizes', so that it serves the other cache functions too).  Either may be NULL. */
+ * least rheo_cache_sizes', so that it serves the other cache functions too: the same where tokens * q_heads / kv_heads is
+ * above 32, some four times that up to there, so a buffer of a few more rows may be too small for fewer).  Either may be NULL. */
 int rheo_packed_sizes(const rheo_cache_config* packed_cfg, int64_t* page_bytes, size_t* scratch_bytes);
 
 /* Packs whole pages, in `layers` layers (layer l at kv->key + l * key_layer elements,

@@ -42,10 +42,6 @@ constexpr int kSlots = 2;            // of a warp
 constexpr float kSlack = 8.0f;
 constexpr int kWaitLimit = 1 << 22;  // polls of a wait before the kernel gives up
 
-// CTAs an SM: lines of 128 channels need more than 128 registers a thread (32 single tokens, contexts to 16,201: 76.8 us with
-// four, 75.6 with three).
-constexpr int few_per_sm(int D) { return D == 128 ? 3 : 4; }
-
 template <int D, int NT> struct Few {
     static constexpr int kPerSm = few_per_sm(D);
     static constexpr int kX = D / 32;
@@ -510,8 +506,7 @@ cudaError_t launch_packed_attend(const AttendArgs& in, cudaStream_t s) {
         return err != cudaSuccess ? err : launch_attend_join(a, 1, s);
     }
     const bool one = rows <= 8;
-    a.item_rows = one ? 8 : 16;
-    a.part_rows = a.item_rows;
+    a.item_rows = a.part_rows = few_item_rows(rows);
     a.ctas = kAttendCtas * few_per_sm(a.D);
     // What an item's start and end cost in tiles (32 single tokens, contexts to 16,201: 99.7, 89.7, 80.7, 80.9 us with 6, 12,
     // 24, 32), and the tiles of a part at least where few items are cut by themselves (one token over 16,201: 28.1, 26.1,

@@ -140,8 +140,21 @@ constexpr int kAttendCtas = 152;  // one a multiprocessor
 // 8,201, 32 query and 8 key/value heads of 128, 20, 32, 48 and 64 rows: 110, 116, 174, 225 us; with the tensor cores' kernel
 // 156, 140, 149, 146.  (To 16,201, 16 rows: 105 and 249.)
 constexpr int kFewRows = 32;
-// CTAs of the attention over packed pages: the small tiles' kernel runs up to four a multiprocessor.
+// The small tiles' launch: rows of an item, CTAs a multiprocessor (lines of 128 channels need more than 128 registers a
+// thread: 32 single tokens, contexts to 16,201: 76.8 us with four, 75.6 with three).
+constexpr int few_item_rows(int64_t rows) { return rows <= 8 ? 8 : 16; }
+constexpr int few_per_sm(int D) { return D == 128 ? 3 : 4; }
+// What scratch is sized for over packed pages: CTAs that leave parts of (T G rounded up to 8) rows each, and no launch of the
+// small tiles leaves more.
 constexpr int packed_attend_most_ctas(int64_t T, int64_t G) { return T * G <= kFewRows ? 4 * kAttendCtas : kAttendCtas; }
+constexpr bool few_parts_fit() {
+    for (int rows = 1; rows <= kFewRows; ++rows)
+        for (int D = 64; D <= 128; D += 64)
+            if (few_per_sm(D) * kAttendCtas > packed_attend_most_ctas(rows, 1) || few_item_rows(rows) > (rows + 7) / 8 * 8)
+                return false;
+    return true;
+}
+static_assert(few_parts_fit());
 // Rows of logits are cut into segments where two CTAs a multiprocessor leave each of them at least two.
 constexpr int kLogprobParts = 2 * 152;
 constexpr int kLogprobCutRows = kLogprobParts / 2;

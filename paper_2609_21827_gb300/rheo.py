@@ -519,7 +519,8 @@ class _Scratch:
 
 
 class CacheWorkspace(_Scratch):
-    """For the functions over packed pages too, which only bf16 caches have and which ask for more."""
+    """For the functions over packed pages too, which only bf16 caches have and which ask for more, some four times as much, up
+    to 32 query rows (tokens * q_heads / kv_heads) of a key/value head: a workspace of a few more rows is refused there."""
 
     @staticmethod
     def _size(cfg) -> int:
