@@ -21,11 +21,13 @@
 // spoil it) and are added at the item's end for the rows that see them.
 //
 // What bounds it: instructions.  32 single tokens, contexts to 16,201, 32 query and 8 key/value heads of 128: 75 us,
-// 3.9 TB/s (57 % of a copy's rate), some 1,000 instructions a warp and tile at 59 % of the issue slots, more than half of
-// which turn numbers into bf16 (a shift, a logic operation and a multiply-add a pair, on pipes of half rate).  48 chains
+// 3.9 TB/s (57 % of a copy's rate), some 730 instructions a tile, 51 % of what the SMs can issue in that time, more than half
+// of which turn numbers into bf16 (a shift, a logic operation and a multiply-add a pair, on pipes of half rate).  48 chains
 // of three tokens, heads of 64, a window of 8,192: 51 us.  With the tensor cores' kernel, whose tiles have 128 rows, these
-// take 251 and 142 us.  (Over 16 bits alone that one is quicker, as nothing is to be turned: 32 single tokens in a window of
-// 1,024 take it 43 us, this one 53.)
+// take 251 and 142 us.  Items of 16 rows spill registers (256 bytes of stores a thread with heads of 64, 360 with heads of 128,
+// which single tokens do not but for 24): chains of 5 and 8, four rows each, 32 requests, contexts to 8,201: 110 and 116 us.
+// (Over 16 bits alone the tensor cores' kernel is quicker, as nothing is to be turned: 32 single tokens in a window of 1,024
+// take it 43 us, this one 53.)
 #include <cuda_bf16.h>
 
 #include "attend.cuh"

@@ -43,9 +43,10 @@
 // units of 64 in the rings 185 / 389 / 29 us where this took 193 / 367 / 24, scores of
 // 128 keys at a time (no second buffer) 196 / 404 / 23.
 // With windows: the 64 trees and 2,048 positions 155 us (floor 84), two prompt pieces of 2,000 tokens and 1,024 positions
-// 107 (33), 32 single tokens 43.5 (19): items of ten to twenty tiles, whose starts and ends take as long as four.  Over packed
-// pages the 64 trees take 326 us (floor 136, the products): tensor cores 31 %, issue slots 55 %, HBM 13 %; the softmax warps'
-// chain, and instruction fetch, as the roles' loops share the instruction cache.
+// 107 (34), 32 single tokens 43.5 (19): items of ten to twenty tiles, whose starts and ends take as long as four.  Over packed
+// pages the 64 trees take 326 us (floor 142, the products): tensor cores 37 %, instructions 57 % of what can be issued, HBM
+// 16 %; the softmax warps' chain, and instruction fetch, as the roles' loops share the instruction cache.  32 trees of 17
+// (68 rows, one stream a half) take 154 to 158 us (floor 24), hardly less with half the rows: a fixed time a tile.
 #include <cuda.h>
 #include <cuda_bf16.h>
 

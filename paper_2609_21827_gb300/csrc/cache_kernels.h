@@ -138,7 +138,7 @@ int attend_least(int dtype);
 constexpr int kAttendCtas = 152;  // one a multiprocessor
 // Query rows of a key/value head up to which packed pages are read by the small tiles, 8 or 16 at a time.  32 requests, contexts to
 // 8,201, 32 query and 8 key/value heads of 128, 20, 32, 48 and 64 rows: 110, 116, 174, 225 us; with the tensor cores' kernel
-// 156, 140, 149, 146.  (To 16,201, 16 rows: 105 and 249.)
+// 156, 140, 149, 146.  (To 16,201, 16 rows: 105 and 249.)  Other head layouts were not measured.
 constexpr int kFewRows = 32;
 // The small tiles' launch: rows of an item, CTAs a multiprocessor (lines of 128 channels need more than 128 registers a
 // thread: 32 single tokens, contexts to 16,201: 76.8 us with four, 75.6 with three).

@@ -15,7 +15,7 @@
 //
 // What bounds it: HBM, sixteen loads of 16 bytes a lane under way.  The prompts of 16 requests (503 to 9,001 tokens, 4 layers, 8
 // heads of 128) packed and unpacked again 521 us, 5.8 TB/s (86 % of a copy's rate); three prefixes of 4,099 to 12,001 tokens in 8
-// layers unpacked 173 us, 5.8 TB/s.  A page of each of 32 layers: a launch for the pages and one for the tables, dependent latencies.
+// layers unpacked 174 us, 5.7 TB/s.  A page of each of 32 layers: a launch for the pages and one for the tables, dependent latencies.
 #include <cuda_bf16.h>
 
 #include "cache_kernels.h"

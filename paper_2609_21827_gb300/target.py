@@ -73,7 +73,8 @@ class Target:
 class Cached:
     """A target with its cache for `batch` requests of up to `most` tokens, `tokens` new ones a call.  With `share`,
     another one of the same sizes, it works on that one's pages: a prompt's calls and a tree's have different `tokens`.
-    With `packed`, pack() moves whole pages into 4 bits."""
+    With `packed`, pack() moves whole pages into 4 bits (both pools have room for all tokens, as a prompt is whole in 16
+    bits before it is packed: this shows the calls, not the memory that they save)."""
 
     def __init__(self, model: Target, batch: int, tokens: int, most: int, page_size: int = 16, share: Cached = None,
                  device="cuda", packed: bool = False):
